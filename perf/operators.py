@@ -98,7 +98,7 @@ def work(case):
     if op == "wgrad":
         return {"bytes": s * T * case["O"] + ck + 4 * case["O"] * C, "flops": 2 * T * C * case["O"]}
     grad = case["grad"]
-    return {"bytes": s * T * C * (3 if grad else 1) + 12 * T * (3 + case["top"]), "flops": (11 if grad else 6) * T * C}
+    return {"bytes": s * T * C * (3 if grad else 1) + T * (24 + 12 * case["top"]), "flops": (11 if grad else 6) * T * C}
 
 
 def _padded(C):
@@ -188,7 +188,7 @@ def prepare(case, seed):
             x[rows, y] = 4.0
             y = torch.where(torch.rand(T, device=dev, generator=gen) < 0.1, -100, y)
         f32, k = torch.float32, case["top"]
-        s.update(x=x, y=y, logp=empty(T, dtype=f32), entropy=empty(T, dtype=f32), lse=empty(T, dtype=f32),
+        s.update(x=x, y=y, logp=empty(T, dtype=f32), entropy=empty(T, dtype=f32), lse=empty(T, 2, dtype=f32),
                  top_ids=empty(T, k, dtype=torch.int64) if k else None, top_logp=empty(T, k, dtype=f32) if k else None)
         if case["grad"]:                                # minus an advantage for each token, and an entropy bonus
             s.update(dlogp=normal(T, std=1.0 / T, dtype=f32), dentropy=torch.full((T,), -0.01 / T, device=dev),
@@ -271,7 +271,7 @@ def _plain_logprob(s):
     logp = torch.where(y < 0, 0.0, (x.gather(1, at) - lse)[:, 0])
     lp = torch.where(p > 0, x - lse, 0.0)
     H = -(p * lp).sum(1)
-    out = {"logp": logp, "entropy": H, "lse": lse[:, 0]}
+    out = {"logp": logp, "entropy": H, "lse": torch.cat([m, torch.log(z)], 1)}
     k = s["case"]["top"]
     if k:                                               # by value, ties to the lowest index: unique 64-bit keys
         bits = torch.where(x == 0, 0.0, x).view(torch.int32).long()
@@ -428,7 +428,7 @@ def exact(case, seed):
         H = -plp.sum(1)
         given = y >= 0
         rows = torch.arange(x.shape[0], device=x.device)
-        o = {"logp": torch.where(given, lp[rows, y.clamp(min=0)], 0.0), "entropy": H, "lse": torch.logsumexp(x, 1)}
+        o = {"logp": torch.where(given, lp[rows, y.clamp(min=0)], 0.0), "entropy": H, "lse": torch.stack([x.amax(1), torch.logsumexp(x, 1) - x.amax(1)], 1)}
         if case["top"]:
             ids = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :case["top"]]
             o.update(top_ids=ids, top_logp=lp.gather(1, ids))
