@@ -1,5 +1,5 @@
-"""Thin ctypes binding of libdef_b200.so: the same entry points as include/def.h, taking
-torch tensors.  It checks dtype / contiguity / device / shape and passes data pointers;
+"""Thin ctypes binding of libdef_b200.so: the same entry points as include/def.h and include/def_train.h,
+taking torch tensors.  It checks dtype / contiguity / device / shape and passes data pointers;
 every step of the method runs inside the library's CUDA kernels.  There is no CPU or
 eager fallback: if the library cannot be built or loaded, importing fails loudly."""
 import ctypes
@@ -20,7 +20,12 @@ DEF_COMPRESSOR_RBGS, DEF_COMPRESSOR_SCALE = 0, 1
 _i64, _u64, _i32, _f32, _ptr = (ctypes.c_int64, ctypes.c_uint64, ctypes.c_int32, ctypes.c_float,
                                 ctypes.c_void_p)
 
-# name -> (restype, argtypes): every symbol include/def.h declares
+DEF_DTYPE_F32, DEF_DTYPE_BF16, DEF_DTYPE_F16 = 0, 1, 2
+DEF_CHECKPOINT_GROUP = 32
+DEF_NORM_MAX_C = 16384
+DEF_LOGPROB_MAX_TOP = 32
+
+# name -> (restype, argtypes): every symbol include/def.h and include/def_train.h declare
 SIGNATURES = {
     "def_create": (_ptr, [_i64, _i32, _i64, _i32, _f32, _f32, _ptr]),
     "def_destroy": (ctypes.c_int, [_ptr]),
@@ -51,6 +56,20 @@ SIGNATURES = {
     "def_set_kernel_timing": (ctypes.c_int, [_ptr, ctypes.c_int]),
     "def_kernel_time": (ctypes.c_int, [_ptr, ctypes.c_int, _ptr, _ptr]),
     "def_last_error": (ctypes.c_char_p, []),
+    "def_checkpoint_layout": (ctypes.c_int, [_i64, _ptr, _ptr]),
+    "def_checkpoint_pack": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _i64, _ptr, _ptr, _ptr]),
+    "def_checkpoint_unpack": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _ptr, _ptr, _i64, _ptr]),
+    "def_checkpoint_weight_grad": (ctypes.c_int, [_i32, _i64, _i64, _i64, _ptr, _i64, _ptr, _ptr, _ptr, _i32, _ptr, _i64, _ptr]),
+    "def_checkpoint_weight_grad_workspace": (ctypes.c_int, [_i32, _i64, _i64, _i64, _ptr, _i64, _ptr]),
+    "def_gated_forward": (ctypes.c_int, [_i32, _i64, _i64] + [_ptr, _i64] * 3 + [_ptr] * 5),
+    "def_gated_backward": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _i64] + [_ptr] * 4 + [_ptr, _i64] * 3 + [_ptr] * 3),
+    "def_norm_forward": (ctypes.c_int, [_i32, _i64, _i64] + [_ptr, _i64] * 2 + [_ptr, _ptr, _i64, _ptr, _f32, _f32]
+                         + [_ptr, _i64] * 2 + [_ptr] * 9),
+    "def_norm_backward": (ctypes.c_int, [_i32, _i64, _i64] + [_ptr, _i64] * 2 + [_ptr, _i64, _ptr, _ptr] * 2
+                          + [_ptr, _ptr, _i64, _ptr, _f32, _ptr, _ptr] + [_ptr, _i64] * 2 + [_ptr] * 3 + [_i32, _ptr, _i64, _ptr]),
+    "def_norm_backward_workspace": (ctypes.c_int, [_i64, _i64, _i64, _ptr]),
+    "def_logprob_forward": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _i64] + [_ptr] * 4 + [_i32] + [_ptr] * 3),
+    "def_logprob_backward": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _i64] + [_ptr] * 5 + [_i32] + [_ptr] * 3 + [_i64, _ptr]),
 }
 
 
@@ -348,3 +367,180 @@ def def_step_rows(ctx, params, grads, errors, mom, block_sum, step, seed, group=
         def_step_rows_apply(ctx, params, block_sum, W_total, step, seed)
     else:
         def_step_rows_apply_detach(ctx, params, block_sum, W_total, detached_out, step, seed)
+
+
+# --- operators of the training step around def_step (include/def_train.h) ------------------------------------------
+#
+# Activations are [T, C] tensors of float32, bfloat16 or float16 with consecutive columns and any row stride; a
+# checkpoint is a pair (q, e) made by def_checkpoint_alloc.  `stream`: as in def_block_start_device.
+
+_DTYPES = {torch.float32: DEF_DTYPE_F32, torch.bfloat16: DEF_DTYPE_BF16, torch.float16: DEF_DTYPE_F16}
+
+
+def _stream(stream):
+    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else (stream or 0)
+
+
+def _act(t, name, like=None):
+    """(dtype code, T, C, pointer, row stride) of an activation; `like`: another's, to agree with."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _DTYPES:
+        raise TypeError("%s must be a two-dimensional float32, bfloat16 or float16 torch tensor" % name)
+    if not t.is_cuda:
+        raise TypeError("%s must live on the GPU" % name)
+    T, C = t.shape
+    ld, inner = t.stride()
+    if inner != 1 and C > 1:
+        raise ValueError("the columns of %s must be consecutive" % name)
+    if T <= 1:
+        ld = C
+    code = _DTYPES[t.dtype]
+    if like is not None and (code != like[0] or T != like[1] or C != like[2]):
+        raise ValueError("%s is %s of %s, expected type %d and shape %s" % (name, t.dtype, (T, C), like[0], like[1:3]))
+    return code, T, C, t.data_ptr(), ld
+
+
+def _opt_act(t, name, like):
+    return (None, 0) if t is None else _act(t, name, like)[3:]
+
+
+def _held(ck, name, T, C):
+    """(q pointer, e pointer) of a checkpoint of [T, C], or of None."""
+    if ck is None:
+        return None, None
+    q, e = ck
+    ldq, lde = -(-C // 16) * 16, (C + 127) // 128 * 4
+    return _dev(q, name + " q", (T, ldq), torch.int8), _dev(e, name + " e", (T, lde), torch.uint8)
+
+
+def _param(t, name, shape):
+    return None if t is None else _dev(t, name, shape)
+
+
+def _work(t, name):
+    if t is None:
+        return None, 0
+    return _dev(t, name, None, torch.uint8), t.numel()
+
+
+def def_checkpoint_layout(C):
+    """(bytes per row of the 8-bit integers, bytes per row of the exponents) of a checkpoint of [T, C]."""
+    ldq, lde = ctypes.c_int64(0), ctypes.c_int64(0)
+    _check(lib.def_checkpoint_layout(int(C), ctypes.byref(ldq), ctypes.byref(lde)))
+    return int(ldq.value), int(lde.value)
+
+
+def def_checkpoint_alloc(T, C, device):
+    """An uninitialised checkpoint (q, e) of [T, C] from torch's allocator."""
+    ldq, lde = def_checkpoint_layout(C)
+    return torch.empty((T, ldq), dtype=torch.int8, device=device), torch.empty((T, lde), dtype=torch.uint8, device=device)
+
+
+def def_checkpoint_pack(x, ck, stream=None):
+    dt, T, C, p, ld = _act(x, "x")
+    q, e = _held(ck, "checkpoint", T, C)
+    _check(lib.def_checkpoint_pack(dt, T, C, p, ld, q, e, _stream(stream)))
+
+
+def def_checkpoint_unpack(ck, out, stream=None):
+    dt, T, C, p, ld = _act(out, "out")
+    q, e = _held(ck, "checkpoint", T, C)
+    _check(lib.def_checkpoint_unpack(dt, T, C, q, e, p, ld, _stream(stream)))
+
+
+def def_checkpoint_weight_grad_workspace(dy, I):
+    dt, T, O, p, ld = _act(dy, "dy")
+    out = ctypes.c_int64(0)
+    _check(lib.def_checkpoint_weight_grad_workspace(dt, T, O, int(I), p, ld, ctypes.byref(out)))
+    return int(out.value)
+
+
+def def_checkpoint_weight_grad(dy, ck, dw, workspace=None, accumulate=False, stream=None):
+    """dw [O, I] (float32) (+)= dy^T times the [T, I] checkpoint."""
+    dt, T, O, p, ld = _act(dy, "dy")
+    if not isinstance(dw, torch.Tensor) or dw.dim() != 2:
+        raise TypeError("dw must be a two-dimensional torch tensor")
+    I = dw.shape[1]
+    q, e = _held(ck, "checkpoint", T, I)
+    w, nw = _work(workspace, "workspace")
+    _check(lib.def_checkpoint_weight_grad(dt, T, O, I, p, ld, q, e, _dev(dw, "dw", (O, I)), 1 if accumulate else 0, w, nw, _stream(stream)))
+
+
+def def_gated_forward(gate, up, h, gate_ck=None, up_ck=None, stream=None):
+    g = _act(gate, "gate")
+    dt, T, F = g[:3]
+    gq, ge = _held(gate_ck, "gate checkpoint", T, F)
+    uq, ue = _held(up_ck, "up checkpoint", T, F)
+    _check(lib.def_gated_forward(dt, T, F, *g[3:], *_act(up, "up", g)[3:], *_act(h, "h", g)[3:], gq, ge, uq, ue, _stream(stream)))
+
+
+def def_gated_backward(dh, gate_ck, up_ck, dgate, dup, h_out=None, h_ck=None, stream=None):
+    d = _act(dh, "dh")
+    dt, T, F = d[:3]
+    gq, ge = _held(gate_ck, "gate checkpoint", T, F)
+    uq, ue = _held(up_ck, "up checkpoint", T, F)
+    hq, he = _held(h_ck, "h checkpoint", T, F)
+    _check(lib.def_gated_backward(dt, T, F, *d[3:], gq, ge, uq, ue, *_act(dgate, "dgate", d)[3:], *_act(dup, "dup", d)[3:],
+                                  *_opt_act(h_out, "h_out", d), hq, he, _stream(stream)))
+
+
+def def_norm_forward(h, b, w_post, gate, w_pre, h_out, n_out, rstd_post, rstd_pre, res_scale=1.0, eps=1e-6, b_ck=None, h_ck=None,
+                     n_ck=None, stream=None):
+    """h_out = res_scale h + gate norm(b) w_post, n_out = norm(h_out) w_pre; with b (and w_post, gate, h_out, rstd_post)
+    None: n_out = norm(h) w_pre.  gate: [groups, C] or None."""
+    a = _act(h, "h")
+    dt, T, C = a[:3]
+    groups = 1 if gate is None else gate.shape[0]
+    bq, be = _held(b_ck, "b checkpoint", T, C)
+    hq, he = _held(h_ck, "h checkpoint", T, C)
+    nq, ne = _held(n_ck, "n checkpoint", T, C)
+    _check(lib.def_norm_forward(dt, T, C, *a[3:], *_opt_act(b, "b", a), _param(w_post, "w_post", (C,)), _param(gate, "gate", (groups, C)),
+                                groups, _param(w_pre, "w_pre", (C,)), res_scale, eps, *_opt_act(h_out, "h_out", a),
+                                *_act(n_out, "n_out", a)[3:], _param(rstd_post, "rstd_post", (T,)), _param(rstd_pre, "rstd_pre", (T,)),
+                                bq, be, hq, he, nq, ne, _stream(stream)))
+
+
+def def_norm_backward_workspace(T, C, groups=1):
+    out = ctypes.c_int64(0)
+    _check(lib.def_norm_backward_workspace(int(T), int(C), int(groups), ctypes.byref(out)))
+    return int(out.value)
+
+
+def def_norm_backward(dn, dh_in, h, b, w_post, gate, w_pre, rstd_post, rstd_pre, dh, db, dw_post, dgate, dw_pre, workspace,
+                      res_scale=1.0, accumulate=False, stream=None):
+    """h and b: the stored tensors, or checkpoints (q, e) of them; dh_in None: zero."""
+    a = _act(dn, "dn")
+    dt, T, C = a[:3]
+    groups = 1 if gate is None else gate.shape[0]
+    hq, he = _held(h, "h checkpoint", T, C) if isinstance(h, tuple) else (None, None)
+    bq, be = _held(b, "b checkpoint", T, C) if isinstance(b, tuple) else (None, None)
+    hp = _opt_act(None if hq is not None else h, "h", a)
+    bp = _opt_act(None if bq is not None else b, "b", a)
+    w, nw = _work(workspace, "workspace")
+    _check(lib.def_norm_backward(dt, T, C, *a[3:], *_opt_act(dh_in, "dh_in", a), *hp, hq, he, *bp, bq, be,
+                                 _param(w_post, "w_post", (C,)), _param(gate, "gate", (groups, C)), groups, _param(w_pre, "w_pre", (C,)),
+                                 res_scale, _param(rstd_post, "rstd_post", (T,)), _param(rstd_pre, "rstd_pre", (T,)),
+                                 *_act(dh, "dh", a)[3:], *_opt_act(db, "db", a), _param(dw_post, "dw_post", (C,)),
+                                 _param(dgate, "dgate", (groups, C)), _param(dw_pre, "dw_pre", (C,)), 1 if accumulate else 0,
+                                 w, nw, _stream(stream)))
+
+
+def def_logprob_forward(logits, targets, logp, entropy, lse, top_ids=None, top_logp=None, stream=None):
+    """targets: int64 [T]; lse: float32 [T, 2] (maximum, log of the sum relative to it); top_ids: int64 [T, top]."""
+    dt, T, V, p, ld = _act(logits, "logits")
+    top = 0 if top_ids is None else top_ids.shape[1]
+    _check(lib.def_logprob_forward(dt, T, V, p, ld, _dev(targets, "targets", (T,), torch.int64), _dev(logp, "logp", (T,)),
+                                   _dev(entropy, "entropy", (T,)), _dev(lse, "lse", (T, 2)), top,
+                                   _dev(top_ids, "top_ids", (T, top), torch.int64, optional=True), _param(top_logp, "top_logp", (T, top)),
+                                   _stream(stream)))
+
+
+def def_logprob_backward(logits, targets, lse, entropy, dlogits, dlogp=None, dentropy=None, top_ids=None, dtop_logp=None, stream=None):
+    a = _act(logits, "logits")
+    dt, T, V, p, ld = a
+    top = 0 if top_ids is None or dtop_logp is None else top_ids.shape[1]
+    if top == 0:
+        top_ids = dtop_logp = None
+    _check(lib.def_logprob_backward(dt, T, V, p, ld, _dev(targets, "targets", (T,), torch.int64), _dev(lse, "lse", (T, 2)),
+                                    _dev(entropy, "entropy", (T,)), _param(dlogp, "dlogp", (T,)), _param(dentropy, "dentropy", (T,)), top,
+                                    _dev(top_ids, "top_ids", (T, top), torch.int64, optional=True), _param(dtop_logp, "dtop_logp", (T, top)),
+                                    *_act(dlogits, "dlogits", a)[3:], _stream(stream)))

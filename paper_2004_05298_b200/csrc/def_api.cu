@@ -3,6 +3,7 @@
 #include "../../include/def.h"
 #include "def_kernels.cuh"
 #include "def_aux_kernels.cuh"
+#include "def_error.cuh"
 
 #include <cmath>
 #include <cstdarg>
@@ -13,10 +14,10 @@
 #include <new>
 
 namespace {
-
 thread_local char g_last_error[512] = "";
+}  // namespace
 
-int fail(int code, const char *fmt, ...) {
+int defk::fail(int code, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
@@ -24,9 +25,14 @@ int fail(int code, const char *fmt, ...) {
     return code;
 }
 
-int cuda_fail(cudaError_t err, const char *what) {
+int defk::cuda_fail(cudaError_t err, const char *what) {
     return fail(DEF_ERR_CUDA, "%s: %s", what, cudaGetErrorString(err));
 }
+
+namespace {
+
+using defk::cuda_fail;
+using defk::fail;
 
 constexpr int kThreads = 256;
 constexpr int kHostSlots = 3;  // staging slots of the host-memory path

@@ -1,0 +1,524 @@
+// C boundary of the operators around the step (see include/def_train.h): argument validation, kernel selection, launch.
+#include "../../include/def_train.h"
+#include "def_checkpoint_kernels.cuh"
+#include "def_error.cuh"
+#include "def_logprob_kernels.cuh"
+#include "def_norm_kernels.cuh"
+#include "def_weight_grad_kernels.cuh"
+
+#include <atomic>
+#include <cstring>
+
+namespace {
+
+using defk::cuda_fail;
+using defk::fail;
+
+constexpr int kMaxDevices = 64;
+
+// SMs of the current device; negative (an error code) if it cannot run these kernels.  The answer is looked up once
+// per device.
+int sm_count() {
+    static std::atomic<int> known[kMaxDevices];
+    int dev = -1;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
+        cudaGetLastError();
+        return fail(DEF_ERR_DEVICE, "no usable CUDA device: %s", cudaGetErrorString(err));
+    }
+    int sms = known[dev].load(std::memory_order_relaxed);
+    if (sms > 0) return sms;
+    int major = 0;
+    if ((err = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev)) != cudaSuccess ||
+        (err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) {
+        cudaGetLastError();
+        return fail(DEF_ERR_DEVICE, "cannot query device %d: %s", dev, cudaGetErrorString(err));
+    }
+    if (major != 10) return fail(DEF_ERR_DEVICE, "device %d is compute capability %d.x; this library is built for 10.x (sm_100a)", dev, major);
+    known[dev].store(sms, std::memory_order_relaxed);
+    return sms;
+}
+
+int element_size(int32_t dtype) { return dtype == DEF_DTYPE_F32 ? 4 : dtype == DEF_DTYPE_BF16 || dtype == DEF_DTYPE_F16 ? 2 : 0; }
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t q_stride(int64_t C) { return ceil_div(C, 16) * 16; }
+int64_t e_stride(int64_t C) { return ceil_div(ceil_div(C, deft::kGroup), 4) * 4; }
+
+// One tensor argument: `rows` runs of `width` bytes, `stride` bytes apart.
+struct View {
+    const void *p;
+    const char *name;
+    int64_t rows, width, stride;
+    unsigned align;
+    bool written;
+};
+
+bool share_bytes(const View &a, const View &b) {
+    if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
+    const uint64_t a0 = (uint64_t)(uintptr_t)a.p, b0 = (uint64_t)(uintptr_t)b.p;
+    const uint64_t a1 = a0 + (uint64_t)(a.rows - 1) * a.stride + a.width, b1 = b0 + (uint64_t)(b.rows - 1) * b.stride + b.width;
+    if (a1 <= b0 || b1 <= a0) return false;
+    if (a.stride != b.stride || a.width > a.stride || b.width > b.stride) return true;
+    const uint64_t s = (uint64_t)a.stride;           // how far b's columns start behind a's, in [0, s)
+    const int64_t d = (int64_t)(b0 >= a0 ? (b0 - a0) % s : (s - (a0 - b0) % s) % s);
+    return !(d >= a.width && d + b.width <= a.stride);      // column ranges of one buffer are apart
+}
+
+// Alignment, and that nothing written shares memory with another argument, except that the output `out` may be the
+// input `in`, row for row.
+template <int N> int check_views(const View (&v)[N], int in = -1, int out = -1) {
+    for (const View &a : v)
+        if (a.p && ((uintptr_t)a.p & (a.align - 1))) return fail(DEF_ERR_ALIGN, "%s is not %u-byte aligned", a.name, a.align);
+    for (int i = 0; i < N; ++i)
+        for (int j = i + 1; j < N; ++j)
+            if ((v[i].written || v[j].written) && share_bytes(v[i], v[j])) {
+                if (i == in && j == out && v[i].p == v[j].p && (v[i].stride == v[j].stride || v[i].rows == 1)) continue;
+                return fail(DEF_ERR_ALIAS, "%s and %s overlap", v[i].name, v[j].name);
+            }
+    return DEF_OK;
+}
+
+int check_rows(int32_t dtype, int64_t T, int64_t C, const char *width) {
+    if (!element_size(dtype)) return fail(DEF_ERR_ARG, "dtype must be one of DEF_DTYPE_F32, _BF16, _F16 (got %d)", dtype);
+    if (T < 0) return fail(DEF_ERR_ARG, "T must not be negative (got %lld)", (long long)T);
+    if (C < 1) return fail(DEF_ERR_ARG, "%s must be at least 1 (got %lld)", width, (long long)C);
+    if (T > ((int64_t)1 << 40) || C > ((int64_t)1 << 31) - 64) return fail(DEF_ERR_ARG, "T or %s is too large", width);
+    return DEF_OK;
+}
+int check_stride(const void *p, int64_t ld, int64_t C, const char *name) {
+    if (p && (ld < C || ld > (int64_t)1 << 40)) return fail(DEF_ERR_ARG, "the row stride of %s must be at least its width (got %lld)", name, (long long)ld);
+    return DEF_OK;
+}
+int check_pair(const void *q, const void *e, const char *name) {
+    if (!q != !e) return fail(DEF_ERR_NULL, "%s_q and %s_e must both be given or both be NULL", name, name);
+    return DEF_OK;
+}
+#define DEF_TRY(call) do { const int rc_ = (call); if (rc_ != DEF_OK) return rc_; } while (0)
+
+View rows_view(const void *p, const char *name, int64_t T, int64_t C, int64_t ld, int64_t es, bool written) {
+    return {p, name, T, C * es, ld * es, (unsigned)es, written};
+}
+View q_view(const void *p, const char *name, int64_t T, int64_t C, bool written) { return {p, name, T, C, q_stride(C), 16, written}; }
+View e_view(const void *p, const char *name, int64_t T, int64_t C, bool written) {
+    return {p, name, T, ceil_div(C, deft::kGroup), e_stride(C), 4, written};
+}
+View floats_view(const void *p, const char *name, int64_t n, bool written) { return {p, name, p ? 1 : 0, n * 4, n * 4, 4, written}; }
+
+// Whether rows of C elements at p, stride ld, can be read and written 8 elements at a time.
+bool wide(const void *p, int64_t ld, int64_t es) { return !p || (((uintptr_t)p & 15u) == 0 && ld * es % 16 == 0); }
+
+int launched(const char *what) {
+    const cudaError_t err = cudaGetLastError();
+    return err == cudaSuccess ? DEF_OK : cuda_fail(err, what);
+}
+
+// Calls f with a value of the element type.
+template <typename F> void by_dtype(int32_t dtype, F f) {
+    if (dtype == DEF_DTYPE_F32) f(float());
+    else if (dtype == DEF_DTYPE_BF16) f(__nv_bfloat16());
+    else f(__half());
+}
+
+template <int N> struct Width { static constexpr int value = N; };
+template <typename F> void by_width(bool eight, F f) {
+    if (eight) f(Width<8>());
+    else f(Width<1>());
+}
+
+// Grid of the kernels that work on rows by columns without sums: a warp lies in one row.
+struct Plane {
+    dim3 grid, block;
+};
+Plane plane(int64_t T, int64_t C, int V) {
+    const int64_t lanes = ceil_div(C, V);
+    unsigned bx = 32;
+    while (bx < 256 && bx < lanes) bx *= 2;
+    const unsigned by = 256 / bx;
+    const int64_t gy = ceil_div(T, by);
+    return {dim3((unsigned)ceil_div(lanes, bx), (unsigned)(gy < 65535 ? gy : 65535)), dim3(bx, by)};
+}
+
+}  // namespace
+
+extern "C" int def_checkpoint_layout(int64_t C, int64_t *ldq_out, int64_t *lde_out) {
+    if (!ldq_out || !lde_out) return fail(DEF_ERR_NULL, "ldq_out and lde_out must not be NULL");
+    if (C < 1 || C > ((int64_t)1 << 31) - 64) return fail(DEF_ERR_ARG, "C must be in [1, 2^31 - 64] (got %lld)", (long long)C);
+    *ldq_out = q_stride(C);
+    *lde_out = e_stride(C);
+    return DEF_OK;
+}
+
+extern "C" int def_checkpoint_pack(int32_t dtype, int64_t T, int64_t C, const void *x, int64_t ldx, int8_t *q, uint8_t *e,
+                                   void *cuda_stream) {
+    DEF_TRY(check_rows(dtype, T, C, "C"));
+    if (T == 0) return DEF_OK;
+    if (!x || !q || !e) return fail(DEF_ERR_NULL, "x, q and e must not be NULL");
+    DEF_TRY(check_stride(x, ldx, C, "x"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(x, "x", T, C, ldx, es, false), q_view(q, "q", T, C, true), e_view(e, "e", T, C, true)};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    const bool eight = C % 8 == 0 && wide(x, ldx, es);
+    by_dtype(dtype, [&](auto type) {
+        using E = decltype(type);
+        by_width(eight, [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            const Plane p = plane(T, C, V);
+            deft::pack_kernel<E, V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>((const E *)x, ldx, T, C, q, e, q_stride(C), e_stride(C));
+        });
+    });
+    return launched("def_checkpoint_pack");
+}
+
+extern "C" int def_checkpoint_unpack(int32_t dtype, int64_t T, int64_t C, const int8_t *q, const uint8_t *e, void *out,
+                                     int64_t ldout, void *cuda_stream) {
+    DEF_TRY(check_rows(dtype, T, C, "C"));
+    if (T == 0) return DEF_OK;
+    if (!out || !q || !e) return fail(DEF_ERR_NULL, "q, e and out must not be NULL");
+    DEF_TRY(check_stride(out, ldout, C, "out"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(out, "out", T, C, ldout, es, true), q_view(q, "q", T, C, false), e_view(e, "e", T, C, false)};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    const bool eight = C % 8 == 0 && wide(out, ldout, es);
+    by_dtype(dtype, [&](auto type) {
+        using E = decltype(type);
+        by_width(eight, [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            const Plane p = plane(T, C, V);
+            deft::unpack_kernel<E, V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>(q, e, q_stride(C), e_stride(C), T, C, (E *)out, ldout);
+        });
+    });
+    return launched("def_checkpoint_unpack");
+}
+
+extern "C" int def_gated_forward(int32_t dtype, int64_t T, int64_t F, const void *gate, int64_t ldg, const void *up, int64_t ldu,
+                                 void *h, int64_t ldh, int8_t *gate_q, uint8_t *gate_e, int8_t *up_q, uint8_t *up_e,
+                                 void *cuda_stream) {
+    DEF_TRY(check_rows(dtype, T, F, "F"));
+    if (T == 0) return DEF_OK;
+    if (!gate || !up || !h) return fail(DEF_ERR_NULL, "gate, up and h must not be NULL");
+    DEF_TRY(check_pair(gate_q, gate_e, "gate"));
+    DEF_TRY(check_pair(up_q, up_e, "up"));
+    DEF_TRY(check_stride(gate, ldg, F, "gate"));
+    DEF_TRY(check_stride(up, ldu, F, "up"));
+    DEF_TRY(check_stride(h, ldh, F, "h"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(gate, "gate", T, F, ldg, es, false), rows_view(up, "up", T, F, ldu, es, false),
+                          rows_view(h, "h", T, F, ldh, es, true), q_view(gate_q, "gate_q", T, F, true), e_view(gate_e, "gate_e", T, F, true),
+                          q_view(up_q, "up_q", T, F, true), e_view(up_e, "up_e", T, F, true)};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    deft::GatedForward a = {gate, up, h, ldg, ldu, ldh, gate_q, up_q, gate_e, up_e, T, F, q_stride(F), e_stride(F)};
+    const bool eight = F % 8 == 0 && wide(gate, ldg, es) && wide(up, ldu, es) && wide(h, ldh, es);
+    by_dtype(dtype, [&](auto type) {
+        by_width(eight, [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            const Plane p = plane(T, F, V);
+            deft::gated_forward_kernel<decltype(type), V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>(a);
+        });
+    });
+    return launched("def_gated_forward");
+}
+
+extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const void *dh, int64_t lddh, const int8_t *gate_q,
+                                  const uint8_t *gate_e, const int8_t *up_q, const uint8_t *up_e, void *dgate, int64_t lddg,
+                                  void *dup, int64_t lddu, void *h_out, int64_t ldh, int8_t *h_q, uint8_t *h_e, void *cuda_stream) {
+    DEF_TRY(check_rows(dtype, T, F, "F"));
+    if (T == 0) return DEF_OK;
+    if (!dh || !gate_q || !gate_e || !up_q || !up_e || !dgate || !dup)
+        return fail(DEF_ERR_NULL, "dh, the checkpoints of gate and up, dgate and dup must not be NULL");
+    DEF_TRY(check_pair(h_q, h_e, "h"));
+    DEF_TRY(check_stride(dh, lddh, F, "dh"));
+    DEF_TRY(check_stride(dgate, lddg, F, "dgate"));
+    DEF_TRY(check_stride(dup, lddu, F, "dup"));
+    DEF_TRY(check_stride(h_out, ldh, F, "h_out"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(dh, "dh", T, F, lddh, es, false), q_view(gate_q, "gate_q", T, F, false), e_view(gate_e, "gate_e", T, F, false),
+                          q_view(up_q, "up_q", T, F, false), e_view(up_e, "up_e", T, F, false), rows_view(dgate, "dgate", T, F, lddg, es, true),
+                          rows_view(dup, "dup", T, F, lddu, es, true), rows_view(h_out, "h_out", T, F, ldh, es, true),
+                          q_view(h_q, "h_q", T, F, true), e_view(h_e, "h_e", T, F, true)};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    deft::GatedBackward a = {dh, gate_q, up_q, gate_e, up_e, dgate, dup, h_out, lddh, lddg, lddu, ldh, h_q, h_e, T, F, q_stride(F), e_stride(F)};
+    const bool eight = F % 8 == 0 && wide(dh, lddh, es) && wide(dgate, lddg, es) && wide(dup, lddu, es) && wide(h_out, ldh, es);
+    by_dtype(dtype, [&](auto type) {
+        by_width(eight, [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            const Plane p = plane(T, F, V);
+            deft::gated_backward_kernel<decltype(type), V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>(a);
+        });
+    });
+    return launched("def_gated_backward");
+}
+
+// ---------------------------------------------------------------------------
+// Norms
+// ---------------------------------------------------------------------------
+namespace {
+
+template <int THREADS, int ITERS> struct Shape { static constexpr int threads = THREADS, iters = ITERS; };
+// Threads per row and accesses per thread for rows of C columns, V at a time.
+template <int V, typename F> void by_row_shape(int64_t C, F f) {
+    const int64_t n = ceil_div(C, V);
+    if constexpr (V == 8) {
+        if (n <= 32) f(Shape<32, 1>());
+        else if (n <= 128) f(Shape<128, 1>());
+        else if (n <= 256) f(Shape<256, 1>());
+        else if (n <= 512) f(Shape<256, 2>());
+        else if (n <= 1024) f(Shape<512, 2>());
+        else f(Shape<1024, 2>());
+    } else {
+        if (n <= 256) f(Shape<32, 8>());
+        else if (n <= 1024) f(Shape<128, 8>());
+        else if (n <= 4096) f(Shape<256, 16>());
+        else if (n <= 8192) f(Shape<512, 16>());
+        else f(Shape<1024, 16>());
+    }
+}
+
+int check_groups(int64_t T, int64_t groups) {
+    if (groups < 1 || T % groups) return fail(DEF_ERR_ARG, "groups must divide T (got %lld groups, %lld rows)", (long long)groups, (long long)T);
+    return DEF_OK;
+}
+
+// Parts per group of the backward pass (each part: one CTA, one row of partial sums): about kNormParts in all, at most
+// one per row.
+constexpr int64_t kNormParts = 592;
+int64_t norm_parts(int64_t T, int64_t groups) {
+    const int64_t rows = T / groups, want = ceil_div(kNormParts, groups);
+    return rows < want ? rows : want;
+}
+
+}  // namespace
+
+extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void *h, int64_t ldh, const void *b, int64_t ldb,
+                                const float *w_post, const float *gate, int64_t groups, const float *w_pre, float res_scale,
+                                float eps, void *h_out, int64_t ldho, void *n_out, int64_t ldn, float *rstd_post, float *rstd_pre,
+                                int8_t *b_q, uint8_t *b_e, int8_t *h_q, uint8_t *h_e, int8_t *n_q, uint8_t *n_e, void *cuda_stream) {
+    DEF_TRY(check_rows(dtype, T, C, "C"));
+    if (C > DEF_NORM_MAX_C) return fail(DEF_ERR_ARG, "C must be at most %d (got %lld)", DEF_NORM_MAX_C, (long long)C);
+    if (T == 0) return DEF_OK;
+    if (!h || !w_pre || !n_out || !rstd_pre) return fail(DEF_ERR_NULL, "h, w_pre, n_out and rstd_pre must not be NULL");
+    if (b && (!w_post || !h_out || !rstd_post)) return fail(DEF_ERR_NULL, "w_post, h_out and rstd_post must not be NULL where b is given");
+    if (!b && (w_post || gate || h_out || rstd_post || b_q || b_e))
+        return fail(DEF_ERR_ARG, "w_post, gate, h_out, rstd_post, b_q and b_e must be NULL where b is");
+    DEF_TRY(check_pair(b_q, b_e, "b"));
+    DEF_TRY(check_pair(h_q, h_e, "h"));
+    DEF_TRY(check_pair(n_q, n_e, "n"));
+    DEF_TRY(check_groups(T, groups));
+    if (!(eps >= 0.f) || !(eps <= 1e30f)) return fail(DEF_ERR_ARG, "eps must be a finite number that is not negative");
+    DEF_TRY(check_stride(h, ldh, C, "h"));
+    DEF_TRY(check_stride(b, ldb, C, "b"));
+    DEF_TRY(check_stride(h_out, ldho, C, "h_out"));
+    DEF_TRY(check_stride(n_out, ldn, C, "n_out"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(h, "h", T, C, ldh, es, false), rows_view(b, "b", T, C, ldb, es, false),
+                          floats_view(w_post, "w_post", C, false), floats_view(gate, "gate", groups * C, false), floats_view(w_pre, "w_pre", C, false),
+                          rows_view(h_out, "h_out", T, C, ldho, es, true), rows_view(n_out, "n_out", T, C, ldn, es, true),
+                          floats_view(rstd_post, "rstd_post", T, true), floats_view(rstd_pre, "rstd_pre", T, true),
+                          q_view(b_q, "b_q", T, C, true), e_view(b_e, "b_e", T, C, true), q_view(h_q, "h_q", T, C, true), e_view(h_e, "h_e", T, C, true),
+                          q_view(n_q, "n_q", T, C, true), e_view(n_e, "n_e", T, C, true)};
+    DEF_TRY(check_views(views, 0, 5));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    deft::NormForward a;
+    a.h = h; a.b = b; a.h_out = h_out; a.n_out = n_out;
+    a.ldh = ldh; a.ldb = ldb; a.ldho = ldho; a.ldn = ldn;
+    a.w_post = w_post; a.gate = gate; a.w_pre = w_pre; a.rstd_post = rstd_post; a.rstd_pre = rstd_pre;
+    a.hb = {b_q, b_e}; a.hh = {h_q, h_e}; a.hn = {n_q, n_e};
+    a.T = T; a.C = C; a.rows_per_group = T / groups; a.ldq = q_stride(C); a.lde = e_stride(C);
+    a.res_scale = res_scale; a.eps = eps; a.inv_C = 1.f / (float)C;
+    const bool eight = C % 8 == 0 && wide(h, ldh, es) && wide(b, ldb, es) && wide(h_out, ldho, es) && wide(n_out, ldn, es);
+    by_dtype(dtype, [&](auto type) {
+        by_width(eight, [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            by_row_shape<V>(C, [&](auto shape) {
+                using S = decltype(shape);
+                const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
+                deft::norm_forward_kernel<decltype(type), V, S::threads, S::iters><<<grid, S::threads, 0, (cudaStream_t)cuda_stream>>>(a);
+            });
+        });
+    });
+    return launched("def_norm_forward");
+}
+
+extern "C" int def_norm_backward_workspace(int64_t T, int64_t C, int64_t groups, int64_t *bytes_out) {
+    if (!bytes_out) return fail(DEF_ERR_NULL, "bytes_out must not be NULL");
+    DEF_TRY(check_rows(DEF_DTYPE_F32, T, C, "C"));
+    if (C > DEF_NORM_MAX_C) return fail(DEF_ERR_ARG, "C must be at most %d (got %lld)", DEF_NORM_MAX_C, (long long)C);
+    DEF_TRY(check_groups(T, groups));
+    *bytes_out = groups * norm_parts(T, groups) * 2 * C * (int64_t)sizeof(float);
+    return DEF_OK;
+}
+
+extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void *dn, int64_t lddn, const void *dh_in, int64_t lddhi,
+                                 const void *h, int64_t ldh, const int8_t *h_q, const uint8_t *h_e, const void *b, int64_t ldb,
+                                 const int8_t *b_q, const uint8_t *b_e, const float *w_post, const float *gate, int64_t groups,
+                                 const float *w_pre, float res_scale, const float *rstd_post, const float *rstd_pre, void *dh,
+                                 int64_t lddh, void *db, int64_t lddb, float *dw_post, float *dgate, float *dw_pre, int32_t accumulate,
+                                 void *workspace, int64_t workspace_bytes, void *cuda_stream) {
+    int64_t need = 0;
+    if (!element_size(dtype)) return fail(DEF_ERR_ARG, "dtype must be one of DEF_DTYPE_F32, _BF16, _F16 (got %d)", dtype);
+    DEF_TRY(def_norm_backward_workspace(T, C, groups, &need));
+    DEF_TRY(check_pair(h_q, h_e, "h"));
+    DEF_TRY(check_pair(b_q, b_e, "b"));
+    const bool has_b = b || b_q;
+    if (!w_pre || !dw_pre) return fail(DEF_ERR_NULL, "w_pre and dw_pre must not be NULL");
+    if (T > 0 && (!dn || (!h && !h_q) || !rstd_pre || !dh)) return fail(DEF_ERR_NULL, "dn, h (or its checkpoint), rstd_pre and dh must not be NULL");
+    if ((h && h_q) || (b && b_q)) return fail(DEF_ERR_ARG, "h and b are given as values or as a checkpoint, not both");
+    if (has_b && (!w_post || !rstd_post || !db || !dw_post)) return fail(DEF_ERR_NULL, "w_post, rstd_post, db and dw_post must not be NULL where b is given");
+    if (has_b && !gate != !dgate) return fail(DEF_ERR_NULL, "gate and dgate must both be given or both be NULL");
+    if (!has_b && T > 0 && (w_post || gate || rstd_post || db || dw_post || dgate))
+        return fail(DEF_ERR_ARG, "w_post, gate, rstd_post, db, dw_post and dgate must be NULL where b is");
+    if (T > 0 && !workspace) return fail(DEF_ERR_NULL, "workspace must not be NULL");
+    if (workspace_bytes < need) return fail(DEF_ERR_ARG, "the workspace must have %lld bytes (got %lld)", (long long)need, (long long)workspace_bytes);
+    DEF_TRY(check_stride(dn, lddn, C, "dn"));
+    DEF_TRY(check_stride(dh_in, lddhi, C, "dh_in"));
+    DEF_TRY(check_stride(h, ldh, C, "h"));
+    DEF_TRY(check_stride(b, ldb, C, "b"));
+    DEF_TRY(check_stride(dh, lddh, C, "dh"));
+    DEF_TRY(check_stride(db, lddb, C, "db"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(dn, "dn", T, C, lddn, es, false), rows_view(dh_in, "dh_in", T, C, lddhi, es, false),
+                          rows_view(h, "h", T, C, ldh, es, false), rows_view(b, "b", T, C, ldb, es, false),
+                          q_view(h_q, "h_q", T, C, false), e_view(h_e, "h_e", T, C, false), q_view(b_q, "b_q", T, C, false), e_view(b_e, "b_e", T, C, false),
+                          floats_view(w_post, "w_post", C, false), floats_view(gate, "gate", groups * C, false), floats_view(w_pre, "w_pre", C, false),
+                          floats_view(rstd_post, "rstd_post", T, false), floats_view(rstd_pre, "rstd_pre", T, false),
+                          rows_view(dh, "dh", T, C, lddh, es, true), rows_view(db, "db", T, C, lddb, es, true),
+                          floats_view(dw_post, "dw_post", C, true), floats_view(dgate, "dgate", groups * C, true), floats_view(dw_pre, "dw_pre", C, true),
+                          {workspace, "workspace", workspace ? 1 : 0, need, need, 16, true}};
+    DEF_TRY(check_views(views, 1, 13));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (T == 0) {
+        cudaError_t err = cudaSuccess;
+        if (!accumulate) {
+            err = cudaMemsetAsync(dw_pre, 0, (size_t)C * 4, stream);
+            if (err == cudaSuccess && dw_post) err = cudaMemsetAsync(dw_post, 0, (size_t)C * 4, stream);
+            if (err == cudaSuccess && dgate) err = cudaMemsetAsync(dgate, 0, (size_t)(groups * C) * 4, stream);
+        }
+        return err == cudaSuccess ? DEF_OK : cuda_fail(err, "def_norm_backward");
+    }
+    deft::NormBackward a;
+    a.dn = dn; a.dh_in = dh_in; a.h = h; a.b = b; a.hh = {h_q, h_e}; a.hb = {b_q, b_e}; a.dh = dh; a.db = db;
+    a.lddn = lddn; a.lddhi = lddhi; a.ldh = ldh; a.ldb = ldb; a.lddh = lddh; a.lddb = lddb;
+    a.w_post = w_post; a.gate = gate; a.w_pre = w_pre; a.rstd_post = rstd_post; a.rstd_pre = rstd_pre;
+    a.partial = (float *)workspace;
+    a.T = T; a.C = C; a.rows_per_group = T / groups; a.ldq = q_stride(C); a.lde = e_stride(C);
+    a.parts_per_group = norm_parts(T, groups);
+    a.res_scale = res_scale; a.inv_C = 1.f / (float)C;
+    const int64_t parts = groups * a.parts_per_group;
+    if (parts > 0x7fffffff) return fail(DEF_ERR_ARG, "problem too large for one grid");
+    const bool eight = C % 8 == 0 && wide(dn, lddn, es) && wide(dh_in, lddhi, es) && wide(h, ldh, es) && wide(b, ldb, es) && wide(dh, lddh, es) && wide(db, lddb, es);
+    by_dtype(dtype, [&](auto type) {
+        by_width(eight, [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            by_row_shape<V>(C, [&](auto shape) {
+                using S = decltype(shape);
+                deft::norm_backward_kernel<decltype(type), V, S::threads, S::iters><<<(unsigned)parts, S::threads, 0, stream>>>(a);
+            });
+        });
+    });
+    DEF_TRY(launched("def_norm_backward"));
+    deft::norm_reduce_kernel<<<(unsigned)ceil_div(C, 32), dim3(32, 32), 0, stream>>>((const float *)workspace, w_post, gate, C, groups, a.parts_per_group,
+                                                                                      has_b, accumulate, dw_post, dgate, dw_pre);
+    return launched("def_norm_backward (sums)");
+}
+
+// ---------------------------------------------------------------------------
+// Weight gradient
+// ---------------------------------------------------------------------------
+extern "C" int def_checkpoint_weight_grad_workspace(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *dy, int64_t lddy,
+                                                    int64_t *bytes_out) {
+    if (!bytes_out) return fail(DEF_ERR_NULL, "bytes_out must not be NULL");
+    DEF_TRY(check_rows(dtype, T, O, "O"));
+    DEF_TRY(check_rows(dtype, T, I, "I"));
+    DEF_TRY(check_stride(dy, lddy, O, "dy"));
+    *bytes_out = 0;
+    return DEF_OK;
+}
+
+extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *dy, int64_t lddy, const int8_t *q,
+                                          const uint8_t *e, float *dw, int32_t accumulate, void *workspace, int64_t workspace_bytes,
+                                          void *cuda_stream) {
+    int64_t need = 0;
+    DEF_TRY(def_checkpoint_weight_grad_workspace(dtype, T, O, I, dy, lddy, &need));
+    if (!dw || (T > 0 && (!dy || !q || !e))) return fail(DEF_ERR_NULL, "dy, q, e and dw must not be NULL");
+    if (need > 0 && !workspace) return fail(DEF_ERR_NULL, "workspace must not be NULL");
+    if (workspace_bytes < need) return fail(DEF_ERR_ARG, "the workspace must have %lld bytes (got %lld)", (long long)need, (long long)workspace_bytes);
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(dy, "dy", T, O, lddy, es, false), q_view(q, "q", T, I, false), e_view(e, "e", T, I, false),
+                          floats_view(dw, "dw", O * I, true), {workspace, "workspace", need > 0 ? 1 : 0, need, need, 16, true}};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (T == 0) {
+        if (accumulate) return DEF_OK;
+        const cudaError_t err = cudaMemsetAsync(dw, 0, (size_t)(O * I) * 4, stream);
+        return err == cudaSuccess ? DEF_OK : cuda_fail(err, "def_checkpoint_weight_grad");
+    }
+    by_dtype(dtype, [&](auto type) {
+        using E = decltype(type);
+        const dim3 grid((unsigned)ceil_div(I, 64), (unsigned)ceil_div(O, 64));
+        deft::weight_grad_simple_kernel<E><<<grid, 256, 0, stream>>>((const E *)dy, lddy, q, e, q_stride(I), e_stride(I), T, O, I, dw, accumulate);
+    });
+    return launched("def_checkpoint_weight_grad");
+}
+
+// ---------------------------------------------------------------------------
+// Log probabilities
+// ---------------------------------------------------------------------------
+extern "C" int def_logprob_forward(int32_t dtype, int64_t T, int64_t V, const void *logits, int64_t ldx, const int64_t *targets,
+                                   float *logp, float *entropy, float *lse, int32_t top, int64_t *top_ids, float *top_logp,
+                                   void *cuda_stream) {
+    DEF_TRY(check_rows(dtype, T, V, "V"));
+    if (top < 0 || top > DEF_LOGPROB_MAX_TOP || top > V) return fail(DEF_ERR_ARG, "top must be in [0, min(V, %d)] (got %d)", DEF_LOGPROB_MAX_TOP, top);
+    if (T == 0) return DEF_OK;
+    if (!logits || !targets || !logp || !entropy || !lse) return fail(DEF_ERR_NULL, "logits, targets, logp, entropy and lse must not be NULL");
+    if ((top > 0) != (top_ids != nullptr) || (top > 0) != (top_logp != nullptr)) return fail(DEF_ERR_NULL, "top_ids and top_logp must be given if and only if top > 0");
+    DEF_TRY(check_stride(logits, ldx, V, "logits"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(logits, "logits", T, V, ldx, es, false), {targets, "targets", 1, T * 8, T * 8, 8, false},
+                          floats_view(logp, "logp", T, true), floats_view(entropy, "entropy", T, true), floats_view(lse, "lse", 2 * T, true),
+                          {top_ids, "top_ids", top_ids ? 1 : 0, T * top * 8, T * top * 8, 8, true}, floats_view(top_logp, "top_logp", T * top, true)};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    deft::LogprobForward a = {logits, ldx, T, V, targets, logp, entropy, lse, top_ids, top_logp, top};
+    const bool eight = V % 8 == 0 && wide(logits, ldx, es);
+    by_dtype(dtype, [&](auto type) {
+        by_width(eight, [&](auto width) {
+            const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
+            deft::logprob_forward_kernel<decltype(type), decltype(width)::value, 512><<<grid, 512, 0, (cudaStream_t)cuda_stream>>>(a);
+        });
+    });
+    return launched("def_logprob_forward");
+}
+
+extern "C" int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const void *logits, int64_t ldx, const int64_t *targets,
+                                    const float *lse, const float *entropy, const float *dlogp, const float *dentropy, int32_t top,
+                                    const int64_t *top_ids, const float *dtop_logp, void *dlogits, int64_t lddx, void *cuda_stream) {
+    DEF_TRY(check_rows(dtype, T, V, "V"));
+    if (top < 0 || top > DEF_LOGPROB_MAX_TOP || top > V) return fail(DEF_ERR_ARG, "top must be in [0, min(V, %d)] (got %d)", DEF_LOGPROB_MAX_TOP, top);
+    if (T == 0) return DEF_OK;
+    if (!logits || !targets || !lse || !entropy || !dlogits) return fail(DEF_ERR_NULL, "logits, targets, lse, entropy and dlogits must not be NULL");
+    if ((top > 0) != (top_ids != nullptr) || (top > 0) != (dtop_logp != nullptr)) return fail(DEF_ERR_NULL, "top_ids and dtop_logp must be given if and only if top > 0");
+    DEF_TRY(check_stride(logits, ldx, V, "logits"));
+    DEF_TRY(check_stride(dlogits, lddx, V, "dlogits"));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(logits, "logits", T, V, ldx, es, false), rows_view(dlogits, "dlogits", T, V, lddx, es, true),
+                          {targets, "targets", 1, T * 8, T * 8, 8, false}, floats_view(lse, "lse", 2 * T, false), floats_view(entropy, "entropy", T, false),
+                          floats_view(dlogp, "dlogp", T, false), floats_view(dentropy, "dentropy", T, false),
+                          {top_ids, "top_ids", top_ids ? 1 : 0, T * top * 8, T * top * 8, 8, false}, floats_view(dtop_logp, "dtop_logp", T * top, false)};
+    DEF_TRY(check_views(views, 0, 1));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    deft::LogprobBackward a = {logits, dlogits, ldx, lddx, T, V, targets, top_ids, lse, entropy, dlogp, dentropy, dtop_logp, top};
+    const bool eight = V % 8 == 0 && wide(logits, ldx, es) && wide(dlogits, lddx, es);
+    by_dtype(dtype, [&](auto type) {
+        by_width(eight, [&](auto width) {
+            const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
+            deft::logprob_backward_kernel<decltype(type), decltype(width)::value, 512><<<grid, 512, 0, (cudaStream_t)cuda_stream>>>(a);
+        });
+    });
+    return launched("def_logprob_backward");
+}
