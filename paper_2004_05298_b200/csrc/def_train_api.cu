@@ -9,6 +9,8 @@
 #include <atomic>
 #include <cstring>
 
+#include <cuda.h>
+
 namespace {
 
 using defk::cuda_fail;
@@ -429,13 +431,64 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
 // ---------------------------------------------------------------------------
 // Weight gradient
 // ---------------------------------------------------------------------------
+namespace {
+
+// What a call launches and keeps in its workspace: partial tiles first, then the 16-bit pieces of dy.
+struct GradPlan {
+    bool copy_dy;
+    int planes, ctas;
+    bool split;
+    int64_t ld_planes, partial_bytes, plane_bytes;
+    int64_t tiles_i, tiles_o, blocks;
+};
+GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *dy, int64_t lddy, int sms) {
+    GradPlan p;
+    const int es = element_size(dtype);
+    p.copy_dy = es == 4 || !wide(dy, lddy, es);
+    p.planes = es == 4 ? 3 : 1;
+    p.ld_planes = ceil_div(O, 8) * 8;
+    p.plane_bytes = p.copy_dy ? p.planes * T * p.ld_planes * 2 : 0;
+    p.tiles_i = ceil_div(I, deft::kTileI);
+    p.tiles_o = ceil_div(O, deft::kTileO);
+    p.blocks = ceil_div(T, deft::kTileT);
+    // One CTA per SM.  Whole tiles while they fill the last round of CTAs well; otherwise the blocks of all tiles are cut
+    // into equal runs, which costs a pass over the shared tiles' partial sums.
+    const int64_t tiles = p.tiles_i * p.tiles_o, rounds = ceil_div(tiles, sms);
+    p.split = p.blocks * p.planes > 1 && tiles * 10 < rounds * sms * 9;
+    const int64_t most = p.split ? tiles * p.blocks * p.planes : tiles;
+    p.ctas = (int)(most < sms ? most : sms);
+    p.partial_bytes = p.split ? (int64_t)p.ctas * 2 * deft::kTileO * deft::kTileI * 4 : 0;
+    return p;
+}
+constexpr int kUsualSms = 148;      // what a workspace is sized for before a device is looked at
+
+// The driver's entry point for tensor maps, found at run time: the library itself does not link the driver.
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static std::atomic<void *> known{nullptr};
+    void *f = known.load();
+    if (f) return (EncodeTiled)f;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+        return nullptr;
+    known.store(f);
+    return (EncodeTiled)f;
+}
+
+}  // namespace
+
 extern "C" int def_checkpoint_weight_grad_workspace(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *dy, int64_t lddy,
                                                     int64_t *bytes_out) {
     if (!bytes_out) return fail(DEF_ERR_NULL, "bytes_out must not be NULL");
     DEF_TRY(check_rows(dtype, T, O, "O"));
     DEF_TRY(check_rows(dtype, T, I, "I"));
     DEF_TRY(check_stride(dy, lddy, O, "dy"));
-    *bytes_out = 0;
+    if (T >= (int64_t)1 << 31) return fail(DEF_ERR_ARG, "T must be below 2^31 (got %lld)", (long long)T);
+    const GradPlan p = grad_plan(dtype, T, O, I, dy, lddy, kUsualSms);
+    *bytes_out = p.partial_bytes + p.plane_bytes;
     return DEF_OK;
 }
 
@@ -458,12 +511,46 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         const cudaError_t err = cudaMemsetAsync(dw, 0, (size_t)(O * I) * 4, stream);
         return err == cudaSuccess ? DEF_OK : cuda_fail(err, "def_checkpoint_weight_grad");
     }
-    by_dtype(dtype, [&](auto type) {
-        using E = decltype(type);
-        const dim3 grid((unsigned)ceil_div(I, 64), (unsigned)ceil_div(O, 64));
-        deft::weight_grad_simple_kernel<E><<<grid, 256, 0, stream>>>((const E *)dy, lddy, q, e, q_stride(I), e_stride(I), T, O, I, dw, accumulate);
-    });
-    return launched("def_checkpoint_weight_grad");
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return fail(DEF_ERR_CUDA, "the driver does not offer tensor maps");
+    // The plan the workspace was sized by, on as many CTAs as the device has SMs for.
+    GradPlan p = grad_plan(dtype, T, O, I, dy, lddy, kUsualSms);
+    const bool half = dtype == DEF_DTYPE_F16;
+    const void *rows = dy;
+    int64_t ld = lddy;
+    if (p.copy_dy) {
+        void *planes = (char *)workspace + p.partial_bytes;
+        const int64_t want = ceil_div(T * O, 256);
+        const unsigned grid = (unsigned)(want < 148 * 32 ? want : 148 * 32);
+        if (es == 4)
+            deft::weight_grad_planes_kernel<float, __nv_bfloat16><<<grid, 256, 0, stream>>>((const float *)dy, lddy, T, O, (__nv_bfloat16 *)planes, p.ld_planes);
+        else
+            deft::weight_grad_planes_kernel<uint16_t, uint16_t><<<grid, 256, 0, stream>>>((const uint16_t *)dy, lddy, T, O, (uint16_t *)planes, p.ld_planes);
+        DEF_TRY(launched("def_checkpoint_weight_grad (copy)"));
+        rows = planes;
+        ld = p.ld_planes;
+    }
+    CUtensorMap map_y, map_q;
+    const cuuint64_t dim_y[3] = {(cuuint64_t)O, (cuuint64_t)T, (cuuint64_t)p.planes}, stride_y[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)T};
+    const cuuint32_t box_y[3] = {64, deft::kTileT, 1}, one[3] = {1, 1, 1};
+    const cuuint64_t dim_q[2] = {(cuuint64_t)I, (cuuint64_t)T}, stride_q[1] = {(cuuint64_t)q_stride(I)};
+    const cuuint32_t box_q[2] = {deft::kTileI, deft::kTileT};
+    if (encode(&map_y, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(rows), dim_y, stride_y, box_y, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+        encode(&map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(q), dim_q, stride_q, box_q, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return fail(DEF_ERR_CUDA, "the driver refused a tensor map of dy or q");
+    deft::WeightGrad a = {e, dw, (float *)workspace, T, O, I, e_stride(I), (int)p.tiles_i, (int)p.tiles_o, (int)p.blocks, p.planes, accumulate, p.split};
+    const auto kernel = half ? deft::weight_grad_kernel<__half> : deft::weight_grad_kernel<__nv_bfloat16>;
+    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, deft::kGradSmem);
+    if (err != cudaSuccess) return cuda_fail(err, "def_checkpoint_weight_grad");
+    kernel<<<(unsigned)p.ctas, deft::kGradThreads, deft::kGradSmem, stream>>>(a, map_y, map_q);
+    DEF_TRY(launched("def_checkpoint_weight_grad"));
+    if (p.split) {
+        deft::weight_grad_join_kernel<<<(unsigned)(p.tiles_i * p.tiles_o * (deft::kTileO / 8)), 256, 0, stream>>>(a, p.ctas);
+        DEF_TRY(launched("def_checkpoint_weight_grad (join)"));
+    }
+    return DEF_OK;
 }
 
 // ---------------------------------------------------------------------------

@@ -1,41 +1,361 @@
 // Weight gradient of a linear layer from the 8-bit checkpoint of its input (see include/def_train.h).
+//
+//     dw[o, i] = sum_t dy[t, o] x^[t, i],     x^ = q 2^k
+//
+// Tensor cores (tcgen05), D = A B with A = x^ (M runs over i), B = dy (N runs over o), k over tokens: both operands lie
+// in memory with M resp. N consecutive, which is how they are fed; D's lanes are i, so that a store of one column of D
+// is 128 consecutive floats of a row of dw, whatever dw's alignment.  q 2^k is exact in bf16, products are exact, and the
+// accumulator in tensor memory is emptied into fp32 registers every kChunk blocks of tokens: the matrix unit truncates
+// when it accumulates, and a short chain keeps that below the rounding of plain fp32 sums.
 #pragma once
 
+#include <cuda.h>
+
+#include "def_sm100.cuh"
 #include "def_train_common.cuh"
 
 namespace deft {
 
-// dw[o, i] (+)= sum_t dy[t, o] x^[t, i].  CTA: 64 x 64 of dw, 16 tokens at a time through shared memory.
-template <typename T>
-__global__ void __launch_bounds__(256) weight_grad_simple_kernel(const T *__restrict__ dy, int64_t lddy, const int8_t *__restrict__ q,
-                                                                 const uint8_t *__restrict__ e, int64_t ldq, int64_t lde, int64_t tokens,
-                                                                 int64_t O, int64_t I, float *dw, int accumulate) {
-    __shared__ float sy[16][64], sx[16][64];
-    const int64_t o0 = (int64_t)blockIdx.y * 64, i0 = (int64_t)blockIdx.x * 64;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    for (int64_t t0 = 0; t0 < tokens; t0 += 16) {
-        for (int k = threadIdx.x; k < 1024; k += 256) {
-            const int64_t t = t0 + k / 64, o = o0 + k % 64, i = i0 + k % 64;
-            sy[k / 64][k % 64] = t < tokens && o < O ? to_float<T>(dy[t * lddy + o]) : 0.f;
-            float x = 0.f;
-            if (t < tokens && i < I) x = to_float<T>(from_float<T>((float)q[t * ldq + i] * group_scale(e[t * lde + i / kGroup])));
-            sx[k / 64][k % 64] = x;
+constexpr int kTileI = 128, kTileO = 256, kTileT = 64;      // of one accumulator, and tokens per pipeline stage
+constexpr int kGradStages = 4, kGradThreads = 512;
+constexpr int kChunk = 8;                                    // stages per accumulator hand-over
+constexpr int kBytesA = kTileI * kTileT * 2, kBytesB = kTileO * kTileT * 2, kBytesQ = kTileI * kTileT, kBytesE = kTileT * 4;
+constexpr int kBarrierBytes = 1024;
+constexpr int kGradSmem = kBarrierBytes + 1024 + kGradStages * (kBytesA + kBytesB + kBytesQ + kBytesE);
+
+struct WeightGrad {
+    const uint8_t *e;
+    float *dw, *partial;                  // partial: [CTA][2][kTileO][kTileI]
+    int64_t tokens, O, I, lde;
+    int tiles_i, tiles_o, blocks, planes; // blocks: of kTileT tokens, per plane of dy
+    int accumulate, split;                // split: CTAs share tiles (contiguous ranges of all tiles' blocks)
+};
+
+// The pieces of work of one CTA: (tile, blocks [k0, k1)).  Split: an equal run of the blocks of all tiles in order; a
+// tile that is cut goes to partial slot 0 of the CTAs that do not hold its first block, slot 1 of the one that does.
+struct Pieces {
+    int64_t pos, end, step, per_tile;
+    bool split;
+    __device__ Pieces(const WeightGrad &a) {
+        per_tile = (int64_t)a.blocks * a.planes;
+        split = a.split;
+        const int64_t tiles = (int64_t)a.tiles_i * a.tiles_o;
+        if (split) {
+            const int64_t all = tiles * per_tile;
+            pos = all * blockIdx.x / gridDim.x;
+            end = all * (blockIdx.x + 1) / gridDim.x;
+        } else {
+            pos = blockIdx.x;
+            end = tiles;
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(sy[k][ty * 4 + a], sx[k][tx + 16 * b], acc[a][b]);
-        __syncthreads();
     }
-    for (int a = 0; a < 4; ++a)
-        for (int b = 0; b < 4; ++b) {
-            const int64_t o = o0 + ty * 4 + a, i = i0 + tx + 16 * b;
-            if (o < O && i < I) dw[o * I + i] = accumulate ? dw[o * I + i] + acc[a][b] : acc[a][b];
+    __device__ bool next(int64_t &tile, int &k0, int &k1) {
+        if (pos >= end) return false;
+        if (split) {
+            tile = pos / per_tile;
+            k0 = (int)(pos - tile * per_tile);
+            k1 = (int)(end - tile * per_tile < per_tile ? end - tile * per_tile : per_tile);
+            pos += k1 - k0;
+        } else {
+            tile = pos;
+            k0 = 0;
+            k1 = (int)per_tile;
+            pos += gridDim.x;
         }
+        return true;
+    }
+};
+
+// Tiles in bands of 8 along o, so that the CTAs at work at one time share rows of dy and of q in the L2.
+__device__ __forceinline__ void tile_place(const WeightGrad &a, int64_t tile, int &i0, int &o0) {
+    const int64_t band = tile / (8LL * a.tiles_i), r = tile - band * 8 * a.tiles_i;
+    const int wide = (int)(a.tiles_o - band * 8 < 8 ? a.tiles_o - band * 8 : 8);
+    i0 = (int)(r / wide) * kTileI;
+    o0 = (int)(band * 8 + r % wide) * kTileO;
+}
+
+// 16 bytes of q times 2^k as 16-bit floats.
+template <typename T> __device__ __forceinline__ void widen16(uint4 q, uint32_t e, uint4 &lo, uint4 &hi) {
+    const uint32_t in[4] = {q.x, q.y, q.z, q.w};
+    uint32_t out[8];
+    if constexpr (sizeof(T) == 2 && !__is_same(T, __half)) {
+        // q = (low 7 bits + 128) - (128 or 256), both exact bf16 numbers made by bit operations
+        const uint32_t s = e << 7 | e << 23;
+        __nv_bfloat162 scale;
+        memcpy(&scale, &s, 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t two = __byte_perm(in[i / 2], 0, i % 2 ? 0x4342 : 0x4140);
+            const uint32_t a = (two & 0x007f007fu) | 0x43004300u, b = (two & 0x00800080u) | 0x43004300u;
+            __nv_bfloat162 x, y;
+            memcpy(&x, &a, 4);
+            memcpy(&y, &b, 4);
+            x = __hmul2(__hsub2(x, y), scale);
+            memcpy(&out[i], &x, 4);
+        }
+    } else {
+        const float scale = group_scale(e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int a = (int)(int8_t)(in[i / 2] >> (i % 2 * 16)), b = (int)(int8_t)(in[i / 2] >> (i % 2 * 16 + 8));
+            const __half2 x = __floats2half2_rn((float)a * scale, (float)b * scale);
+            memcpy(&out[i], &x, 4);
+        }
+    }
+    lo = make_uint4(out[0], out[1], out[2], out[3]);
+    hi = make_uint4(out[4], out[5], out[6], out[7]);
+}
+
+// Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread), 2 and 3 fetch exponents, 4-7 widen q,
+// 8-15 empty accumulators and store.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads, 1)
+    weight_grad_kernel(const WeightGrad a, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_q) {
+    extern __shared__ uint8_t raw[];
+    uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *sa = base, *sb = sa + kGradStages * kBytesA, *sq = sb + kGradStages * kBytesB, *se = sq + kGradStages * kBytesQ;
+    uint64_t *bars = (uint64_t *)(se + kGradStages * kBytesE);
+    const uint32_t full = smem_address(bars), ready = full + 8 * kGradStages, empty = ready + 8 * kGradStages, acc_full = empty + 8 * kGradStages,
+                   acc_empty = acc_full + 16, drained = acc_empty + 16;
+    uint32_t *tmem_slot = (uint32_t *)(bars + 3 * kGradStages + 5);
+    volatile int *failed = (volatile int *)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kGradStages; ++s) {
+            barrier_init(full + 8 * s, 1 + 64);
+            barrier_init(ready + 8 * s, 128);
+            barrier_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            barrier_init(acc_full + 8 * b, 1);
+            barrier_init(acc_empty + 8 * b, 256);
+        }
+        barrier_init(drained, 1);
+        *failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        __syncwarp();
+        tmem_alloc<512>(smem_address(tmem_slot));
+    }
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    Pieces work(a);
+    int64_t tile;
+    int k0, k1, i0, o0;
+
+    if (warp < 4) {
+        registers_down<64>();
+        if (warp == 0 && lane == 0) {
+            prefetch_map(&map_y);
+            prefetch_map(&map_q);
+            uint32_t n = 0;
+            bool ok = true;
+            while (ok && work.next(tile, k0, k1)) {
+                tile_place(a, tile, i0, o0);
+                for (int k = k0; k < k1; ++k, ++n) {
+                    const uint32_t s = n % kGradStages, round = n / kGradStages;
+                    if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
+                    const int plane = k / a.blocks, t0 = (k - plane * a.blocks) * kTileT;
+                    const uint32_t bar = full + 8 * s;
+                    barrier_expect(bar, kBytesB + kBytesQ);
+                    tensor_load_2d(smem_address(sq + s * kBytesQ), &map_q, i0, t0, bar);
+#pragma unroll
+                    for (int j = 0; j < kTileO / 64; ++j)
+                        tensor_load_3d(smem_address(sb + s * kBytesB + j * (kTileT * 128)), &map_y, o0 + 64 * j, t0, plane, bar);
+                }
+            }
+            // the copies in flight end before the CTA does
+            const uint64_t start = nanoseconds();
+            for (uint32_t m = n > kGradStages ? n - kGradStages : 0; m < n; ++m)
+                while (!barrier_try(full + 8 * (m % kGradStages), (m / kGradStages) & 1) && nanoseconds() - start < kWaitLimit) {}
+        } else if (warp == 1 && lane == 0) {
+            constexpr uint32_t idesc = instruction_descriptor(!__is_same(T, __half), kTileI, kTileO);
+            uint32_t n = 0, chunk = 0;
+            bool ok = true;
+            while (ok && work.next(tile, k0, k1)) {
+                for (int k = k0; k < k1 && ok; ++chunk) {
+                    const uint32_t buf = chunk & 1, round = chunk >> 1;
+                    if (!(ok = barrier_wait(acc_empty + 8 * buf, (round & 1) ^ 1, failed))) break;
+                    tmem_fence_after();
+                    const int stop = k + kChunk < k1 ? k + kChunk : k1;
+                    for (int first = k; k < stop; ++k, ++n) {
+                        const uint32_t s = n % kGradStages, parity = (n / kGradStages) & 1;
+                        if (!(ok = barrier_wait(full + 8 * s, parity, failed) && barrier_wait(ready + 8 * s, parity, failed))) break;
+                        tmem_fence_after();
+                        const uint64_t da = operand_descriptor(smem_address(sa + s * kBytesA), kTileT * 128);
+                        const uint64_t db = operand_descriptor(smem_address(sb + s * kBytesB), kTileT * 128);
+#pragma unroll
+                        for (int j = 0; j < kTileT / 16; ++j)     // 16 tokens each: 2048 bytes further along k
+                            mma(tmem + buf * kTileO, da + j * (2048 >> 4), db + j * (2048 >> 4), idesc, k > first || j > 0);
+                        mma_commit(empty + 8 * s);
+                    }
+                    if (ok) mma_commit(acc_full + 8 * buf);
+                }
+            }
+            mma_commit(drained);
+            const uint64_t start = nanoseconds();
+            while (!barrier_try(drained, 0) && nanoseconds() - start < kWaitLimit) {}
+        } else if (warp >= 2) {
+            const int row = threadIdx.x - 64;                      // token of a stage
+            uint32_t n = 0;
+            bool ok = true;
+            while (ok && work.next(tile, k0, k1)) {
+                tile_place(a, tile, i0, o0);
+                for (int k = k0; k < k1; ++k, ++n) {
+                    const uint32_t s = n % kGradStages, round = n / kGradStages;
+                    if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
+                    const int64_t t = (int64_t)(k % a.blocks) * kTileT + row;
+                    const uint8_t *src = a.e + (t < a.tokens ? t : 0) * a.lde + i0 / kGroup;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_address(se + s * kBytesE + row * 4)), "l"(src),
+                                 "r"(t < a.tokens ? 4 : 0)
+                                 : "memory");                      // tokens past the end: exponent 0, q is 0 there
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * s) : "memory");
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        }
+    } else if (warp < 8) {
+        registers_down<96>();
+        // 8 threads per token, 16 columns each: a warp reads four whole rows of q
+        const int id = threadIdx.x - 128, part = id & 7, row = id >> 3;
+        const int run = part >> 2, c = (part & 3) * 2;
+        uint32_t n = 0;
+        bool ok = true;
+        while (ok && work.next(tile, k0, k1)) {
+            for (int k = k0; k < k1; ++k, ++n) {
+                const uint32_t s = n % kGradStages;
+                if (!(ok = barrier_wait(full + 8 * s, (n / kGradStages) & 1, failed))) break;
+                const uint8_t *q = sq + s * kBytesQ, *e = se + s * kBytesE;
+                uint8_t *out = sa + s * kBytesA + run * (kTileT * 128);
+#pragma unroll
+                for (int p = 0; p < kTileT / 16; ++p) {
+                    const int t = row + 16 * p;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(q + t * kTileI + part * 16);
+                    uint4 lo, hi;
+                    widen16<T>(v, e[t * 4 + (part >> 1)], lo, hi);
+                    // the two halves of a token's 128-byte rows store even and odd pieces alternately: no bank twice
+                    uint8_t *r = out + t * 128;
+                    const int first = run ? c + 1 : c, second = run ? c : c + 1;
+                    *reinterpret_cast<uint4 *>(r + ((first ^ (t & 7)) << 4)) = run ? hi : lo;
+                    *reinterpret_cast<uint4 *>(r + ((second ^ (t & 7)) << 4)) = run ? lo : hi;
+                }
+                fence_async_shared();
+                barrier_arrive(ready + 8 * s);
+            }
+        }
+    } else {
+        registers_up<176>();
+        const int half = (warp - 8) >> 2, quarter = warp & 3;       // columns half * 128.., lanes quarter * 32..
+        const int row = quarter * 32 + lane;
+        const uint32_t source = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
+        uint32_t chunk = 0;
+        bool ok = true;
+        while (work.next(tile, k0, k1)) {
+            tile_place(a, tile, i0, o0);
+            float acc[128];
+#pragma unroll
+            for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+            for (int k = k0; k < k1; k += kChunk, ++chunk) {
+                const uint32_t buf = chunk & 1, round = chunk >> 1;
+                ok = ok && barrier_wait(acc_full + 8 * buf, round & 1, failed);
+                if (__any_sync(0xffffffffu, !ok)) break;
+                tmem_fence_after();
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    uint32_t v[32];
+                    tmem_load_32(source + buf * kTileO + p * 32, v);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[p * 32 + i] += __uint_as_float(v[i]);
+                }
+                tmem_fence_before();
+                barrier_arrive(acc_empty + 8 * buf);
+            }
+            if (*failed) {                                          // a wait ran out: no numbers rather than wrong ones
+                ok = false;
+#pragma unroll
+                for (int i = 0; i < 128; ++i) acc[i] = NAN;
+            }
+            if (a.split && (k0 > 0 || k1 < work.per_tile)) {
+                float *out = a.partial + ((int64_t)blockIdx.x * 2 + (k0 > 0 ? 0 : 1)) * (kTileO * kTileI) + half * 128 * kTileI + row;
+#pragma unroll
+                for (int i = 0; i < 128; ++i) out[i * kTileI] = acc[i];
+            } else if (i0 + row < a.I) {
+                float *out = a.dw + (int64_t)(o0 + half * 128) * a.I + i0 + row;
+                const int64_t rows = a.O - (o0 + half * 128);
+                if (a.accumulate) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i < rows) out[i * a.I] += acc[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i < rows) out[i * a.I] = acc[i];
+                }
+            }
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tmem_free<512>(tmem);
+    }
+}
+
+// The tiles that CTAs of the split kernel shared: their parts, added in the order of the tokens.  One CTA per 8 rows of
+// a tile.
+__global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad a, int ctas) {
+    const int64_t per_tile = (int64_t)a.blocks * a.planes, all = per_tile * a.tiles_i * a.tiles_o;
+    const int64_t tile = blockIdx.x / (kTileO / 8);
+    const int col = (int)(blockIdx.x % (kTileO / 8)) * 8 + threadIdx.x / 32;
+    const int64_t begin = tile * per_tile, end = begin + per_tile;
+    // CTA c holds blocks [all c / ctas, all (c + 1) / ctas)
+    int64_t c = begin * ctas / all;
+    while (c + 1 < ctas && all * (c + 1) / ctas <= begin) ++c;
+    if (all * c / ctas <= begin && all * (c + 1) / ctas >= end) return;          // whole in one CTA: written there
+    int i0, o0;
+    tile_place(a, tile, i0, o0);
+    const int i = threadIdx.x % 32 * 4;
+    if (o0 + col >= a.O) return;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (; c < ctas; ++c) {
+        const int64_t from = all * c / ctas;
+        if (from >= end) break;
+        if (all * (c + 1) / ctas <= from) continue;
+        const int slot = from > begin ? 0 : 1;
+        const float4 v = *reinterpret_cast<const float4 *>(a.partial + (c * 2 + slot) * (kTileO * kTileI) + col * kTileI + i);
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    }
+    float *out = a.dw + (int64_t)(o0 + col) * a.I + i0 + i;
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i0 + i + j < a.I) out[j] = a.accumulate ? out[j] + v[j] : v[j];
+}
+
+// dy as the tensor cores take it, where it is not already: 16-bit pieces in rows of ld elements (a multiple of 8).
+// 16-bit types: a copy.  fp32: three bf16 numbers of 8 bits each, by truncation, whose sum is dy exactly.
+template <typename T, typename U>
+__global__ void __launch_bounds__(256) weight_grad_planes_kernel(const T *__restrict__ dy, int64_t lddy, int64_t tokens, int64_t O,
+                                                                 U *__restrict__ out, int64_t ld) {
+    const int64_t n = tokens * O;
+    for (int64_t j = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; j < n; j += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t t = j / O, o = j - t * O;
+        if constexpr (sizeof(T) == 2) {
+            out[t * ld + o] = dy[t * lddy + o];
+        } else {
+            const float x = dy[t * lddy + o];
+            const bool finite = fabsf(x) <= 3.402823466e38f;
+            const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u), rest = x - hi;
+            const float mid = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+            out[t * ld + o] = from_float<__nv_bfloat16>(finite ? hi : x);
+            out[(tokens + t) * ld + o] = from_float<__nv_bfloat16>(finite ? mid : 0.f);
+            out[(2 * tokens + t) * ld + o] = from_float<__nv_bfloat16>(finite ? rest - mid : 0.f);
+        }
+    }
 }
 
 }  // namespace deft
