@@ -436,7 +436,7 @@ namespace {
 // What a call launches and keeps in its workspace: partial tiles first, then the 16-bit pieces of dy.
 struct GradPlan {
     bool copy_dy;
-    int planes, ctas;
+    int planes, pairs;
     bool split;
     int64_t ld_planes, partial_bytes, plane_bytes;
     int64_t tiles_i, tiles_o, blocks;
@@ -448,16 +448,16 @@ GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *d
     p.planes = es == 4 ? 3 : 1;
     p.ld_planes = ceil_div(O, 8) * 8;
     p.plane_bytes = p.copy_dy ? p.planes * T * p.ld_planes * 2 : 0;
-    p.tiles_i = ceil_div(I, deft::kTileI);
+    p.tiles_i = ceil_div(I, deft::kPairI);
     p.tiles_o = ceil_div(O, deft::kTileO);
     p.blocks = ceil_div(T, deft::kTileT);
-    // One CTA per SM.  Whole tiles while they fill the last round of CTAs well; otherwise the blocks of all tiles are cut
+    // A pair of CTAs per pair of SMs.  Whole tiles while they fill the last round of pairs well; otherwise the blocks of all tiles are cut
     // into equal runs, which costs a pass over the shared tiles' partial sums.
-    const int64_t tiles = p.tiles_i * p.tiles_o, rounds = ceil_div(tiles, sms);
-    p.split = p.blocks * p.planes > 1 && tiles * 10 < rounds * sms * 9;
+    const int64_t tiles = p.tiles_i * p.tiles_o, workers = sms / 2, rounds = ceil_div(tiles, workers);
+    p.split = p.blocks * p.planes > 1 && tiles * 10 < rounds * workers * 9;
     const int64_t most = p.split ? tiles * p.blocks * p.planes : tiles;
-    p.ctas = (int)(most < sms ? most : sms);
-    p.partial_bytes = p.split ? (int64_t)p.ctas * 2 * deft::kTileO * deft::kTileI * 4 : 0;
+    p.pairs = (int)(most < workers ? most : workers);
+    p.partial_bytes = p.split ? (int64_t)p.pairs * 4 * deft::kTileO * deft::kTileI * 4 : 0;
     return p;
 }
 constexpr int kUsualSms = 148;      // what a workspace is sized for before a device is looked at
@@ -513,7 +513,7 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
     }
     const EncodeTiled encode = encode_tiled();
     if (!encode) return fail(DEF_ERR_CUDA, "the driver does not offer tensor maps");
-    // The plan the workspace was sized by, on as many CTAs as the device has SMs for.
+    // The plan the workspace was sized by, on as many CTAs.
     GradPlan p = grad_plan(dtype, T, O, I, dy, lddy, kUsualSms);
     const bool half = dtype == DEF_DTYPE_F16;
     const void *rows = dy;
@@ -530,7 +530,7 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         rows = planes;
         ld = p.ld_planes;
     }
-    CUtensorMap map_y, map_q;
+    CUtensorMap map_y, map_q, map_e = {};
     const cuuint64_t dim_y[3] = {(cuuint64_t)O, (cuuint64_t)T, (cuuint64_t)p.planes}, stride_y[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)T};
     const cuuint32_t box_y[3] = {64, deft::kTileT, 1}, one[3] = {1, 1, 1};
     const cuuint64_t dim_q[2] = {(cuuint64_t)I, (cuuint64_t)T}, stride_q[1] = {(cuuint64_t)q_stride(I)};
@@ -540,14 +540,36 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         encode(&map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(q), dim_q, stride_q, box_q, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return fail(DEF_ERR_CUDA, "the driver refused a tensor map of dy or q");
+    const bool wide_e = e_stride(I) % 16 == 0 && ((uintptr_t)e & 15u) == 0;
+    if (wide_e) {
+        const cuuint64_t dim_e[2] = {(cuuint64_t)e_stride(I), (cuuint64_t)T}, stride_e[1] = {(cuuint64_t)e_stride(I)};
+        const cuuint32_t box_e[2] = {16, deft::kTileT};
+        if (encode(&map_e, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(e), dim_e, stride_e, box_e, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return fail(DEF_ERR_CUDA, "the driver refused a tensor map of e");
+    }
     deft::WeightGrad a = {e, dw, (float *)workspace, T, O, I, e_stride(I), (int)p.tiles_i, (int)p.tiles_o, (int)p.blocks, p.planes, accumulate, p.split};
-    const auto kernel = half ? deft::weight_grad_kernel<__half> : deft::weight_grad_kernel<__nv_bfloat16>;
+    const auto kernel = half ? (wide_e ? deft::weight_grad_kernel<__half, true> : deft::weight_grad_kernel<__half, false>)
+                             : (wide_e ? deft::weight_grad_kernel<__nv_bfloat16, true> : deft::weight_grad_kernel<__nv_bfloat16, false>);
     cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, deft::kGradSmem);
     if (err != cudaSuccess) return cuda_fail(err, "def_checkpoint_weight_grad");
-    kernel<<<(unsigned)p.ctas, deft::kGradThreads, deft::kGradSmem, stream>>>(a, map_y, map_q);
-    DEF_TRY(launched("def_checkpoint_weight_grad"));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.pairs * 2);
+    cfg.blockDim = dim3(deft::kGradThreads);
+    cfg.dynamicSmemBytes = deft::kGradSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if ((err = cudaLaunchKernelEx(&cfg, kernel, a, map_y, map_q, map_e)) != cudaSuccess) {
+        cudaGetLastError();
+        return cuda_fail(err, "def_checkpoint_weight_grad");
+    }
     if (p.split) {
-        deft::weight_grad_join_kernel<<<(unsigned)(p.tiles_i * p.tiles_o * (deft::kTileO / 8)), 256, 0, stream>>>(a, p.ctas);
+        deft::weight_grad_join_kernel<<<(unsigned)(p.tiles_i * p.tiles_o * 2 * (deft::kTileO / 8)), 256, 0, stream>>>(a, p.pairs);
         DEF_TRY(launched("def_checkpoint_weight_grad (join)"));
     }
     return DEF_OK;

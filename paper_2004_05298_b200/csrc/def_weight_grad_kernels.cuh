@@ -16,12 +16,14 @@
 
 namespace deft {
 
-constexpr int kTileI = 128, kTileO = 256, kTileT = 64;      // of one accumulator, and tokens per pipeline stage
-constexpr int kGradStages = 4, kGradThreads = 512;
+constexpr int kTileI = 128, kTileO = 256, kTileT = 64;      // of one CTA's accumulator, and tokens per pipeline stage
+constexpr int kPairI = 2 * kTileI, kHalfO = kTileO / 2;      // a pair's rows of D; the columns of dy each CTA brings
+constexpr int kLoadStages = 7, kWideStages = 3;             // of what is loaded; of widened q
+constexpr int kWidenThreads = 256, kGradThreads = 128 + kWidenThreads + 256;
 constexpr int kChunk = 8;                                    // stages per accumulator hand-over
-constexpr int kBytesA = kTileI * kTileT * 2, kBytesB = kTileO * kTileT * 2, kBytesQ = kTileI * kTileT, kBytesE = kTileT * 4;
-constexpr int kBarrierBytes = 1024;
-constexpr int kGradSmem = kBarrierBytes + 1024 + kGradStages * (kBytesA + kBytesB + kBytesQ + kBytesE);
+constexpr int kBytesA = kTileI * kTileT * 2, kBytesB = kHalfO * kTileT * 2, kBytesQ = kTileI * kTileT, kBytesE = kTileT * 16;
+constexpr int kBarrierBytes = 256;
+constexpr int kGradSmem = 1024 + kWideStages * kBytesA + kLoadStages * (kBytesB + kBytesQ + kBytesE) + kBarrierBytes;
 
 struct WeightGrad {
     const uint8_t *e;
@@ -31,8 +33,8 @@ struct WeightGrad {
     int accumulate, split;                // split: CTAs share tiles (contiguous ranges of all tiles' blocks)
 };
 
-// The pieces of work of one CTA: (tile, blocks [k0, k1)).  Split: an equal run of the blocks of all tiles in order; a
-// tile that is cut goes to partial slot 0 of the CTAs that do not hold its first block, slot 1 of the one that does.
+// The pieces of work of one pair of CTAs: (tile, blocks [k0, k1)).  Split: an equal run of the blocks of all tiles in order; a
+// tile that is cut goes to partial slot 0 of the pairs that do not hold its first block, slot 1 of the one that does.
 struct Pieces {
     int64_t pos, end, step, per_tile;
     bool split;
@@ -42,10 +44,10 @@ struct Pieces {
         const int64_t tiles = (int64_t)a.tiles_i * a.tiles_o;
         if (split) {
             const int64_t all = tiles * per_tile;
-            pos = all * blockIdx.x / gridDim.x;
-            end = all * (blockIdx.x + 1) / gridDim.x;
+            pos = all * (blockIdx.x / 2) / (gridDim.x / 2);
+            end = all * (blockIdx.x / 2 + 1) / (gridDim.x / 2);
         } else {
-            pos = blockIdx.x;
+            pos = blockIdx.x / 2;
             end = tiles;
         }
     }
@@ -60,7 +62,7 @@ struct Pieces {
             tile = pos;
             k0 = 0;
             k1 = (int)per_tile;
-            pos += gridDim.x;
+            pos += gridDim.x / 2;
         }
         return true;
     }
@@ -70,7 +72,7 @@ struct Pieces {
 __device__ __forceinline__ void tile_place(const WeightGrad &a, int64_t tile, int &i0, int &o0) {
     const int64_t band = tile / (8LL * a.tiles_i), r = tile - band * 8 * a.tiles_i;
     const int wide = (int)(a.tiles_o - band * 8 < 8 ? a.tiles_o - band * 8 : 8);
-    i0 = (int)(r / wide) * kTileI;
+    i0 = (int)(r / wide) * kPairI;
     o0 = (int)(band * 8 + r % wide) * kTileO;
 }
 
@@ -80,7 +82,7 @@ template <typename T> __device__ __forceinline__ void widen16(uint4 q, uint32_t 
     uint32_t out[8];
     if constexpr (sizeof(T) == 2 && !__is_same(T, __half)) {
         // q = (low 7 bits + 128) - (128 or 256), both exact bf16 numbers made by bit operations
-        const uint32_t s = e << 7 | e << 23;
+        const uint32_t s = e * 0x00800080u;
         __nv_bfloat162 scale;
         memcpy(&scale, &s, 4);
 #pragma unroll
@@ -106,29 +108,39 @@ template <typename T> __device__ __forceinline__ void widen16(uint4 q, uint32_t 
     hi = make_uint4(out[4], out[5], out[6], out[7]);
 }
 
-// Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread), 2 and 3 fetch exponents, 4-7 widen q,
-// 8-15 empty accumulators and store.
-template <typename T>
+// WIDE_E: rows of e are multiples of 16 bytes, and 16 of them (512 columns) come per token with the other copies; else
+// two warps fetch the 4 that a tile needs with one small copy per token, which costs shared memory 15 % of its cycles
+// more (4-byte copies from scattered rows are stored one by one).
+//
+// Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread), 2 and 3 fetch exponents, 4-11 widen q,
+// 12-19 empty accumulators and store.
+template <typename T, bool WIDE_E>
 __global__ void __launch_bounds__(kGradThreads, 1)
-    weight_grad_kernel(const WeightGrad a, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_q) {
+    weight_grad_kernel(const WeightGrad a, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_q,
+                       const __grid_constant__ CUtensorMap map_e) {
+    constexpr int kRowE = WIDE_E ? 16 : 4;
     extern __shared__ uint8_t raw[];
     uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sa = base, *sb = sa + kGradStages * kBytesA, *sq = sb + kGradStages * kBytesB, *se = sq + kGradStages * kBytesQ;
-    uint64_t *bars = (uint64_t *)(se + kGradStages * kBytesE);
-    const uint32_t full = smem_address(bars), ready = full + 8 * kGradStages, empty = ready + 8 * kGradStages, acc_full = empty + 8 * kGradStages,
-                   acc_empty = acc_full + 16, drained = acc_empty + 16;
-    uint32_t *tmem_slot = (uint32_t *)(bars + 3 * kGradStages + 5);
+    uint8_t *sa = base, *sb = sa + kWideStages * kBytesA, *sq = sb + kLoadStages * kBytesB, *se = sq + kLoadStages * kBytesQ;
+    uint64_t *bars = (uint64_t *)(se + kLoadStages * kBytesE);
+    const uint32_t full = smem_address(bars), empty = full + 8 * kLoadStages, ready = empty + 8 * kLoadStages, used = ready + 8 * kWideStages,
+                   acc_full = used + 8 * kWideStages, acc_empty = acc_full + 16, drained = acc_empty + 16;
+    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * kLoadStages + 2 * kWideStages + 5);
     volatile int *failed = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kGradStages; ++s) {
-            barrier_init(full + 8 * s, 1 + 64);
-            barrier_init(ready + 8 * s, 128);
+        for (int s = 0; s < kLoadStages; ++s) {
+            barrier_init(full + 8 * s, WIDE_E ? 1 : 1 + 64);
             barrier_init(empty + 8 * s, 1);
+        }
+        for (int s = 0; s < kWideStages; ++s) {
+            barrier_init(ready + 8 * s, 2 * 4);
+            barrier_init(used + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(acc_full + 8 * b, 1);
-            barrier_init(acc_empty + 8 * b, 256);
+            barrier_init(acc_empty + 8 * b, 2 * 8);
         }
         barrier_init(drained, 1);
         *failed = 0;
@@ -140,6 +152,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     }
     tmem_fence_before();
     __syncthreads();
+    cluster_sync();
     tmem_fence_after();
     const uint32_t tmem = *tmem_slot;
     Pieces work(a);
@@ -147,32 +160,38 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     int k0, k1, i0, o0;
 
     if (warp < 4) {
-        registers_down<64>();
+        registers_down<48>();
         if (warp == 0 && lane == 0) {
             prefetch_map(&map_y);
             prefetch_map(&map_q);
+            if (WIDE_E) prefetch_map(&map_e);
             uint32_t n = 0;
             bool ok = true;
             while (ok && work.next(tile, k0, k1)) {
                 tile_place(a, tile, i0, o0);
+                i0 += rank * kTileI;
                 for (int k = k0; k < k1; ++k, ++n) {
-                    const uint32_t s = n % kGradStages, round = n / kGradStages;
+                    const uint32_t s = n % kLoadStages, round = n / kLoadStages;
                     if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
                     const int plane = k / a.blocks, t0 = (k - plane * a.blocks) * kTileT;
                     const uint32_t bar = full + 8 * s;
-                    barrier_expect(bar, kBytesB + kBytesQ);
+                    barrier_expect(bar, kBytesB + kBytesQ + (WIDE_E ? kBytesE : 0));
                     tensor_load_2d(smem_address(sq + s * kBytesQ), &map_q, i0, t0, bar);
+                    if (WIDE_E) tensor_load_2d(smem_address(se + s * kBytesE), &map_e, i0 / kGroup & ~15, t0, bar);
 #pragma unroll
-                    for (int j = 0; j < kTileO / 64; ++j)
-                        tensor_load_3d(smem_address(sb + s * kBytesB + j * (kTileT * 128)), &map_y, o0 + 64 * j, t0, plane, bar);
+                    for (int j = 0; j < kHalfO / 64; ++j)
+                        tensor_load_3d(smem_address(sb + s * kBytesB + j * (kTileT * 128)), &map_y, o0 + rank * kHalfO + 64 * j, t0, plane, bar);
                 }
             }
             // the copies in flight end before the CTA does
             const uint64_t start = nanoseconds();
-            for (uint32_t m = n > kGradStages ? n - kGradStages : 0; m < n; ++m)
-                while (!barrier_try(full + 8 * (m % kGradStages), (m / kGradStages) & 1) && nanoseconds() - start < kWaitLimit) {}
+            for (uint32_t m = n > kLoadStages ? n - kLoadStages : 0; m < n; ++m)
+                while (!barrier_try(full + 8 * (m % kLoadStages), (m / kLoadStages) & 1) && nanoseconds() - start < kWaitLimit) {}
+        } else if (warp == 1 && lane == 0 && rank != 0) {
+            const uint64_t start = nanoseconds();                  // the other CTA's last commit arrives here too
+            while (!barrier_try(drained, 0) && nanoseconds() - start < 2 * kWaitLimit) {}
         } else if (warp == 1 && lane == 0) {
-            constexpr uint32_t idesc = instruction_descriptor(!__is_same(T, __half), kTileI, kTileO);
+            constexpr uint32_t idesc = instruction_descriptor(!__is_same(T, __half), kPairI, kTileO);
             uint32_t n = 0, chunk = 0;
             bool ok = true;
             while (ok && work.next(tile, k0, k1)) {
@@ -182,14 +201,15 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                     tmem_fence_after();
                     const int stop = k + kChunk < k1 ? k + kChunk : k1;
                     for (int first = k; k < stop; ++k, ++n) {
-                        const uint32_t s = n % kGradStages, parity = (n / kGradStages) & 1;
-                        if (!(ok = barrier_wait(full + 8 * s, parity, failed) && barrier_wait(ready + 8 * s, parity, failed))) break;
+                        const uint32_t w = n % kWideStages, s = n % kLoadStages;
+                        if (!(ok = barrier_wait(ready + 8 * w, (n / kWideStages) & 1, failed))) break;   // both CTAs' dy has landed, too
                         tmem_fence_after();
-                        const uint64_t da = operand_descriptor(smem_address(sa + s * kBytesA), kTileT * 128);
+                        const uint64_t da = operand_descriptor(smem_address(sa + w * kBytesA), kTileT * 128);
                         const uint64_t db = operand_descriptor(smem_address(sb + s * kBytesB), kTileT * 128);
 #pragma unroll
                         for (int j = 0; j < kTileT / 16; ++j)     // 16 tokens each: 2048 bytes further along k
                             mma(tmem + buf * kTileO, da + j * (2048 >> 4), db + j * (2048 >> 4), idesc, k > first || j > 0);
+                        mma_commit(used + 8 * w);
                         mma_commit(empty + 8 * s);
                     }
                     if (ok) mma_commit(acc_full + 8 * buf);
@@ -198,63 +218,78 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             mma_commit(drained);
             const uint64_t start = nanoseconds();
             while (!barrier_try(drained, 0) && nanoseconds() - start < kWaitLimit) {}
-        } else if (warp >= 2) {
+        } else if (!WIDE_E && warp >= 2) {
             const int row = threadIdx.x - 64;                      // token of a stage
             uint32_t n = 0;
             bool ok = true;
             while (ok && work.next(tile, k0, k1)) {
                 tile_place(a, tile, i0, o0);
+                i0 += rank * kTileI;
                 for (int k = k0; k < k1; ++k, ++n) {
-                    const uint32_t s = n % kGradStages, round = n / kGradStages;
+                    const uint32_t s = n % kLoadStages, round = n / kLoadStages;
                     if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
                     const int64_t t = (int64_t)(k % a.blocks) * kTileT + row;
-                    const uint8_t *src = a.e + (t < a.tokens ? t : 0) * a.lde + i0 / kGroup;
+                    const bool there = t < a.tokens && i0 < a.I;
+                    const uint8_t *src = there ? a.e + t * a.lde + i0 / kGroup : a.e;
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_address(se + s * kBytesE + row * 4)), "l"(src),
-                                 "r"(t < a.tokens ? 4 : 0)
+                                 "r"(there ? 4 : 0)
                                  : "memory");                      // tokens past the end: exponent 0, q is 0 there
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * s) : "memory");
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
         }
-    } else if (warp < 8) {
-        registers_down<96>();
-        // 8 threads per token, 16 columns each: a warp reads four whole rows of q
-        const int id = threadIdx.x - 128, part = id & 7, row = id >> 3;
-        const int run = part >> 2, c = (part & 3) * 2;
+    } else if (warp < 4 + kWidenThreads / 32) {
+        registers_down<56>();
+        // Two groups of four warps take stages in turn.  8 threads per token, 16 columns each: a warp reads four whole
+        // rows of q, and then the tokens 16, 32 and 48 further on.
+        const int id = threadIdx.x & 127, part = id & 7, row = id >> 3;
+        const uint32_t group = (warp - 4) >> 2;
+        // The two runs of 64 columns write their even and odd 16-byte pieces alternately: no bank twice.
+        const int run = part >> 2, c = (part & 3) * 2 + run;
+        const int first = run * (kTileT * 128) + row * 128 + ((c ^ (row & 7)) << 4), second = first ^ 16;
         uint32_t n = 0;
         bool ok = true;
         while (ok && work.next(tile, k0, k1)) {
+            tile_place(a, tile, i0, o0);
+            i0 += rank * kTileI;
+            const int e0 = (WIDE_E ? i0 / kGroup & 15 : 0) + (part >> 1);
             for (int k = k0; k < k1; ++k, ++n) {
-                const uint32_t s = n % kGradStages;
-                if (!(ok = barrier_wait(full + 8 * s, (n / kGradStages) & 1, failed))) break;
-                const uint8_t *q = sq + s * kBytesQ, *e = se + s * kBytesE;
-                uint8_t *out = sa + s * kBytesA + run * (kTileT * 128);
+                if (n % 2 != group) continue;
+                const uint32_t s = n % kLoadStages, w = n % kWideStages;
+                if (!(ok = barrier_wait(full + 8 * s, (n / kLoadStages) & 1, failed))) break;
+                const uint8_t *q = sq + s * kBytesQ + row * kTileI + part * 16, *e = se + s * kBytesE + row * kRowE + e0;
+                uint8_t *out = sa + w * kBytesA;
+                uint4 v[4];
+                uint32_t ex[4];
 #pragma unroll
-                for (int p = 0; p < kTileT / 16; ++p) {
-                    const int t = row + 16 * p;
-                    const uint4 v = *reinterpret_cast<const uint4 *>(q + t * kTileI + part * 16);
+                for (int p = 0; p < 4; ++p) {
+                    v[p] = *reinterpret_cast<const uint4 *>(q + p * 16 * kTileI);
+                    ex[p] = e[p * 16 * kRowE];
+                }
+                if (!(ok = barrier_wait(used + 8 * w, ((n / kWideStages) & 1) ^ 1, failed))) break;
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
                     uint4 lo, hi;
-                    widen16<T>(v, e[t * 4 + (part >> 1)], lo, hi);
-                    // the two halves of a token's 128-byte rows store even and odd pieces alternately: no bank twice
-                    uint8_t *r = out + t * 128;
-                    const int first = run ? c + 1 : c, second = run ? c : c + 1;
-                    *reinterpret_cast<uint4 *>(r + ((first ^ (t & 7)) << 4)) = run ? hi : lo;
-                    *reinterpret_cast<uint4 *>(r + ((second ^ (t & 7)) << 4)) = run ? lo : hi;
+                    widen16<T>(v[p], ex[p], lo, hi);
+                    *reinterpret_cast<uint4 *>(out + first + p * 16 * 128) = run ? hi : lo;
+                    *reinterpret_cast<uint4 *>(out + second + p * 16 * 128) = run ? lo : hi;
                 }
                 fence_async_shared();
-                barrier_arrive(ready + 8 * s);
+                __syncwarp();
+                if (lane == 0) barrier_arrive_at(ready + 8 * w, 0);
             }
         }
     } else {
-        registers_up<176>();
-        const int half = (warp - 8) >> 2, quarter = warp & 3;       // columns half * 128.., lanes quarter * 32..
+        registers_up<160>();
+        const int half = (warp - 4 - kWidenThreads / 32) >> 2, quarter = warp & 3;       // columns half * 128.., lanes quarter * 32..
         const int row = quarter * 32 + lane;
         const uint32_t source = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
         uint32_t chunk = 0;
         bool ok = true;
         while (work.next(tile, k0, k1)) {
             tile_place(a, tile, i0, o0);
+            i0 += rank * kTileI;
             float acc[128];
 #pragma unroll
             for (int i = 0; i < 128; ++i) acc[i] = 0.f;
@@ -264,14 +299,15 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 if (__any_sync(0xffffffffu, !ok)) break;
                 tmem_fence_after();
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    uint32_t v[32];
-                    tmem_load_32(source + buf * kTileO + p * 32, v);
+                for (int p = 0; p < 8; ++p) {
+                    uint32_t v[16];
+                    tmem_load_16(source + buf * kTileO + p * 16, v);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) acc[p * 32 + i] += __uint_as_float(v[i]);
+                    for (int i = 0; i < 16; ++i) acc[p * 16 + i] += __uint_as_float(v[i]);
                 }
                 tmem_fence_before();
-                barrier_arrive(acc_empty + 8 * buf);
+                __syncwarp();
+                if (lane == 0) barrier_arrive_at(acc_empty + 8 * buf, 0);
             }
             if (*failed) {                                          // a wait ran out: no numbers rather than wrong ones
                 ok = false;
@@ -299,34 +335,37 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     }
     tmem_fence_before();
     __syncthreads();
+    cluster_sync();                                                // nothing of this CTA is used by the other any more
     if (warp == 1) {
         __syncwarp();
         tmem_free<512>(tmem);
     }
 }
 
-// The tiles that CTAs of the split kernel shared: their parts, added in the order of the tokens.  One CTA per 8 rows of
-// a tile.
-__global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad a, int ctas) {
+// The tiles that pairs of the split kernel shared: their parts, added in the order of the tokens.  One CTA per 8 rows of
+// dw of half a tile.
+__global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad a, int pairs) {
     const int64_t per_tile = (int64_t)a.blocks * a.planes, all = per_tile * a.tiles_i * a.tiles_o;
-    const int64_t tile = blockIdx.x / (kTileO / 8);
+    const int64_t half_tile = blockIdx.x / (kTileO / 8), tile = half_tile / 2;
+    const int rank = (int)(half_tile % 2);
     const int col = (int)(blockIdx.x % (kTileO / 8)) * 8 + threadIdx.x / 32;
     const int64_t begin = tile * per_tile, end = begin + per_tile;
-    // CTA c holds blocks [all c / ctas, all (c + 1) / ctas)
-    int64_t c = begin * ctas / all;
-    while (c + 1 < ctas && all * (c + 1) / ctas <= begin) ++c;
-    if (all * c / ctas <= begin && all * (c + 1) / ctas >= end) return;          // whole in one CTA: written there
+    // pair c holds blocks [all c / pairs, all (c + 1) / pairs)
+    int64_t c = begin * pairs / all;
+    while (c + 1 < pairs && all * (c + 1) / pairs <= begin) ++c;
+    if (all * c / pairs <= begin && all * (c + 1) / pairs >= end) return;        // whole in one pair: written there
     int i0, o0;
     tile_place(a, tile, i0, o0);
+    i0 += rank * kTileI;
     const int i = threadIdx.x % 32 * 4;
-    if (o0 + col >= a.O) return;
+    if (o0 + col >= a.O || i0 + i >= a.I) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (; c < ctas; ++c) {
-        const int64_t from = all * c / ctas;
+    for (; c < pairs; ++c) {
+        const int64_t from = all * c / pairs;
         if (from >= end) break;
-        if (all * (c + 1) / ctas <= from) continue;
+        if (all * (c + 1) / pairs <= from) continue;
         const int slot = from > begin ? 0 : 1;
-        const float4 v = *reinterpret_cast<const float4 *>(a.partial + (c * 2 + slot) * (kTileO * kTileI) + col * kTileI + i);
+        const float4 v = *reinterpret_cast<const float4 *>(a.partial + ((c * 2 + rank) * 2 + slot) * (kTileO * kTileI) + col * kTileI + i);
         sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
     }
     float *out = a.dw + (int64_t)(o0 + col) * a.I + i0 + i;
