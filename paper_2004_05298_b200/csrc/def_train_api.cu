@@ -433,12 +433,11 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
 // ---------------------------------------------------------------------------
 namespace {
 
-// What a call launches and keeps in its workspace: partial tiles first, then the 16-bit pieces of dy.
+// What a call launches and keeps in its workspace: partial tiles first, then the 16-bit pieces of dy, then x^ in 16 bits.
 struct GradPlan {
-    bool copy_dy;
+    bool copy_dy, copy_x, split;
     int planes, pairs;
-    bool split;
-    int64_t ld_planes, partial_bytes, plane_bytes;
+    int64_t ld_planes, ld_x, partial_bytes, plane_bytes, x_bytes;
     int64_t tiles_i, tiles_o, blocks;
 };
 GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *dy, int64_t lddy, int sms) {
@@ -447,17 +446,24 @@ GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *d
     p.copy_dy = es == 4 || !wide(dy, lddy, es);
     p.planes = es == 4 ? 3 : 1;
     p.ld_planes = ceil_div(O, 8) * 8;
+    p.ld_x = ceil_div(I, 8) * 8;
     p.plane_bytes = p.copy_dy ? p.planes * T * p.ld_planes * 2 : 0;
     p.tiles_i = ceil_div(I, deft::kPairI);
     p.tiles_o = ceil_div(O, deft::kTileO);
     p.blocks = ceil_div(T, deft::kTileT);
-    // A pair of CTAs per pair of SMs.  Whole tiles while they fill the last round of pairs well; otherwise the blocks of all tiles are cut
-    // into equal runs, which costs a pass over the shared tiles' partial sums.
+    // A pair of CTAs per pair of SMs.  Whole tiles while they fill the last round of pairs well; otherwise the blocks of all
+    // tiles are cut into equal runs, which costs a pass over the shared tiles' partial sums.
     const int64_t tiles = p.tiles_i * p.tiles_o, workers = sms / 2, rounds = ceil_div(tiles, workers);
     p.split = p.blocks * p.planes > 1 && tiles * 10 < rounds * workers * 9;
     const int64_t most = p.split ? tiles * p.blocks * p.planes : tiles;
     p.pairs = (int)(most < workers ? most : workers);
     p.partial_bytes = p.split ? (int64_t)p.pairs * 4 * deft::kTileO * deft::kTileI * 4 : 0;
+    // A tile of x^ is widened once for each tile of dw along o (and each piece of dy).  From kWidenOnce of them on it is
+    // cheaper to widen x^ to memory first, as long as that keeps to the documented size of the workspace.
+    p.x_bytes = T * p.ld_x * 2;
+    p.copy_x = p.tiles_o * p.planes >= deft::kWidenOnce &&
+               p.partial_bytes + p.plane_bytes + p.x_bytes <= ((int64_t)68 << 20) + 8 * O * I + 6 * T * O;
+    if (!p.copy_x) p.x_bytes = 0;
     return p;
 }
 constexpr int kUsualSms = 148;      // what a workspace is sized for before a device is looked at
@@ -488,7 +494,7 @@ extern "C" int def_checkpoint_weight_grad_workspace(int32_t dtype, int64_t T, in
     DEF_TRY(check_stride(dy, lddy, O, "dy"));
     if (T >= (int64_t)1 << 31) return fail(DEF_ERR_ARG, "T must be below 2^31 (got %lld)", (long long)T);
     const GradPlan p = grad_plan(dtype, T, O, I, dy, lddy, kUsualSms);
-    *bytes_out = p.partial_bytes + p.plane_bytes;
+    *bytes_out = p.partial_bytes + p.plane_bytes + p.x_bytes;
     return DEF_OK;
 }
 
@@ -530,17 +536,33 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         rows = planes;
         ld = p.ld_planes;
     }
-    CUtensorMap map_y, map_q, map_e = {};
+    const void *xs = q;
+    if (p.copy_x) {
+        void *wide_x = (char *)workspace + p.partial_bytes + p.plane_bytes;
+        by_width(I % 8 == 0, [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            const Plane g = plane(T, I, V);
+            if (half)
+                deft::unpack_kernel<__half, V><<<g.grid, g.block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, I, (__half *)wide_x, p.ld_x);
+            else
+                deft::unpack_kernel<__nv_bfloat16, V><<<g.grid, g.block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, I, (__nv_bfloat16 *)wide_x, p.ld_x);
+        });
+        DEF_TRY(launched("def_checkpoint_weight_grad (widen)"));
+        xs = wide_x;
+    }
+    CUtensorMap map_y, map_x, map_e = {};
     const cuuint64_t dim_y[3] = {(cuuint64_t)O, (cuuint64_t)T, (cuuint64_t)p.planes}, stride_y[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)T};
     const cuuint32_t box_y[3] = {64, deft::kTileT, 1}, one[3] = {1, 1, 1};
-    const cuuint64_t dim_q[2] = {(cuuint64_t)I, (cuuint64_t)T}, stride_q[1] = {(cuuint64_t)q_stride(I)};
-    const cuuint32_t box_q[2] = {deft::kTileI, deft::kTileT};
-    if (encode(&map_y, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(rows), dim_y, stride_y, box_y, one,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
-        encode(&map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(q), dim_q, stride_q, box_q, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return fail(DEF_ERR_CUDA, "the driver refused a tensor map of dy or q");
-    const bool wide_e = e_stride(I) % 16 == 0 && ((uintptr_t)e & 15u) == 0;
+    const cuuint64_t dim_x[2] = {(cuuint64_t)I, (cuuint64_t)T}, stride_x[1] = {(cuuint64_t)(p.copy_x ? p.ld_x * 2 : q_stride(I))};
+    const cuuint32_t box_x[2] = {p.copy_x ? 64u : (cuuint32_t)deft::kTileI, deft::kTileT};
+    const CUtensorMapDataType type16 = half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    if (encode(&map_y, type16, 3, const_cast<void *>(rows), dim_y, stride_y, box_y, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+        encode(&map_x, p.copy_x ? type16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(xs), dim_x, stride_x, box_x, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               p.copy_x ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return fail(DEF_ERR_CUDA, "the driver refused a tensor map of dy or x");
+    const bool wide_e = !p.copy_x && e_stride(I) % 16 == 0 && ((uintptr_t)e & 15u) == 0;
     if (wide_e) {
         const cuuint64_t dim_e[2] = {(cuuint64_t)e_stride(I), (cuuint64_t)T}, stride_e[1] = {(cuuint64_t)e_stride(I)};
         const cuuint32_t box_e[2] = {16, deft::kTileT};
@@ -549,22 +571,32 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
             return fail(DEF_ERR_CUDA, "the driver refused a tensor map of e");
     }
     deft::WeightGrad a = {e, dw, (float *)workspace, T, O, I, e_stride(I), (int)p.tiles_i, (int)p.tiles_o, (int)p.blocks, p.planes, accumulate, p.split};
-    const auto kernel = half ? (wide_e ? deft::weight_grad_kernel<__half, true> : deft::weight_grad_kernel<__half, false>)
-                             : (wide_e ? deft::weight_grad_kernel<__nv_bfloat16, true> : deft::weight_grad_kernel<__nv_bfloat16, false>);
-    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, deft::kGradSmem);
-    if (err != cudaSuccess) return cuda_fail(err, "def_checkpoint_weight_grad");
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.pairs * 2);
-    cfg.blockDim = dim3(deft::kGradThreads);
-    cfg.dynamicSmemBytes = deft::kGradSmem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if ((err = cudaLaunchKernelEx(&cfg, kernel, a, map_y, map_q, map_e)) != cudaSuccess) {
+    cudaError_t err = cudaSuccess;
+    auto launch = [&](auto kernel, auto shape) {
+        using S = decltype(shape);
+        if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem)) != cudaSuccess) return;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)p.pairs * 2);
+        cfg.blockDim = dim3(S::threads);
+        cfg.dynamicSmemBytes = S::smem;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        err = cudaLaunchKernelEx(&cfg, kernel, a, map_y, map_x, map_e);
+    };
+    auto by_operand = [&](auto type) {
+        using E = decltype(type);
+        if (p.copy_x) launch(deft::weight_grad_kernel<E, false, false>, deft::GradShape<false>());
+        else if (wide_e) launch(deft::weight_grad_kernel<E, true, true>, deft::GradShape<true>());
+        else launch(deft::weight_grad_kernel<E, true, false>, deft::GradShape<true>());
+    };
+    if (half) by_operand(__half());
+    else by_operand(__nv_bfloat16());
+    if (err != cudaSuccess) {
         cudaGetLastError();
         return cuda_fail(err, "def_checkpoint_weight_grad");
     }

@@ -18,12 +18,18 @@ namespace deft {
 
 constexpr int kTileI = 128, kTileO = 256, kTileT = 64;      // of one CTA's accumulator, and tokens per pipeline stage
 constexpr int kPairI = 2 * kTileI, kHalfO = kTileO / 2;      // a pair's rows of D; the columns of dy each CTA brings
-constexpr int kLoadStages = 7, kWideStages = 3;             // of what is loaded; of widened q
-constexpr int kWidenThreads = 256, kGradThreads = 128 + kWidenThreads + 256;
-constexpr int kChunk = 8;                                    // stages per accumulator hand-over
+constexpr int kChunk = 16;                                   // stages per accumulator hand-over
 constexpr int kBytesA = kTileI * kTileT * 2, kBytesB = kHalfO * kTileT * 2, kBytesQ = kTileI * kTileT, kBytesE = kTileT * 16;
-constexpr int kBarrierBytes = 256;
-constexpr int kGradSmem = 1024 + kWideStages * kBytesA + kLoadStages * (kBytesB + kBytesQ + kBytesE) + kBarrierBytes;
+
+// Two ways to the operand x^.  Widening: q is loaded and widened in shared memory by two groups of four warps, each time
+// a tile needs it.  Else x^ lies in memory in 16 bits (widened once by a kernel of its own) and is loaded like dy.
+constexpr int kWidenOnce = 4;
+template <bool WIDEN> struct GradShape {
+    static constexpr int loads = 7, wides = WIDEN ? 3 : 0;   // stages of what is loaded; of widened q
+    static constexpr int bytes_x = WIDEN ? kBytesQ + kBytesE : kBytesA;
+    static constexpr int threads = 128 + (WIDEN ? 256 : 0) + 256;
+    static constexpr int smem = 1024 + wides * kBytesA + loads * (kBytesB + bytes_x) + 256;
+};
 
 struct WeightGrad {
     const uint8_t *e;
@@ -112,30 +118,32 @@ template <typename T> __device__ __forceinline__ void widen16(uint4 q, uint32_t 
 // two warps fetch the 4 that a tile needs with one small copy per token, which costs shared memory 15 % of its cycles
 // more (4-byte copies from scattered rows are stored one by one).
 //
-// Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread), 2 and 3 fetch exponents, 4-11 widen q,
-// 12-19 empty accumulators and store.
-template <typename T, bool WIDE_E>
-__global__ void __launch_bounds__(kGradThreads, 1)
-    weight_grad_kernel(const WeightGrad a, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_q,
+// Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread of the even CTA), 2 and 3 fetch exponents
+// (where x^ is loaded, 2 reports its landing instead), the next 8 widen q, the last 8 empty accumulators and store.
+template <typename T, bool WIDEN, bool WIDE_E>
+__global__ void __launch_bounds__(GradShape<WIDEN>::threads, 1)
+    weight_grad_kernel(const WeightGrad a, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_x,
                        const __grid_constant__ CUtensorMap map_e) {
+    using S = GradShape<WIDEN>;
+    constexpr int kLoads = S::loads, kWides = WIDEN ? S::wides : S::loads;       // x^ is ready wide by wide, or load by load
     constexpr int kRowE = WIDE_E ? 16 : 4;
     extern __shared__ uint8_t raw[];
     uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sa = base, *sb = sa + kWideStages * kBytesA, *sq = sb + kLoadStages * kBytesB, *se = sq + kLoadStages * kBytesQ;
-    uint64_t *bars = (uint64_t *)(se + kLoadStages * kBytesE);
-    const uint32_t full = smem_address(bars), empty = full + 8 * kLoadStages, ready = empty + 8 * kLoadStages, used = ready + 8 * kWideStages,
-                   acc_full = used + 8 * kWideStages, acc_empty = acc_full + 16, drained = acc_empty + 16;
-    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * kLoadStages + 2 * kWideStages + 5);
+    uint8_t *sa = base, *sb = sa + kWides * kBytesA, *sq = sb + kLoads * kBytesB, *se = sq + (WIDEN ? kLoads * kBytesQ : 0);
+    uint64_t *bars = (uint64_t *)(se + (WIDEN ? kLoads * kBytesE : 0));
+    const uint32_t full = smem_address(bars), empty = full + 8 * kLoads, ready = empty + 8 * kLoads, used = ready + 8 * kWides,
+                   acc_full = used + 8 * kWides, acc_empty = acc_full + 16, drained = acc_empty + 16;
+    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * kLoads + 2 * kWides + 5);
     volatile int *failed = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kLoadStages; ++s) {
-            barrier_init(full + 8 * s, WIDE_E ? 1 : 1 + 64);
+        for (int s = 0; s < kLoads; ++s) {
+            barrier_init(full + 8 * s, WIDEN && !WIDE_E ? 1 + 64 : 1);
             barrier_init(empty + 8 * s, 1);
         }
-        for (int s = 0; s < kWideStages; ++s) {
-            barrier_init(ready + 8 * s, 2 * 4);
+        for (int s = 0; s < kWides; ++s) {
+            barrier_init(ready + 8 * s, WIDEN ? 2 * 4 : 2);
             barrier_init(used + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -160,24 +168,30 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     int k0, k1, i0, o0;
 
     if (warp < 4) {
-        registers_down<48>();
+        if (WIDEN) registers_down<48>();
         if (warp == 0 && lane == 0) {
             prefetch_map(&map_y);
-            prefetch_map(&map_q);
-            if (WIDE_E) prefetch_map(&map_e);
+            prefetch_map(&map_x);
+            if (WIDEN && WIDE_E) prefetch_map(&map_e);
             uint32_t n = 0;
             bool ok = true;
             while (ok && work.next(tile, k0, k1)) {
                 tile_place(a, tile, i0, o0);
                 i0 += rank * kTileI;
                 for (int k = k0; k < k1; ++k, ++n) {
-                    const uint32_t s = n % kLoadStages, round = n / kLoadStages;
+                    const uint32_t s = n % kLoads, round = n / kLoads;
                     if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
                     const int plane = k / a.blocks, t0 = (k - plane * a.blocks) * kTileT;
                     const uint32_t bar = full + 8 * s;
-                    barrier_expect(bar, kBytesB + kBytesQ + (WIDE_E ? kBytesE : 0));
-                    tensor_load_2d(smem_address(sq + s * kBytesQ), &map_q, i0, t0, bar);
-                    if (WIDE_E) tensor_load_2d(smem_address(se + s * kBytesE), &map_e, i0 / kGroup & ~15, t0, bar);
+                    barrier_expect(bar, kBytesB + (!WIDEN ? kBytesA : kBytesQ + (WIDE_E ? kBytesE : 0)));
+                    if constexpr (WIDEN) {
+                        tensor_load_2d(smem_address(sq + s * kBytesQ), &map_x, i0, t0, bar);
+                        if (WIDE_E) tensor_load_2d(smem_address(se + s * kBytesE), &map_e, i0 / kGroup & ~15, t0, bar);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kTileI / 64; ++j)
+                            tensor_load_2d(smem_address(sa + s * kBytesA + j * (kTileT * 128)), &map_x, i0 + 64 * j, t0, bar);
+                    }
 #pragma unroll
                     for (int j = 0; j < kHalfO / 64; ++j)
                         tensor_load_3d(smem_address(sb + s * kBytesB + j * (kTileT * 128)), &map_y, o0 + rank * kHalfO + 64 * j, t0, plane, bar);
@@ -185,8 +199,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             }
             // the copies in flight end before the CTA does
             const uint64_t start = nanoseconds();
-            for (uint32_t m = n > kLoadStages ? n - kLoadStages : 0; m < n; ++m)
-                while (!barrier_try(full + 8 * (m % kLoadStages), (m / kLoadStages) & 1) && nanoseconds() - start < kWaitLimit) {}
+            for (uint32_t m = n > kLoads ? n - kLoads : 0; m < n; ++m)
+                while (!barrier_try(full + 8 * (m % kLoads), (m / kLoads) & 1) && nanoseconds() - start < kWaitLimit) {}
         } else if (warp == 1 && lane == 0 && rank != 0) {
             const uint64_t start = nanoseconds();                  // the other CTA's last commit arrives here too
             while (!barrier_try(drained, 0) && nanoseconds() - start < 2 * kWaitLimit) {}
@@ -201,15 +215,15 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                     tmem_fence_after();
                     const int stop = k + kChunk < k1 ? k + kChunk : k1;
                     for (int first = k; k < stop; ++k, ++n) {
-                        const uint32_t w = n % kWideStages, s = n % kLoadStages;
-                        if (!(ok = barrier_wait(ready + 8 * w, (n / kWideStages) & 1, failed))) break;   // both CTAs' dy has landed, too
+                        const uint32_t w = n % kWides, s = n % kLoads;
+                        if (!(ok = barrier_wait(ready + 8 * w, (n / kWides) & 1, failed))) break;   // both CTAs' dy has landed, too
                         tmem_fence_after();
                         const uint64_t da = operand_descriptor(smem_address(sa + w * kBytesA), kTileT * 128);
                         const uint64_t db = operand_descriptor(smem_address(sb + s * kBytesB), kTileT * 128);
 #pragma unroll
                         for (int j = 0; j < kTileT / 16; ++j)     // 16 tokens each: 2048 bytes further along k
                             mma(tmem + buf * kTileO, da + j * (2048 >> 4), db + j * (2048 >> 4), idesc, k > first || j > 0);
-                        mma_commit(used + 8 * w);
+                        if (WIDEN) mma_commit(used + 8 * w);
                         mma_commit(empty + 8 * s);
                     }
                     if (ok) mma_commit(acc_full + 8 * buf);
@@ -218,7 +232,15 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             mma_commit(drained);
             const uint64_t start = nanoseconds();
             while (!barrier_try(drained, 0) && nanoseconds() - start < kWaitLimit) {}
-        } else if (!WIDE_E && warp >= 2) {
+        } else if (!WIDEN && warp == 2 && lane == 0) {
+            uint32_t n = 0;
+            bool ok = true;
+            while (ok && work.next(tile, k0, k1))
+                for (int k = k0; k < k1; ++k, ++n) {
+                    if (!(ok = barrier_wait(full + 8 * (n % kLoads), (n / kLoads) & 1, failed))) break;
+                    barrier_arrive_at(ready + 8 * (n % kLoads), 0);
+                }
+        } else if (WIDEN && !WIDE_E && warp >= 2) {
             const int row = threadIdx.x - 64;                      // token of a stage
             uint32_t n = 0;
             bool ok = true;
@@ -226,7 +248,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 tile_place(a, tile, i0, o0);
                 i0 += rank * kTileI;
                 for (int k = k0; k < k1; ++k, ++n) {
-                    const uint32_t s = n % kLoadStages, round = n / kLoadStages;
+                    const uint32_t s = n % kLoads, round = n / kLoads;
                     if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
                     const int64_t t = (int64_t)(k % a.blocks) * kTileT + row;
                     const bool there = t < a.tokens && i0 < a.I;
@@ -239,7 +261,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
         }
-    } else if (warp < 4 + kWidenThreads / 32) {
+    } else if (WIDEN && warp < 12) {
         registers_down<56>();
         // Two groups of four warps take stages in turn.  8 threads per token, 16 columns each: a warp reads four whole
         // rows of q, and then the tokens 16, 32 and 48 further on.
@@ -256,8 +278,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             const int e0 = (WIDE_E ? i0 / kGroup & 15 : 0) + (part >> 1);
             for (int k = k0; k < k1; ++k, ++n) {
                 if (n % 2 != group) continue;
-                const uint32_t s = n % kLoadStages, w = n % kWideStages;
-                if (!(ok = barrier_wait(full + 8 * s, (n / kLoadStages) & 1, failed))) break;
+                const uint32_t s = n % kLoads, w = n % kWides;
+                if (!(ok = barrier_wait(full + 8 * s, (n / kLoads) & 1, failed))) break;
                 const uint8_t *q = sq + s * kBytesQ + row * kTileI + part * 16, *e = se + s * kBytesE + row * kRowE + e0;
                 uint8_t *out = sa + w * kBytesA;
                 uint4 v[4];
@@ -267,7 +289,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                     v[p] = *reinterpret_cast<const uint4 *>(q + p * 16 * kTileI);
                     ex[p] = e[p * 16 * kRowE];
                 }
-                if (!(ok = barrier_wait(used + 8 * w, ((n / kWideStages) & 1) ^ 1, failed))) break;
+                if (!(ok = barrier_wait(used + 8 * w, ((n / kWides) & 1) ^ 1, failed))) break;
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
                     uint4 lo, hi;
@@ -281,8 +303,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             }
         }
     } else {
-        registers_up<160>();
-        const int half = (warp - 4 - kWidenThreads / 32) >> 2, quarter = warp & 3;       // columns half * 128.., lanes quarter * 32..
+        if (WIDEN) registers_up<160>();
+        const int half = (warp & 7) >> 2, quarter = warp & 3;       // columns half * 128.., lanes quarter * 32..
         const int row = quarter * 32 + lane;
         const uint32_t source = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
         uint32_t chunk = 0;
