@@ -435,10 +435,10 @@ namespace {
 
 // What a call launches and keeps in its workspace: partial tiles first, then the 16-bit pieces of dy, then x^ in 16 bits.
 struct GradPlan {
-    bool copy_dy, copy_x, split;
+    bool copy_dy, copy_x;
     int planes, pairs;
     int64_t ld_planes, ld_x, partial_bytes, plane_bytes, x_bytes;
-    int64_t tiles_i, tiles_o, blocks;
+    int64_t tiles_i, tiles_o, blocks, whole;
 };
 GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *dy, int64_t lddy, int sms) {
     GradPlan p;
@@ -451,13 +451,13 @@ GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *d
     p.tiles_i = ceil_div(I, deft::kPairI);
     p.tiles_o = ceil_div(O, deft::kTileO);
     p.blocks = ceil_div(T, deft::kTileT);
-    // A pair of CTAs per pair of SMs.  Whole tiles while they fill the last round of pairs well; otherwise the blocks of all
-    // tiles are cut into equal runs, which costs a pass over the shared tiles' partial sums.
-    const int64_t tiles = p.tiles_i * p.tiles_o, workers = sms / 2, rounds = ceil_div(tiles, workers);
-    p.split = p.blocks * p.planes > 1 && tiles * 10 < rounds * workers * 9;
-    const int64_t most = p.split ? tiles * p.blocks * p.planes : tiles;
+    // A pair of CTAs per pair of SMs.  Rounds of whole tiles; the tiles of a last round that would leave a tenth of the
+    // pairs idle or more are cut by tokens into equal runs instead, which costs a pass over their partial sums.
+    const int64_t tiles = p.tiles_i * p.tiles_o, workers = sms / 2, rest = tiles % workers, per_tile = p.blocks * p.planes;
+    p.whole = rest * 10 >= workers * 9 || per_tile == 1 ? tiles : tiles - rest;
+    const int64_t most = p.whole == 0 ? tiles * per_tile : tiles;
     p.pairs = (int)(most < workers ? most : workers);
-    p.partial_bytes = p.split ? (int64_t)p.pairs * 4 * deft::kTileO * deft::kTileI * 4 : 0;
+    p.partial_bytes = p.whole < tiles ? (int64_t)p.pairs * 4 * deft::kTileO * deft::kTileI * 4 : 0;
     // A tile of x^ is widened once for each tile of dw along o (and each piece of dy).  From kWidenOnce of them on it is
     // cheaper to widen x^ to memory first, as long as that keeps to the documented size of the workspace.
     p.x_bytes = T * p.ld_x * 2;
@@ -570,7 +570,7 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return fail(DEF_ERR_CUDA, "the driver refused a tensor map of e");
     }
-    deft::WeightGrad a = {e, dw, (float *)workspace, T, O, I, e_stride(I), (int)p.tiles_i, (int)p.tiles_o, (int)p.blocks, p.planes, accumulate, p.split};
+    deft::WeightGrad a = {e, dw, (float *)workspace, T, O, I, e_stride(I), (int)p.tiles_i, (int)p.tiles_o, (int)p.blocks, p.planes, accumulate, p.whole};
     cudaError_t err = cudaSuccess;
     auto launch = [&](auto kernel, auto shape) {
         using S = decltype(shape);
@@ -600,8 +600,8 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         cudaGetLastError();
         return cuda_fail(err, "def_checkpoint_weight_grad");
     }
-    if (p.split) {
-        deft::weight_grad_join_kernel<<<(unsigned)(p.tiles_i * p.tiles_o * 2 * (deft::kTileO / 8)), 256, 0, stream>>>(a, p.pairs);
+    if (const int64_t cut = p.tiles_i * p.tiles_o - p.whole; cut > 0) {
+        deft::weight_grad_join_kernel<<<(unsigned)(cut * 2 * (deft::kTileO / 8)), 256, 0, stream>>>(a, p.pairs);
         DEF_TRY(launched("def_checkpoint_weight_grad (join)"));
     }
     return DEF_OK;

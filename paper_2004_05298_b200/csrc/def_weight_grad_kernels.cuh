@@ -23,7 +23,7 @@ constexpr int kBytesA = kTileI * kTileT * 2, kBytesB = kHalfO * kTileT * 2, kByt
 
 // Two ways to the operand x^.  Widening: q is loaded and widened in shared memory by two groups of four warps, each time
 // a tile needs it.  Else x^ lies in memory in 16 bits (widened once by a kernel of its own) and is loaded like dy.
-constexpr int kWidenOnce = 4;
+constexpr int kWidenOnce = 12;
 template <bool WIDEN> struct GradShape {
     static constexpr int loads = 7, wides = WIDEN ? 3 : 0;   // stages of what is loaded; of widened q
     static constexpr int bytes_x = WIDEN ? kBytesQ + kBytesE : kBytesA;
@@ -36,40 +36,38 @@ struct WeightGrad {
     float *dw, *partial;                  // partial: [CTA][2][kTileO][kTileI]
     int64_t tokens, O, I, lde;
     int tiles_i, tiles_o, blocks, planes; // blocks: of kTileT tokens, per plane of dy
-    int accumulate, split;                // split: CTAs share tiles (contiguous ranges of all tiles' blocks)
+    int accumulate;
+    int64_t whole;                        // tiles [0, whole) go to pairs one by one; the blocks of the others are cut evenly
 };
 
-// The pieces of work of one pair of CTAs: (tile, blocks [k0, k1)).  Split: an equal run of the blocks of all tiles in order; a
-// tile that is cut goes to partial slot 0 of the pairs that do not hold its first block, slot 1 of the one that does.
+// The pieces of work of one pair of CTAs: (tile, blocks [k0, k1)).  First its share of the whole tiles, then an equal run
+// of the blocks of the remaining tiles in order; a tile that is cut goes to partial slot 0 of the pairs that do not hold
+// its first block, slot 1 of the one that does.
 struct Pieces {
-    int64_t pos, end, step, per_tile;
-    bool split;
+    int64_t tile, pos, end, whole, per_tile;
     __device__ Pieces(const WeightGrad &a) {
+        const int64_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
         per_tile = (int64_t)a.blocks * a.planes;
-        split = a.split;
-        const int64_t tiles = (int64_t)a.tiles_i * a.tiles_o;
-        if (split) {
-            const int64_t all = tiles * per_tile;
-            pos = all * (blockIdx.x / 2) / (gridDim.x / 2);
-            end = all * (blockIdx.x / 2 + 1) / (gridDim.x / 2);
-        } else {
-            pos = blockIdx.x / 2;
-            end = tiles;
-        }
+        whole = a.whole;
+        tile = pair;
+        const int64_t rest = ((int64_t)a.tiles_i * a.tiles_o - whole) * per_tile;
+        pos = rest * pair / pairs;
+        end = rest * (pair + 1) / pairs;
     }
-    __device__ bool next(int64_t &tile, int &k0, int &k1) {
-        if (pos >= end) return false;
-        if (split) {
-            tile = pos / per_tile;
-            k0 = (int)(pos - tile * per_tile);
-            k1 = (int)(end - tile * per_tile < per_tile ? end - tile * per_tile : per_tile);
-            pos += k1 - k0;
-        } else {
-            tile = pos;
+    __device__ bool next(int64_t &t, int &k0, int &k1) {
+        if (tile < whole) {
+            t = tile;
             k0 = 0;
             k1 = (int)per_tile;
-            pos += gridDim.x / 2;
+            tile += gridDim.x / 2;
+            return true;
         }
+        if (pos >= end) return false;
+        t = pos / per_tile;
+        k0 = (int)(pos - t * per_tile);
+        k1 = (int)(end - t * per_tile < per_tile ? end - t * per_tile : per_tile);
+        pos += k1 - k0;
+        t += whole;
         return true;
     }
 };
@@ -336,7 +334,7 @@ __global__ void __launch_bounds__(GradShape<WIDEN>::threads, 1)
 #pragma unroll
                 for (int i = 0; i < 128; ++i) acc[i] = NAN;
             }
-            if (a.split && (k0 > 0 || k1 < work.per_tile)) {
+            if (k0 > 0 || k1 < work.per_tile) {
                 float *out = a.partial + ((int64_t)blockIdx.x * 2 + (k0 > 0 ? 0 : 1)) * (kTileO * kTileI) + half * 128 * kTileI + row;
 #pragma unroll
                 for (int i = 0; i < 128; ++i) out[i * kTileI] = acc[i];
@@ -364,11 +362,11 @@ __global__ void __launch_bounds__(GradShape<WIDEN>::threads, 1)
     }
 }
 
-// The tiles that pairs of the split kernel shared: their parts, added in the order of the tokens.  One CTA per 8 rows of
+// The tiles that pairs shared: their parts, added in the order of the tokens.  One CTA per 8 rows of
 // dw of half a tile.
 __global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad a, int pairs) {
-    const int64_t per_tile = (int64_t)a.blocks * a.planes, all = per_tile * a.tiles_i * a.tiles_o;
-    const int64_t half_tile = blockIdx.x / (kTileO / 8), tile = half_tile / 2;
+    const int64_t per_tile = (int64_t)a.blocks * a.planes, all = ((int64_t)a.tiles_i * a.tiles_o - a.whole) * per_tile;
+    const int64_t half_tile = blockIdx.x / (kTileO / 8), tile = half_tile / 2;       // of the tiles that were cut
     const int rank = (int)(half_tile % 2);
     const int col = (int)(blockIdx.x % (kTileO / 8)) * 8 + threadIdx.x / 32;
     const int64_t begin = tile * per_tile, end = begin + per_tile;
@@ -377,7 +375,7 @@ __global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad 
     while (c + 1 < pairs && all * (c + 1) / pairs <= begin) ++c;
     if (all * c / pairs <= begin && all * (c + 1) / pairs >= end) return;        // whole in one pair: written there
     int i0, o0;
-    tile_place(a, tile, i0, o0);
+    tile_place(a, a.whole + tile, i0, o0);
     i0 += rank * kTileI;
     const int i = threadIdx.x % 32 * 4;
     if (o0 + col >= a.O || i0 + i >= a.I) return;
