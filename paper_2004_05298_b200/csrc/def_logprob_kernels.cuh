@@ -12,13 +12,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Maximum that keeps a NaN (fmaxf drops it).
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
-}
-
 // A logit at or below this is masked; -infinity and the lowest value of bf16 and fp32 are.
 constexpr float kMasked = -1e30f;
 

@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
         const T *hr = (const T *)a.h + t * a.ldh;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+            const int col = (it * THREADS + (int)threadIdx.x) * V;
             if (col < a.C) load_floats<T, V>(hr + col, h[it]);
             else
                 for (int i = 0; i < V; ++i) h[it][i] = 0.f;
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             const T *br = (const T *)a.b + t * a.ldb;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+                const int col = (it * THREADS + (int)threadIdx.x) * V;
                 if (col < a.C) load_floats<T, V>(br + col, b[it]);
                 else
                     for (int i = 0; i < V; ++i) b[it][i] = 0.f;
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             if (a.hb.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+                    const int col = (it * THREADS + (int)threadIdx.x) * V;
                     store_held<V>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, col < a.C, b[it]);
                 }
             sum = cta_sum<THREADS>(sum, scratch[0]);
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             sum = 0.f;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+                const int col = (it * THREADS + (int)threadIdx.x) * V;
                 if (col < a.C) {
                     float w[V], g[V];
                     load_params<V>(a.w_post + col, w);
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             if (a.hh.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+                    const int col = (it * THREADS + (int)threadIdx.x) * V;
                     float x[V];
 #pragma unroll
                     for (int i = 0; i < V; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));   // h' as stored
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             if (a.hh.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+                    const int col = (it * THREADS + (int)threadIdx.x) * V;
                     store_held<V>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, col < a.C, h[it]);
                 }
         }
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
         T *no = (T *)a.n_out + t * a.ldn;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+            const int col = (it * THREADS + (int)threadIdx.x) * V;
             float n[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) n[i] = 0.f;
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
         float dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+            const int col = (it * THREADS + (int)threadIdx.x) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) D[it][i] = x[it][i] = 0.f;
             if (col < a.C) {
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
         dot = cta_sum<THREADS>(dot, scratch[0]) * a.inv_C;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+            const int col = (it * THREADS + (int)threadIdx.x) * V;
             if (col < a.C) {
                 float in[V], out[V];
                 if (a.dh_in) load_floats<T, V>((const T *)a.dh_in + t * a.lddhi + col, in);
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
             dot = 0.f;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+                const int col = (it * THREADS + (int)threadIdx.x) * V;
                 if (col < a.C) {
                     float w[V], g[V];
                     if (a.hb.q) load_held<V>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, x[it]);
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
             dot = cta_sum<THREADS>(dot, scratch[1]) * a.inv_C;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+                const int col = (it * THREADS + (int)threadIdx.x) * V;
                 if (col < a.C) {
                     float out[V];
 #pragma unroll
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
     float *px = a.partial + (int64_t)blockIdx.x * 2 * a.C;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int64_t col = (int64_t)(it * THREADS + threadIdx.x) * V;
+        const int col = (it * THREADS + (int)threadIdx.x) * V;
         if (col < a.C)
 #pragma unroll
             for (int i = 0; i < V; ++i) {

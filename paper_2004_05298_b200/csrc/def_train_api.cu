@@ -122,23 +122,28 @@ template <typename F> void by_dtype(int32_t dtype, F f) {
     else f(__half());
 }
 
+constexpr int kUsualSms = 148;      // what launches and workspaces are sized for before a device is looked at
+
 template <int N> struct Width { static constexpr int value = N; };
 template <typename F> void by_width(bool eight, F f) {
     if (eight) f(Width<8>());
     else f(Width<1>());
 }
 
-// Grid of the kernels that work on rows by columns without sums: a warp lies in one row.
-struct Plane {
-    dim3 grid, block;
-};
-Plane plane(int64_t T, int64_t C, int V) {
-    const int64_t lanes = ceil_div(C, V);
-    unsigned bx = 32;
-    while (bx < 256 && bx < lanes) bx *= 2;
-    const unsigned by = 256 / bx;
-    const int64_t gy = ceil_div(T, by);
-    return {dim3((unsigned)ceil_div(lanes, bx), (unsigned)(gy < 65535 ? gy : 65535)), dim3(bx, by)};
+constexpr int kPlaneRows = 4;
+// Launch of a kernel that works on rows by columns without sums: a warp lies in one row.  f(V, grid, block).
+template <typename F> void on_plane(bool eight, int64_t T, int64_t C, F f) {
+    by_width(eight, [&](auto width) {
+        const int64_t lanes = ceil_div(C, width.value);
+        unsigned bx = 32;
+        while (bx < 256 && bx < lanes) bx *= 2;
+        const dim3 block(bx, 256 / bx);
+        // A CTA walks kPlaneRows rows of its columns where that leaves enough CTAs: fewer instructions go into addresses.
+        const int64_t gx = ceil_div(lanes, bx), all = ceil_div(T, block.y);
+        int64_t gy = ceil_div(all, kPlaneRows);
+        if (gx * gy < 32 * kUsualSms) gy = ceil_div(32 * kUsualSms, gx) < all ? ceil_div(32 * kUsualSms, gx) : all;
+        f(width, dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), block);
+    });
 }
 
 }  // namespace
@@ -164,10 +169,8 @@ extern "C" int def_checkpoint_pack(int32_t dtype, int64_t T, int64_t C, const vo
     const bool eight = C % 8 == 0 && wide(x, ldx, es);
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
-        by_width(eight, [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            const Plane p = plane(T, C, V);
-            deft::pack_kernel<E, V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>((const E *)x, ldx, T, C, q, e, q_stride(C), e_stride(C));
+        on_plane(eight, T, C, [&](auto v, dim3 grid, dim3 block) {
+            deft::pack_kernel<E, v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>((const E *)x, ldx, T, (int)C, q, e, q_stride(C), e_stride(C));
         });
     });
     return launched("def_checkpoint_pack");
@@ -186,10 +189,8 @@ extern "C" int def_checkpoint_unpack(int32_t dtype, int64_t T, int64_t C, const 
     const bool eight = C % 8 == 0 && wide(out, ldout, es);
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
-        by_width(eight, [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            const Plane p = plane(T, C, V);
-            deft::unpack_kernel<E, V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>(q, e, q_stride(C), e_stride(C), T, C, (E *)out, ldout);
+        on_plane(eight, T, C, [&](auto v, dim3 grid, dim3 block) {
+            deft::unpack_kernel<E, v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>(q, e, q_stride(C), e_stride(C), T, (int)C, (E *)out, ldout);
         });
     });
     return launched("def_checkpoint_unpack");
@@ -215,10 +216,8 @@ extern "C" int def_gated_forward(int32_t dtype, int64_t T, int64_t F, const void
     deft::GatedForward a = {gate, up, h, ldg, ldu, ldh, gate_q, up_q, gate_e, up_e, T, F, q_stride(F), e_stride(F)};
     const bool eight = F % 8 == 0 && wide(gate, ldg, es) && wide(up, ldu, es) && wide(h, ldh, es);
     by_dtype(dtype, [&](auto type) {
-        by_width(eight, [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            const Plane p = plane(T, F, V);
-            deft::gated_forward_kernel<decltype(type), V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>(a);
+        on_plane(eight, T, F, [&](auto v, dim3 grid, dim3 block) {
+            deft::gated_forward_kernel<decltype(type), v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>(a);
         });
     });
     return launched("def_gated_forward");
@@ -246,10 +245,8 @@ extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const voi
     deft::GatedBackward a = {dh, gate_q, up_q, gate_e, up_e, dgate, dup, h_out, lddh, lddg, lddu, ldh, h_q, h_e, T, F, q_stride(F), e_stride(F)};
     const bool eight = F % 8 == 0 && wide(dh, lddh, es) && wide(dgate, lddg, es) && wide(dup, lddu, es) && wide(h_out, ldh, es);
     by_dtype(dtype, [&](auto type) {
-        by_width(eight, [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            const Plane p = plane(T, F, V);
-            deft::gated_backward_kernel<decltype(type), V><<<p.grid, p.block, 0, (cudaStream_t)cuda_stream>>>(a);
+        on_plane(eight, T, F, [&](auto v, dim3 grid, dim3 block) {
+            deft::gated_backward_kernel<decltype(type), v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>(a);
         });
     });
     return launched("def_gated_backward");
@@ -466,7 +463,6 @@ GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *d
     if (!p.copy_x) p.x_bytes = 0;
     return p;
 }
-constexpr int kUsualSms = 148;      // what a workspace is sized for before a device is looked at
 
 // The driver's entry point for tensor maps, found at run time: the library itself does not link the driver.
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -539,13 +535,11 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
     const void *xs = q;
     if (p.copy_x) {
         void *wide_x = (char *)workspace + p.partial_bytes + p.plane_bytes;
-        by_width(I % 8 == 0, [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            const Plane g = plane(T, I, V);
+        on_plane(I % 8 == 0, T, I, [&](auto v, dim3 grid, dim3 block) {
             if (half)
-                deft::unpack_kernel<__half, V><<<g.grid, g.block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, I, (__half *)wide_x, p.ld_x);
+                deft::unpack_kernel<__half, v.value><<<grid, block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, (int)I, (__half *)wide_x, p.ld_x);
             else
-                deft::unpack_kernel<__nv_bfloat16, V><<<g.grid, g.block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, I, (__nv_bfloat16 *)wide_x, p.ld_x);
+                deft::unpack_kernel<__nv_bfloat16, v.value><<<grid, block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, (int)I, (__nv_bfloat16 *)wide_x, p.ld_x);
         });
         DEF_TRY(launched("def_checkpoint_weight_grad (widen)"));
         xs = wide_x;

@@ -84,61 +84,109 @@ template <int V> __device__ __forceinline__ void load_params(const float *p, flo
 // is exact and the only rounding is the one to an integer; q 2^k has at most 7 bits of magnitude and is exact in
 // bf16 and fp32.
 // ---------------------------------------------------------------------------
-template <int V> __device__ __forceinline__ uint32_t group_exponent(const float (&x)[V]) {
-    // Magnitudes as integers: ordered like the magnitudes, and an infinity or NaN (>= 0x7f800000) wins.
-    uint32_t top = 0;
+__device__ __forceinline__ float max_nan(float a, float b) {       // keeps a NaN (fmaxf drops it)
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+// Bits of the group's largest magnitude; at least 0x7f800000 if it holds an infinity or a NaN.
+template <int V> __device__ __forceinline__ uint32_t group_top(float top) {
+    uint32_t bits = __float_as_uint(top) & 0x7fffffffu;
 #pragma unroll
-    for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int s = 1; s < kGroup / V; s <<= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, s));
+    return bits;
+}
+template <int V> __device__ __forceinline__ uint32_t group_top(const float (&x)[V]) {
+    float top = fabsf(x[0]);
 #pragma unroll
-    for (int s = 1; s < kGroup / V; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+    for (int i = 1; i < V; ++i) top = max_nan(top, fabsf(x[i]));
+    return group_top<V>(top);
+}
+// The same from 16-bit values as loaded: magnitudes of either type order like the integers they are held in.
+template <typename T, int V> __device__ __forceinline__ uint32_t group_top(const Frag<T, V> &f) {
+    if constexpr (sizeof(T) == 2 && V == 8) {
+        uint32_t w[4];
+        memcpy(w, &f, sizeof(w));
+        const uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+        const uint16_t top = (uint16_t)max(m & 0xffffu, m >> 16);
+        T t;
+        memcpy(&t, &top, sizeof(t));
+        return group_top<V>(to_float<T>(t));
+    } else {
+        float x[V];
+        to_floats<T, V>(f, x);
+        return group_top<V>(x);
+    }
+}
+__device__ __forceinline__ uint32_t group_exponent(uint32_t top) {
     const int biased = (int)(top >> 23);            // floor(log2 amax) + 127; 0 for zero and subnormals
     return biased == 255 ? 255u : (uint32_t)max(biased - 6, 1);
 }
-template <int V> __device__ __forceinline__ void quantise(const float (&x)[V], uint32_t e, int8_t (&q)[V]) {
-    const float inv = e == 255 ? 0.f : __uint_as_float((254u - e) << 23);   // 2^-k, e in [1, 248]
+// x 2^-k is rounded to the nearest integer by adding 1.5 2^23 in the same operation: the sum's last bits are the integer,
+// in two's complement (a conversion instruction runs at an eighth of that rate).  Only a group whose largest magnitude
+// rounds to 128 steps is clamped, and only one with an infinity or a NaN is cleared.
+template <int V> __device__ __forceinline__ void quantise(const float (&x)[V], uint32_t top, uint32_t e, uint32_t (&q)[V]) {
+    const float inv = __uint_as_float((254u - e) << 23);                    // 2^-k, e in [1, 248]; -infinity for 255
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int r = e == 255 ? 0 : __float2int_rn(x[i] * inv);
-        q[i] = (int8_t)max(-127, min(127, r));
+    for (int i = 0; i < V; ++i) q[i] = __float_as_uint(fmaf(x[i], inv, 12582912.f));
+    if (!(fabsf(__uint_as_float(top) * inv) < 127.5f)) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) q[i] = e == 255 ? 0u : min(max(q[i], 0x4b400000u - 127u), 0x4b400000u + 127u);
     }
 }
 // 2^k; +infinity for e = 255, which makes q e NaN because q is 0 there.
 __device__ __forceinline__ float group_scale(uint32_t e) { return __uint_as_float(e << 23); }
 
-template <int V> __device__ __forceinline__ void store_q(int8_t *p, const int8_t (&q)[V]) {
+// Stores the low bytes of q.
+template <int V> __device__ __forceinline__ void store_q(int8_t *p, const uint32_t (&q)[V]) {
     if constexpr (V == 1) {
-        *p = q[0];
+        *p = (int8_t)q[0];
     } else {
         uint2 w;
-        memcpy(&w, q, sizeof(w));
+        w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+        w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
         *reinterpret_cast<uint2 *>(p) = w;
     }
 }
-template <int V> __device__ __forceinline__ void load_held(const int8_t *q, const uint8_t *e, int64_t col, float (&x)[V]) {
-    int8_t v[V];
-    if constexpr (V == 1) {
-        v[0] = q[col];
-    } else {
-        uint2 w;
-        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "l"(q + col));
-        memcpy(v, &w, sizeof(w));
-    }
-    const float scale = group_scale(e[col / kGroup]);
+// V of a row's 8-bit integers as they lie in memory, and the values they stand for.
+template <int V> struct RawQ { uint32_t w[V == 1 ? 1 : V / 4]; };
+template <int V> __device__ __forceinline__ RawQ<V> load_q(const int8_t *p) {
+    RawQ<V> r;
+    if constexpr (V == 1) r.w[0] = (uint8_t)*p;
+    else asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
+    return r;
+}
+// q 2^k as the difference of 2^k (2^23 + q + 128), which the byte completes to a float's bits, and 2^k (2^23 + 128); both
+// and the difference are exact.  Steps above 2^104 (and the marker 255) take the plain way.
+template <int V> __device__ __forceinline__ void held_values(const RawQ<V> &q, uint32_t e, float (&x)[V]) {
+    const uint32_t base = (e + 23u) << 23;
+    const float zero = __uint_as_float(base | 128u);
+    if (e < 232u) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = (float)v[i] * scale;
+        for (int i = 0; i < V; ++i) x[i] = __uint_as_float(__byte_perm(q.w[i / 4] ^ 0x80808080u, base, 0x7650 + i % 4)) - zero;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (float)(int8_t)(q.w[i / 4] >> (i % 4 * 8)) * group_scale(e);
+    }
+}
+template <int V> __device__ __forceinline__ void load_held(const int8_t *q, const uint8_t *e, int col, float (&x)[V]) {
+    held_values<V>(load_q<V>(q + col), e[(unsigned)col / kGroup], x);
 }
 
-// Writes the checkpoint of V columns at `col`; every lane of the warp calls it, `valid` where the columns exist
-// (the others pass zeros).
+// Writes the checkpoint of V columns at `col`; every lane of the warp calls it, `valid` where the columns exist (the
+// others pass zeros).  `top`: group_top of the same values.
 template <int V>
-__device__ __forceinline__ void store_held(int8_t *q, uint8_t *e, int64_t col, bool valid, const float (&x)[V]) {
-    const uint32_t ex = group_exponent<V>(x);
-    int8_t v[V];
-    quantise<V>(x, ex, v);
+__device__ __forceinline__ void store_held(int8_t *q, uint8_t *e, int col, bool valid, const float (&x)[V], uint32_t top) {
+    const uint32_t ex = group_exponent(top);
+    uint32_t v[V];
+    quantise<V>(x, top, ex, v);
     if (valid) {
         store_q<V>(q + col, v);
-        if (col % kGroup == 0) e[col / kGroup] = (uint8_t)ex;
+        if (col % kGroup == 0) e[(unsigned)col / kGroup] = (uint8_t)ex;
     }
+}
+template <int V> __device__ __forceinline__ void store_held(int8_t *q, uint8_t *e, int col, bool valid, const float (&x)[V]) {
+    store_held<V>(q, e, col, valid, x, group_top<V>(x));
 }
 
 // ---------------------------------------------------------------------------
