@@ -1,6 +1,7 @@
 // Token log probabilities with entropy and top alternatives, and their gradient (see include/def_train.h).
 #pragma once
 
+#include "def_sm100.cuh"
 #include "def_train_common.cuh"
 
 namespace deft {
@@ -15,28 +16,30 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // A logit at or below this is masked; -infinity and the lowest value of bf16 and fp32 are.
 constexpr float kMasked = -1e30f;
 
-// Running statistics of part of a row, relative to its maximum m:  s = sum 2^y,  u = sum y 2^y with
-// y = (x - m) log2(e).  The difference is taken first: it is small where it counts, whatever m is.
+// Running statistics of part of a row:  s = sum 2^y,  u = sum y 2^y with y = x log2(e) - r.  The reference r is m log2(e)
+// rounded to an integer, m the maximum so far: the product is not rounded before r is taken from it, so that y is as good
+// as if m had been subtracted first, in one operation.
 struct Stats {
-    float m, s, u;
+    float m, r, s, u;
 };
-__device__ __forceinline__ Stats empty_stats() { return {kMasked, 0.f, 0.f}; }
+__device__ __forceinline__ Stats empty_stats() { return {kMasked, kMasked, 0.f, 0.f}; }
 // y is held at -1e4, where 2^y is 0 and 0 times y still is.
-__device__ __forceinline__ float exponent(float x, float m) { return max_nan((x - m) * kLog2e, -1e4f); }
-__device__ __forceinline__ void rebase(Stats &a, float m) {              // m >= a.m
-    const float d = exponent(a.m, m), f = exp2_fast(d);
+__device__ __forceinline__ float exponent(float x, float r) { return max_nan(fmaf(x, kLog2e, -r), -1e4f); }
+__device__ __forceinline__ void rebase(Stats &a, float m, float r) {     // m >= a.m
+    const float d = max_nan(a.r - r, -1e4f), f = exp2_fast(d);
     a.u = fmaf(d, a.s, a.u) * f;
     a.s *= f;
     a.m = m;
+    a.r = r;
 }
 __device__ __forceinline__ Stats join(Stats a, Stats b) {
-    const float m = fmaxf(a.m, b.m);
-    rebase(a, m);
-    rebase(b, m);
-    return {m, a.s + b.s, a.u + b.u};
+    const float m = fmaxf(a.m, b.m), r = a.m >= b.m ? a.r : b.r;
+    rebase(a, m, r);
+    rebase(b, m, r);
+    return {m, r, a.s + b.s, a.u + b.u};
 }
 __device__ __forceinline__ Stats shfl_xor(const Stats &a, int lane) {
-    return {__shfl_xor_sync(0xffffffffu, a.m, lane), __shfl_xor_sync(0xffffffffu, a.s, lane),
+    return {__shfl_xor_sync(0xffffffffu, a.m, lane), __shfl_xor_sync(0xffffffffu, a.r, lane), __shfl_xor_sync(0xffffffffu, a.s, lane),
             __shfl_xor_sync(0xffffffffu, a.u, lane)};
 }
 
@@ -107,111 +110,184 @@ struct LogprobForward {
     int top;
 };
 
-// One CTA per row.  Thread i reads chunks i, i + THREADS, ... of V elements and keeps the running maximum, sum and
-// weighted sum, and which chunk first held its maximum.
+// A row as chunks of 8 elements that start on 16-byte boundaries, wherever the row starts: chunks [0, body), then chunk
+// `body` for the elements before the first of them and chunk body + 1 for those behind the last.
+template <typename T> struct RowChunks {
+    const T *row;
+    int head, body, tail;
+    __device__ RowChunks(const T *p, int V) : row(p) {
+        const int off = (int)((16u - ((uint32_t)(uintptr_t)p & 15u)) & 15u) / (int)sizeof(T);
+        head = off < V ? off : V;
+        body = (V - head) / 8;
+        tail = V - head - body * 8;
+    }
+    __device__ int start(int c) const { return c < body ? head + 8 * c : c == body ? 0 : head + 8 * body; }
+    __device__ int count(int c) const { return c < body ? 8 : c == body ? head : tail; }
+    __device__ Frag<T, 8> wide(int c) const { return load_frag<T, 8>(row + head + 8 * c); }
+    __device__ void any(int c, float (&v)[8]) const {                 // -infinity where there is no element
+        if (c < body) {
+            to_floats<T, 8>(wide(c), v);
+        } else {
+            const int n = count(c), at = start(c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? to_float<T>(row[at + i]) : -INFINITY;
+        }
+    }
+};
+
+__device__ __forceinline__ float largest(const float (&v)[8]) {
+    return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+}
+// Adds a chunk to a thread's statistics; `best` is the first chunk that held the thread's maximum.
+__device__ __forceinline__ void add_chunk(Stats &st, int &best, int c, const float (&v)[8], float top) {
+    if (top > st.m) {
+        rebase(st, top, rintf(top * kLog2e));
+        best = c;
+    }
+    if (st.m == kMasked) {                            // nothing but masked logits, or NaN, so far
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (v[i] != v[i]) st.s = st.u = NAN;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = exponent(v[i], st.r), p = exp2_fast(y);
+            st.s += p;
+            st.u = fmaf(p, y, st.u);
+        }
+    }
+}
+
+// A row is read by a cluster of `split` CTAs (one CTA where there are many rows).  Thread g of all their threads takes
+// chunks g, g + G, ... and keeps the running maximum, sum and weighted sum, and which chunk first held its maximum.
 //
-// Alternatives: an element among the row's `top` largest lies in the list of a thread whose own largest element is
-// also among the `top` largest; at most `top` threads have one.  So the threads' maxima are ranked, and only the
-// elements of the `top` best threads are looked at again (they are few, and in the L2).
-template <typename T, int V, int THREADS>
-__global__ void __launch_bounds__(THREADS) logprob_forward_kernel(const LogprobForward a) {
-    constexpr int kWarps = THREADS / 32;
+// Alternatives: an element among a CTA's `top` largest lies in the list of a thread whose own largest element is among
+// them too, and at most `top` threads have one.  So the threads' maxima are ranked, and only the elements of the `top` best
+// threads are looked at again (they are few, and in the L2).  The CTAs' lists are joined at the end.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_forward_kernel(const LogprobForward a, const int split) {
+    constexpr int kWarps = THREADS / 32, kAhead = 4;
     __shared__ Stats parts[32];
+    __shared__ Stats whole;
     __shared__ uint64_t lists[kWarps][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t chunks = a.V / V;                   // V divides a.V on this path
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const T *row = (const T *)a.x + t * a.ldx;
-        Stats st = empty_stats();
-        int64_t best = threadIdx.x;
-        for (int64_t c = threadIdx.x; c < chunks; c += THREADS) {
-            float v[V];
-            load_floats<T, V>(row + c * V, v);
-            float top = v[0];
+    const int rank = split == 1 ? 0 : (int)(blockIdx.x % split), G = split * THREADS, g = rank * THREADS + threadIdx.x;
+    const int V = (int)a.V;
+    const int64_t t = blockIdx.x / split;
+    const RowChunks<T> row((const T *)a.x + t * a.ldx, V);
+    Stats st = empty_stats();
+    int best = -1;
+    float v[8];
+    if (g == 0 && row.head) {
+        row.any(row.body, v);
+        add_chunk(st, best, row.body, v, largest(v));
+    }
+    int c = g;
+    for (; c + (kAhead - 1) * G < row.body; c += kAhead * G) {
+        Frag<T, 8> f[kAhead];
 #pragma unroll
-            for (int i = 1; i < V; ++i) top = fmaxf(top, v[i]);
-            if (top > st.m) {
-                rebase(st, top);
-                best = c;
-            }
-            if (st.m == kMasked) {                    // nothing but masked logits, or NaN, so far
+        for (int k = 0; k < kAhead; ++k) f[k] = row.wide(c + k * G);
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (v[i] != v[i]) st.s = st.u = NAN;
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float y = exponent(v[i], st.m), p = exp2_fast(y);
-                    st.s += p;
-                    st.u = fmaf(p, y, st.u);
-                }
-            }
+        for (int k = 0; k < kAhead; ++k) {
+            to_floats<T, 8>(f[k], v);
+            add_chunk(st, best, c + k * G, v, largest(v));
         }
-        const float own_max = st.m;
+    }
+    for (; c < row.body; c += G) {
+        row.any(c, v);
+        add_chunk(st, best, c, v, largest(v));
+    }
+    if (g == 1 && row.tail) {
+        row.any(row.body + 1, v);
+        add_chunk(st, best, row.body + 1, v, largest(v));
+    }
+    const float own_max = st.m;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) st = join(st, shfl_xor(st, d));
-        if (lane == 0) parts[warp] = st;
-        __syncthreads();
-        st = lane < kWarps ? parts[lane] : empty_stats();
+    for (int d = 16; d > 0; d >>= 1) st = join(st, shfl_xor(st, d));
+    if (lane == 0) parts[warp] = st;
+    __syncthreads();
+    st = lane < kWarps ? parts[lane] : empty_stats();
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) st = join(st, shfl_xor(st, d));
-        const bool none = st.m == kMasked && st.s == 0.f;            // the row is masked throughout
-        const float log_s = none ? 0.f : logf(st.s), m = none ? INFINITY : st.m;     // log p = (x - m) - log s
-        if (threadIdx.x == 0) {
-            a.lse[2 * t] = none ? -INFINITY : st.m;
-            a.lse[2 * t + 1] = log_s;
-            a.entropy[t] = none ? 0.f : log_s - st.u / st.s * kLn2;
-            const int64_t y = a.y[t];
-            a.logp[t] = y < 0 ? 0.f : y >= a.V ? NAN : none ? -INFINITY : (to_float<T>(row[y]) - m) - log_s;
-        }
-        if (a.top == 0) {
-            __syncthreads();                          // parts
-            continue;
-        }
-        // the best element of every thread
-        uint64_t key = 0;
+    for (int d = 16; d > 0; d >>= 1) st = join(st, shfl_xor(st, d));
+
+    uint64_t list = 0;
+    if (a.top > 0) {
+        uint64_t key = 0;                             // the best element of this thread
         if (own_max > kMasked) {
-#pragma unroll
-            for (int i = V - 1; i >= 0; --i) {
-                const float v = to_float<T>(row[best * V + i]);
-                if (v == own_max) key = make_key(v, best * V + i);
+            const int n = row.count(best), at = row.start(best);
+            for (int i = n - 1; i >= 0; --i) {
+                const float x = to_float<T>(row.row[at + i]);
+                if (x == own_max) key = make_key(x, at + i);
             }
         } else {                                      // masked logits order like others: look at all of them
-            for (int64_t c = threadIdx.x; c < chunks; c += THREADS)
-                for (int i = 0; i < V; ++i) {
-                    const uint64_t k = make_key(to_float<T>(row[c * V + i]), c * V + i);
+            auto look = [&](int chunk) {
+                row.any(chunk, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint64_t k = i < row.count(chunk) ? make_key(v[i], row.start(chunk) + i) : 0;
                     if (k > key) key = k;
                 }
+            };
+            for (int chunk = g; chunk < row.body; chunk += G) look(chunk);
+            if (g < 2) look(row.body + g);
         }
-        uint64_t list = cta_join<kWarps>(warp_sort(key), lists);
-        const uint64_t threshold = lists[0][a.top - 1];              // at least `top` elements are this good
-        uint64_t owner = lists[0][lane];
+        cta_join<kWarps>(warp_sort(key), lists);
+        const uint64_t threshold = lists[0][a.top - 1];              // 0, or `top` elements of this CTA are this good
+        const uint64_t owners = lists[0][lane];
         __syncthreads();
-        list = 0;
         for (int k = warp; k < a.top; k += kWarps) {
-            const uint64_t o = __shfl_sync(0xffffffffu, owner, k);
+            const uint64_t o = __shfl_sync(0xffffffffu, owners, k);
             if (o == 0) break;
-            const int64_t first = key_index(o) / V % THREADS;
-            for (int64_t c0 = first; c0 < chunks; c0 += (int64_t)THREADS * 32) {
-                const int64_t c = c0 + (int64_t)lane * THREADS;
-                float v[V];
+            const int index = (int)key_index(o), past = index - row.head;
+            const int from = past < 0 ? 0 : past >= 8 * row.body ? 1 : past / 8 % G;       // the owner's first chunk, if it has one
+            auto offer = [&](uint64_t cand) {
+                if (cand < threshold) cand = 0;
+                if (__any_sync(0xffffffffu, cand > __shfl_sync(0xffffffffu, list, 31))) list = warp_join(list, warp_sort(cand));
+            };
+            for (int c0 = from; c0 < row.body; c0 += G * 32) {
+                const int chunk = c0 + lane * G;
+                const bool there = chunk < row.body;
+                float w[8];
+                row.any(there ? chunk : row.body + 1, w);
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = 0.f;
-                if (c < chunks) load_floats<T, V>(row + c * V, v);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    uint64_t cand = c < chunks ? make_key(v[i], c * V + i) : 0;
-                    if (cand < threshold) cand = 0;
-                    if (__any_sync(0xffffffffu, cand > __shfl_sync(0xffffffffu, list, 31))) list = warp_join(list, warp_sort(cand));
-                }
+                for (int i = 0; i < 8; ++i) offer(there ? make_key(w[i], row.start(chunk) + i) : 0);
+            }
+            if (from < 2) {                           // thread 0 also has the row's first elements, thread 1 the last
+                const int at = row.start(row.body + from) + lane;
+                offer(lane < row.count(row.body + from) ? make_key(to_float<T>(row.row[at]), at) : 0);
             }
         }
         list = cta_join<kWarps>(list, lists);
-        if (warp == 0 && lane < a.top) {
-            a.top_ids[t * a.top + lane] = key_index(list);
-            a.top_logp[t * a.top + lane] = none ? -INFINITY : (key_value(list) - m) - log_s;
+    }
+    if (split > 1) {                                  // the even CTA of the cluster joins what the others found
+        if (threadIdx.x == 0) whole = st;
+        cluster_sync();
+        if (rank == 0) {
+            for (int r = 1; r < split; ++r) {
+                Stats other;
+                const uint32_t at = cluster_address(smem_address(&whole), r);
+                other = {cluster_load(at), cluster_load(at + 4), cluster_load(at + 8), cluster_load(at + 12)};
+                st = join(st, other);
+                if (a.top > 0 && warp == 0) list = warp_join(list, cluster_load64(cluster_address(smem_address(&lists[0][lane]), r)));
+            }
         }
-        __syncthreads();
+        cluster_sync();
+        if (rank != 0) return;
+    }
+    const bool none = st.m == kMasked && st.s == 0.f;                // the row is masked throughout
+    const float m = none ? INFINITY : st.m;                          // log p = (x - m) - log_s
+    const float log2_s = log2f(st.s), shift = fmaf(-st.m, kLog2e, st.r);          // of the sum relative to 2^r; r - m log2(e)
+    const float log_s = none ? 0.f : (log2_s + shift) * kLn2;
+    if (threadIdx.x == 0) {
+        a.lse[2 * t] = none ? -INFINITY : st.m;
+        a.lse[2 * t + 1] = log_s;
+        a.entropy[t] = none ? 0.f : (log2_s - st.u / st.s) * kLn2;
+        const int64_t y = a.y[t];
+        a.logp[t] = y < 0 ? 0.f : y >= a.V ? NAN : none ? -INFINITY : (to_float<T>(row.row[y]) - m) - log_s;
+    }
+    if (warp == 0 && lane < a.top) {
+        a.top_ids[t * a.top + lane] = key_index(list);
+        a.top_logp[t * a.top + lane] = none ? -INFINITY : (key_value(list) - m) - log_s;
     }
 }
 
@@ -224,52 +300,82 @@ struct LogprobBackward {
     int top;
 };
 
-// One CTA per row.  dx_j = -p_j (G + dH (log p_j + H)) everywhere; the at most 33 elements that also get a term of their
-// own (the target, the alternatives) are worked out first, from the logits, and stored last, so dx may be x.
-template <typename T, int V, int THREADS>
-__global__ void __launch_bounds__(THREADS) logprob_backward_kernel(const LogprobBackward a) {
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const T *row = (const T *)a.x + t * a.ldx;
-        T *out = (T *)a.dx + t * a.lddx;
-        const float m = a.lse[2 * t], log_s = a.lse[2 * t + 1], H = a.entropy[t], dH = a.dentropy ? a.dentropy[t] : 0.f;
-        const int64_t y = a.y[t];
-        const float dl = a.dlogp && y >= 0 ? (y < a.V ? a.dlogp[t] : NAN) : 0.f;
-        float G = dl;
-        for (int i = 0; i < a.top; ++i) G += a.dtop[t * a.top + i];
-        const bool none = m == -INFINITY;
-        auto spread = [&](float x) {                  // -p (G + dH (log p + H)); 0 where p is 0
-            const float lp = (x - m) - log_s, p = exp2_fast(lp * kLog2e);
-            const float g = -p * fmaf(dH, lp + H, G);
-            return none || p == 0.f ? 0.f : g;
-        };
-        // Thread k < top owns alternative k, thread `top` the target; the first owner of an index sums its terms.
-        int64_t at = -1;
-        float special = 0.f;
-        if (threadIdx.x <= a.top) {
-            const int k = threadIdx.x;
-            at = k < a.top ? a.top_ids[t * a.top + k] : y;
-            if (at < 0 || at >= a.V) at = -1;
-            for (int i = 0; i < k && at >= 0; ++i)
-                if (a.top_ids[t * a.top + i] == at) at = -1;
-            if (at >= 0) {
-                float own = 0.f;
-                for (int i = 0; i < a.top; ++i)
-                    if (a.top_ids[t * a.top + i] == at) own += a.dtop[t * a.top + i];
-                if (y == at) own += dl;
-                special = none ? 0.f : spread(to_float<T>(row[at])) + own;
-            }
+// A row is written by `split` CTAs, their chunks interleaved.  dx_j = -p_j (G + dH (log p_j + H)) everywhere; the at most 33
+// elements that also get a term of their own (the target, the alternatives) are worked out first, from the logits, by the
+// CTA whose chunk they lie in, and stored last, so dx may be x.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_backward_kernel(const LogprobBackward a, const int split) {
+    constexpr int kAhead = 4;
+    const int rank = (int)(blockIdx.x % split), G = split * THREADS, lane = threadIdx.x & 31;
+    const int64_t t = blockIdx.x / split;
+    const RowChunks<T> row((const T *)a.x + t * a.ldx, (int)a.V);
+    T *out = (T *)a.dx + t * a.lddx;
+    const bool wide = (((uintptr_t)row.row ^ (uintptr_t)out) & 15u) == 0;
+    const float m = a.lse[2 * t], log_s = a.lse[2 * t + 1], H = a.entropy[t], dH = a.dentropy ? a.dentropy[t] : 0.f;
+    const int64_t y = a.y[t];
+    const float dl = a.dlogp && y >= 0 ? (y < a.V ? a.dlogp[t] : NAN) : 0.f;
+    const float dt = lane < a.top ? a.dtop[t * a.top + lane] : 0.f;
+    const bool none = m == -INFINITY;
+    // log2 p = (x log2(e) - r) - shift, r = m log2(e) rounded to an integer; G + dH (log p + H) = slope log2 p + rise
+    const float r = rintf(m * kLog2e), shift = fmaf(m, kLog2e, -r) + log_s * kLog2e;
+    const float slope = dH * kLn2, rise = fmaf(dH, H, dl + warp_sum(dt));
+    auto spread = [&](float x) {
+        const float z = max_nan(fmaf(x, kLog2e, -r) - shift, -1e4f);      // p is 0 there, and 0 times the rest
+        return none ? 0.f : -exp2_fast(z) * fmaf(slope, z, rise);
+    };
+    // Thread k < top owns alternative k, thread `top` the target; the first owner of an index sums its terms.
+    int64_t at = -1;
+    float special = 0.f;
+    if (threadIdx.x <= a.top) {
+        const int k = threadIdx.x;
+        at = k < a.top ? a.top_ids[t * a.top + k] : y;
+        if (at < 0 || at >= a.V) at = -1;
+        const int past = (int)at - row.head, from = past < 0 ? 0 : past >= 8 * row.body ? 1 : past / 8 % G;
+        if (from / THREADS != rank) at = -1;
+        for (int i = 0; i < k && at >= 0; ++i)
+            if (a.top_ids[t * a.top + i] == at) at = -1;
+        if (at >= 0) {
+            float own = 0.f;
+            for (int i = 0; i < a.top; ++i)
+                if (a.top_ids[t * a.top + i] == at) own += a.dtop[t * a.top + i];
+            if (y == at) own += dl;
+            special = none ? 0.f : spread(to_float<T>(row.row[at])) + own;
         }
-        __syncthreads();
-        for (int64_t c = threadIdx.x; c < a.V / V; c += THREADS) {
-            float v[V];
-            load_floats<T, V>(row + c * V, v);
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = spread(v[i]);
-            store_floats<T, V>(out + c * V, v);
-        }
-        __syncthreads();
-        if (at >= 0) out[at] = from_float<T>(special);
     }
+    __syncthreads();
+    const int g = rank * THREADS + threadIdx.x;
+    int c = g;
+    if (wide) {
+        auto put = [&](int chunk, const Frag<T, 8> &f) {
+            float v[8];
+            to_floats<T, 8>(f, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = spread(v[i]);
+            store_floats<T, 8>(out + row.head + 8 * chunk, v);
+        };
+        for (; c + (kAhead - 1) * G < row.body; c += kAhead * G) {
+            Frag<T, 8> f[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) f[k] = row.wide(c + k * G);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) put(c + k * G, f[k]);
+        }
+        for (; c < row.body; c += G) put(c, row.wide(c));
+    } else {
+        for (; c < row.body; c += G) {
+            float v[8];
+            row.any(c, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[row.start(c) + i] = from_float<T>(spread(v[i]));
+        }
+    }
+    if (g < 2)
+        for (int i = 0; i < row.count(row.body + g); ++i) {
+            const int j = row.start(row.body + g) + i;
+            out[j] = from_float<T>(spread(to_float<T>(row.row[j])));
+        }
+    __syncthreads();
+    if (at >= 0) out[at] = from_float<T>(special);
 }
 
 }  // namespace deft

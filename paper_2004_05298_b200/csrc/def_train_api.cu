@@ -604,6 +604,11 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
 // ---------------------------------------------------------------------------
 // Log probabilities
 // ---------------------------------------------------------------------------
+namespace {
+constexpr int64_t kLogprobNarrow = 8192;   // rows up to this go to CTAs of 128 threads, longer ones to CTAs of 512
+constexpr int64_t kLogprobLeast = 4096;
+}  // namespace
+
 extern "C" int def_logprob_forward(int32_t dtype, int64_t T, int64_t V, const void *logits, int64_t ldx, const int64_t *targets,
                                    float *logp, float *entropy, float *lse, int32_t top, int64_t *top_ids, float *top_logp,
                                    void *cuda_stream) {
@@ -620,14 +625,31 @@ extern "C" int def_logprob_forward(int32_t dtype, int64_t T, int64_t V, const vo
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
     deft::LogprobForward a = {logits, ldx, T, V, targets, logp, entropy, lse, top_ids, top_logp, top};
-    const bool eight = V % 8 == 0 && wide(logits, ldx, es);
+    // A row is cut over up to 8 CTAs while that leaves each SM no more than one and each CTA kLogprobLeast elements.
+    const bool narrow = V <= kLogprobNarrow;
+    int split = 1;
+    while (split < 8 && T * split * 2 <= kUsualSms && V >= kLogprobLeast * split * 2) split *= 2;
+    if (T * split > 0x7fffffff) return fail(DEF_ERR_ARG, "T is too large (got %lld)", (long long)T);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(T * split));
+    cfg.blockDim = dim3(narrow ? 128 : 512);
+    cfg.stream = (cudaStream_t)cuda_stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = split > 1 ? 1 : 0;
+    cudaError_t err = cudaSuccess;
     by_dtype(dtype, [&](auto type) {
-        by_width(eight, [&](auto width) {
-            const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
-            deft::logprob_forward_kernel<decltype(type), decltype(width)::value, 512><<<grid, 512, 0, (cudaStream_t)cuda_stream>>>(a);
-        });
+        using E = decltype(type);
+        err = narrow ? cudaLaunchKernelEx(&cfg, deft::logprob_forward_kernel<E, 128>, a, split) : cudaLaunchKernelEx(&cfg, deft::logprob_forward_kernel<E, 512>, a, split);
     });
-    return launched("def_logprob_forward");
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        return cuda_fail(err, "def_logprob_forward");
+    }
+    return DEF_OK;
 }
 
 extern "C" int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const void *logits, int64_t ldx, const int64_t *targets,
@@ -648,12 +670,15 @@ extern "C" int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const v
     DEF_TRY(check_views(views, 0, 1));
     if (const int sms = sm_count(); sms < 0) return sms;
     deft::LogprobBackward a = {logits, dlogits, ldx, lddx, T, V, targets, top_ids, lse, entropy, dlogp, dentropy, dtop_logp, top};
-    const bool eight = V % 8 == 0 && wide(logits, ldx, es) && wide(dlogits, lddx, es);
+    const bool narrow = V <= kLogprobNarrow;
+    int split = 1;
+    while (split < 8 && T * split * 2 <= 2 * kUsualSms && V >= kLogprobLeast * split * 2) split *= 2;
+    if (T * split > 0x7fffffff) return fail(DEF_ERR_ARG, "T is too large (got %lld)", (long long)T);
     by_dtype(dtype, [&](auto type) {
-        by_width(eight, [&](auto width) {
-            const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
-            deft::logprob_backward_kernel<decltype(type), decltype(width)::value, 512><<<grid, 512, 0, (cudaStream_t)cuda_stream>>>(a);
-        });
+        using E = decltype(type);
+        const unsigned grid = (unsigned)(T * split);
+        if (narrow) deft::logprob_backward_kernel<E, 128><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(a, split);
+        else deft::logprob_backward_kernel<E, 512><<<grid, 512, 0, (cudaStream_t)cuda_stream>>>(a, split);
     });
     return launched("def_logprob_backward");
 }
