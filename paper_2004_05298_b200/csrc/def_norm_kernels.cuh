@@ -1,6 +1,7 @@
 // Norms before and after a block, fused with its gate and residual scale (see include/def_train.h).
 #pragma once
 
+#include "def_sm100.cuh"
 #include "def_train_common.cuh"
 
 namespace deft {
@@ -16,6 +17,7 @@ struct NormForward {
     float *rstd_post, *rstd_pre;
     Held hb, hh, hn;
     int64_t T, C, rows_per_group, ldq, lde;
+    int64_t parts_per_group;             // of the stream kernel
     float res_scale, eps, inv_C;
 };
 
@@ -243,58 +245,347 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
     }
 }
 
-// The parts' sums, in the order of the parts: dw_pre; and per group S = sum D y, from which dgate = w_post S and
-// dw_post = sum over groups of gate S.  CTA: 32 columns by 32 slices of the parts.
-__global__ void __launch_bounds__(1024) norm_reduce_kernel(const float *__restrict__ partial, const float *__restrict__ w_post,
-                                                           const float *__restrict__ gate, int64_t C, int64_t groups,
-                                                           int64_t parts_per_group, int has_b, int accumulate,
-                                                           float *dw_post, float *dgate, float *dw_pre) {
-    __shared__ float tile[32][33];
-    const int64_t col = (int64_t)blockIdx.x * 32 + threadIdx.x;
-    const bool live = col < C;
-    auto total = [&](int64_t first, int64_t count, int which) {      // sum over parts [first, first + count); in row 0
-        float s = 0.f;
-        if (live)
-            for (int64_t p = threadIdx.y; p < count; p += 32) s += partial[((first + p) * 2 + which) * C + col];
-        tile[threadIdx.y][threadIdx.x] = s;
-        __syncthreads();
-        s = 0.f;
-        if (threadIdx.y == 0)
-            for (int i = 0; i < 32; ++i) s += tile[i][threadIdx.x];
-        __syncthreads();
-        return s;
+// ---------------------------------------------------------------------------
+// Stream kernels: the same rows where there are many and all of them can be read 16 bytes at a time.  A CTA walks a slice
+// of a group's rows; the next rows are on their way to shared memory by bulk copies while one is worked on, and the
+// parameters stay there in fp32.  What bounds these kernels otherwise is the latency of a row: its loads, then two sums
+// over the CTA that each wait for all of it.  (16384 x 4096 bf16 in 8 groups, one row per CTA without copies ahead:
+// forward 132 us, backward from 8-bit saves 367 us.)
+// ---------------------------------------------------------------------------
+constexpr int kMaxStages = 4;
+
+template <typename T> __device__ __forceinline__ Frag<T, 8> shared_frag(const uint8_t *p) {
+    Frag<T, 8> f;
+    constexpr int kWords = sizeof(T) * 8 / 16;
+    uint4 w[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4 *>(p)[i];
+    memcpy(&f, w, sizeof(f));
+    return f;
+}
+__device__ __forceinline__ void shared_floats(const float *p, float (&x)[8]) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+// What rows a slice holds.
+struct Slice {
+    int64_t group, first, last;
+    __device__ Slice(int64_t rows_per_group, int64_t parts_per_group) {
+        group = blockIdx.x / parts_per_group;
+        const int64_t slice = blockIdx.x % parts_per_group, base = group * rows_per_group;
+        first = base + rows_per_group * slice / parts_per_group;
+        last = base + rows_per_group * (slice + 1) / parts_per_group;
+    }
+};
+
+// MINB: CTAs per SM that the registers are meant for.
+template <typename T, int THREADS, int ITERS, int MINB>
+__global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(const NormForward a, const int stages) {
+    extern __shared__ __align__(128) uint8_t dynamic[];
+    __shared__ float scratch[2][32];
+    __shared__ uint64_t full[kMaxStages];
+    __shared__ int failed_flag;
+    volatile int *failed = &failed_flag;
+    const int C = (int)a.C, row_bytes = C * (int)sizeof(T), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
+    float *w_pre = (float *)dynamic, *w_post = w_pre + C;            // w_post times the group's gate
+    uint8_t *ring = dynamic + (a.b ? 8 : 4) * C;
+    const Slice slice(a.rows_per_group, a.parts_per_group);
+    auto fetch = [&](int64_t t, int s) {
+        const uint32_t bar = smem_address(&full[s]), dst = smem_address(ring + s * stage_bytes);
+        barrier_expect(bar, stage_bytes);
+        run_load(dst, (const T *)a.h + t * a.ldh, row_bytes, bar);
+        if (a.b) run_load(dst + row_bytes, (const T *)a.b + t * a.ldb, row_bytes, bar);
     };
-    const float x = total(0, groups * parts_per_group, 0);
-    const bool writer = live && threadIdx.y == 0;
-    if (writer) dw_pre[col] = accumulate ? dw_pre[col] + x : x;
-    if (!has_b) return;
-    float w = 0.f;
-    if (gate && groups >= 32) {                       // many groups: a thread sums whole groups
-        for (int64_t g = threadIdx.y; live && g < groups; g += 32) {
-            float s = 0.f;
-            for (int64_t p = 0; p < parts_per_group; ++p) s += partial[((g * parts_per_group + p) * 2 + 1) * C + col];
-            const float d = w_post[col] * s;
-            dgate[g * C + col] = accumulate ? dgate[g * C + col] + d : d;
-            w = fmaf(gate[g * C + col], s, w);
-        }
-        tile[threadIdx.y][threadIdx.x] = w;
-        __syncthreads();
-        w = 0.f;
-        if (threadIdx.y == 0)
-            for (int i = 0; i < 32; ++i) w += tile[i][threadIdx.x];
-    } else {
-        for (int64_t g = 0; g < groups; ++g) {
-            const float s = total(g * parts_per_group, parts_per_group, 1);
-            if (writer && gate) {
-                const float d = w_post[col] * s;
-                dgate[g * C + col] = accumulate ? dgate[g * C + col] + d : d;
-                w = fmaf(gate[g * C + col], s, w);
-            } else {
-                w += s;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < stages; ++s) barrier_init(smem_address(&full[s]), 1);
+        failed_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
+    }
+    for (int i = threadIdx.x; i < C; i += THREADS) {
+        w_pre[i] = a.w_pre[i];
+        if (a.b) w_post[i] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+    }
+    __syncthreads();
+    int s = 0;
+    uint32_t parity = 0;
+    for (int64_t t = slice.first; t < slice.last; ++t) {
+        const bool ok = barrier_wait(smem_address(&full[s]), parity, failed);
+        const uint8_t *row = ring + s * stage_bytes;
+        float h[ITERS][8], b[ITERS][8];
+        float sum = 0.f;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[it][i] = b[it][i] = 0.f;
+            if (col < C) {
+                to_floats<T, 8>(shared_frag<T>(row + col * sizeof(T)), h[it]);
+                if (a.b) to_floats<T, 8>(shared_frag<T>(row + row_bytes + col * sizeof(T)), b[it]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = a.b ? b[it][i] : h[it][i];
+                sum = fmaf(x, x, sum);
             }
         }
+        sum = cta_sum<THREADS>(sum, scratch[0]);
+        if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);       // every thread has read the stage
+        float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
+        if (!ok) r = NAN;                                             // the wait ran out: no numbers rather than wrong ones
+        if (a.b) {
+            if (threadIdx.x == 0) a.rstd_post[t] = r;
+            if (a.hb.q)
+#pragma unroll
+                for (int it = 0; it < ITERS; ++it) {
+                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    store_held<8>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, col < C, b[it]);
+                }
+            sum = 0.f;
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it) {
+                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                if (col < C) {
+                    float w[8];
+                    shared_floats(w_post + col, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[it][i] = fmaf(b[it][i] * r, w[i], a.res_scale * h[it][i]);
+                    store_floats<T, 8>((T *)a.h_out + t * a.ldho + col, h[it]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
+            }
+            sum = cta_sum<THREADS>(sum, scratch[1]);
+            r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
+        } else {
+            __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next
+        }
+        if (threadIdx.x == 0) a.rstd_pre[t] = r;
+        if (a.hh.q)
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it) {
+                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));       // h' as stored
+                store_held<8>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, col < C, x);
+            }
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            if (col < C) {
+                float w[8];
+                shared_floats(w_pre + col, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[it][i] = h[it][i] * r * w[i];
+                store_floats<T, 8>((T *)a.n_out + t * a.ldn + col, h[it]);
+            }
+            if (a.hn.q) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[it][i] = to_float<T>(from_float<T>(h[it][i]));   // n as stored
+                store_held<8>(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, col < C, h[it]);
+            }
+        }
+        if (++s == stages) {
+            s = 0;
+            parity ^= 1;
+        }
     }
-    if (writer) dw_post[col] = accumulate ? dw_post[col] + w : w;
+}
+
+template <typename T, int THREADS, int ITERS, int MINB>
+__global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(const NormBackward a, const int stages) {
+    extern __shared__ __align__(128) uint8_t dynamic[];
+    __shared__ float scratch[2][32];
+    __shared__ uint64_t full[kMaxStages];
+    __shared__ int failed_flag;
+    volatile int *failed = &failed_flag;
+    const bool has_b = a.b || a.hb.q;
+    const int C = (int)a.C, row_bytes = C * (int)sizeof(T), held_bytes = (int)a.ldq;
+    const int h_bytes = a.hh.q ? held_bytes : row_bytes, b_bytes = !has_b ? 0 : a.hb.q ? held_bytes : row_bytes;
+    const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + h_bytes, stage_bytes = at_b + b_bytes;
+    float *w_pre = (float *)dynamic, *w_post = w_pre + C;            // w_post times the group's gate
+    uint8_t *ring = dynamic + (has_b ? 8 : 4) * C;
+    const Slice slice(a.rows_per_group, a.parts_per_group);
+    auto fetch = [&](int64_t t, int s) {
+        const uint32_t bar = smem_address(&full[s]), dst = smem_address(ring + s * stage_bytes);
+        barrier_expect(bar, stage_bytes);
+        run_load(dst, (const T *)a.dn + t * a.lddn, row_bytes, bar);
+        if (a.dh_in) run_load(dst + at_in, (const T *)a.dh_in + t * a.lddhi, row_bytes, bar);
+        run_load(dst + at_h, a.hh.q ? (const void *)(a.hh.q + t * a.ldq) : (const T *)a.h + t * a.ldh, h_bytes, bar);
+        if (has_b) run_load(dst + at_b, a.hb.q ? (const void *)(a.hb.q + t * a.ldq) : (const T *)a.b + t * a.ldb, b_bytes, bar);
+    };
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < stages; ++s) barrier_init(smem_address(&full[s]), 1);
+        failed_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
+    }
+    for (int i = threadIdx.x; i < C; i += THREADS) {
+        w_pre[i] = a.w_pre[i];
+        if (has_b) w_post[i] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+    }
+    __syncthreads();
+    float sum_x[ITERS][8], sum_y[ITERS][8];
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum_x[it][i] = sum_y[it][i] = 0.f;
+    // The statistics and exponents of a row are fetched while the one before it is worked on.
+    float next_r = 0.f, next_rp = 0.f;
+    uint32_t next_eh[ITERS], next_eb[ITERS];
+    auto ahead = [&](int64_t t) {
+        next_r = a.rstd_pre[t];
+        if (has_b) next_rp = a.rstd_post[t];
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            next_eh[it] = a.hh.q && col < C ? a.hh.e[t * a.lde + col / kGroup] : 0;
+            next_eb[it] = a.hb.q && col < C ? a.hb.e[t * a.lde + col / kGroup] : 0;
+        }
+    };
+    if (slice.first < slice.last) ahead(slice.first);
+    int s = 0;
+    uint32_t parity = 0;
+    for (int64_t t = slice.first; t < slice.last; ++t) {
+        const bool ok = barrier_wait(smem_address(&full[s]), parity, failed);
+        const uint8_t *row = ring + s * stage_bytes;
+        const float r = ok ? next_r : NAN, rp = next_rp;
+        float D[ITERS][8], x[ITERS][8];
+        Frag<T, 8> in[ITERS], fb[ITERS];
+        RawQ<8> qb[ITERS];
+        uint32_t eb[ITERS];
+        float dot = 0.f;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            eb[it] = next_eb[it];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) D[it][i] = x[it][i] = 0.f;
+            if (col < C) {
+                float w[8];
+                to_floats<T, 8>(shared_frag<T>(row + col * sizeof(T)), D[it]);
+                if (a.hh.q) {
+                    const uint2 q = *reinterpret_cast<const uint2 *>(row + at_h + col);
+                    held_values<8>(RawQ<8>{q.x, q.y}, next_eh[it], x[it]);
+                } else {
+                    to_floats<T, 8>(shared_frag<T>(row + at_h + col * sizeof(T)), x[it]);
+                }
+                if (a.dh_in) in[it] = shared_frag<T>(row + at_in + col * sizeof(T));
+                if (a.hb.q) {
+                    const uint2 q = *reinterpret_cast<const uint2 *>(row + at_b + col);
+                    qb[it] = RawQ<8>{q.x, q.y};
+                } else if (has_b) {
+                    fb[it] = shared_frag<T>(row + at_b + col * sizeof(T));
+                }
+                shared_floats(w_pre + col, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[it][i] *= r;
+                    sum_x[it][i] = fmaf(D[it][i], x[it][i], sum_x[it][i]);
+                    D[it][i] *= w[i];
+                    dot = fmaf(D[it][i], x[it][i], dot);
+                }
+            }
+        }
+        if (t + 1 < slice.last) ahead(t + 1);
+        dot = cta_sum<THREADS>(dot, scratch[0]) * a.inv_C;
+        if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);       // every thread has read the stage
+        float dot_b = 0.f;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            if (col < C) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = 0.f;
+                if (a.dh_in) to_floats<T, 8>(in[it], v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    D[it][i] = fmaf(r, fmaf(-x[it][i], dot, D[it][i]), v[i]);
+                    v[i] = a.res_scale * D[it][i];
+                }
+                store_floats<T, 8>((T *)a.dh + t * a.lddh + col, v);
+                if (has_b) {
+                    if (a.hb.q) held_values<8>(qb[it], eb[it], x[it]);
+                    else to_floats<T, 8>(fb[it], x[it]);
+                    shared_floats(w_post + col, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        x[it][i] *= rp;
+                        sum_y[it][i] = fmaf(D[it][i], x[it][i], sum_y[it][i]);
+                        D[it][i] *= v[i];
+                        dot_b = fmaf(D[it][i], x[it][i], dot_b);
+                    }
+                }
+            }
+        }
+        if (has_b) {
+            dot_b = cta_sum<THREADS>(dot_b, scratch[1]) * a.inv_C;
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it) {
+                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                if (col < C) {
+                    float out[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) out[i] = rp * fmaf(-x[it][i], dot_b, D[it][i]);
+                    store_floats<T, 8>((T *)a.db + t * a.lddb + col, out);
+                }
+            }
+        } else {
+            __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next
+        }
+        if (++s == stages) {
+            s = 0;
+            parity ^= 1;
+        }
+    }
+    float *px = a.partial + (int64_t)blockIdx.x * 2 * C;
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it) {
+        const int col = (it * THREADS + (int)threadIdx.x) * 8;
+        if (col < C)
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                *reinterpret_cast<float4 *>(px + col + i) = make_float4(sum_x[it][i], sum_x[it][i + 1], sum_x[it][i + 2], sum_x[it][i + 3]);
+                if (has_b) *reinterpret_cast<float4 *>(px + C + col + i) = make_float4(sum_y[it][i], sum_y[it][i + 1], sum_y[it][i + 2], sum_y[it][i + 3]);
+            }
+    }
+}
+
+// The parts' sums, in a fixed order: CTA (32 columns, job) adds them with 8 threads per column.  Job g < jobs_gate: dgate of
+// group g, w_post times the sum of D y over the group's parts.  Then dw_pre, the sum of dn x over all parts, and dw_post,
+// the sum of gate times D y.
+__global__ void __launch_bounds__(256) norm_reduce_kernel(const float *__restrict__ partial, const float *__restrict__ w_post,
+                                                          const float *__restrict__ gate, int64_t C, int64_t groups,
+                                                          int64_t parts_per_group, int64_t jobs_gate, int accumulate,
+                                                          float *dw_post, float *dgate, float *dw_pre) {
+    __shared__ float tile[8][33];
+    asm volatile("griddepcontrol.wait;" ::: "memory");               // the partial sums are those of the kernel before
+    const int64_t col = (int64_t)blockIdx.x * 32 + threadIdx.x;
+    const bool live = col < C;
+    for (int64_t job = blockIdx.y; job < jobs_gate + (dw_post ? 2 : 1); job += gridDim.y) {
+        const int64_t first = job < jobs_gate ? job * parts_per_group : 0, count = (job < jobs_gate ? 1 : groups) * parts_per_group;
+        const bool of_y = job != jobs_gate, gated = job == jobs_gate + 1 && gate;
+        float s = 0.f;
+        if (live)
+#pragma unroll 4
+            for (int64_t p = threadIdx.y; p < count; p += 8) {
+                const float v = partial[((first + p) * 2 + of_y) * C + col];
+                s = gated ? fmaf(gate[p / parts_per_group * C + col], v, s) : s + v;
+            }
+        tile[threadIdx.y][threadIdx.x] = s;
+        __syncthreads();
+        if (threadIdx.y == 0 && live) {
+            s = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += tile[i][threadIdx.x];
+            float *out = job < jobs_gate ? dgate + job * C + col : of_y ? dw_post + col : dw_pre + col;
+            if (job < jobs_gate) s *= w_post[col];
+            *out = accumulate ? *out + s : s;
+        }
+        __syncthreads();
+    }
 }
 
 }  // namespace deft

@@ -99,6 +99,11 @@ __device__ __forceinline__ void tensor_load_2d(uint32_t dst, const void *map, in
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+// Copies a run of bytes (a multiple of 16, both addresses on 16-byte boundaries) to shared memory.
+__device__ __forceinline__ void run_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const void *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }

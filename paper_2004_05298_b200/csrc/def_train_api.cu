@@ -257,7 +257,7 @@ extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const voi
 // ---------------------------------------------------------------------------
 namespace {
 
-template <int THREADS, int ITERS> struct Shape { static constexpr int threads = THREADS, iters = ITERS; };
+template <int THREADS, int ITERS, int MINB = 1> struct Shape { static constexpr int threads = THREADS, iters = ITERS, min_ctas = MINB; };
 // Threads per row and accesses per thread for rows of C columns, V at a time.
 template <int V, typename F> void by_row_shape(int64_t C, F f) {
     const int64_t n = ceil_div(C, V);
@@ -271,10 +271,25 @@ template <int V, typename F> void by_row_shape(int64_t C, F f) {
     } else {
         if (n <= 256) f(Shape<32, 8>());
         else if (n <= 1024) f(Shape<128, 8>());
-        else if (n <= 4096) f(Shape<256, 16>());
-        else if (n <= 8192) f(Shape<512, 16>());
+        else if (n <= 2048) f(Shape<256, 8>());
+        else if (n <= 4096) f(Shape<512, 8>());
+        else if (n <= 8192) f(Shape<1024, 8>());
         else f(Shape<1024, 16>());
     }
+}
+// The same for the stream kernels, with the CTAs per SM that their registers are meant for.
+template <typename F> void by_stream_shape(int64_t C, F f) {
+    const int64_t n = C / 8;
+    if (n <= 128) f(Shape<128, 1, 6>());
+    else if (n <= 256) f(Shape<128, 2, 4>());
+    else if (n <= 512) f(Shape<256, 2, 2>());
+    else if (n <= 1024) f(Shape<512, 2, 1>());
+    else f(Shape<1024, 2, 1>());
+}
+// Stages of a stream kernel's ring: as many as fit beside the parameters with `ctas` on an SM (below 2: not for it).
+int stream_stages(int64_t params, int64_t stage, int ctas) {
+    const int64_t n = ((int64_t)224 * 1024 / ctas - 2048 - params) / stage;
+    return (int)(n < deft::kMaxStages ? n : deft::kMaxStages);
 }
 
 int check_groups(int64_t T, int64_t groups) {
@@ -282,13 +297,15 @@ int check_groups(int64_t T, int64_t groups) {
     return DEF_OK;
 }
 
-// Parts per group of the backward pass (each part: one CTA, one row of partial sums): about kNormParts in all, at most
-// one per row.
-constexpr int64_t kNormParts = 592;
-int64_t norm_parts(int64_t T, int64_t groups) {
-    const int64_t rows = T / groups, want = ceil_div(kNormParts, groups);
-    return rows < want ? rows : want;
+// Slices per group that rows are cut into (each: one CTA, and in the backward pass one row of partial sums): about `want`
+// in all, at most one per row.
+constexpr int64_t kNormParts = 8 * kUsualSms;     // the most in all, which the workspace is sized for
+int64_t norm_parts(int64_t T, int64_t groups, int64_t want) {
+    const int64_t rows = T / groups, each = ceil_div(want, groups);
+    return rows < each ? rows : each;
 }
+// A stream kernel pays off from this many rows per slice on.
+constexpr int64_t kStreamRows = 3;
 
 }  // namespace
 
@@ -329,6 +346,26 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
     a.T = T; a.C = C; a.rows_per_group = T / groups; a.ldq = q_stride(C); a.lde = e_stride(C);
     a.res_scale = res_scale; a.eps = eps; a.inv_C = 1.f / (float)C;
     const bool eight = C % 8 == 0 && wide(h, ldh, es) && wide(b, ldb, es) && wide(h_out, ldho, es) && wide(n_out, ldn, es);
+    cudaError_t err = cudaSuccess;
+    bool streamed = false;
+    if (eight)
+        by_stream_shape(C, [&](auto shape) {
+            using S = decltype(shape);
+            const int64_t params = (b ? 8 : 4) * C, stage = (b ? 2 : 1) * C * es, want = S::min_ctas * kUsualSms;
+            const int stages = stream_stages(params, stage, S::min_ctas);
+            if (stages < 2 || T < want * kStreamRows) return;
+            streamed = true;
+            a.parts_per_group = norm_parts(T, groups, want);
+            const unsigned grid = (unsigned)(groups * a.parts_per_group);
+            const int smem = (int)(params + stages * stage);
+            by_dtype(dtype, [&](auto type) {
+                const auto kernel = deft::norm_forward_stream_kernel<decltype(type), S::threads, S::iters, S::min_ctas>;
+                if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
+                kernel<<<grid, S::threads, smem, (cudaStream_t)cuda_stream>>>(a, stages);
+            });
+        });
+    if (err != cudaSuccess) return cuda_fail(err, "def_norm_forward");
+    if (streamed) return launched("def_norm_forward");
     by_dtype(dtype, [&](auto type) {
         by_width(eight, [&](auto width) {
             constexpr int V = decltype(width)::value;
@@ -347,7 +384,7 @@ extern "C" int def_norm_backward_workspace(int64_t T, int64_t C, int64_t groups,
     DEF_TRY(check_rows(DEF_DTYPE_F32, T, C, "C"));
     if (C > DEF_NORM_MAX_C) return fail(DEF_ERR_ARG, "C must be at most %d (got %lld)", DEF_NORM_MAX_C, (long long)C);
     DEF_TRY(check_groups(T, groups));
-    *bytes_out = groups * norm_parts(T, groups) * 2 * C * (int64_t)sizeof(float);
+    *bytes_out = groups * norm_parts(T, groups, kNormParts) * 2 * C * (int64_t)sizeof(float);
     return DEF_OK;
 }
 
@@ -405,24 +442,58 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     a.w_post = w_post; a.gate = gate; a.w_pre = w_pre; a.rstd_post = rstd_post; a.rstd_pre = rstd_pre;
     a.partial = (float *)workspace;
     a.T = T; a.C = C; a.rows_per_group = T / groups; a.ldq = q_stride(C); a.lde = e_stride(C);
-    a.parts_per_group = norm_parts(T, groups);
     a.res_scale = res_scale; a.inv_C = 1.f / (float)C;
-    const int64_t parts = groups * a.parts_per_group;
-    if (parts > 0x7fffffff) return fail(DEF_ERR_ARG, "problem too large for one grid");
     const bool eight = C % 8 == 0 && wide(dn, lddn, es) && wide(dh_in, lddhi, es) && wide(h, ldh, es) && wide(b, ldb, es) && wide(dh, lddh, es) && wide(db, lddb, es);
-    by_dtype(dtype, [&](auto type) {
-        by_width(eight, [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            by_row_shape<V>(C, [&](auto shape) {
-                using S = decltype(shape);
-                deft::norm_backward_kernel<decltype(type), V, S::threads, S::iters><<<(unsigned)parts, S::threads, 0, stream>>>(a);
+    if (groups > 0x7fffffff / 2) return fail(DEF_ERR_ARG, "groups is too large (got %lld)", (long long)groups);
+    cudaError_t err = cudaSuccess;
+    bool streamed = false;
+    if (eight)
+        by_stream_shape(C, [&](auto shape) {
+            using S = decltype(shape);
+            const int64_t params = (has_b ? 8 : 4) * C, want = S::min_ctas * kUsualSms;
+            const int64_t stage = C * es * (dh_in ? 2 : 1) + (h_q ? q_stride(C) : C * es) + (!has_b ? 0 : b_q ? q_stride(C) : C * es);
+            const int stages = stream_stages(params, stage, S::min_ctas);
+            if (stages < 2 || T < want * kStreamRows) return;
+            streamed = true;
+            a.parts_per_group = norm_parts(T, groups, want);
+            const int smem = (int)(params + stages * stage);
+            by_dtype(dtype, [&](auto type) {
+                const auto kernel = deft::norm_backward_stream_kernel<decltype(type), S::threads, S::iters, S::min_ctas>;
+                if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
+                kernel<<<(unsigned)(groups * a.parts_per_group), S::threads, smem, stream>>>(a, stages);
             });
         });
-    });
+    if (err != cudaSuccess) return cuda_fail(err, "def_norm_backward");
+    if (!streamed)
+        by_dtype(dtype, [&](auto type) {
+            by_width(eight, [&](auto width) {
+                constexpr int V = decltype(width)::value;
+                by_row_shape<V>(C, [&](auto shape) {
+                    using S = decltype(shape);
+                    a.parts_per_group = norm_parts(T, groups, S::threads <= 128 ? kNormParts : S::threads <= 256 ? kNormParts / 2 : kNormParts / 4);
+                    deft::norm_backward_kernel<decltype(type), V, S::threads, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads, 0, stream>>>(a);
+                });
+            });
+        });
     DEF_TRY(launched("def_norm_backward"));
-    deft::norm_reduce_kernel<<<(unsigned)ceil_div(C, 32), dim3(32, 32), 0, stream>>>((const float *)workspace, w_post, gate, C, groups, a.parts_per_group,
-                                                                                      has_b, accumulate, dw_post, dgate, dw_pre);
-    return launched("def_norm_backward (sums)");
+    // The sums' kernel may be set up while the other still runs; it waits for it before it reads.
+    const int64_t jobs_gate = gate ? groups : 0, jobs = jobs_gate + (has_b ? 2 : 1);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ceil_div(C, 32), (unsigned)(jobs < 1024 ? jobs : 1024));
+    cfg.blockDim = dim3(32, 8);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    err = cudaLaunchKernelEx(&cfg, deft::norm_reduce_kernel, (const float *)workspace, w_post, gate, C, groups, a.parts_per_group, jobs_gate, (int)accumulate,
+                             has_b ? dw_post : (float *)nullptr, dgate, dw_pre);
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        return cuda_fail(err, "def_norm_backward (sums)");
+    }
+    return DEF_OK;
 }
 
 // ---------------------------------------------------------------------------

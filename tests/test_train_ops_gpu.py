@@ -284,6 +284,54 @@ def test_norm_backward(B, dtype, saves):
         _close(dw, want["dw_pre"], mag["dw_pre"], F32, n=T + 128)
 
 
+MANY_ROWS = [(2700, 64, 1), (2701, 200, 0), (2672, 1024, 8), (1800, 1032, 3), (1776, 2048, 1), (900, 2056, 4), (889, 4096, 0), (450, 4104, 5),
+             (444, 8192, 2), (450, 8200, 1), (446, 12288, 2)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,C,groups", MANY_ROWS)
+def test_norm_many_rows(B, dtype, T, C, groups):
+    """Enough rows that each CTA walks several of them; rows that are not a whole number of accesses per thread."""
+    h, b, w_post, gate, w_pre = _norm_inputs(T, C, dtype, "rows", groups, T)
+    n_out, h_out, r2, r1 = torch.empty_like(h), torch.empty_like(h), torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+    cks = [B.def_checkpoint_alloc(T, C, DEV) for _ in range(3)]
+    B.def_norm_forward(h, b, w_post, gate, w_pre, h_out, n_out, r2, r1, res_scale=0.75, eps=1e-5, b_ck=cks[0], h_ck=cks[1], n_ck=cks[2])
+    f = R.norm_forward(h, b, w_post, gate, w_pre, 0.75, 1e-5)
+    row = (f["scale_h"] ** 2).mean(1).sqrt() * f["rstd_pre"]
+    _close(r2, f["rstd_post"], f["rstd_post"], F32)
+    _close(r1, f["rstd_pre"], f["rstd_pre"] * row, F32, n=128)
+    _close(h_out, f["h"], f["scale_h"], dtype)
+    _close(n_out, f["n"], (f["scale_h"] * f["rstd_pre"][:, None] + f["n"].abs() / w_pre.double().abs() * row[:, None]) * w_pre.double().abs(), dtype, n=128)
+    for x, ck in ((b, cks[0]), (h_out, cks[1]), (n_out, cks[2])):
+        mine = _checkpoint(B, x)
+        assert torch.equal(mine[0][:, :C], ck[0][:, :C]) and torch.equal(mine[1][:, :-(-C // 32)], ck[1][:, :-(-C // 32)])
+    alone, s1 = torch.empty_like(h), torch.empty(T, device=DEV)
+    B.def_norm_forward(b, None, None, None, w_pre, None, alone, None, s1)
+    g = R.norm_forward(b, None, None, None, w_pre, 1.0, 1e-6)
+    _close(alone, g["n"], g["n"].abs(), dtype)
+    dn, dh_in = (_normal((T, C), dtype, T + k, std=0.1) for k in (7, 8))
+    hs, bs = _checkpoint(B, h), _checkpoint(B, b)
+    hv, bv = R.read(hs, C).to(DEV), R.read(bs, C).to(DEV)
+    r2, r1 = (torch.rsqrt(v.float().square().mean(1) + 1e-5) for v in (b, h))
+    dh, db, dwp, dw = torch.empty_like(h), torch.empty_like(h), torch.empty(C, device=DEV), torch.empty(C, device=DEV)
+    dg = None if gate is None else torch.empty(groups, C, device=DEV)
+    work = torch.empty(B.def_norm_backward_workspace(T, C, max(1, groups)), dtype=torch.uint8, device=DEV)
+    for hx, bx, hy, by, into in ((h, b, h, b, dh_in), (hs, bs, hv, bv, None), (h, bs, h, bv, dh_in), (hs, b, hv, b, dh_in)):
+        B.def_norm_backward(dn, into, hx, bx, w_post, gate, w_pre, r2, r1, dh, db, dwp, dg, dw, work, res_scale=0.75)
+        want, mag = R.norm_backward(dn, into, hy, by, w_post, gate, w_pre, 0.75, r2, r1)
+        _close(dh, want["dh"], mag["dh"], dtype, n=128)
+        _close(db, want["db"], mag["db"], dtype, n=256)
+        for name, got in (("dw_pre", dw), ("dw_post", dwp)) + ((("dgate", dg),) if dg is not None else ()):
+            _close(got, want[name], mag[name], F32, n=T + 128)
+    B.def_norm_backward(dn, None, hs, None, None, None, w_pre, None, r1, dh, None, None, None, dw, work)
+    want, mag = R.norm_backward(dn, None, hv, None, None, None, w_pre, 1.0, None, r1)
+    _close(dh, want["dh"], mag["dh"], dtype, n=128)
+    _close(dw, want["dw_pre"], mag["dw_pre"], F32, n=T + 128)
+    first = (dh.clone(), dw.clone())
+    B.def_norm_backward(dn, None, hs, None, None, None, w_pre, None, r1, dh, None, None, None, dw, work)
+    assert torch.equal(first[0], dh) and torch.equal(first[1], dw)
+
+
 def test_norm_many_groups_and_no_rows(B):
     T, C = 600, 72
     for groups in (600, 200, 40):
