@@ -152,7 +152,31 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
 #pragma unroll
         for (int i = 0; i < V; ++i) sum_x[it][i] = sum_y[it][i] = 0.f;
     for (int64_t t = first; t < last; ++t) {
-        const float r = a.rstd_pre[t];
+        // All loads of the row first: it waits for memory once.
+        Frag<T, V> fn[ITERS], fi[ITERS], fh[ITERS], fb[ITERS];
+        RawQ<V> qh[ITERS], qb[ITERS];
+        uint32_t eh[ITERS], eb[ITERS];
+        const float r = a.rstd_pre[t], rp = has_b ? a.rstd_post[t] : 0.f;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int col = (it * THREADS + (int)threadIdx.x) * V;
+            if (col < a.C) {
+                fn[it] = load_frag<T, V>((const T *)a.dn + t * a.lddn + col);
+                if (a.hh.q) {
+                    qh[it] = load_q<V>(a.hh.q + t * a.ldq + col);
+                    eh[it] = a.hh.e[t * a.lde + col / kGroup];
+                } else {
+                    fh[it] = load_frag<T, V>((const T *)a.h + t * a.ldh + col);
+                }
+                if (a.dh_in) fi[it] = load_frag<T, V>((const T *)a.dh_in + t * a.lddhi + col);
+                if (a.hb.q) {
+                    qb[it] = load_q<V>(a.hb.q + t * a.ldq + col);
+                    eb[it] = a.hb.e[t * a.lde + col / kGroup];
+                } else if (has_b) {
+                    fb[it] = load_frag<T, V>((const T *)a.b + t * a.ldb + col);
+                }
+            }
+        }
         float D[ITERS][V], x[ITERS][V];
         float dot = 0.f;
 #pragma unroll
@@ -162,9 +186,9 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
             for (int i = 0; i < V; ++i) D[it][i] = x[it][i] = 0.f;
             if (col < a.C) {
                 float w[V];
-                load_floats<T, V>((const T *)a.dn + t * a.lddn + col, D[it]);
-                if (a.hh.q) load_held<V>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, x[it]);
-                else load_floats<T, V>((const T *)a.h + t * a.ldh + col, x[it]);
+                to_floats<T, V>(fn[it], D[it]);
+                if (a.hh.q) held_values<V>(qh[it], eh[it], x[it]);
+                else to_floats<T, V>(fh[it], x[it]);
                 load_params<V>(a.w_pre + col, w);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
@@ -176,55 +200,50 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
             }
         }
         dot = cta_sum<THREADS>(dot, scratch[0]) * a.inv_C;
+        float dot_b = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
             const int col = (it * THREADS + (int)threadIdx.x) * V;
             if (col < a.C) {
-                float in[V], out[V];
-                if (a.dh_in) load_floats<T, V>((const T *)a.dh_in + t * a.lddhi + col, in);
-                else
-                    for (int i = 0; i < V; ++i) in[i] = 0.f;
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = 0.f;
+                if (a.dh_in) to_floats<T, V>(fi[it], v);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    D[it][i] = fmaf(r, fmaf(-x[it][i], dot, D[it][i]), in[i]);
-                    out[i] = a.res_scale * D[it][i];
+                    D[it][i] = fmaf(r, fmaf(-x[it][i], dot, D[it][i]), v[i]);
+                    v[i] = a.res_scale * D[it][i];
                 }
-                store_floats<T, V>((T *)a.dh + t * a.lddh + col, out);
-            }
-        }
-        if (has_b) {
-            const float rp = a.rstd_post[t];
-            dot = 0.f;
-#pragma unroll
-            for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * V;
-                if (col < a.C) {
-                    float w[V], g[V];
-                    if (a.hb.q) load_held<V>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, x[it]);
-                    else load_floats<T, V>((const T *)a.b + t * a.ldb + col, x[it]);
+                store_floats<T, V>((T *)a.dh + t * a.lddh + col, v);
+                if (has_b) {
+                    float w[V];
+                    if (a.hb.q) held_values<V>(qb[it], eb[it], x[it]);
+                    else to_floats<T, V>(fb[it], x[it]);
                     load_params<V>(a.w_post + col, w);
                     if (a.gate) {
-                        load_params<V>(a.gate + group * a.C + col, g);
+                        load_params<V>(a.gate + group * a.C + col, v);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) w[i] *= g[i];
+                        for (int i = 0; i < V; ++i) w[i] *= v[i];
                     }
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         x[it][i] *= rp;
                         sum_y[it][i] = fmaf(D[it][i], x[it][i], sum_y[it][i]);
                         D[it][i] *= w[i];
-                        dot = fmaf(D[it][i], x[it][i], dot);
+                        dot_b = fmaf(D[it][i], x[it][i], dot_b);
                     }
                 }
             }
-            dot = cta_sum<THREADS>(dot, scratch[1]) * a.inv_C;
+        }
+        if (has_b) {
+            dot_b = cta_sum<THREADS>(dot_b, scratch[1]) * a.inv_C;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
                 const int col = (it * THREADS + (int)threadIdx.x) * V;
                 if (col < a.C) {
                     float out[V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) out[i] = rp * fmaf(-x[it][i], dot, D[it][i]);
+                    for (int i = 0; i < V; ++i) out[i] = rp * fmaf(-x[it][i], dot_b, D[it][i]);
                     store_floats<T, V>((T *)a.db + t * a.lddb + col, out);
                 }
             }
@@ -263,8 +282,11 @@ template <typename T> __device__ __forceinline__ Frag<T, 8> shared_frag(const ui
     memcpy(&f, w, sizeof(f));
     return f;
 }
-__device__ __forceinline__ void shared_floats(const float *p, float (&x)[8]) {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+// Parameters in shared memory: of every 8 columns the first four in one half of the array, the last four in the other, so
+// that a warp's accesses lie side by side.
+__device__ __forceinline__ int param_place(int i, int C) { return (i % 8 < 4 ? 0 : C / 2) + i / 8 * 4 + i % 4; }
+__device__ __forceinline__ void shared_params(const float *p, int col, int C, float (&x)[8]) {
+    const float4 a = *reinterpret_cast<const float4 *>(p + col / 2), b = *reinterpret_cast<const float4 *>(p + C / 2 + col / 2);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
 }
 // What rows a slice holds.
@@ -303,8 +325,9 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
         for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
     }
     for (int i = threadIdx.x; i < C; i += THREADS) {
-        w_pre[i] = a.w_pre[i];
-        if (a.b) w_post[i] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+        const int at = param_place(i, C);
+        w_pre[at] = a.w_pre[i];
+        if (a.b) w_post[at] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
     }
     __syncthreads();
     int s = 0;
@@ -347,7 +370,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
                 const int col = (it * THREADS + (int)threadIdx.x) * 8;
                 if (col < C) {
                     float w[8];
-                    shared_floats(w_post + col, w);
+                    shared_params(w_post, col, C, w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[it][i] = fmaf(b[it][i] * r, w[i], a.res_scale * h[it][i]);
                     store_floats<T, 8>((T *)a.h_out + t * a.ldho + col, h[it]);
@@ -375,7 +398,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
             const int col = (it * THREADS + (int)threadIdx.x) * 8;
             if (col < C) {
                 float w[8];
-                shared_floats(w_pre + col, w);
+                shared_params(w_pre, col, C, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[it][i] = h[it][i] * r * w[i];
                 store_floats<T, 8>((T *)a.n_out + t * a.ldn + col, h[it]);
@@ -422,8 +445,9 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
         for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
     }
     for (int i = threadIdx.x; i < C; i += THREADS) {
-        w_pre[i] = a.w_pre[i];
-        if (has_b) w_post[i] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+        const int at = param_place(i, C);
+        w_pre[at] = a.w_pre[i];
+        if (has_b) w_post[at] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
     }
     __syncthreads();
     float sum_x[ITERS][8], sum_y[ITERS][8];
@@ -478,7 +502,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
                 } else if (has_b) {
                     fb[it] = shared_frag<T>(row + at_b + col * sizeof(T));
                 }
-                shared_floats(w_pre + col, w);
+                shared_params(w_pre, col, C, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     x[it][i] *= r;
@@ -509,7 +533,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
                 if (has_b) {
                     if (a.hb.q) held_values<8>(qb[it], eb[it], x[it]);
                     else to_floats<T, 8>(fb[it], x[it]);
-                    shared_floats(w_post + col, v);
+                    shared_params(w_post, col, C, v);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         x[it][i] *= rp;
@@ -553,14 +577,14 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
     }
 }
 
-// The parts' sums, in a fixed order: CTA (32 columns, job) adds them with 8 threads per column.  Job g < jobs_gate: dgate of
+// The parts' sums, in a fixed order: CTA (32 columns, job) adds them with 32 threads per column.  Job g < jobs_gate: dgate of
 // group g, w_post times the sum of D y over the group's parts.  Then dw_pre, the sum of dn x over all parts, and dw_post,
 // the sum of gate times D y.
-__global__ void __launch_bounds__(256) norm_reduce_kernel(const float *__restrict__ partial, const float *__restrict__ w_post,
+__global__ void __launch_bounds__(1024) norm_reduce_kernel(const float *__restrict__ partial, const float *__restrict__ w_post,
                                                           const float *__restrict__ gate, int64_t C, int64_t groups,
                                                           int64_t parts_per_group, int64_t jobs_gate, int accumulate,
                                                           float *dw_post, float *dgate, float *dw_pre) {
-    __shared__ float tile[8][33];
+    __shared__ float tile[32][33];
     asm volatile("griddepcontrol.wait;" ::: "memory");               // the partial sums are those of the kernel before
     const int64_t col = (int64_t)blockIdx.x * 32 + threadIdx.x;
     const bool live = col < C;
@@ -570,16 +594,16 @@ __global__ void __launch_bounds__(256) norm_reduce_kernel(const float *__restric
         float s = 0.f;
         if (live)
 #pragma unroll 4
-            for (int64_t p = threadIdx.y; p < count; p += 8) {
+            for (int64_t p = threadIdx.y; p < count; p += 32) {
                 const float v = partial[((first + p) * 2 + of_y) * C + col];
-                s = gated ? fmaf(gate[p / parts_per_group * C + col], v, s) : s + v;
+                s = gated ? fmaf(gate[(int64_t)((uint32_t)p / (uint32_t)parts_per_group) * C + col], v, s) : s + v;
             }
         tile[threadIdx.y][threadIdx.x] = s;
         __syncthreads();
         if (threadIdx.y == 0 && live) {
             s = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += tile[i][threadIdx.x];
+            for (int i = 0; i < 32; ++i) s += tile[i][threadIdx.x];
             float *out = job < jobs_gate ? dgate + job * C + col : of_y ? dw_post + col : dw_pre + col;
             if (job < jobs_gate) s *= w_post[col];
             *out = accumulate ? *out + s : s;

@@ -257,7 +257,8 @@ extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const voi
 // ---------------------------------------------------------------------------
 namespace {
 
-template <int THREADS, int ITERS, int MINB = 1> struct Shape { static constexpr int threads = THREADS, iters = ITERS, min_ctas = MINB; };
+template <int THREADS, int ITERS> struct Shape { static constexpr int threads = THREADS, iters = ITERS; };
+template <int THREADS, int ITERS, int MINB> struct StreamShape { static constexpr int threads = THREADS, iters = ITERS, min_ctas = MINB; };
 // Threads per row and accesses per thread for rows of C columns, V at a time.
 template <int V, typename F> void by_row_shape(int64_t C, F f) {
     const int64_t n = ceil_div(C, V);
@@ -280,11 +281,11 @@ template <int V, typename F> void by_row_shape(int64_t C, F f) {
 // The same for the stream kernels, with the CTAs per SM that their registers are meant for.
 template <typename F> void by_stream_shape(int64_t C, F f) {
     const int64_t n = C / 8;
-    if (n <= 128) f(Shape<128, 1, 6>());
-    else if (n <= 256) f(Shape<128, 2, 4>());
-    else if (n <= 512) f(Shape<256, 2, 2>());
-    else if (n <= 1024) f(Shape<512, 2, 1>());
-    else f(Shape<1024, 2, 1>());
+    if (n <= 128) f(StreamShape<128, 1, 6>());
+    else if (n <= 256) f(StreamShape<128, 2, 4>());
+    else if (n <= 512) f(StreamShape<256, 2, 2>());
+    else if (n <= 1024) f(StreamShape<512, 2, 1>());
+    else f(StreamShape<1024, 2, 1>());
 }
 // Stages of a stream kernel's ring: as many as fit beside the parameters with `ctas` on an SM (below 2: not for it).
 int stream_stages(int64_t params, int64_t stage, int ctas) {
@@ -470,7 +471,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
                 constexpr int V = decltype(width)::value;
                 by_row_shape<V>(C, [&](auto shape) {
                     using S = decltype(shape);
-                    a.parts_per_group = norm_parts(T, groups, S::threads <= 128 ? kNormParts : S::threads <= 256 ? kNormParts / 2 : kNormParts / 4);
+                    a.parts_per_group = norm_parts(T, groups, S::threads <= 128 ? kNormParts / 2 : S::threads <= 256 ? kNormParts / 4 : kNormParts / 8);
                     deft::norm_backward_kernel<decltype(type), V, S::threads, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads, 0, stream>>>(a);
                 });
             });
@@ -480,7 +481,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     const int64_t jobs_gate = gate ? groups : 0, jobs = jobs_gate + (has_b ? 2 : 1);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ceil_div(C, 32), (unsigned)(jobs < 1024 ? jobs : 1024));
-    cfg.blockDim = dim3(32, 8);
+    cfg.blockDim = dim3(32, 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
