@@ -16,12 +16,6 @@ template <int V> struct Place {
         : col((int)(blockIdx.x * blockDim.x + threadIdx.x) * V), row((int64_t)blockIdx.y * blockDim.y + threadIdx.y),
           step((int64_t)gridDim.y * blockDim.y) {}
 };
-template <typename T, int V> __device__ __forceinline__ Frag<T, V> zeros() {
-    Frag<T, V> f;
-    memset(&f, 0, sizeof(f));
-    return f;
-}
-
 template <typename T, int V>
 __global__ void __launch_bounds__(256, 8) pack_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int C,
                                                       int8_t *__restrict__ q, uint8_t *__restrict__ e, int64_t ldq, int64_t lde) {

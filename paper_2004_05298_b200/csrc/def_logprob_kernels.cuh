@@ -16,25 +16,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // A logit at or below this (about -1e30, and exact in bf16) is masked; -infinity and the lowest value of bf16 and fp32 are.
 constexpr float kMasked = -0x1.92p+99f;
 
-// Two fp32 operations in one instruction.
-struct Pair { uint64_t bits; };
-__device__ __forceinline__ Pair make_pair(float a, float b) {
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p.bits) : "f"(a), "f"(b));
-    return p;
-}
-__device__ __forceinline__ void split_pair(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.bits)); }
-__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c) {
-    Pair d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
-    return d;
-}
-__device__ __forceinline__ Pair pair_add(Pair a, Pair b) {
-    Pair d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits));
-    return d;
-}
-
 // Running statistics of part of a row:  s = sum 2^y,  u = sum y 2^y with y = x log2(e) - r.  The reference r is m log2(e)
 // rounded to an integer, m the maximum so far: the product is not rounded before r is taken from it, so that y is as good
 // as if m had been subtracted first, in one operation.

@@ -416,27 +416,60 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
     }
 }
 
-template <typename T, int THREADS, int ITERS, int MINB>
+// Eight columns of a saved tensor as they lie in shared memory, and what they have to be multiplied by.
+template <typename T, bool HELD> struct Saved;
+template <typename T> struct Saved<T, false> {
+    Frag<T, 8> f;
+    float factor;
+    __device__ __forceinline__ void values(float (&x)[8]) const {
+        to_floats<T, 8>(f, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= factor;
+    }
+};
+template <typename T> struct Saved<T, true> {
+    uint2 q;
+    float factor;
+    __device__ __forceinline__ void values(float (&x)[8]) const {
+        const uint32_t w[2] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (__uint_as_float(__byte_perm(w[i / 4], 0x4b400000u, 0x7650 + i % 4)) - 12583040.f) * factor;
+    }
+};
+// The backward pass is bound by instructions and registers as much as by bytes: addresses advance from row to row, the step
+// of a checkpoint's group and the row's statistic, both factors, are multiplied first, and what the second half of a row
+// needs stays in shared memory until then (two registers too many cost 20 us in spills that miss the L1).  HELD: h' and b
+// are checkpoints (else both are values).
+template <typename T, int THREADS, int ITERS, int MINB, bool HELD>
 __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(const NormBackward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
     __shared__ float scratch[2][32];
     __shared__ uint64_t full[kMaxStages];
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
-    const bool has_b = a.b || a.hb.q;
-    const int C = (int)a.C, row_bytes = C * (int)sizeof(T), held_bytes = (int)a.ldq;
-    const int h_bytes = a.hh.q ? held_bytes : row_bytes, b_bytes = !has_b ? 0 : a.hb.q ? held_bytes : row_bytes;
-    const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + h_bytes, stage_bytes = at_b + b_bytes;
+    const bool has_b = HELD ? a.hb.q != nullptr : a.b != nullptr;
+    const bool ring_e = a.lde % 16 == 0;                             // exponents come with the ring where their rows can
+    const int C = (int)a.C, row_bytes = C * (int)sizeof(T), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
+    const int saved_bytes = HELD ? held_bytes : row_bytes;
+    const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + saved_bytes, stage_bytes = at_b + (has_b ? saved_bytes : 0);
     float *w_pre = (float *)dynamic, *w_post = w_pre + C;            // w_post times the group's gate
     uint8_t *ring = dynamic + (has_b ? 8 : 4) * C;
     const Slice slice(a.rows_per_group, a.parts_per_group);
+    auto fetch_saved = [&](uint32_t dst, const void *values, int64_t ld, const HeldIn &held, int64_t t, uint32_t bar) {
+        if constexpr (HELD) {
+            run_load(dst, held.q + t * a.ldq, (uint32_t)a.ldq, bar);
+            if (ring_e) run_load(dst + (uint32_t)a.ldq, held.e + t * a.lde, e_bytes, bar);
+        } else {
+            run_load(dst, (const T *)values + t * ld, row_bytes, bar);
+        }
+    };
     auto fetch = [&](int64_t t, int s) {
         const uint32_t bar = smem_address(&full[s]), dst = smem_address(ring + s * stage_bytes);
         barrier_expect(bar, stage_bytes);
         run_load(dst, (const T *)a.dn + t * a.lddn, row_bytes, bar);
         if (a.dh_in) run_load(dst + at_in, (const T *)a.dh_in + t * a.lddhi, row_bytes, bar);
-        run_load(dst + at_h, a.hh.q ? (const void *)(a.hh.q + t * a.ldq) : (const T *)a.h + t * a.ldh, h_bytes, bar);
-        if (has_b) run_load(dst + at_b, a.hb.q ? (const void *)(a.hb.q + t * a.ldq) : (const T *)a.b + t * a.ldb, b_bytes, bar);
+        fetch_saved(dst + at_h, a.h, a.ldh, a.hh, t, bar);
+        if (has_b) fetch_saved(dst + at_b, a.b, a.ldb, a.hb, t, bar);
     };
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) barrier_init(smem_address(&full[s]), 1);
@@ -455,109 +488,97 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
     for (int it = 0; it < ITERS; ++it)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum_x[it][i] = sum_y[it][i] = 0.f;
-    // The statistics and exponents of a row are fetched while the one before it is worked on.
+    // The statistics of a row are fetched while the one before it is worked on.
+    const float *stat = a.rstd_pre + slice.first, *stat_b = has_b ? a.rstd_post + slice.first : stat;
     float next_r = 0.f, next_rp = 0.f;
-    uint32_t next_eh[ITERS], next_eb[ITERS];
-    auto ahead = [&](int64_t t) {
-        next_r = a.rstd_pre[t];
-        if (has_b) next_rp = a.rstd_post[t];
-#pragma unroll
-        for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
-            next_eh[it] = a.hh.q && col < C ? a.hh.e[t * a.lde + col / kGroup] : 0;
-            next_eb[it] = a.hb.q && col < C ? a.hb.e[t * a.lde + col / kGroup] : 0;
-        }
-    };
-    if (slice.first < slice.last) ahead(slice.first);
+    if (slice.first < slice.last) {
+        next_r = *stat;
+        next_rp = *stat_b;
+    }
+    const int col0 = (int)threadIdx.x * 8;
+    T *out_h = (T *)a.dh + slice.first * a.lddh + col0, *out_b = (T *)a.db + (has_b ? slice.first * a.lddb + col0 : 0);
     int s = 0;
     uint32_t parity = 0;
     for (int64_t t = slice.first; t < slice.last; ++t) {
         const bool ok = barrier_wait(smem_address(&full[s]), parity, failed);
         const uint8_t *row = ring + s * stage_bytes;
         const float r = ok ? next_r : NAN, rp = next_rp;
+        auto saved = [&](int place, const HeldIn &held, int col, float factor) {
+            Saved<T, HELD> v;
+            if constexpr (HELD) {
+                v.q = *reinterpret_cast<const uint2 *>(row + place + col);
+                factor *= group_scale(ring_e ? row[place + (int)a.ldq + col / kGroup] : held.e[t * a.lde + col / kGroup]);
+            } else {
+                v.f = shared_frag<T>(row + place + col * sizeof(T));
+            }
+            v.factor = factor;
+            return v;
+        };
         float D[ITERS][8], x[ITERS][8];
-        Frag<T, 8> in[ITERS], fb[ITERS];
-        RawQ<8> qb[ITERS];
-        uint32_t eb[ITERS];
         float dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
-            eb[it] = next_eb[it];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) D[it][i] = x[it][i] = 0.f;
+            const int col = it * THREADS * 8 + col0;
             if (col < C) {
                 float w[8];
                 to_floats<T, 8>(shared_frag<T>(row + col * sizeof(T)), D[it]);
-                if (a.hh.q) {
-                    const uint2 q = *reinterpret_cast<const uint2 *>(row + at_h + col);
-                    held_values<8>(RawQ<8>{q.x, q.y}, next_eh[it], x[it]);
-                } else {
-                    to_floats<T, 8>(shared_frag<T>(row + at_h + col * sizeof(T)), x[it]);
-                }
-                if (a.dh_in) in[it] = shared_frag<T>(row + at_in + col * sizeof(T));
-                if (a.hb.q) {
-                    const uint2 q = *reinterpret_cast<const uint2 *>(row + at_b + col);
-                    qb[it] = RawQ<8>{q.x, q.y};
-                } else if (has_b) {
-                    fb[it] = shared_frag<T>(row + at_b + col * sizeof(T));
-                }
+                saved(at_h, a.hh, col, r).values(x[it]);
                 shared_params(w_pre, col, C, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[it][i] *= r;
                     sum_x[it][i] = fmaf(D[it][i], x[it][i], sum_x[it][i]);
                     D[it][i] *= w[i];
                     dot = fmaf(D[it][i], x[it][i], dot);
                 }
             }
         }
-        if (t + 1 < slice.last) ahead(t + 1);
-        dot = cta_sum<THREADS>(dot, scratch[0]) * a.inv_C;
-        if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);       // every thread has read the stage
-        float dot_b = 0.f;
+        if (t + 1 < slice.last) {
+            next_r = *++stat;
+            next_rp = *++stat_b;
+        }
+        const float minus_dot = -cta_sum<THREADS>(dot, scratch[0]) * a.inv_C;
+        dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = it * THREADS * 8 + col0;
             if (col < C) {
                 float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = 0.f;
-                if (a.dh_in) to_floats<T, 8>(in[it], v);
+                Frag<T, 8> in = zeros<T, 8>();
+                if (a.dh_in) in = shared_frag<T>(row + at_in + col * sizeof(T));
+                to_floats<T, 8>(in, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    D[it][i] = fmaf(r, fmaf(-x[it][i], dot, D[it][i]), v[i]);
+                    D[it][i] = fmaf(r, fmaf(x[it][i], minus_dot, D[it][i]), v[i]);
                     v[i] = a.res_scale * D[it][i];
                 }
-                store_floats<T, 8>((T *)a.dh + t * a.lddh + col, v);
+                store_floats<T, 8>(out_h + it * THREADS * 8, v);
                 if (has_b) {
-                    if (a.hb.q) held_values<8>(qb[it], eb[it], x[it]);
-                    else to_floats<T, 8>(fb[it], x[it]);
+                    saved(at_b, a.hb, col, rp).values(x[it]);
                     shared_params(w_post, col, C, v);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        x[it][i] *= rp;
                         sum_y[it][i] = fmaf(D[it][i], x[it][i], sum_y[it][i]);
                         D[it][i] *= v[i];
-                        dot_b = fmaf(D[it][i], x[it][i], dot_b);
+                        dot = fmaf(D[it][i], x[it][i], dot);
                     }
                 }
             }
         }
+        out_h += a.lddh;
         if (has_b) {
-            dot_b = cta_sum<THREADS>(dot_b, scratch[1]) * a.inv_C;
+            const float minus_dot_b = -cta_sum<THREADS>(dot, scratch[1]) * a.inv_C;
+            if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);   // every thread has read the stage
 #pragma unroll
-            for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * 8;
-                if (col < C) {
-                    float out[8];
+            for (int it = 0; it < ITERS; ++it)
+                if (it * THREADS * 8 + col0 < C) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) out[i] = rp * fmaf(-x[it][i], dot_b, D[it][i]);
-                    store_floats<T, 8>((T *)a.db + t * a.lddb + col, out);
+                    for (int i = 0; i < 8; ++i) D[it][i] = rp * fmaf(x[it][i], minus_dot_b, D[it][i]);
+                    store_floats<T, 8>(out_b + it * THREADS * 8, D[it]);
                 }
-            }
+            out_b += a.lddb;
         } else {
             __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next
+            if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);
         }
         if (++s == stages) {
             s = 0;
@@ -567,7 +588,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
     float *px = a.partial + (int64_t)blockIdx.x * 2 * C;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int col = (it * THREADS + (int)threadIdx.x) * 8;
+        const int col = it * THREADS * 8 + col0;
         if (col < C)
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {

@@ -452,14 +452,17 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
         by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
             const int64_t params = (has_b ? 8 : 4) * C, want = S::min_ctas * kUsualSms;
-            const int64_t stage = C * es * (dh_in ? 2 : 1) + (h_q ? q_stride(C) : C * es) + (!has_b ? 0 : b_q ? q_stride(C) : C * es);
+            const int64_t held = q_stride(C) + (e_stride(C) % 16 == 0 ? e_stride(C) : 0);
+            const int64_t stage = C * es * (dh_in ? 2 : 1) + (h_q ? held : C * es) + (!has_b ? 0 : b_q ? held : C * es);
             const int stages = stream_stages(params, stage, S::min_ctas);
-            if (stages < 2 || T < want * kStreamRows) return;
+            if (stages < 2 || T < want * kStreamRows || (has_b && !h_q != !b_q)) return;
             streamed = true;
             a.parts_per_group = norm_parts(T, groups, want);
             const int smem = (int)(params + stages * stage);
             by_dtype(dtype, [&](auto type) {
-                const auto kernel = deft::norm_backward_stream_kernel<decltype(type), S::threads, S::iters, S::min_ctas>;
+                using E = decltype(type);
+                const auto kernel = h_q ? deft::norm_backward_stream_kernel<E, S::threads, S::iters, S::min_ctas, true>
+                                        : deft::norm_backward_stream_kernel<E, S::threads, S::iters, S::min_ctas, false>;
                 if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
                 kernel<<<(unsigned)(groups * a.parts_per_group), S::threads, smem, stream>>>(a, stages);
             });

@@ -62,6 +62,11 @@ template <typename T, int V> __device__ __forceinline__ void store_floats(T *p, 
         for (int i = 0; i < kWords; ++i) reinterpret_cast<uint4 *>(p)[i] = w[i];
     }
 }
+template <typename T, int V> __device__ __forceinline__ Frag<T, V> zeros() {
+    Frag<T, V> f;
+    memset(&f, 0, sizeof(f));
+    return f;
+}
 // fp32 parameters, read by every row: cached.
 template <int V> __device__ __forceinline__ void load_params(const float *p, float (&out)[V]) {
     if constexpr (V == 1) {
@@ -78,6 +83,30 @@ template <int V> __device__ __forceinline__ void load_params(const float *p, flo
     }
 }
 
+// Two fp32 operations in one instruction.
+struct Pair { uint64_t bits; };
+__device__ __forceinline__ Pair make_pair(float a, float b) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.bits) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ void split_pair(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.bits)); }
+__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+    return d;
+}
+__device__ __forceinline__ Pair pair_add(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits));
+    return d;
+}
+__device__ __forceinline__ Pair pair_mul(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits));
+    return d;
+}
+__device__ __forceinline__ Pair both(float a) { return make_pair(a, a); }
 // ---------------------------------------------------------------------------
 // Checkpoint group: 32 consecutive columns of a row, held by 32 / V consecutive lanes of a warp (V columns each).
 // k = max(floor(log2 amax) - 6, -126) is read off the exponent bits of amax: the steps are powers of two, so x 2^-k
