@@ -598,36 +598,44 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
     }
 }
 
-// The parts' sums, in a fixed order: CTA (32 columns, job) adds them with 32 threads per column.  Job g < jobs_gate: dgate of
-// group g, w_post times the sum of D y over the group's parts.  Then dw_pre, the sum of dn x over all parts, and dw_post,
-// the sum of gate times D y.
-__global__ void __launch_bounds__(1024) norm_reduce_kernel(const float *__restrict__ partial, const float *__restrict__ w_post,
-                                                          const float *__restrict__ gate, int64_t C, int64_t groups,
-                                                          int64_t parts_per_group, int64_t jobs_gate, int accumulate,
-                                                          float *dw_post, float *dgate, float *dw_pre) {
+// The parts' sums, in a fixed order: CTA (32 columns, job) adds them with 32 threads per V columns.  Job g < jobs_gate: dgate
+// of group g, w_post times the sum of D y over the group's parts.  Then dw_pre, the sum of dn x over all parts, and
+// dw_post, the sum of gate times D y.
+template <int V>
+__global__ void __launch_bounds__(1024 / V) norm_reduce_kernel(const float *__restrict__ partial, const float *__restrict__ w_post,
+                                                               const float *__restrict__ gate, int C, int64_t groups,
+                                                               int64_t parts_per_group, int64_t jobs_gate, int accumulate,
+                                                               float *dw_post, float *dgate, float *dw_pre) {
     __shared__ float tile[32][33];
     asm volatile("griddepcontrol.wait;" ::: "memory");               // the partial sums are those of the kernel before
-    const int64_t col = (int64_t)blockIdx.x * 32 + threadIdx.x;
-    const bool live = col < C;
+    const int col = (int)(blockIdx.x * 32 + threadIdx.x * V);
+    const bool live = col < C;                                       // V columns at a time: C is a multiple of V
     for (int64_t job = blockIdx.y; job < jobs_gate + (dw_post ? 2 : 1); job += gridDim.y) {
         const int64_t first = job < jobs_gate ? job * parts_per_group : 0, count = (job < jobs_gate ? 1 : groups) * parts_per_group;
         const bool of_y = job != jobs_gate, gated = job == jobs_gate + 1 && gate;
-        float s = 0.f;
+        float s[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] = 0.f;
         if (live)
 #pragma unroll 4
             for (int64_t p = threadIdx.y; p < count; p += 32) {
-                const float v = partial[((first + p) * 2 + of_y) * C + col];
-                s = gated ? fmaf(gate[(int64_t)((uint32_t)p / (uint32_t)parts_per_group) * C + col], v, s) : s + v;
-            }
-        tile[threadIdx.y][threadIdx.x] = s;
-        __syncthreads();
-        if (threadIdx.y == 0 && live) {
-            s = 0.f;
+                struct alignas(V * 4) Run { float v[V]; };
+                const Run v = *reinterpret_cast<const Run *>(partial + ((first + p) * 2 + of_y) * C + col);
+                const float *g = gate + (int64_t)(gated ? (uint32_t)p / (uint32_t)parts_per_group : 0) * C + col;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s += tile[i][threadIdx.x];
-            float *out = job < jobs_gate ? dgate + job * C + col : of_y ? dw_post + col : dw_pre + col;
-            if (job < jobs_gate) s *= w_post[col];
-            *out = accumulate ? *out + s : s;
+                for (int i = 0; i < V; ++i) s[i] = gated ? fmaf(g[i], v.v[i], s[i]) : s[i] + v.v[i];
+            }
+#pragma unroll
+        for (int i = 0; i < V; ++i) tile[threadIdx.y][threadIdx.x * V + i] = s[i];
+        __syncthreads();
+        const int c = (int)(threadIdx.y * blockDim.x + threadIdx.x), column = (int)blockIdx.x * 32 + c;
+        if (c < 32 && column < C) {
+            float total = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) total += tile[i][c];
+            float *out = job < jobs_gate ? dgate + job * C + column : of_y ? dw_post + column : dw_pre + column;
+            if (job < jobs_gate) total *= w_post[column];
+            *out = accumulate ? *out + total : total;
         }
         __syncthreads();
     }

@@ -484,14 +484,14 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     const int64_t jobs_gate = gate ? groups : 0, jobs = jobs_gate + (has_b ? 2 : 1);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ceil_div(C, 32), (unsigned)(jobs < 1024 ? jobs : 1024));
-    cfg.blockDim = dim3(32, 32);
+    cfg.blockDim = C % 4 == 0 ? dim3(8, 32) : dim3(32, 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    err = cudaLaunchKernelEx(&cfg, deft::norm_reduce_kernel, (const float *)workspace, w_post, gate, C, groups, a.parts_per_group, jobs_gate, (int)accumulate,
+    err = cudaLaunchKernelEx(&cfg, C % 4 == 0 ? deft::norm_reduce_kernel<4> : deft::norm_reduce_kernel<1>, (const float *)workspace, w_post, gate, (int)C, groups, a.parts_per_group, jobs_gate, (int)accumulate,
                              has_b ? dw_post : (float *)nullptr, dgate, dw_pre);
     if (err != cudaSuccess) {
         cudaGetLastError();
