@@ -383,17 +383,18 @@ def _stream(stream):
 
 def _act(t, name, like=None):
     """(dtype code, T, C, pointer, row stride) of an activation; `like`: another's, to agree with."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _DTYPES:
-        raise TypeError("%s must be a two-dimensional float32, bfloat16 or float16 torch tensor" % name)
+    try:
+        code = _DTYPES[t.dtype]
+        T, C = t.shape
+        ld, inner = t.stride()
+    except (AttributeError, KeyError, ValueError, TypeError):
+        raise TypeError("%s must be a two-dimensional float32, bfloat16 or float16 torch tensor" % name) from None
     if not t.is_cuda:
         raise TypeError("%s must live on the GPU" % name)
-    T, C = t.shape
-    ld, inner = t.stride()
     if inner != 1 and C > 1:
         raise ValueError("the columns of %s must be consecutive" % name)
     if T <= 1:
         ld = C
-    code = _DTYPES[t.dtype]
     if like is not None and (code != like[0] or T != like[1] or C != like[2]):
         raise ValueError("%s is %s of %s, expected type %d and shape %s" % (name, t.dtype, (T, C), like[0], like[1:3]))
     return code, T, C, t.data_ptr(), ld
@@ -408,12 +409,23 @@ def _held(ck, name, T, C):
     if ck is None:
         return None, None
     q, e = ck
-    ldq, lde = -(-C // 16) * 16, (C + 127) // 128 * 4
-    return _dev(q, name + " q", (T, ldq), torch.int8), _dev(e, name + " e", (T, lde), torch.uint8)
+    return (_param(q, name, (T, (C + 15) // 16 * 16), torch.int8), _param(e, name, (T, (C + 127) // 128 * 4), torch.uint8))
 
 
-def _param(t, name, shape):
-    return None if t is None else _dev(t, name, shape)
+def _param(t, name, shape, dtype=torch.float32):
+    """Pointer of a contiguous tensor of this shape, or of None; _dev says what is wrong where something is."""
+    if t is None:
+        return None
+    try:
+        if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _dev(t, name, shape, dtype)
+
+
+def _need(t, name, shape, dtype=torch.float32):
+    return _dev(t, name, shape, dtype) if t is None else _param(t, name, shape, dtype)
 
 
 def _work(t, name):
@@ -462,7 +474,7 @@ def def_checkpoint_weight_grad(dy, ck, dw, workspace=None, accumulate=False, str
     I = dw.shape[1]
     q, e = _held(ck, "checkpoint", T, I)
     w, nw = _work(workspace, "workspace")
-    _check(lib.def_checkpoint_weight_grad(dt, T, O, I, p, ld, q, e, _dev(dw, "dw", (O, I)), 1 if accumulate else 0, w, nw, _stream(stream)))
+    _check(lib.def_checkpoint_weight_grad(dt, T, O, I, p, ld, q, e, _need(dw, "dw", (O, I)), 1 if accumulate else 0, w, nw, _stream(stream)))
 
 
 def def_gated_forward(gate, up, h, gate_ck=None, up_ck=None, stream=None):
@@ -528,9 +540,9 @@ def def_logprob_forward(logits, targets, logp, entropy, lse, top_ids=None, top_l
     """targets: int64 [T]; lse: float32 [T, 2] (maximum, log of the sum relative to it); top_ids: int64 [T, top]."""
     dt, T, V, p, ld = _act(logits, "logits")
     top = 0 if top_ids is None else top_ids.shape[1]
-    _check(lib.def_logprob_forward(dt, T, V, p, ld, _dev(targets, "targets", (T,), torch.int64), _dev(logp, "logp", (T,)),
-                                   _dev(entropy, "entropy", (T,)), _dev(lse, "lse", (T, 2)), top,
-                                   _dev(top_ids, "top_ids", (T, top), torch.int64, optional=True), _param(top_logp, "top_logp", (T, top)),
+    _check(lib.def_logprob_forward(dt, T, V, p, ld, _need(targets, "targets", (T,), torch.int64), _need(logp, "logp", (T,)),
+                                   _need(entropy, "entropy", (T,)), _need(lse, "lse", (T, 2)), top,
+                                   _param(top_ids, "top_ids", (T, top), torch.int64), _param(top_logp, "top_logp", (T, top)),
                                    _stream(stream)))
 
 
@@ -540,7 +552,7 @@ def def_logprob_backward(logits, targets, lse, entropy, dlogits, dlogp=None, den
     top = 0 if top_ids is None or dtop_logp is None else top_ids.shape[1]
     if top == 0:
         top_ids = dtop_logp = None
-    _check(lib.def_logprob_backward(dt, T, V, p, ld, _dev(targets, "targets", (T,), torch.int64), _dev(lse, "lse", (T, 2)),
-                                    _dev(entropy, "entropy", (T,)), _param(dlogp, "dlogp", (T,)), _param(dentropy, "dentropy", (T,)), top,
-                                    _dev(top_ids, "top_ids", (T, top), torch.int64, optional=True), _param(dtop_logp, "dtop_logp", (T, top)),
+    _check(lib.def_logprob_backward(dt, T, V, p, ld, _need(targets, "targets", (T,), torch.int64), _need(lse, "lse", (T, 2)),
+                                    _need(entropy, "entropy", (T,)), _param(dlogp, "dlogp", (T,)), _param(dentropy, "dentropy", (T,)), top,
+                                    _param(top_ids, "top_ids", (T, top), torch.int64), _param(dtop_logp, "dtop_logp", (T, top)),
                                     *_act(dlogits, "dlogits", a)[3:], _stream(stream)))
