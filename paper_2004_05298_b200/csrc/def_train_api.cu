@@ -649,12 +649,14 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         cfg.blockDim = dim3(S::threads);
         cfg.dynamicSmemBytes = S::smem;
         cfg.stream = stream;
-        cudaLaunchAttribute attr[1];
+        cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = 2;
         attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
-        cfg.numAttrs = 1;
+        cfg.numAttrs = 2;
         err = cudaLaunchKernelEx(&cfg, kernel, a, map_y, map_x, map_e);
     };
     auto by_operand = [&](auto type) {
@@ -670,8 +672,19 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         return cuda_fail(err, "def_checkpoint_weight_grad");
     }
     if (const int64_t cut = p.tiles_i * p.tiles_o - p.whole; cut > 0) {
-        deft::weight_grad_join_kernel<<<(unsigned)(cut * 2 * (deft::kTileO / 8)), 256, 0, stream>>>(a, p.pairs);
-        DEF_TRY(launched("def_checkpoint_weight_grad (join)"));
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(cut * 2 * (deft::kTileO / 8)));
+        cfg.blockDim = dim3(256);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if ((err = cudaLaunchKernelEx(&cfg, deft::weight_grad_join_kernel, a, p.pairs)) != cudaSuccess) {
+            cudaGetLastError();
+            return cuda_fail(err, "def_checkpoint_weight_grad (join)");
+        }
     }
     return DEF_OK;
 }

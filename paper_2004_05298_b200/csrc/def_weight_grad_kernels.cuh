@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(GradShape<WIDEN>::threads, 1)
     cluster_sync();
     tmem_fence_after();
     const uint32_t tmem = *tmem_slot;
+    asm volatile("griddepcontrol.wait;" ::: "memory");             // the set-up above may overlap the kernel before
     Pieces work(a);
     int64_t tile;
     int k0, k1, i0, o0;
@@ -362,30 +363,26 @@ __global__ void __launch_bounds__(GradShape<WIDEN>::threads, 1)
     }
 }
 
-// The tiles that pairs shared: their parts, added in the order of the tokens.  One CTA per 8 rows of
-// dw of half a tile.
+// The tiles that pairs shared: their parts, added in the order of the tokens.  One CTA per 8 rows of dw of half a tile.
 __global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad a, int pairs) {
     const int64_t per_tile = (int64_t)a.blocks * a.planes, all = ((int64_t)a.tiles_i * a.tiles_o - a.whole) * per_tile;
     const int64_t half_tile = blockIdx.x / (kTileO / 8), tile = half_tile / 2;       // of the tiles that were cut
     const int rank = (int)(half_tile % 2);
     const int col = (int)(blockIdx.x % (kTileO / 8)) * 8 + threadIdx.x / 32;
+    // pair c holds blocks [all c / pairs, all (c + 1) / pairs); none is empty
     const int64_t begin = tile * per_tile, end = begin + per_tile;
-    // pair c holds blocks [all c / pairs, all (c + 1) / pairs)
-    int64_t c = begin * pairs / all;
-    while (c + 1 < pairs && all * (c + 1) / pairs <= begin) ++c;
-    if (all * c / pairs <= begin && all * (c + 1) / pairs >= end) return;        // whole in one pair: written there
+    const int first = (int)(((begin + 1) * pairs - 1) / all), last = (int)((end * pairs - 1) / all);
+    asm volatile("griddepcontrol.wait;" ::: "memory");                                // the parts are those of the kernel before
+    if (first == last) return;                                                        // whole in one pair: written there
     int i0, o0;
     tile_place(a, a.whole + tile, i0, o0);
     i0 += rank * kTileI;
     const int i = threadIdx.x % 32 * 4;
     if (o0 + col >= a.O || i0 + i >= a.I) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (; c < pairs; ++c) {
-        const int64_t from = all * c / pairs;
-        if (from >= end) break;
-        if (all * (c + 1) / pairs <= from) continue;
-        const int slot = from > begin ? 0 : 1;
-        const float4 v = *reinterpret_cast<const float4 *>(a.partial + ((c * 2 + rank) * 2 + slot) * (kTileO * kTileI) + col * kTileI + i);
+#pragma unroll 4
+    for (int c = first; c <= last; ++c) {                                             // the first holds the tile's first block
+        const float4 v = *reinterpret_cast<const float4 *>(a.partial + (((int64_t)c * 2 + rank) * 2 + (c == first)) * (kTileO * kTileI) + col * kTileI + i);
         sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
     }
     float *out = a.dw + (int64_t)(o0 + col) * a.I + i0 + i;
