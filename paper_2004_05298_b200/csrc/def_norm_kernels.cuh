@@ -22,37 +22,38 @@ struct NormForward {
 };
 
 // One CTA per row; the row stays in registers between its two norms.
-template <typename T, int V, int THREADS, int ITERS>
+template <typename T, bool ALIGNED, int THREADS, int ITERS>
 __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward a) {
     __shared__ float scratch[2][32];
+    const int C = (int)a.C;
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        float h[ITERS][V];
+        float h[ITERS][8];
         const T *hr = (const T *)a.h + t * a.ldh;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * V;
-            if (col < a.C) load_floats<T, V>(hr + col, h[it]);
-            else
-                for (int i = 0; i < V; ++i) h[it][i] = 0.f;
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            Frag<T, 8> f = zeros<T, 8>();
+            if (col < C) f = load_cols<T, ALIGNED>(hr, col, C);
+            to_floats<T, 8>(f, h[it]);
         }
         float sum = 0.f;
         if (a.b) {
-            float b[ITERS][V];
+            float b[ITERS][8];
             const T *br = (const T *)a.b + t * a.ldb;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * V;
-                if (col < a.C) load_floats<T, V>(br + col, b[it]);
-                else
-                    for (int i = 0; i < V; ++i) b[it][i] = 0.f;
+                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                Frag<T, 8> f = zeros<T, 8>();
+                if (col < C) f = load_cols<T, ALIGNED>(br, col, C);
+                to_floats<T, 8>(f, b[it]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum = fmaf(b[it][i], b[it][i], sum);
+                for (int i = 0; i < 8; ++i) sum = fmaf(b[it][i], b[it][i], sum);
             }
             if (a.hb.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int col = (it * THREADS + (int)threadIdx.x) * V;
-                    store_held<V>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, col < a.C, b[it]);
+                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    store_held(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
                 }
             sum = cta_sum<THREADS>(sum, scratch[0]);
             const float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
@@ -62,41 +63,39 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             sum = 0.f;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * V;
-                if (col < a.C) {
-                    float w[V], g[V];
-                    load_params<V>(a.w_post + col, w);
-                    if (gate) {
-                        load_params<V>(gate + col, g);
+                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                float w[8], g[8];
+                load_params(a.w_post, col, C, w);
+                if (gate) {
+                    load_params(gate, col, C, g);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) w[i] *= g[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < V; ++i) h[it][i] = fmaf(b[it][i] * r, w[i], a.res_scale * h[it][i]);
-                    store_floats<T, V>(ho + col, h[it]);
+                    for (int i = 0; i < 8; ++i) w[i] *= g[i];
                 }
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum = fmaf(h[it][i], h[it][i], sum);
+                for (int i = 0; i < 8; ++i) h[it][i] = fmaf(b[it][i] * r, w[i], a.res_scale * h[it][i]);
+                store_cols<T, ALIGNED>(ho, col, C, h[it]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
             }
             if (a.hh.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int col = (it * THREADS + (int)threadIdx.x) * V;
-                    float x[V];
+                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    float x[8];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));   // h' as stored
-                    store_held<V>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, col < a.C, x);
+                    for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));   // h' as stored
+                    store_held(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, x);
                 }
         } else {
 #pragma unroll
             for (int it = 0; it < ITERS; ++it)
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum = fmaf(h[it][i], h[it][i], sum);
+                for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
             if (a.hh.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int col = (it * THREADS + (int)threadIdx.x) * V;
-                    store_held<V>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, col < a.C, h[it]);
+                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    store_held(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, h[it]);
                 }
         }
         sum = cta_sum<THREADS>(sum, scratch[1]);
@@ -105,21 +104,16 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
         T *no = (T *)a.n_out + t * a.ldn;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * V;
-            float n[V];
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            float n[8], w[8];
+            load_params(a.w_pre, col, C, w);
 #pragma unroll
-            for (int i = 0; i < V; ++i) n[i] = 0.f;
-            if (col < a.C) {
-                float w[V];
-                load_params<V>(a.w_pre + col, w);
-#pragma unroll
-                for (int i = 0; i < V; ++i) n[i] = h[it][i] * r * w[i];
-                store_floats<T, V>(no + col, n);
-            }
+            for (int i = 0; i < 8; ++i) n[i] = h[it][i] * r * w[i];
+            store_cols<T, ALIGNED>(no, col, C, n);
             if (a.hn.q) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) n[i] = to_float<T>(from_float<T>(n[i]));           // n as stored
-                store_held<V>(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, col < a.C, n);
+                for (int i = 0; i < 8; ++i) n[i] = to_float<T>(from_float<T>(n[i]));           // n as stored
+                store_held(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, n);
             }
         }
         if (THREADS > 32 && !a.b) __syncthreads();   // one sum per row: scratch[1] is rewritten by the next
@@ -139,59 +133,60 @@ struct NormBackward {
 };
 
 // Part p = (group, slice of the group's rows): one CTA walks the slice, the column sums stay in registers.
-template <typename T, int V, int THREADS, int ITERS>
+template <typename T, bool ALIGNED, int THREADS, int ITERS>
 __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackward a) {
     __shared__ float scratch[2][32];
+    const int C = (int)a.C;
     const int64_t group = blockIdx.x / a.parts_per_group, slice = blockIdx.x % a.parts_per_group;
     const int64_t first = group * a.rows_per_group + a.rows_per_group * slice / a.parts_per_group;
     const int64_t last = group * a.rows_per_group + a.rows_per_group * (slice + 1) / a.parts_per_group;
     const bool has_b = a.b || a.hb.q;
-    float sum_x[ITERS][V], sum_y[ITERS][V];
+    float sum_x[ITERS][8], sum_y[ITERS][8];
 #pragma unroll
     for (int it = 0; it < ITERS; ++it)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum_x[it][i] = sum_y[it][i] = 0.f;
+        for (int i = 0; i < 8; ++i) sum_x[it][i] = sum_y[it][i] = 0.f;
     for (int64_t t = first; t < last; ++t) {
         // All loads of the row first: it waits for memory once.
-        Frag<T, V> fn[ITERS], fi[ITERS], fh[ITERS], fb[ITERS];
-        RawQ<V> qh[ITERS], qb[ITERS];
+        Frag<T, 8> fn[ITERS], fi[ITERS], fh[ITERS], fb[ITERS];
+        RawQ qh[ITERS], qb[ITERS];
         uint32_t eh[ITERS], eb[ITERS];
         const float r = a.rstd_pre[t], rp = has_b ? a.rstd_post[t] : 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * V;
-            if (col < a.C) {
-                fn[it] = load_frag<T, V>((const T *)a.dn + t * a.lddn + col);
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            if (col < C) {
+                fn[it] = load_cols<T, ALIGNED>((const T *)a.dn + t * a.lddn, col, C);
                 if (a.hh.q) {
-                    qh[it] = load_q<V>(a.hh.q + t * a.ldq + col);
+                    qh[it] = load_q(a.hh.q + t * a.ldq + col);
                     eh[it] = a.hh.e[t * a.lde + col / kGroup];
                 } else {
-                    fh[it] = load_frag<T, V>((const T *)a.h + t * a.ldh + col);
+                    fh[it] = load_cols<T, ALIGNED>((const T *)a.h + t * a.ldh, col, C);
                 }
-                if (a.dh_in) fi[it] = load_frag<T, V>((const T *)a.dh_in + t * a.lddhi + col);
+                if (a.dh_in) fi[it] = load_cols<T, ALIGNED>((const T *)a.dh_in + t * a.lddhi, col, C);
                 if (a.hb.q) {
-                    qb[it] = load_q<V>(a.hb.q + t * a.ldq + col);
+                    qb[it] = load_q(a.hb.q + t * a.ldq + col);
                     eb[it] = a.hb.e[t * a.lde + col / kGroup];
                 } else if (has_b) {
-                    fb[it] = load_frag<T, V>((const T *)a.b + t * a.ldb + col);
+                    fb[it] = load_cols<T, ALIGNED>((const T *)a.b + t * a.ldb, col, C);
                 }
             }
         }
-        float D[ITERS][V], x[ITERS][V];
+        float D[ITERS][8], x[ITERS][8];
         float dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * V;
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
 #pragma unroll
-            for (int i = 0; i < V; ++i) D[it][i] = x[it][i] = 0.f;
-            if (col < a.C) {
-                float w[V];
-                to_floats<T, V>(fn[it], D[it]);
-                if (a.hh.q) held_values<V>(qh[it], eh[it], x[it]);
-                else to_floats<T, V>(fh[it], x[it]);
-                load_params<V>(a.w_pre + col, w);
+            for (int i = 0; i < 8; ++i) D[it][i] = x[it][i] = 0.f;
+            if (col < C) {
+                float w[8];
+                to_floats<T, 8>(fn[it], D[it]);
+                if (a.hh.q) held_cols<ALIGNED>(qh[it], eh[it], col, C, x[it]);
+                else to_floats<T, 8>(fh[it], x[it]);
+                load_params(a.w_pre, col, C, w);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
+                for (int i = 0; i < 8; ++i) {
                     x[it][i] *= r;
                     sum_x[it][i] = fmaf(D[it][i], x[it][i], sum_x[it][i]);
                     D[it][i] *= w[i];
@@ -203,35 +198,33 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
         float dot_b = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * V;
-            if (col < a.C) {
-                float v[V];
+            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            float v[8];
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = 0.f;
-                if (a.dh_in) to_floats<T, V>(fi[it], v);
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            if (a.dh_in && col < C) to_floats<T, 8>(fi[it], v);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    D[it][i] = fmaf(r, fmaf(-x[it][i], dot, D[it][i]), v[i]);
-                    v[i] = a.res_scale * D[it][i];
+            for (int i = 0; i < 8; ++i) {
+                D[it][i] = fmaf(r, fmaf(-x[it][i], dot, D[it][i]), v[i]);
+                v[i] = a.res_scale * D[it][i];
+            }
+            store_cols<T, ALIGNED>((T *)a.dh + t * a.lddh, col, C, v);
+            if (has_b && col < C) {
+                float w[8];
+                if (a.hb.q) held_cols<ALIGNED>(qb[it], eb[it], col, C, x[it]);
+                else to_floats<T, 8>(fb[it], x[it]);
+                load_params(a.w_post, col, C, w);
+                if (a.gate) {
+                    load_params(a.gate + group * a.C, col, C, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] *= v[i];
                 }
-                store_floats<T, V>((T *)a.dh + t * a.lddh + col, v);
-                if (has_b) {
-                    float w[V];
-                    if (a.hb.q) held_values<V>(qb[it], eb[it], x[it]);
-                    else to_floats<T, V>(fb[it], x[it]);
-                    load_params<V>(a.w_post + col, w);
-                    if (a.gate) {
-                        load_params<V>(a.gate + group * a.C + col, v);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) w[i] *= v[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        x[it][i] *= rp;
-                        sum_y[it][i] = fmaf(D[it][i], x[it][i], sum_y[it][i]);
-                        D[it][i] *= w[i];
-                        dot_b = fmaf(D[it][i], x[it][i], dot_b);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    x[it][i] *= rp;
+                    sum_y[it][i] = fmaf(D[it][i], x[it][i], sum_y[it][i]);
+                    D[it][i] *= w[i];
+                    dot_b = fmaf(D[it][i], x[it][i], dot_b);
                 }
             }
         }
@@ -239,13 +232,11 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
             dot_b = cta_sum<THREADS>(dot_b, scratch[1]) * a.inv_C;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * V;
-                if (col < a.C) {
-                    float out[V];
+                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                float out[8];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) out[i] = rp * fmaf(-x[it][i], dot_b, D[it][i]);
-                    store_floats<T, V>((T *)a.db + t * a.lddb + col, out);
-                }
+                for (int i = 0; i < 8; ++i) out[i] = rp * fmaf(-x[it][i], dot_b, D[it][i]);
+                store_cols<T, ALIGNED>((T *)a.db + t * a.lddb, col, C, out);
             }
         } else if constexpr (THREADS > 32) {
             __syncthreads();                         // scratch[0] is rewritten by the next row
@@ -254,12 +245,12 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
     float *px = a.partial + (int64_t)blockIdx.x * 2 * a.C;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int col = (it * THREADS + (int)threadIdx.x) * V;
-        if (col < a.C)
+        const int col = (it * THREADS + (int)threadIdx.x) * 8;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < 8; ++i)
+            if (col + i < C) {
                 px[col + i] = sum_x[it][i];
-                if (has_b) px[a.C + col + i] = sum_y[it][i];
+                if (has_b) px[C + col + i] = sum_y[it][i];
             }
     }
 }
@@ -362,7 +353,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
                     const int col = (it * THREADS + (int)threadIdx.x) * 8;
-                    store_held<8>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, col < C, b[it]);
+                    store_held(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
                 }
             sum = 0.f;
 #pragma unroll
@@ -391,7 +382,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));       // h' as stored
-                store_held<8>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, col < C, x);
+                store_held(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, x);
             }
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
@@ -406,7 +397,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
             if (a.hn.q) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[it][i] = to_float<T>(from_float<T>(h[it][i]));   // n as stored
-                store_held<8>(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, col < C, h[it]);
+                store_held(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, h[it]);
             }
         }
         if (++s == stages) {

@@ -124,26 +124,25 @@ template <typename F> void by_dtype(int32_t dtype, F f) {
 
 constexpr int kUsualSms = 148;      // what launches and workspaces are sized for before a device is looked at
 
-template <int N> struct Width { static constexpr int value = N; };
-template <typename F> void by_width(bool eight, F f) {
-    if (eight) f(Width<8>());
-    else f(Width<1>());
+template <bool B> struct Is { static constexpr bool value = B; };
+template <typename F> void by_alignment(bool aligned, F f) {
+    if (aligned) f(Is<true>());
+    else f(Is<false>());
 }
 
 constexpr int kPlaneRows = 4;
-// Launch of a kernel that works on rows by columns without sums: a warp lies in one row.  f(V, grid, block).
-template <typename F> void on_plane(bool eight, int64_t T, int64_t C, F f) {
-    by_width(eight, [&](auto width) {
-        const int64_t lanes = ceil_div(C, width.value);
-        unsigned bx = 32;
-        while (bx < 256 && bx < lanes) bx *= 2;
-        const dim3 block(bx, 256 / bx);
-        // A CTA walks kPlaneRows rows of its columns where that leaves enough CTAs: fewer instructions go into addresses.
-        const int64_t gx = ceil_div(lanes, bx), all = ceil_div(T, block.y);
-        int64_t gy = ceil_div(all, kPlaneRows);
-        if (gx * gy < 32 * kUsualSms) gy = ceil_div(32 * kUsualSms, gx) < all ? ceil_div(32 * kUsualSms, gx) : all;
-        f(width, dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), block);
-    });
+// Launch of a kernel that works on rows by columns without sums: a warp lies in one row.  f(aligned, grid, block).
+template <typename F> void on_plane(bool aligned, int64_t T, int64_t C, F f) {
+    const int64_t lanes = ceil_div(C, 8);
+    unsigned bx = 32;
+    while (bx < 256 && bx < lanes) bx *= 2;
+    const dim3 block(bx, 256 / bx);
+    // A CTA walks kPlaneRows rows of its columns where that leaves enough CTAs: fewer instructions go into addresses.
+    const int64_t gx = ceil_div(lanes, bx), all = ceil_div(T, block.y);
+    int64_t gy = ceil_div(all, kPlaneRows);
+    if (gx * gy < 32 * kUsualSms) gy = ceil_div(32 * kUsualSms, gx) < all ? ceil_div(32 * kUsualSms, gx) : all;
+    const dim3 grid((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535));
+    by_alignment(aligned, [&](auto is_aligned) { f(is_aligned, grid, block); });
 }
 
 }  // namespace
@@ -166,10 +165,10 @@ extern "C" int def_checkpoint_pack(int32_t dtype, int64_t T, int64_t C, const vo
     const View views[] = {rows_view(x, "x", T, C, ldx, es, false), q_view(q, "q", T, C, true), e_view(e, "e", T, C, true)};
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
-    const bool eight = C % 8 == 0 && wide(x, ldx, es);
+    const bool aligned_rows = C % 8 == 0 && wide(x, ldx, es);
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
-        on_plane(eight, T, C, [&](auto v, dim3 grid, dim3 block) {
+        on_plane(aligned_rows, T, C, [&](auto v, dim3 grid, dim3 block) {
             deft::pack_kernel<E, v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>((const E *)x, ldx, T, (int)C, q, e, q_stride(C), e_stride(C));
         });
     });
@@ -186,10 +185,10 @@ extern "C" int def_checkpoint_unpack(int32_t dtype, int64_t T, int64_t C, const 
     const View views[] = {rows_view(out, "out", T, C, ldout, es, true), q_view(q, "q", T, C, false), e_view(e, "e", T, C, false)};
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
-    const bool eight = C % 8 == 0 && wide(out, ldout, es);
+    const bool aligned_rows = C % 8 == 0 && wide(out, ldout, es);
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
-        on_plane(eight, T, C, [&](auto v, dim3 grid, dim3 block) {
+        on_plane(aligned_rows, T, C, [&](auto v, dim3 grid, dim3 block) {
             deft::unpack_kernel<E, v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>(q, e, q_stride(C), e_stride(C), T, (int)C, (E *)out, ldout);
         });
     });
@@ -214,9 +213,9 @@ extern "C" int def_gated_forward(int32_t dtype, int64_t T, int64_t F, const void
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
     deft::GatedForward a = {gate, up, h, ldg, ldu, ldh, gate_q, up_q, gate_e, up_e, T, F, q_stride(F), e_stride(F)};
-    const bool eight = F % 8 == 0 && wide(gate, ldg, es) && wide(up, ldu, es) && wide(h, ldh, es);
+    const bool aligned_rows = F % 8 == 0 && wide(gate, ldg, es) && wide(up, ldu, es) && wide(h, ldh, es);
     by_dtype(dtype, [&](auto type) {
-        on_plane(eight, T, F, [&](auto v, dim3 grid, dim3 block) {
+        on_plane(aligned_rows, T, F, [&](auto v, dim3 grid, dim3 block) {
             deft::gated_forward_kernel<decltype(type), v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>(a);
         });
     });
@@ -243,9 +242,9 @@ extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const voi
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
     deft::GatedBackward a = {dh, gate_q, up_q, gate_e, up_e, dgate, dup, h_out, lddh, lddg, lddu, ldh, h_q, h_e, T, F, q_stride(F), e_stride(F)};
-    const bool eight = F % 8 == 0 && wide(dh, lddh, es) && wide(dgate, lddg, es) && wide(dup, lddu, es) && wide(h_out, ldh, es);
+    const bool aligned_rows = F % 8 == 0 && wide(dh, lddh, es) && wide(dgate, lddg, es) && wide(dup, lddu, es) && wide(h_out, ldh, es);
     by_dtype(dtype, [&](auto type) {
-        on_plane(eight, T, F, [&](auto v, dim3 grid, dim3 block) {
+        on_plane(aligned_rows, T, F, [&](auto v, dim3 grid, dim3 block) {
             deft::gated_backward_kernel<decltype(type), v.value><<<grid, block, 0, (cudaStream_t)cuda_stream>>>(a);
         });
     });
@@ -259,24 +258,15 @@ namespace {
 
 template <int THREADS, int ITERS> struct Shape { static constexpr int threads = THREADS, iters = ITERS; };
 template <int THREADS, int ITERS, int MINB> struct StreamShape { static constexpr int threads = THREADS, iters = ITERS, min_ctas = MINB; };
-// Threads per row and accesses per thread for rows of C columns, V at a time.
-template <int V, typename F> void by_row_shape(int64_t C, F f) {
-    const int64_t n = ceil_div(C, V);
-    if constexpr (V == 8) {
-        if (n <= 32) f(Shape<32, 1>());
-        else if (n <= 128) f(Shape<128, 1>());
-        else if (n <= 256) f(Shape<256, 1>());
-        else if (n <= 512) f(Shape<256, 2>());
-        else if (n <= 1024) f(Shape<512, 2>());
-        else f(Shape<1024, 2>());
-    } else {
-        if (n <= 256) f(Shape<32, 8>());
-        else if (n <= 1024) f(Shape<128, 8>());
-        else if (n <= 2048) f(Shape<256, 8>());
-        else if (n <= 4096) f(Shape<512, 8>());
-        else if (n <= 8192) f(Shape<1024, 8>());
-        else f(Shape<1024, 16>());
-    }
+// Threads per row and runs of 8 columns per thread for rows of C columns.
+template <typename F> void by_row_shape(int64_t C, F f) {
+    const int64_t n = ceil_div(C, 8);
+    if (n <= 32) f(Shape<32, 1>());
+    else if (n <= 128) f(Shape<128, 1>());
+    else if (n <= 256) f(Shape<256, 1>());
+    else if (n <= 512) f(Shape<256, 2>());
+    else if (n <= 1024) f(Shape<512, 2>());
+    else f(Shape<1024, 2>());
 }
 // The same for the stream kernels, with the CTAs per SM that their registers are meant for.
 template <typename F> void by_stream_shape(int64_t C, F f) {
@@ -346,10 +336,10 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
     a.hb = {b_q, b_e}; a.hh = {h_q, h_e}; a.hn = {n_q, n_e};
     a.T = T; a.C = C; a.rows_per_group = T / groups; a.ldq = q_stride(C); a.lde = e_stride(C);
     a.res_scale = res_scale; a.eps = eps; a.inv_C = 1.f / (float)C;
-    const bool eight = C % 8 == 0 && wide(h, ldh, es) && wide(b, ldb, es) && wide(h_out, ldho, es) && wide(n_out, ldn, es);
+    const bool aligned_rows = C % 8 == 0 && wide(h, ldh, es) && wide(b, ldb, es) && wide(h_out, ldho, es) && wide(n_out, ldn, es);
     cudaError_t err = cudaSuccess;
     bool streamed = false;
-    if (eight)
+    if (aligned_rows)
         by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
             const int64_t params = (b ? 8 : 4) * C, stage = (b ? 2 : 1) * C * es, want = S::min_ctas * kUsualSms;
@@ -368,12 +358,11 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
     if (err != cudaSuccess) return cuda_fail(err, "def_norm_forward");
     if (streamed) return launched("def_norm_forward");
     by_dtype(dtype, [&](auto type) {
-        by_width(eight, [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            by_row_shape<V>(C, [&](auto shape) {
+        by_alignment(aligned_rows, [&](auto aligned) {
+            by_row_shape(C, [&](auto shape) {
                 using S = decltype(shape);
                 const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
-                deft::norm_forward_kernel<decltype(type), V, S::threads, S::iters><<<grid, S::threads, 0, (cudaStream_t)cuda_stream>>>(a);
+                deft::norm_forward_kernel<decltype(type), aligned.value, S::threads, S::iters><<<grid, S::threads, 0, (cudaStream_t)cuda_stream>>>(a);
             });
         });
     });
@@ -444,11 +433,11 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     a.partial = (float *)workspace;
     a.T = T; a.C = C; a.rows_per_group = T / groups; a.ldq = q_stride(C); a.lde = e_stride(C);
     a.res_scale = res_scale; a.inv_C = 1.f / (float)C;
-    const bool eight = C % 8 == 0 && wide(dn, lddn, es) && wide(dh_in, lddhi, es) && wide(h, ldh, es) && wide(b, ldb, es) && wide(dh, lddh, es) && wide(db, lddb, es);
+    const bool aligned_rows = C % 8 == 0 && wide(dn, lddn, es) && wide(dh_in, lddhi, es) && wide(h, ldh, es) && wide(b, ldb, es) && wide(dh, lddh, es) && wide(db, lddb, es);
     if (groups > 0x7fffffff / 2) return fail(DEF_ERR_ARG, "groups is too large (got %lld)", (long long)groups);
     cudaError_t err = cudaSuccess;
     bool streamed = false;
-    if (eight)
+    if (aligned_rows)
         by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
             const int64_t params = (has_b ? 8 : 4) * C, want = S::min_ctas * kUsualSms;
@@ -470,12 +459,11 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     if (err != cudaSuccess) return cuda_fail(err, "def_norm_backward");
     if (!streamed)
         by_dtype(dtype, [&](auto type) {
-            by_width(eight, [&](auto width) {
-                constexpr int V = decltype(width)::value;
-                by_row_shape<V>(C, [&](auto shape) {
+            by_alignment(aligned_rows, [&](auto aligned) {
+                by_row_shape(C, [&](auto shape) {
                     using S = decltype(shape);
                     a.parts_per_group = norm_parts(T, groups, S::threads <= 128 ? kNormParts / 2 : S::threads <= 256 ? kNormParts / 4 : kNormParts / 8);
-                    deft::norm_backward_kernel<decltype(type), V, S::threads, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads, 0, stream>>>(a);
+                    deft::norm_backward_kernel<decltype(type), aligned.value, S::threads, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads, 0, stream>>>(a);
                 });
             });
         });
