@@ -256,11 +256,13 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
 }
 
 // ---------------------------------------------------------------------------
-// Stream kernels: the same rows where there are many and all of them can be read 16 bytes at a time.  A CTA walks a slice
-// of a group's rows; the next rows are on their way to shared memory by bulk copies while one is worked on, and the
-// parameters stay there in fp32.  What bounds these kernels otherwise is the latency of a row: its loads, then two sums
-// over the CTA that each wait for all of it.  (16384 x 4096 bf16 in 8 groups, one row per CTA without copies ahead:
-// forward 132 us, backward from 8-bit saves 367 us.)
+// Stream kernels: the same rows where there are many.  A CTA walks a slice of a group's rows; the next rows are on their way
+// to shared memory by bulk copies while one is worked on, and the parameters stay there in fp32.  What bounds these
+// kernels otherwise is the latency of a row: its loads, then two sums over the CTA that each wait for all of it.
+// (16384 x 4096 bf16 in 8 groups, one row per CTA without copies ahead: forward 132 us, backward from 8-bit saves 367 us.)
+//
+// Rows that are not ALIGNED are copied with the 16-byte words around them, shifted into place when they are read, and
+// written as store_run does.
 // ---------------------------------------------------------------------------
 constexpr int kMaxStages = 4;
 
@@ -274,11 +276,75 @@ template <typename T> __device__ __forceinline__ Frag<T, 8> shared_frag(const ui
     return f;
 }
 // Parameters in shared memory: of every 8 columns the first four in one half of the array, the last four in the other, so
-// that a warp's accesses lie side by side.
+// that a warp's accesses lie side by side.  C: columns rounded up to 8; those that do not exist are 0.
 __device__ __forceinline__ int param_place(int i, int C) { return (i % 8 < 4 ? 0 : C / 2) + i / 8 * 4 + i % 4; }
 __device__ __forceinline__ void shared_params(const float *p, int col, int C, float (&x)[8]) {
     const float4 a = *reinterpret_cast<const float4 *>(p + col / 2), b = *reinterpret_cast<const float4 *>(p + C / 2 + col / 2);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+
+// A tensor's row in the ring.  ALIGNED: its bytes.  Else: the whole 16-byte words it touches -- but never a word that is
+// partly outside the tensor, which only rows at its two ends can have; patch() brings their few elements.
+template <typename T, bool ALIGNED> struct RowCopy {
+    const T *p;
+    int C;
+    uintptr_t from, to;                  // the bytes that are copied
+    __device__ RowCopy(const void *base, int64_t ld, int64_t t, int64_t rows, int columns) : p((const T *)base + t * ld), C(columns) {
+        from = (uintptr_t)p;
+        to = (uintptr_t)(p + C);
+        if constexpr (!ALIGNED) {
+            const uintptr_t begin = (uintptr_t)base, end = (uintptr_t)((const T *)base + (rows - 1) * ld + C);
+            from &= ~(uintptr_t)15;
+            to = (to + 15) & ~(uintptr_t)15;
+            if (from < begin) from = (begin + 15) & ~(uintptr_t)15;
+            if (to > end) to = end & ~(uintptr_t)15;
+        }
+    }
+    __device__ uint32_t bytes() const { return to > from ? (uint32_t)(to - from) : 0; }
+    __device__ uint32_t offset() const { return ALIGNED ? 0 : (uint32_t)((uintptr_t)p & 15); }   // of the row in its slot
+    __device__ void copy(uint32_t slot, uint32_t bar) const {
+        if (bytes()) run_load(slot + (uint32_t)(from - ((uintptr_t)p & ~(uintptr_t)15)), (const void *)from, bytes(), bar);
+    }
+    __device__ bool whole() const { return ALIGNED || (from <= (uintptr_t)p && to >= (uintptr_t)(p + C)); }
+    // The elements that copy() left out, fewer than 16 bytes at either end; by the first threads of the CTA.
+    __device__ void patch(uint8_t *slot) const {
+        const T *a = to > from ? (const T *)from : p + C, *b = to > from ? (const T *)to : p + C;
+        const int head = a > p ? (int)(a - p) : 0, tail = p + C > b ? (int)(p + C - b) : 0;
+        T *row = reinterpret_cast<T *>(slot + offset());
+        for (int i = threadIdx.x; i < head + tail; i += blockDim.x) {
+            const int col = i < head ? i : C - tail + (i - head);
+            row[col] = p[col];
+        }
+        fence_async_shared();            // the slot's next copy comes after these stores
+    }
+};
+// Bytes of a row's slot.
+template <typename T, bool ALIGNED> __host__ __device__ __forceinline__ int slot_bytes(int C) {
+    return ALIGNED ? C * (int)sizeof(T) : (C * (int)sizeof(T) + 31) / 32 * 32 + 16;
+}
+// Columns [col, col + 8) of a row that starts `off` bytes into its slot; 0 for columns from C on.
+template <typename T, bool ALIGNED> __device__ __forceinline__ Frag<T, 8> slot_run(const uint8_t *slot, uint32_t off, int col, int C) {
+    if constexpr (ALIGNED) {
+        return shared_frag<T>(slot + col * sizeof(T));
+    } else {
+        constexpr int kWords = 2 * (int)sizeof(T);
+        uint32_t w[kWords + 4], out[kWords];
+        const uint4 *q = reinterpret_cast<const uint4 *>(slot + col * sizeof(T));
+#pragma unroll
+        for (int i = 0; i < kWords / 4 + 1; ++i) {
+            const uint4 v = q[i];
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+        shift_words<kWords>(w, off, out);
+        Frag<T, 8> f;
+        memcpy(&f, out, sizeof(f));
+        if (col + 8 > C) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i >= C) f.v[i] = from_float<T>(0.f);
+        }
+        return f;
+    }
 }
 // What rows a slice holds.
 struct Slice {
@@ -292,22 +358,23 @@ struct Slice {
 };
 
 // MINB: CTAs per SM that the registers are meant for.
-template <typename T, int THREADS, int ITERS, int MINB>
+template <typename T, bool ALIGNED, int THREADS, int ITERS, int MINB>
 __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(const NormForward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
     __shared__ float scratch[2][32];
     __shared__ uint64_t full[kMaxStages];
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
-    const int C = (int)a.C, row_bytes = C * (int)sizeof(T), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
-    float *w_pre = (float *)dynamic, *w_post = w_pre + C;            // w_post times the group's gate
-    uint8_t *ring = dynamic + (a.b ? 8 : 4) * C;
+    const int C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
+    float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
+    uint8_t *ring = dynamic + (a.b ? 8 : 4) * Cp;
     const Slice slice(a.rows_per_group, a.parts_per_group);
     auto fetch = [&](int64_t t, int s) {
         const uint32_t bar = smem_address(&full[s]), dst = smem_address(ring + s * stage_bytes);
-        barrier_expect(bar, stage_bytes);
-        run_load(dst, (const T *)a.h + t * a.ldh, row_bytes, bar);
-        if (a.b) run_load(dst + row_bytes, (const T *)a.b + t * a.ldb, row_bytes, bar);
+        const RowCopy<T, ALIGNED> h(a.h, a.ldh, t, a.T, C), b(a.b, a.ldb, t, a.T, C);
+        barrier_expect(bar, h.bytes() + (a.b ? b.bytes() : 0));
+        h.copy(dst, bar);
+        if (a.b) b.copy(dst + row_bytes, bar);
     };
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) barrier_init(smem_address(&full[s]), 1);
@@ -315,17 +382,23 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
     }
-    for (int i = threadIdx.x; i < C; i += THREADS) {
-        const int at = param_place(i, C);
-        w_pre[at] = a.w_pre[i];
-        if (a.b) w_post[at] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+    for (int i = threadIdx.x; i < Cp; i += THREADS) {
+        const int at = param_place(i, Cp);
+        w_pre[at] = i < C ? a.w_pre[i] : 0.f;
+        if (a.b) w_post[at] = i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
     }
     __syncthreads();
     int s = 0;
     uint32_t parity = 0;
     for (int64_t t = slice.first; t < slice.last; ++t) {
         const bool ok = barrier_wait(smem_address(&full[s]), parity, failed);
-        const uint8_t *row = ring + s * stage_bytes;
+        uint8_t *row = ring + s * stage_bytes;
+        const RowCopy<T, ALIGNED> copy_h(a.h, a.ldh, t, a.T, C), copy_b(a.b, a.ldb, t, a.T, C);
+        if (!copy_h.whole() || (a.b && !copy_b.whole())) {
+            copy_h.patch(row);
+            if (a.b) copy_b.patch(row + row_bytes);
+            __syncthreads();
+        }
         float h[ITERS][8], b[ITERS][8];
         float sum = 0.f;
 #pragma unroll
@@ -334,8 +407,8 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[it][i] = b[it][i] = 0.f;
             if (col < C) {
-                to_floats<T, 8>(shared_frag<T>(row + col * sizeof(T)), h[it]);
-                if (a.b) to_floats<T, 8>(shared_frag<T>(row + row_bytes + col * sizeof(T)), b[it]);
+                to_floats<T, 8>(slot_run<T, ALIGNED>(row, copy_h.offset(), col, C), h[it]);
+                if (a.b) to_floats<T, 8>(slot_run<T, ALIGNED>(row + row_bytes, copy_b.offset(), col, C), b[it]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -361,11 +434,11 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
                 const int col = (it * THREADS + (int)threadIdx.x) * 8;
                 if (col < C) {
                     float w[8];
-                    shared_params(w_post, col, C, w);
+                    shared_params(w_post, col, Cp, w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[it][i] = fmaf(b[it][i] * r, w[i], a.res_scale * h[it][i]);
-                    store_floats<T, 8>((T *)a.h_out + t * a.ldho + col, h[it]);
                 }
+                store_cols<T, ALIGNED>((T *)a.h_out + t * a.ldho, col, C, h[it]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
             }
@@ -389,11 +462,11 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
             const int col = (it * THREADS + (int)threadIdx.x) * 8;
             if (col < C) {
                 float w[8];
-                shared_params(w_pre, col, C, w);
+                shared_params(w_pre, col, Cp, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[it][i] = h[it][i] * r * w[i];
-                store_floats<T, 8>((T *)a.n_out + t * a.ldn + col, h[it]);
             }
+            store_cols<T, ALIGNED>((T *)a.n_out + t * a.ldn, col, C, h[it]);
             if (a.hn.q) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[it][i] = to_float<T>(from_float<T>(h[it][i]));   // n as stored
@@ -427,11 +500,19 @@ template <typename T> struct Saved<T, true> {
         for (int i = 0; i < 8; ++i) x[i] = (__uint_as_float(__byte_perm(w[i / 4], 0x4b400000u, 0x7650 + i % 4)) - 12583040.f) * factor;
     }
 };
+// Zeros in place of what a padded row holds past its last column.
+template <bool NOTHING> __device__ __forceinline__ void clear_past(float (&x)[8], int col, int C) {
+    if constexpr (!NOTHING) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i >= C) x[i] = 0.f;
+    }
+}
 // The backward pass is bound by instructions and registers as much as by bytes: addresses advance from row to row, the step
 // of a checkpoint's group and the row's statistic, both factors, are multiplied first, and what the second half of a row
 // needs stays in shared memory until then (two registers too many cost 20 us in spills that miss the L1).  HELD: h' and b
 // are checkpoints (else both are values).
-template <typename T, int THREADS, int ITERS, int MINB, bool HELD>
+template <typename T, bool ALIGNED, int THREADS, int ITERS, int MINB, bool HELD>
 __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(const NormBackward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
     __shared__ float scratch[2][32];
@@ -440,27 +521,30 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
     volatile int *failed = &failed_flag;
     const bool has_b = HELD ? a.hb.q != nullptr : a.b != nullptr;
     const bool ring_e = a.lde % 16 == 0;                             // exponents come with the ring where their rows can
-    const int C = (int)a.C, row_bytes = C * (int)sizeof(T), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
+    const int C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
     const int saved_bytes = HELD ? held_bytes : row_bytes;
     const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + saved_bytes, stage_bytes = at_b + (has_b ? saved_bytes : 0);
-    float *w_pre = (float *)dynamic, *w_post = w_pre + C;            // w_post times the group's gate
-    uint8_t *ring = dynamic + (has_b ? 8 : 4) * C;
+    float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
+    uint8_t *ring = dynamic + (has_b ? 8 : 4) * Cp;
     const Slice slice(a.rows_per_group, a.parts_per_group);
-    auto fetch_saved = [&](uint32_t dst, const void *values, int64_t ld, const HeldIn &held, int64_t t, uint32_t bar) {
+    using Copy = RowCopy<T, ALIGNED>;
+    auto saved_bytes_of = [&](const Copy &values) { return HELD ? (uint32_t)held_bytes : values.bytes(); };
+    auto fetch_saved = [&](uint32_t dst, const Copy &values, const HeldIn &held, int64_t t, uint32_t bar) {
         if constexpr (HELD) {
             run_load(dst, held.q + t * a.ldq, (uint32_t)a.ldq, bar);
             if (ring_e) run_load(dst + (uint32_t)a.ldq, held.e + t * a.lde, e_bytes, bar);
         } else {
-            run_load(dst, (const T *)values + t * ld, row_bytes, bar);
+            values.copy(dst, bar);
         }
     };
     auto fetch = [&](int64_t t, int s) {
         const uint32_t bar = smem_address(&full[s]), dst = smem_address(ring + s * stage_bytes);
-        barrier_expect(bar, stage_bytes);
-        run_load(dst, (const T *)a.dn + t * a.lddn, row_bytes, bar);
-        if (a.dh_in) run_load(dst + at_in, (const T *)a.dh_in + t * a.lddhi, row_bytes, bar);
-        fetch_saved(dst + at_h, a.h, a.ldh, a.hh, t, bar);
-        if (has_b) fetch_saved(dst + at_b, a.b, a.ldb, a.hb, t, bar);
+        const Copy n(a.dn, a.lddn, t, a.T, C), in(a.dh_in, a.lddhi, t, a.T, C), h(a.h, a.ldh, t, a.T, C), b(a.b, a.ldb, t, a.T, C);
+        barrier_expect(bar, n.bytes() + (a.dh_in ? in.bytes() : 0) + saved_bytes_of(h) + (has_b ? saved_bytes_of(b) : 0));
+        n.copy(dst, bar);
+        if (a.dh_in) in.copy(dst + at_in, bar);
+        fetch_saved(dst + at_h, h, a.hh, t, bar);
+        if (has_b) fetch_saved(dst + at_b, b, a.hb, t, bar);
     };
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) barrier_init(smem_address(&full[s]), 1);
@@ -468,10 +552,10 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
     }
-    for (int i = threadIdx.x; i < C; i += THREADS) {
-        const int at = param_place(i, C);
-        w_pre[at] = a.w_pre[i];
-        if (has_b) w_post[at] = a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+    for (int i = threadIdx.x; i < Cp; i += THREADS) {
+        const int at = param_place(i, Cp);
+        w_pre[at] = i < C ? a.w_pre[i] : 0.f;
+        if (has_b) w_post[at] = i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
     }
     __syncthreads();
     float sum_x[ITERS][8], sum_y[ITERS][8];
@@ -487,20 +571,28 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
         next_rp = *stat_b;
     }
     const int col0 = (int)threadIdx.x * 8;
-    T *out_h = (T *)a.dh + slice.first * a.lddh + col0, *out_b = (T *)a.db + (has_b ? slice.first * a.lddb + col0 : 0);
+    T *out_h = (T *)a.dh + slice.first * a.lddh, *out_b = (T *)a.db + (has_b ? slice.first * a.lddb : 0);
     int s = 0;
     uint32_t parity = 0;
     for (int64_t t = slice.first; t < slice.last; ++t) {
         const bool ok = barrier_wait(smem_address(&full[s]), parity, failed);
-        const uint8_t *row = ring + s * stage_bytes;
+        uint8_t *row = ring + s * stage_bytes;
+        const Copy copy_n(a.dn, a.lddn, t, a.T, C), copy_in(a.dh_in, a.lddhi, t, a.T, C), copy_h(a.h, a.ldh, t, a.T, C), copy_b(a.b, a.ldb, t, a.T, C);
+        if (!copy_n.whole() || (a.dh_in && !copy_in.whole()) || (!HELD && (!copy_h.whole() || (has_b && !copy_b.whole())))) {
+            copy_n.patch(row);
+            if (a.dh_in) copy_in.patch(row + at_in);
+            if (!HELD) copy_h.patch(row + at_h);
+            if (!HELD && has_b) copy_b.patch(row + at_b);
+            __syncthreads();
+        }
         const float r = ok ? next_r : NAN, rp = next_rp;
-        auto saved = [&](int place, const HeldIn &held, int col, float factor) {
+        auto saved = [&](int place, const Copy &copy, const HeldIn &held, int col, float factor) {
             Saved<T, HELD> v;
             if constexpr (HELD) {
                 v.q = *reinterpret_cast<const uint2 *>(row + place + col);
                 factor *= group_scale(ring_e ? row[place + (int)a.ldq + col / kGroup] : held.e[t * a.lde + col / kGroup]);
             } else {
-                v.f = shared_frag<T>(row + place + col * sizeof(T));
+                v.f = slot_run<T, ALIGNED>(row + place, copy.offset(), col, C);
             }
             v.factor = factor;
             return v;
@@ -512,9 +604,10 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
             const int col = it * THREADS * 8 + col0;
             if (col < C) {
                 float w[8];
-                to_floats<T, 8>(shared_frag<T>(row + col * sizeof(T)), D[it]);
-                saved(at_h, a.hh, col, r).values(x[it]);
-                shared_params(w_pre, col, C, w);
+                to_floats<T, 8>(slot_run<T, ALIGNED>(row, copy_n.offset(), col, C), D[it]);
+                saved(at_h, copy_h, a.hh, col, r).values(x[it]);
+                clear_past<ALIGNED || !HELD>(x[it], col, C);
+                shared_params(w_pre, col, Cp, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     sum_x[it][i] = fmaf(D[it][i], x[it][i], sum_x[it][i]);
@@ -532,26 +625,27 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
             const int col = it * THREADS * 8 + col0;
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
             if (col < C) {
-                float v[8];
-                Frag<T, 8> in = zeros<T, 8>();
-                if (a.dh_in) in = shared_frag<T>(row + at_in + col * sizeof(T));
-                to_floats<T, 8>(in, v);
+                if (a.dh_in) to_floats<T, 8>(slot_run<T, ALIGNED>(row + at_in, copy_in.offset(), col, C), v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     D[it][i] = fmaf(r, fmaf(x[it][i], minus_dot, D[it][i]), v[i]);
                     v[i] = a.res_scale * D[it][i];
                 }
-                store_floats<T, 8>(out_h + it * THREADS * 8, v);
-                if (has_b) {
-                    saved(at_b, a.hb, col, rp).values(x[it]);
-                    shared_params(w_post, col, C, v);
+            }
+            store_cols<T, ALIGNED>(out_h, col, C, v);
+            if (has_b && col < C) {
+                saved(at_b, copy_b, a.hb, col, rp).values(x[it]);
+                clear_past<ALIGNED || !HELD>(x[it], col, C);
+                shared_params(w_post, col, Cp, v);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        sum_y[it][i] = fmaf(D[it][i], x[it][i], sum_y[it][i]);
-                        D[it][i] *= v[i];
-                        dot = fmaf(D[it][i], x[it][i], dot);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    sum_y[it][i] = fmaf(D[it][i], x[it][i], sum_y[it][i]);
+                    D[it][i] *= v[i];
+                    dot = fmaf(D[it][i], x[it][i], dot);
                 }
             }
         }
@@ -560,12 +654,11 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
             const float minus_dot_b = -cta_sum<THREADS>(dot, scratch[1]) * a.inv_C;
             if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);   // every thread has read the stage
 #pragma unroll
-            for (int it = 0; it < ITERS; ++it)
-                if (it * THREADS * 8 + col0 < C) {
+            for (int it = 0; it < ITERS; ++it) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) D[it][i] = rp * fmaf(x[it][i], minus_dot_b, D[it][i]);
-                    store_floats<T, 8>(out_b + it * THREADS * 8, D[it]);
-                }
+                for (int i = 0; i < 8; ++i) D[it][i] = rp * fmaf(x[it][i], minus_dot_b, D[it][i]);
+                store_cols<T, ALIGNED>(out_b, it * THREADS * 8 + col0, C, D[it]);
+            }
             out_b += a.lddb;
         } else {
             __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next
@@ -580,12 +673,20 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
         const int col = it * THREADS * 8 + col0;
-        if (col < C)
+        if (ALIGNED && col < C) {
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {
                 *reinterpret_cast<float4 *>(px + col + i) = make_float4(sum_x[it][i], sum_x[it][i + 1], sum_x[it][i + 2], sum_x[it][i + 3]);
                 if (has_b) *reinterpret_cast<float4 *>(px + C + col + i) = make_float4(sum_y[it][i], sum_y[it][i + 1], sum_y[it][i + 2], sum_y[it][i + 3]);
             }
+        } else if (!ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i < C) {
+                    px[col + i] = sum_x[it][i];
+                    if (has_b) px[C + col + i] = sum_y[it][i];
+                }
+        }
     }
 }
 

@@ -270,7 +270,7 @@ template <typename F> void by_row_shape(int64_t C, F f) {
 }
 // The same for the stream kernels, with the CTAs per SM that their registers are meant for.
 template <typename F> void by_stream_shape(int64_t C, F f) {
-    const int64_t n = C / 8;
+    const int64_t n = ceil_div(C, 8);
     if (n <= 128) f(StreamShape<128, 1, 6>());
     else if (n <= 256) f(StreamShape<128, 2, 4>());
     else if (n <= 512) f(StreamShape<256, 2, 2>());
@@ -339,10 +339,11 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
     const bool aligned_rows = C % 8 == 0 && wide(h, ldh, es) && wide(b, ldb, es) && wide(h_out, ldho, es) && wide(n_out, ldn, es);
     cudaError_t err = cudaSuccess;
     bool streamed = false;
-    if (aligned_rows)
-        by_stream_shape(C, [&](auto shape) {
+    // Bytes of a row in a stream kernel's ring; parameters are padded to 8 columns there.
+    const int64_t slot = aligned_rows ? C * es : ceil_div(C * es, 32) * 32 + 16, padded = ceil_div(C, 8) * 8;
+    by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
-            const int64_t params = (b ? 8 : 4) * C, stage = (b ? 2 : 1) * C * es, want = S::min_ctas * kUsualSms;
+            const int64_t params = (b ? 8 : 4) * padded, stage = (b ? 2 : 1) * slot, want = S::min_ctas * kUsualSms;
             const int stages = stream_stages(params, stage, S::min_ctas);
             if (stages < 2 || T < want * kStreamRows) return;
             streamed = true;
@@ -350,7 +351,9 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
             const unsigned grid = (unsigned)(groups * a.parts_per_group);
             const int smem = (int)(params + stages * stage);
             by_dtype(dtype, [&](auto type) {
-                const auto kernel = deft::norm_forward_stream_kernel<decltype(type), S::threads, S::iters, S::min_ctas>;
+                using E = decltype(type);
+                const auto kernel = aligned_rows ? deft::norm_forward_stream_kernel<E, true, S::threads, S::iters, S::min_ctas>
+                                                 : deft::norm_forward_stream_kernel<E, false, S::threads, S::iters, S::min_ctas>;
                 if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
                 kernel<<<grid, S::threads, smem, (cudaStream_t)cuda_stream>>>(a, stages);
             });
@@ -437,12 +440,12 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     if (groups > 0x7fffffff / 2) return fail(DEF_ERR_ARG, "groups is too large (got %lld)", (long long)groups);
     cudaError_t err = cudaSuccess;
     bool streamed = false;
-    if (aligned_rows)
-        by_stream_shape(C, [&](auto shape) {
+    const int64_t slot = aligned_rows ? C * es : ceil_div(C * es, 32) * 32 + 16, padded = ceil_div(C, 8) * 8;
+    by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
-            const int64_t params = (has_b ? 8 : 4) * C, want = S::min_ctas * kUsualSms;
+            const int64_t params = (has_b ? 8 : 4) * padded, want = S::min_ctas * kUsualSms;
             const int64_t held = q_stride(C) + (e_stride(C) % 16 == 0 ? e_stride(C) : 0);
-            const int64_t stage = C * es * (dh_in ? 2 : 1) + (h_q ? held : C * es) + (!has_b ? 0 : b_q ? held : C * es);
+            const int64_t stage = slot * (dh_in ? 2 : 1) + (h_q ? held : slot) + (!has_b ? 0 : b_q ? held : slot);
             const int stages = stream_stages(params, stage, S::min_ctas);
             if (stages < 2 || T < want * kStreamRows || (has_b && !h_q != !b_q)) return;
             streamed = true;
@@ -450,8 +453,11 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
             const int smem = (int)(params + stages * stage);
             by_dtype(dtype, [&](auto type) {
                 using E = decltype(type);
-                const auto kernel = h_q ? deft::norm_backward_stream_kernel<E, S::threads, S::iters, S::min_ctas, true>
-                                        : deft::norm_backward_stream_kernel<E, S::threads, S::iters, S::min_ctas, false>;
+                const auto pick = [&](auto aligned) {
+                    return h_q ? deft::norm_backward_stream_kernel<E, aligned.value, S::threads, S::iters, S::min_ctas, true>
+                               : deft::norm_backward_stream_kernel<E, aligned.value, S::threads, S::iters, S::min_ctas, false>;
+                };
+                const auto kernel = aligned_rows ? pick(Is<true>()) : pick(Is<false>());
                 if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
                 kernel<<<(unsigned)(groups * a.parts_per_group), S::threads, smem, stream>>>(a, stages);
             });

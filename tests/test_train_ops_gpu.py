@@ -286,14 +286,16 @@ def test_norm_backward(B, dtype, saves):
 
 MANY_ROWS = [(2700, 64, 1), (2701, 200, 0), (2672, 1024, 8), (1800, 1032, 3), (1776, 2048, 1), (900, 2056, 4), (889, 4096, 0), (450, 4104, 5),
              (444, 8192, 2), (450, 8200, 1), (446, 12288, 2)]
+MANY_ODD = [(3000, 1, 2, "rows"), (2701, 3, 1, "off"), (2672, 33, 8, "rows"), (2700, 257, 0, "off"), (1800, 1111, 3, "rows"), (1777, 2047, 1, "rows"),
+            (1790, 1284, 2, "off"), (900, 2052, 4, "rows"), (889, 4095, 1, "off"), (450, 4097, 5, "rows"), (448, 8191, 2, "rows"), (450, 8201, 0, "rows")]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("T,C,groups", MANY_ROWS)
-def test_norm_many_rows(B, dtype, T, C, groups):
+@pytest.mark.parametrize("T,C,groups,layout", [m + ("rows",) for m in MANY_ROWS] + MANY_ODD)
+def test_norm_many_rows(B, dtype, T, C, groups, layout):
     """Enough rows that each CTA walks several of them; rows that are not a whole number of accesses per thread."""
-    h, b, w_post, gate, w_pre = _norm_inputs(T, C, dtype, "rows", groups, T)
-    n_out, h_out, r2, r1 = torch.empty_like(h), torch.empty_like(h), torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+    h, b, w_post, gate, w_pre = _norm_inputs(T, C, dtype, layout, groups, T)
+    n_out, h_out, r2, r1 = _out(T, C, dtype, layout), _out(T, C, dtype, layout), torch.empty(T, device=DEV), torch.empty(T, device=DEV)
     cks = [B.def_checkpoint_alloc(T, C, DEV) for _ in range(3)]
     B.def_norm_forward(h, b, w_post, gate, w_pre, h_out, n_out, r2, r1, res_scale=0.75, eps=1e-5, b_ck=cks[0], h_ck=cks[1], n_ck=cks[2])
     f = R.norm_forward(h, b, w_post, gate, w_pre, 0.75, 1e-5)
@@ -305,15 +307,15 @@ def test_norm_many_rows(B, dtype, T, C, groups):
     for x, ck in ((b, cks[0]), (h_out, cks[1]), (n_out, cks[2])):
         mine = _checkpoint(B, x)
         assert torch.equal(mine[0][:, :C], ck[0][:, :C]) and torch.equal(mine[1][:, :-(-C // 32)], ck[1][:, :-(-C // 32)])
-    alone, s1 = torch.empty_like(h), torch.empty(T, device=DEV)
+    alone, s1 = _out(T, C, dtype, layout), torch.empty(T, device=DEV)
     B.def_norm_forward(b, None, None, None, w_pre, None, alone, None, s1)
     g = R.norm_forward(b, None, None, None, w_pre, 1.0, 1e-6)
     _close(alone, g["n"], g["n"].abs(), dtype)
-    dn, dh_in = (_normal((T, C), dtype, T + k, std=0.1) for k in (7, 8))
+    dn, dh_in = (_laid(_normal((T, C), dtype, T + k, std=0.1), layout) for k in (7, 8))
     hs, bs = _checkpoint(B, h), _checkpoint(B, b)
     hv, bv = R.read(hs, C).to(DEV), R.read(bs, C).to(DEV)
     r2, r1 = (torch.rsqrt(v.float().square().mean(1) + 1e-5) for v in (b, h))
-    dh, db, dwp, dw = torch.empty_like(h), torch.empty_like(h), torch.empty(C, device=DEV), torch.empty(C, device=DEV)
+    dh, db, dwp, dw = _out(T, C, dtype, layout), _out(T, C, dtype, layout), torch.empty(C, device=DEV), torch.empty(C, device=DEV)
     dg = None if gate is None else torch.empty(groups, C, device=DEV)
     work = torch.empty(B.def_norm_backward_workspace(T, C, max(1, groups)), dtype=torch.uint8, device=DEV)
     for hx, bx, hy, by, into in ((h, b, h, b, dh_in), (hs, bs, hv, bv, None), (h, bs, h, bv, dh_in), (hs, b, hv, b, dh_in)):
@@ -327,6 +329,14 @@ def test_norm_many_rows(B, dtype, T, C, groups):
     want, mag = R.norm_backward(dn, None, hv, None, None, None, w_pre, 1.0, None, r1)
     _close(dh, want["dh"], mag["dh"], dtype, n=128)
     _close(dw, want["dw_pre"], mag["dw_pre"], F32, n=T + 128)
+    if layout == "off":                                                       # nothing beside the rows is written
+        for out in (h_out, n_out, dh, db):
+            whole = torch.as_strided(out, (T * out.stride(0) + 1,), (1,), out.storage_offset() - 1)
+            gap = torch.cat([whole[:1], whole[1:1 + (T - 1) * out.stride(0)].view(T - 1, -1)[:, C:].reshape(-1), whole[1 + (T - 1) * out.stride(0) + C:]])
+            assert bool(torch.isnan(gap).all())
+    inplace_h, inplace_n = _laid(h, layout), _out(T, C, dtype, layout)
+    B.def_norm_forward(inplace_h, b, w_post, gate, w_pre, inplace_h, inplace_n, r2.clone(), s1, res_scale=0.75, eps=1e-5)
+    assert torch.equal(inplace_h, h_out) and torch.equal(inplace_n, n_out)
     first = (dh.clone(), dw.clone())
     B.def_norm_backward(dn, None, hs, None, None, None, w_pre, None, r1, dh, None, None, None, dw, work)
     assert torch.equal(first[0], dh) and torch.equal(first[1], dw)
