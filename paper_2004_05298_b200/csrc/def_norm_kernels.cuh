@@ -22,16 +22,16 @@ struct NormForward {
 };
 
 // One CTA per row; the row stays in registers between its two norms.
-template <typename T, bool ALIGNED, int THREADS, int ITERS>
-__global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward a) {
+template <typename T, bool ALIGNED, int MOST, int ITERS>
+__global__ void __launch_bounds__(MOST) norm_forward_kernel(const NormForward a) {
     __shared__ float scratch[2][32];
-    const int C = (int)a.C;
+    const int C = (int)a.C, threads = (int)blockDim.x;
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
         float h[ITERS][8];
         const T *hr = (const T *)a.h + t * a.ldh;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = (it * threads + (int)threadIdx.x) * 8;
             Frag<T, 8> f = zeros<T, 8>();
             if (col < C) f = load_cols<T, ALIGNED>(hr, col, C);
             to_floats<T, 8>(f, h[it]);
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             const T *br = (const T *)a.b + t * a.ldb;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                const int col = (it * threads + (int)threadIdx.x) * 8;
                 Frag<T, 8> f = zeros<T, 8>();
                 if (col < C) f = load_cols<T, ALIGNED>(br, col, C);
                 to_floats<T, 8>(f, b[it]);
@@ -52,10 +52,10 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             if (a.hb.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    const int col = (it * threads + (int)threadIdx.x) * 8;
                     store_held(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
                 }
-            sum = cta_sum<THREADS>(sum, scratch[0]);
+            sum = cta_sum(sum, scratch[0]);
             const float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
             if (threadIdx.x == 0) a.rstd_post[t] = r;
             const float *gate = a.gate ? a.gate + t / a.rows_per_group * a.C : nullptr;
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             sum = 0.f;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                const int col = (it * threads + (int)threadIdx.x) * 8;
                 float w[8], g[8];
                 load_params(a.w_post, col, C, w);
                 if (gate) {
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             if (a.hh.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    const int col = (it * threads + (int)threadIdx.x) * 8;
                     float x[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));   // h' as stored
@@ -94,17 +94,17 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
             if (a.hh.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    const int col = (it * threads + (int)threadIdx.x) * 8;
                     store_held(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, h[it]);
                 }
         }
-        sum = cta_sum<THREADS>(sum, scratch[1]);
+        sum = cta_sum(sum, scratch[1]);
         const float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
         if (threadIdx.x == 0) a.rstd_pre[t] = r;
         T *no = (T *)a.n_out + t * a.ldn;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = (it * threads + (int)threadIdx.x) * 8;
             float n[8], w[8];
             load_params(a.w_pre, col, C, w);
 #pragma unroll
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormForward
                 store_held(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, n);
             }
         }
-        if (THREADS > 32 && !a.b) __syncthreads();   // one sum per row: scratch[1] is rewritten by the next
+        if (!a.b) __syncthreads();   // one sum per row: scratch[1] is rewritten by the next
     }
 }
 
@@ -133,10 +133,10 @@ struct NormBackward {
 };
 
 // Part p = (group, slice of the group's rows): one CTA walks the slice, the column sums stay in registers.
-template <typename T, bool ALIGNED, int THREADS, int ITERS>
-__global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackward a) {
+template <typename T, bool ALIGNED, int MOST, int ITERS>
+__global__ void __launch_bounds__(MOST) norm_backward_kernel(const NormBackward a) {
     __shared__ float scratch[2][32];
-    const int C = (int)a.C;
+    const int C = (int)a.C, threads = (int)blockDim.x;
     const int64_t group = blockIdx.x / a.parts_per_group, slice = blockIdx.x % a.parts_per_group;
     const int64_t first = group * a.rows_per_group + a.rows_per_group * slice / a.parts_per_group;
     const int64_t last = group * a.rows_per_group + a.rows_per_group * (slice + 1) / a.parts_per_group;
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
         const float r = a.rstd_pre[t], rp = has_b ? a.rstd_post[t] : 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = (it * threads + (int)threadIdx.x) * 8;
             if (col < C) {
                 fn[it] = load_cols<T, ALIGNED>((const T *)a.dn + t * a.lddn, col, C);
                 if (a.hh.q) {
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
         float dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = (it * threads + (int)threadIdx.x) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) D[it][i] = x[it][i] = 0.f;
             if (col < C) {
@@ -194,11 +194,11 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
                 }
             }
         }
-        dot = cta_sum<THREADS>(dot, scratch[0]) * a.inv_C;
+        dot = cta_sum(dot, scratch[0]) * a.inv_C;
         float dot_b = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = (it * threads + (int)threadIdx.x) * 8;
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = 0.f;
@@ -229,23 +229,23 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormBackwa
             }
         }
         if (has_b) {
-            dot_b = cta_sum<THREADS>(dot_b, scratch[1]) * a.inv_C;
+            dot_b = cta_sum(dot_b, scratch[1]) * a.inv_C;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                const int col = (it * threads + (int)threadIdx.x) * 8;
                 float out[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) out[i] = rp * fmaf(-x[it][i], dot_b, D[it][i]);
                 store_cols<T, ALIGNED>((T *)a.db + t * a.lddb, col, C, out);
             }
-        } else if constexpr (THREADS > 32) {
+        } else {
             __syncthreads();                         // scratch[0] is rewritten by the next row
         }
     }
     float *px = a.partial + (int64_t)blockIdx.x * 2 * a.C;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int col = (it * THREADS + (int)threadIdx.x) * 8;
+        const int col = (it * threads + (int)threadIdx.x) * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (col + i < C) {
@@ -300,10 +300,11 @@ template <typename T, bool ALIGNED> struct RowCopy {
             if (to > end) to = end & ~(uintptr_t)15;
         }
     }
-    __device__ uint32_t bytes() const { return to > from ? (uint32_t)(to - from) : 0; }
+    __device__ uint32_t bytes() const { return ALIGNED ? C * (uint32_t)sizeof(T) : to > from ? (uint32_t)(to - from) : 0; }
     __device__ uint32_t offset() const { return ALIGNED ? 0 : (uint32_t)((uintptr_t)p & 15); }   // of the row in its slot
     __device__ void copy(uint32_t slot, uint32_t bar) const {
-        if (bytes()) run_load(slot + (uint32_t)(from - ((uintptr_t)p & ~(uintptr_t)15)), (const void *)from, bytes(), bar);
+        if constexpr (ALIGNED) run_load(slot, p, bytes(), bar);
+        else if (bytes()) run_load(slot + (uint32_t)(from - ((uintptr_t)p & ~(uintptr_t)15)), (const void *)from, bytes(), bar);
     }
     __device__ bool whole() const { return ALIGNED || (from <= (uintptr_t)p && to >= (uintptr_t)(p + C)); }
     // The elements that copy() left out, fewer than 16 bytes at either end; by the first threads of the CTA.
@@ -358,14 +359,14 @@ struct Slice {
 };
 
 // MINB: CTAs per SM that the registers are meant for.
-template <typename T, bool ALIGNED, int THREADS, int ITERS, int MINB>
-__global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(const NormForward a, const int stages) {
+template <typename T, bool ALIGNED, int MOST, int ITERS, int MINB>
+__global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const NormForward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
     __shared__ float scratch[2][32];
     __shared__ uint64_t full[kMaxStages];
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
-    const int C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
+    const int threads = (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
     float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
     uint8_t *ring = dynamic + (a.b ? 8 : 4) * Cp;
     const Slice slice(a.rows_per_group, a.parts_per_group);
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
     }
-    for (int i = threadIdx.x; i < Cp; i += THREADS) {
+    for (int i = threadIdx.x; i < Cp; i += threads) {
         const int at = param_place(i, Cp);
         w_pre[at] = i < C ? a.w_pre[i] : 0.f;
         if (a.b) w_post[at] = i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
@@ -403,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
         float sum = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = (it * threads + (int)threadIdx.x) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[it][i] = b[it][i] = 0.f;
             if (col < C) {
@@ -416,7 +417,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
                 sum = fmaf(x, x, sum);
             }
         }
-        sum = cta_sum<THREADS>(sum, scratch[0]);
+        sum = cta_sum(sum, scratch[0]);
         if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);       // every thread has read the stage
         float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
         if (!ok) r = NAN;                                             // the wait ran out: no numbers rather than wrong ones
@@ -425,13 +426,13 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
             if (a.hb.q)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
-                    const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                    const int col = (it * threads + (int)threadIdx.x) * 8;
                     store_held(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
                 }
             sum = 0.f;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                const int col = (it * threads + (int)threadIdx.x) * 8;
                 if (col < C) {
                     float w[8];
                     shared_params(w_post, col, Cp, w);
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
             }
-            sum = cta_sum<THREADS>(sum, scratch[1]);
+            sum = cta_sum(sum, scratch[1]);
             r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
         } else {
             __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
         if (a.hh.q)
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
-                const int col = (it * THREADS + (int)threadIdx.x) * 8;
+                const int col = (it * threads + (int)threadIdx.x) * 8;
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));       // h' as stored
@@ -459,7 +460,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_forward_stream_kernel(cons
             }
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = (it * THREADS + (int)threadIdx.x) * 8;
+            const int col = (it * threads + (int)threadIdx.x) * 8;
             if (col < C) {
                 float w[8];
                 shared_params(w_pre, col, Cp, w);
@@ -512,8 +513,8 @@ template <bool NOTHING> __device__ __forceinline__ void clear_past(float (&x)[8]
 // of a checkpoint's group and the row's statistic, both factors, are multiplied first, and what the second half of a row
 // needs stays in shared memory until then (two registers too many cost 20 us in spills that miss the L1).  HELD: h' and b
 // are checkpoints (else both are values).
-template <typename T, bool ALIGNED, int THREADS, int ITERS, int MINB, bool HELD>
-__global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(const NormBackward a, const int stages) {
+template <typename T, bool ALIGNED, int MOST, int ITERS, int MINB, bool HELD>
+__global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const NormBackward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
     __shared__ float scratch[2][32];
     __shared__ uint64_t full[kMaxStages];
@@ -521,7 +522,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
     volatile int *failed = &failed_flag;
     const bool has_b = HELD ? a.hb.q != nullptr : a.b != nullptr;
     const bool ring_e = a.lde % 16 == 0;                             // exponents come with the ring where their rows can
-    const int C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
+    const int threads = (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
     const int saved_bytes = HELD ? held_bytes : row_bytes;
     const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + saved_bytes, stage_bytes = at_b + (has_b ? saved_bytes : 0);
     float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
@@ -552,7 +553,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int s = 0; s < stages && slice.first + s < slice.last; ++s) fetch(slice.first + s, s);
     }
-    for (int i = threadIdx.x; i < Cp; i += THREADS) {
+    for (int i = threadIdx.x; i < Cp; i += threads) {
         const int at = param_place(i, Cp);
         w_pre[at] = i < C ? a.w_pre[i] : 0.f;
         if (has_b) w_post[at] = i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
@@ -601,7 +602,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
         float dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = it * THREADS * 8 + col0;
+            const int col = it * threads * 8 + col0;
             if (col < C) {
                 float w[8];
                 to_floats<T, 8>(slot_run<T, ALIGNED>(row, copy_n.offset(), col, C), D[it]);
@@ -620,11 +621,11 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
             next_r = *++stat;
             next_rp = *++stat_b;
         }
-        const float minus_dot = -cta_sum<THREADS>(dot, scratch[0]) * a.inv_C;
+        const float minus_dot = -cta_sum(dot, scratch[0]) * a.inv_C;
         dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int col = it * THREADS * 8 + col0;
+            const int col = it * threads * 8 + col0;
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = 0.f;
@@ -651,13 +652,13 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
         }
         out_h += a.lddh;
         if (has_b) {
-            const float minus_dot_b = -cta_sum<THREADS>(dot, scratch[1]) * a.inv_C;
+            const float minus_dot_b = -cta_sum(dot, scratch[1]) * a.inv_C;
             if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);   // every thread has read the stage
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) D[it][i] = rp * fmaf(x[it][i], minus_dot_b, D[it][i]);
-                store_cols<T, ALIGNED>(out_b, it * THREADS * 8 + col0, C, D[it]);
+                store_cols<T, ALIGNED>(out_b, it * threads * 8 + col0, C, D[it]);
             }
             out_b += a.lddb;
         } else {
@@ -672,7 +673,7 @@ __global__ void __launch_bounds__(THREADS, MINB) norm_backward_stream_kernel(con
     float *px = a.partial + (int64_t)blockIdx.x * 2 * C;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int col = it * THREADS * 8 + col0;
+        const int col = it * threads * 8 + col0;
         if (ALIGNED && col < C) {
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {

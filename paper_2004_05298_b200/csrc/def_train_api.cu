@@ -256,26 +256,32 @@ extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const voi
 // ---------------------------------------------------------------------------
 namespace {
 
-template <int THREADS, int ITERS> struct Shape { static constexpr int threads = THREADS, iters = ITERS; };
-template <int THREADS, int ITERS, int MINB> struct StreamShape { static constexpr int threads = THREADS, iters = ITERS, min_ctas = MINB; };
-// Threads per row and runs of 8 columns per thread for rows of C columns.
+// Most threads per CTA that a kernel is compiled for, runs of 8 columns per thread, CTAs per SM that its registers are for.
+template <int MOST, int ITERS, int MINB = 1> struct Shape {
+    static constexpr int most = MOST, iters = ITERS, min_ctas = MINB;
+    // as few threads as cover the row
+    static int threads(int64_t C) { return (int)(ceil_div(ceil_div(C, 8 * ITERS), 32) * 32); }
+};
 template <typename F> void by_row_shape(int64_t C, F f) {
     const int64_t n = ceil_div(C, 8);
-    if (n <= 32) f(Shape<32, 1>());
-    else if (n <= 128) f(Shape<128, 1>());
-    else if (n <= 256) f(Shape<256, 1>());
+    if (n <= 256) f(Shape<256, 1>());
     else if (n <= 512) f(Shape<256, 2>());
     else if (n <= 1024) f(Shape<512, 2>());
     else f(Shape<1024, 2>());
 }
-// The same for the stream kernels, with the CTAs per SM that their registers are meant for.
 template <typename F> void by_stream_shape(int64_t C, F f) {
     const int64_t n = ceil_div(C, 8);
-    if (n <= 128) f(StreamShape<128, 1, 6>());
-    else if (n <= 256) f(StreamShape<128, 2, 4>());
-    else if (n <= 512) f(StreamShape<256, 2, 2>());
-    else if (n <= 1024) f(StreamShape<512, 2, 1>());
-    else f(StreamShape<1024, 2, 1>());
+    if (n <= 128) f(Shape<128, 1, 6>());
+    else if (n <= 256) f(Shape<128, 2, 4>());
+    else if (n <= 512) f(Shape<256, 2, 2>());
+    else if (n <= 576) f(Shape<288, 2, 2>());
+    else if (n <= 1024) f(Shape<512, 2, 1>());
+    else f(Shape<1024, 2, 1>());
+}
+// CTAs of a stream kernel per SM: as many of `threads` as the registers of min_ctas full ones hold, 13 at most.
+template <typename S> int stream_ctas(int threads) {
+    const int n = S::min_ctas * S::most / threads;
+    return n < 13 ? n : 13;
 }
 // Stages of a stream kernel's ring: as many as fit beside the parameters with `ctas` on an SM (below 2: not for it).
 int stream_stages(int64_t params, int64_t stage, int ctas) {
@@ -290,7 +296,7 @@ int check_groups(int64_t T, int64_t groups) {
 
 // Slices per group that rows are cut into (each: one CTA, and in the backward pass one row of partial sums): about `want`
 // in all, at most one per row.
-constexpr int64_t kNormParts = 8 * kUsualSms;     // the most in all, which the workspace is sized for
+constexpr int64_t kNormParts = 13 * kUsualSms;    // the most in all, which the workspace is sized for
 int64_t norm_parts(int64_t T, int64_t groups, int64_t want) {
     const int64_t rows = T / groups, each = ceil_div(want, groups);
     return rows < each ? rows : each;
@@ -343,8 +349,9 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
     const int64_t slot = aligned_rows ? C * es : ceil_div(C * es, 32) * 32 + 16, padded = ceil_div(C, 8) * 8;
     by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
-            const int64_t params = (b ? 8 : 4) * padded, stage = (b ? 2 : 1) * slot, want = S::min_ctas * kUsualSms;
-            const int stages = stream_stages(params, stage, S::min_ctas);
+            const int64_t params = (b ? 8 : 4) * padded, stage = (b ? 2 : 1) * slot;
+            const int threads = S::threads(C), ctas = stream_ctas<S>(threads), stages = stream_stages(params, stage, ctas);
+            const int64_t want = (int64_t)ctas * kUsualSms;
             if (stages < 2 || T < want * kStreamRows) return;
             streamed = true;
             a.parts_per_group = norm_parts(T, groups, want);
@@ -352,10 +359,10 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
             const int smem = (int)(params + stages * stage);
             by_dtype(dtype, [&](auto type) {
                 using E = decltype(type);
-                const auto kernel = aligned_rows ? deft::norm_forward_stream_kernel<E, true, S::threads, S::iters, S::min_ctas>
-                                                 : deft::norm_forward_stream_kernel<E, false, S::threads, S::iters, S::min_ctas>;
+                const auto kernel = aligned_rows ? deft::norm_forward_stream_kernel<E, true, S::most, S::iters, S::min_ctas>
+                                                 : deft::norm_forward_stream_kernel<E, false, S::most, S::iters, S::min_ctas>;
                 if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
-                kernel<<<grid, S::threads, smem, (cudaStream_t)cuda_stream>>>(a, stages);
+                kernel<<<grid, threads, smem, (cudaStream_t)cuda_stream>>>(a, stages);
             });
         });
     if (err != cudaSuccess) return cuda_fail(err, "def_norm_forward");
@@ -365,7 +372,7 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
             by_row_shape(C, [&](auto shape) {
                 using S = decltype(shape);
                 const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
-                deft::norm_forward_kernel<decltype(type), aligned.value, S::threads, S::iters><<<grid, S::threads, 0, (cudaStream_t)cuda_stream>>>(a);
+                deft::norm_forward_kernel<decltype(type), aligned.value, S::most, S::iters><<<grid, S::threads(C), 0, (cudaStream_t)cuda_stream>>>(a);
             });
         });
     });
@@ -443,10 +450,11 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     const int64_t slot = aligned_rows ? C * es : ceil_div(C * es, 32) * 32 + 16, padded = ceil_div(C, 8) * 8;
     by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
-            const int64_t params = (has_b ? 8 : 4) * padded, want = S::min_ctas * kUsualSms;
+            const int64_t params = (has_b ? 8 : 4) * padded;
             const int64_t held = q_stride(C) + (e_stride(C) % 16 == 0 ? e_stride(C) : 0);
             const int64_t stage = slot * (dh_in ? 2 : 1) + (h_q ? held : slot) + (!has_b ? 0 : b_q ? held : slot);
-            const int stages = stream_stages(params, stage, S::min_ctas);
+            const int threads = S::threads(C), ctas = stream_ctas<S>(threads), stages = stream_stages(params, stage, ctas);
+            const int64_t want = (int64_t)ctas * kUsualSms;
             if (stages < 2 || T < want * kStreamRows || (has_b && !h_q != !b_q)) return;
             streamed = true;
             a.parts_per_group = norm_parts(T, groups, want);
@@ -454,12 +462,12 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
             by_dtype(dtype, [&](auto type) {
                 using E = decltype(type);
                 const auto pick = [&](auto aligned) {
-                    return h_q ? deft::norm_backward_stream_kernel<E, aligned.value, S::threads, S::iters, S::min_ctas, true>
-                               : deft::norm_backward_stream_kernel<E, aligned.value, S::threads, S::iters, S::min_ctas, false>;
+                    return h_q ? deft::norm_backward_stream_kernel<E, aligned.value, S::most, S::iters, S::min_ctas, true>
+                               : deft::norm_backward_stream_kernel<E, aligned.value, S::most, S::iters, S::min_ctas, false>;
                 };
                 const auto kernel = aligned_rows ? pick(Is<true>()) : pick(Is<false>());
                 if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
-                kernel<<<(unsigned)(groups * a.parts_per_group), S::threads, smem, stream>>>(a, stages);
+                kernel<<<(unsigned)(groups * a.parts_per_group), threads, smem, stream>>>(a, stages);
             });
         });
     if (err != cudaSuccess) return cuda_fail(err, "def_norm_backward");
@@ -468,8 +476,8 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
             by_alignment(aligned_rows, [&](auto aligned) {
                 by_row_shape(C, [&](auto shape) {
                     using S = decltype(shape);
-                    a.parts_per_group = norm_parts(T, groups, S::threads <= 128 ? kNormParts / 2 : S::threads <= 256 ? kNormParts / 4 : kNormParts / 8);
-                    deft::norm_backward_kernel<decltype(type), aligned.value, S::threads, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads, 0, stream>>>(a);
+                    a.parts_per_group = norm_parts(T, groups, S::threads(C) <= 128 ? 4 * kUsualSms : S::threads(C) <= 256 ? 2 * kUsualSms : kUsualSms);
+                    deft::norm_backward_kernel<decltype(type), aligned.value, S::most, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads(C), 0, stream>>>(a);
                 });
             });
         });

@@ -145,12 +145,13 @@ template <typename T> __device__ __forceinline__ void store_run(T *row, int col,
 #pragma unroll
         for (int i = 0; i < kWords / 4; ++i) q[i] = make_uint4(out[4 * i], out[4 * i + 1], out[4 * i + 2], out[4 * i + 3]);
     }
-    const int from = own ? 8 - before : 0, to = next || off == 0 && own ? 8 - before : 8;
-    if (from < to) {
+    // by element: the run's beginning where this lane's words are not written, its end where the neighbour's are not
+    const int from = own ? 8 - before : 0, to = next || (off == 0 && own) ? 8 - before : 8;
+    const int exist = C - col < 8 ? C - col : 8;
+    const uint32_t mask = exist > 0 ? ((1u << to) - 1u) & ~((1u << from) - 1u) & ((1u << exist) - 1u) : 0u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i >= from && i < to && col + i < C) p[i] = f.v[i];
-    }
+    for (int i = 0; i < 8; ++i)
+        if (mask >> i & 1u) p[i] = f.v[i];
 }
 // Columns [col, col + 8) of a row: whole words where rows are ALIGNED (C is then a multiple of 8), as above elsewhere.
 template <typename T, bool ALIGNED> __device__ __forceinline__ Frag<T, 8> load_cols(const T *row, int col, int C) {
@@ -313,16 +314,13 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int s = 16; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
     return v;
 }
-template <int THREADS> __device__ __forceinline__ float cta_sum(float v, float *scratch) {
+__device__ __forceinline__ float cta_sum(float v, float *scratch) {
+    const int warps = (int)blockDim.x >> 5, lane = threadIdx.x & 31;
     v = warp_sum(v);
-    if constexpr (THREADS == 32) return v;
-    constexpr int kWarps = THREADS / 32;
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    if (warps == 1) return v;
+    if (lane == 0) scratch[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = (threadIdx.x & 31) < kWarps ? scratch[threadIdx.x & 31] : 0.f;
-#pragma unroll
-    for (int s = kWarps / 2; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
-    return kWarps == 32 ? v : __shfl_sync(0xffffffffu, v, 0);
+    return warp_sum(lane < warps ? scratch[lane] : 0.f);
 }
 
 }  // namespace deft
