@@ -358,7 +358,8 @@ struct Slice {
     }
 };
 
-// MINB: CTAs per SM that the registers are meant for.
+// MOST: the threads of the CTA (where rows are not ALIGNED: at most; as few as cover a row).  MINB: CTAs per SM that the
+// registers are meant for.
 template <typename T, bool ALIGNED, int MOST, int ITERS, int MINB>
 __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const NormForward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
@@ -366,7 +367,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
     __shared__ uint64_t full[kMaxStages];
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
-    const int threads = (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
+    const int threads = ALIGNED ? MOST : (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
     float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
     uint8_t *ring = dynamic + (a.b ? 8 : 4) * Cp;
     const Slice slice(a.rows_per_group, a.parts_per_group);
@@ -417,7 +418,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
                 sum = fmaf(x, x, sum);
             }
         }
-        sum = cta_sum(sum, scratch[0]);
+        sum = cta_sum<ALIGNED ? MOST : 0>(sum, scratch[0]);
         if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);       // every thread has read the stage
         float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
         if (!ok) r = NAN;                                             // the wait ran out: no numbers rather than wrong ones
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
             }
-            sum = cta_sum(sum, scratch[1]);
+            sum = cta_sum<ALIGNED ? MOST : 0>(sum, scratch[1]);
             r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
         } else {
             __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
     volatile int *failed = &failed_flag;
     const bool has_b = HELD ? a.hb.q != nullptr : a.b != nullptr;
     const bool ring_e = a.lde % 16 == 0;                             // exponents come with the ring where their rows can
-    const int threads = (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
+    const int threads = ALIGNED ? MOST : (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
     const int saved_bytes = HELD ? held_bytes : row_bytes;
     const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + saved_bytes, stage_bytes = at_b + (has_b ? saved_bytes : 0);
     float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
@@ -621,7 +622,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
             next_r = *++stat;
             next_rp = *++stat_b;
         }
-        const float minus_dot = -cta_sum(dot, scratch[0]) * a.inv_C;
+        const float minus_dot = -cta_sum<ALIGNED ? MOST : 0>(dot, scratch[0]) * a.inv_C;
         dot = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
@@ -652,7 +653,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
         }
         out_h += a.lddh;
         if (has_b) {
-            const float minus_dot_b = -cta_sum(dot, scratch[1]) * a.inv_C;
+            const float minus_dot_b = -cta_sum<ALIGNED ? MOST : 0>(dot, scratch[1]) * a.inv_C;
             if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);   // every thread has read the stage
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {

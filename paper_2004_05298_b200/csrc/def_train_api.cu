@@ -257,11 +257,12 @@ extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const voi
 namespace {
 
 // Most threads per CTA that a kernel is compiled for, runs of 8 columns per thread, CTAs per SM that its registers are for.
-template <int MOST, int ITERS, int MINB = 1> struct Shape {
-    static constexpr int most = MOST, iters = ITERS, min_ctas = MINB;
+template <int MOST, int ITERS> struct Shape {
+    static constexpr int most = MOST, iters = ITERS;
     // as few threads as cover the row
     static int threads(int64_t C) { return (int)(ceil_div(ceil_div(C, 8 * ITERS), 32) * 32); }
 };
+template <int MOST, int ITERS, int MINB> struct StreamShape : Shape<MOST, ITERS> { static constexpr int min_ctas = MINB; };
 template <typename F> void by_row_shape(int64_t C, F f) {
     const int64_t n = ceil_div(C, 8);
     if (n <= 256) f(Shape<256, 1>());
@@ -271,12 +272,12 @@ template <typename F> void by_row_shape(int64_t C, F f) {
 }
 template <typename F> void by_stream_shape(int64_t C, F f) {
     const int64_t n = ceil_div(C, 8);
-    if (n <= 128) f(Shape<128, 1, 6>());
-    else if (n <= 256) f(Shape<128, 2, 4>());
-    else if (n <= 512) f(Shape<256, 2, 2>());
-    else if (n <= 576) f(Shape<288, 2, 2>());
-    else if (n <= 1024) f(Shape<512, 2, 1>());
-    else f(Shape<1024, 2, 1>());
+    if (n <= 128) f(StreamShape<128, 1, 6>());
+    else if (n <= 256) f(StreamShape<128, 2, 4>());
+    else if (n <= 512) f(StreamShape<256, 2, 2>());
+    else if (n <= 576) f(StreamShape<288, 2, 2>());
+    else if (n <= 1024) f(StreamShape<512, 2, 1>());
+    else f(StreamShape<1024, 2, 1>());
 }
 // CTAs of a stream kernel per SM: as many of `threads` as the registers of min_ctas full ones hold, 13 at most.
 template <typename S> int stream_ctas(int threads) {
@@ -350,7 +351,7 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
     by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
             const int64_t params = (b ? 8 : 4) * padded, stage = (b ? 2 : 1) * slot;
-            const int threads = S::threads(C), ctas = stream_ctas<S>(threads), stages = stream_stages(params, stage, ctas);
+            const int threads = aligned_rows ? S::most : S::threads(C), ctas = stream_ctas<S>(threads), stages = stream_stages(params, stage, ctas);
             const int64_t want = (int64_t)ctas * kUsualSms;
             if (stages < 2 || T < want * kStreamRows) return;
             streamed = true;
@@ -453,7 +454,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
             const int64_t params = (has_b ? 8 : 4) * padded;
             const int64_t held = q_stride(C) + (e_stride(C) % 16 == 0 ? e_stride(C) : 0);
             const int64_t stage = slot * (dh_in ? 2 : 1) + (h_q ? held : slot) + (!has_b ? 0 : b_q ? held : slot);
-            const int threads = S::threads(C), ctas = stream_ctas<S>(threads), stages = stream_stages(params, stage, ctas);
+            const int threads = aligned_rows ? S::most : S::threads(C), ctas = stream_ctas<S>(threads), stages = stream_stages(params, stage, ctas);
             const int64_t want = (int64_t)ctas * kUsualSms;
             if (stages < 2 || T < want * kStreamRows || (has_b && !h_q != !b_q)) return;
             streamed = true;

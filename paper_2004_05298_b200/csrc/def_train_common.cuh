@@ -314,13 +314,21 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int s = 16; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
     return v;
 }
-__device__ __forceinline__ float cta_sum(float v, float *scratch) {
-    const int warps = (int)blockDim.x >> 5, lane = threadIdx.x & 31;
+// THREADS: those of the CTA, or 0 where only the launch knows.
+template <int THREADS = 0> __device__ __forceinline__ float cta_sum(float v, float *scratch) {
+    const int warps = (THREADS ? THREADS : (int)blockDim.x) >> 5, lane = threadIdx.x & 31;
     v = warp_sum(v);
     if (warps == 1) return v;
     if (lane == 0) scratch[threadIdx.x >> 5] = v;
     __syncthreads();
-    return warp_sum(lane < warps ? scratch[lane] : 0.f);
+    v = lane < warps ? scratch[lane] : 0.f;
+    if constexpr (THREADS == 0 || THREADS == 1024 || (THREADS & (THREADS - 1)) != 0) {
+        return warp_sum(v);
+    } else {
+#pragma unroll
+        for (int s = THREADS / 64; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
+        return __shfl_sync(0xffffffffu, v, 0);
+    }
 }
 
 }  // namespace deft
