@@ -319,6 +319,16 @@ template <typename T, bool ALIGNED> struct RowCopy {
         fence_async_shared();            // the slot's next copy comes after these stores
     }
 };
+// Where a row starts in its slot.
+template <typename T, bool ALIGNED> __device__ __forceinline__ uint32_t row_offset(const void *base, int64_t ld, int64_t t) {
+    return ALIGNED ? 0 : ((uint32_t)(uintptr_t)base + (uint32_t)t * (uint32_t)(ld * (int64_t)sizeof(T))) & 15u;
+}
+// Whether row t of tensors with these bases and strides in bytes may need patch(): only rows that lie within 16 bytes of
+// an end of the tensor do.
+__device__ __forceinline__ bool near_end(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int64_t t, int64_t rows) {
+    const int64_t least = t < rows - 1 - t ? t : rows - 1 - t;
+    return (a && least * a_stride < 16) || (b && least * b_stride < 16);
+}
 // Bytes of a row's slot.
 template <typename T, bool ALIGNED> __host__ __device__ __forceinline__ int slot_bytes(int C) {
     return ALIGNED ? C * (int)sizeof(T) : (C * (int)sizeof(T) + 31) / 32 * 32 + 16;
@@ -364,6 +374,7 @@ template <typename T, bool ALIGNED, int MOST, int ITERS, int MINB>
 __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const NormForward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
     __shared__ float scratch[2][32];
+    __shared__ uint4 ends[2][ALIGNED ? 1 : ITERS * 32];
     __shared__ uint64_t full[kMaxStages];
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
@@ -395,10 +406,10 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
     for (int64_t t = slice.first; t < slice.last; ++t) {
         const bool ok = barrier_wait(smem_address(&full[s]), parity, failed);
         uint8_t *row = ring + s * stage_bytes;
-        const RowCopy<T, ALIGNED> copy_h(a.h, a.ldh, t, a.T, C), copy_b(a.b, a.ldb, t, a.T, C);
-        if (!copy_h.whole() || (a.b && !copy_b.whole())) {
-            copy_h.patch(row);
-            if (a.b) copy_b.patch(row + row_bytes);
+        const uint32_t off_h = row_offset<T, ALIGNED>(a.h, a.ldh, t), off_b = row_offset<T, ALIGNED>(a.b, a.ldb, t);
+        if (!ALIGNED && near_end(a.h, a.ldh * (int)sizeof(T), a.b, a.ldb * (int)sizeof(T), t, a.T)) {
+            RowCopy<T, ALIGNED>(a.h, a.ldh, t, a.T, C).patch(row);
+            if (a.b) RowCopy<T, ALIGNED>(a.b, a.ldb, t, a.T, C).patch(row + row_bytes);
             __syncthreads();
         }
         float h[ITERS][8], b[ITERS][8];
@@ -409,8 +420,8 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[it][i] = b[it][i] = 0.f;
             if (col < C) {
-                to_floats<T, 8>(slot_run<T, ALIGNED>(row, copy_h.offset(), col, C), h[it]);
-                if (a.b) to_floats<T, 8>(slot_run<T, ALIGNED>(row + row_bytes, copy_b.offset(), col, C), b[it]);
+                to_floats<T, 8>(slot_run<T, ALIGNED>(row, off_h, col, C), h[it]);
+                if (a.b) to_floats<T, 8>(slot_run<T, ALIGNED>(row + row_bytes, off_b, col, C), b[it]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -440,10 +451,11 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[it][i] = fmaf(b[it][i] * r, w[i], a.res_scale * h[it][i]);
                 }
-                store_cols<T, ALIGNED>((T *)a.h_out + t * a.ldho, col, C, h[it]);
+                if (ALIGNED && col < C) store_floats<T, 8>((T *)a.h_out + t * a.ldho + col, h[it]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
             }
+            if constexpr (!ALIGNED) store_row<T, ITERS>((T *)a.h_out + t * a.ldho, threads, C, h, ends[0]);
             sum = cta_sum<ALIGNED ? MOST : 0>(sum, scratch[1]);
             r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
         } else {
@@ -468,13 +480,15 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[it][i] = h[it][i] * r * w[i];
             }
-            store_cols<T, ALIGNED>((T *)a.n_out + t * a.ldn, col, C, h[it]);
+            if (ALIGNED && col < C) store_floats<T, 8>((T *)a.n_out + t * a.ldn + col, h[it]);
             if (a.hn.q) {
+                float x[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[it][i] = to_float<T>(from_float<T>(h[it][i]));   // n as stored
-                store_held(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, h[it]);
+                for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));       // n as stored
+                store_held(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, x);
             }
         }
+        if constexpr (!ALIGNED) store_row<T, ITERS>((T *)a.n_out + t * a.ldn, threads, C, h, ends[1]);
         if (++s == stages) {
             s = 0;
             parity ^= 1;
@@ -518,6 +532,7 @@ template <typename T, bool ALIGNED, int MOST, int ITERS, int MINB, bool HELD>
 __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const NormBackward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];
     __shared__ float scratch[2][32];
+    __shared__ uint4 ends[2][ALIGNED ? 1 : ITERS * 32];
     __shared__ uint64_t full[kMaxStages];
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
@@ -579,22 +594,24 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
     for (int64_t t = slice.first; t < slice.last; ++t) {
         const bool ok = barrier_wait(smem_address(&full[s]), parity, failed);
         uint8_t *row = ring + s * stage_bytes;
-        const Copy copy_n(a.dn, a.lddn, t, a.T, C), copy_in(a.dh_in, a.lddhi, t, a.T, C), copy_h(a.h, a.ldh, t, a.T, C), copy_b(a.b, a.ldb, t, a.T, C);
-        if (!copy_n.whole() || (a.dh_in && !copy_in.whole()) || (!HELD && (!copy_h.whole() || (has_b && !copy_b.whole())))) {
-            copy_n.patch(row);
-            if (a.dh_in) copy_in.patch(row + at_in);
-            if (!HELD) copy_h.patch(row + at_h);
-            if (!HELD && has_b) copy_b.patch(row + at_b);
+        const uint32_t off_n = row_offset<T, ALIGNED>(a.dn, a.lddn, t), off_in = row_offset<T, ALIGNED>(a.dh_in, a.lddhi, t),
+                       off_h = row_offset<T, ALIGNED>(a.h, a.ldh, t), off_b = row_offset<T, ALIGNED>(a.b, a.ldb, t);
+        if (!ALIGNED && (near_end(a.dn, a.lddn * (int)sizeof(T), a.dh_in, a.lddhi * (int)sizeof(T), t, a.T) ||
+                         near_end(a.h, a.ldh * (int)sizeof(T), a.b, a.ldb * (int)sizeof(T), t, a.T))) {
+            Copy(a.dn, a.lddn, t, a.T, C).patch(row);
+            if (a.dh_in) Copy(a.dh_in, a.lddhi, t, a.T, C).patch(row + at_in);
+            if (!HELD) Copy(a.h, a.ldh, t, a.T, C).patch(row + at_h);
+            if (!HELD && has_b) Copy(a.b, a.ldb, t, a.T, C).patch(row + at_b);
             __syncthreads();
         }
         const float r = ok ? next_r : NAN, rp = next_rp;
-        auto saved = [&](int place, const Copy &copy, const HeldIn &held, int col, float factor) {
+        auto saved = [&](int place, uint32_t off, const HeldIn &held, int col, float factor) {
             Saved<T, HELD> v;
             if constexpr (HELD) {
                 v.q = *reinterpret_cast<const uint2 *>(row + place + col);
                 factor *= group_scale(ring_e ? row[place + (int)a.ldq + col / kGroup] : held.e[t * a.lde + col / kGroup]);
             } else {
-                v.f = slot_run<T, ALIGNED>(row + place, copy.offset(), col, C);
+                v.f = slot_run<T, ALIGNED>(row + place, off, col, C);
             }
             v.factor = factor;
             return v;
@@ -606,8 +623,8 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
             const int col = it * threads * 8 + col0;
             if (col < C) {
                 float w[8];
-                to_floats<T, 8>(slot_run<T, ALIGNED>(row, copy_n.offset(), col, C), D[it]);
-                saved(at_h, copy_h, a.hh, col, r).values(x[it]);
+                to_floats<T, 8>(slot_run<T, ALIGNED>(row, off_n, col, C), D[it]);
+                saved(at_h, off_h, a.hh, col, r).values(x[it]);
                 clear_past<ALIGNED || !HELD>(x[it], col, C);
                 shared_params(w_pre, col, Cp, w);
 #pragma unroll
@@ -624,6 +641,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
         }
         const float minus_dot = -cta_sum<ALIGNED ? MOST : 0>(dot, scratch[0]) * a.inv_C;
         dot = 0.f;
+        float first_half[ALIGNED ? 1 : ITERS][8];                     // dh, to be stored by the CTA together
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
             const int col = it * threads * 8 + col0;
@@ -631,16 +649,20 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = 0.f;
             if (col < C) {
-                if (a.dh_in) to_floats<T, 8>(slot_run<T, ALIGNED>(row + at_in, copy_in.offset(), col, C), v);
+                if (a.dh_in) to_floats<T, 8>(slot_run<T, ALIGNED>(row + at_in, off_in, col, C), v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     D[it][i] = fmaf(r, fmaf(x[it][i], minus_dot, D[it][i]), v[i]);
                     v[i] = a.res_scale * D[it][i];
                 }
+                if (ALIGNED) store_floats<T, 8>(out_h + col, v);
             }
-            store_cols<T, ALIGNED>(out_h, col, C, v);
+            if constexpr (!ALIGNED) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) first_half[it][i] = v[i];
+            }
             if (has_b && col < C) {
-                saved(at_b, copy_b, a.hb, col, rp).values(x[it]);
+                saved(at_b, off_b, a.hb, col, rp).values(x[it]);
                 clear_past<ALIGNED || !HELD>(x[it], col, C);
                 shared_params(w_post, col, Cp, v);
 #pragma unroll
@@ -651,6 +673,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
                 }
             }
         }
+        if constexpr (!ALIGNED) store_row<T, ITERS>(out_h, threads, C, first_half, ends[0]);
         out_h += a.lddh;
         if (has_b) {
             const float minus_dot_b = -cta_sum<ALIGNED ? MOST : 0>(dot, scratch[1]) * a.inv_C;
@@ -659,8 +682,9 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
             for (int it = 0; it < ITERS; ++it) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) D[it][i] = rp * fmaf(x[it][i], minus_dot_b, D[it][i]);
-                store_cols<T, ALIGNED>(out_b, it * threads * 8 + col0, C, D[it]);
+                if (ALIGNED && it * threads * 8 + col0 < C) store_floats<T, 8>(out_b + it * threads * 8 + col0, D[it]);
             }
+            if constexpr (!ALIGNED) store_row<T, ITERS>(out_b, threads, C, D, ends[1]);
             out_b += a.lddb;
         } else {
             __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next

@@ -117,20 +117,17 @@ template <typename T> __device__ __forceinline__ Frag<T, 8> load_run(const T *ro
     }
     return f;
 }
-// Every lane of the warp calls it; lanes with col >= C store nothing.
-template <typename T> __device__ __forceinline__ void store_run(T *row, int col, int C, const float (&x)[8]) {
+// Stores run [col, col + 8) given the last 16 bytes of the run before it.  `own`: this thread writes the words that begin
+// with the neighbour's end; `next`: its neighbour writes those that begin with this run's end.  What neither covers goes
+// element by element.
+template <typename T> __device__ __forceinline__ void store_shifted(T *row, int col, int C, const Frag<T, 8> &f, const uint4 &neighbour, bool own, bool next) {
     constexpr int kWords = 2 * (int)sizeof(T), kSize = (int)sizeof(T);
-    const int lane = threadIdx.x & 31;
-    Frag<T, 8> f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f.v[i] = from_float<T>(x[i]);
     T *p = row + col;
     const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
-    const int before = (int)off / kSize;              // elements of the neighbour's run in this lane's first word
+    const int before = (int)off / kSize;              // elements of the neighbour's run in this run's first word
     uint32_t w[kWords + 4], out[kWords];
+    w[0] = neighbour.x; w[1] = neighbour.y; w[2] = neighbour.z; w[3] = neighbour.w;
     memcpy(w + 4, &f, sizeof(f));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, w[kWords + i], 1);    // the end of the neighbour's run
     // the words start `before` elements before the run, that is 16 - off bytes into w
     if (off == 0) {
 #pragma unroll
@@ -138,20 +135,66 @@ template <typename T> __device__ __forceinline__ void store_run(T *row, int col,
     } else {
         shift_words<kWords>(w, 16u - off, out);
     }
-    const bool own = (lane > 0 || off == 0) && col - before + 8 <= C;            // this lane's words are wholly in the row
-    const bool next = lane < 31 && col - before + 16 <= C;                       // its neighbour's, which take this run's end
+    own = (own || off == 0) && col - before + 8 <= C;
+    next = next && col - before + 16 <= C;
     if (own) {
         uint4 *q = reinterpret_cast<uint4 *>(reinterpret_cast<uintptr_t>(p) - off);
 #pragma unroll
         for (int i = 0; i < kWords / 4; ++i) q[i] = make_uint4(out[4 * i], out[4 * i + 1], out[4 * i + 2], out[4 * i + 3]);
     }
-    // by element: the run's beginning where this lane's words are not written, its end where the neighbour's are not
     const int from = own ? 8 - before : 0, to = next || (off == 0 && own) ? 8 - before : 8;
     const int exist = C - col < 8 ? C - col : 8;
     const uint32_t mask = exist > 0 ? ((1u << to) - 1u) & ~((1u << from) - 1u) & ((1u << exist) - 1u) : 0u;
+    if (mask) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (mask >> i & 1u) p[i] = f.v[i];
+        for (int i = 0; i < 8; ++i)
+            if (mask >> i & 1u) p[i] = f.v[i];
+    }
+}
+template <typename T> __device__ __forceinline__ Frag<T, 8> round_run(const float (&x)[8]) {
+    Frag<T, 8> f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.v[i] = from_float<T>(x[i]);
+    return f;
+}
+template <typename T> __device__ __forceinline__ uint4 end_of_run(const Frag<T, 8> &f) {
+    uint4 w[sizeof(T) / 2];
+    memcpy(w, &f, sizeof(f));
+    return w[sizeof(T) / 2 - 1];
+}
+// Every lane of the warp calls it; lanes with col >= C store nothing.  The ends of the warp's columns go by element.
+template <typename T> __device__ __forceinline__ void store_run(T *row, int col, int C, const float (&x)[8]) {
+    const int lane = threadIdx.x & 31;
+    const Frag<T, 8> f = round_run<T>(x);
+    uint4 n = end_of_run<T>(f);
+    n.x = __shfl_up_sync(0xffffffffu, n.x, 1);
+    n.y = __shfl_up_sync(0xffffffffu, n.y, 1);
+    n.z = __shfl_up_sync(0xffffffffu, n.z, 1);
+    n.w = __shfl_up_sync(0xffffffffu, n.w, 1);
+    store_shifted<T>(row, col, C, f, n, lane > 0, lane < 31);
+}
+// A whole row by a CTA, thread i holding runs i, i + threads, ...: warps hand their ends on in `ends` [ITERS * 32], so only
+// the row's own ends go by element.  Every thread calls it; it waits for all of them once.
+template <typename T, int ITERS> __device__ __forceinline__ void store_row(T *row, int threads, int C, const float (&x)[ITERS][8], uint4 *ends) {
+    const int lane = threadIdx.x & 31, warps = threads >> 5;
+    Frag<T, 8> f[ITERS];
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it) {
+        f[it] = round_run<T>(x[it]);
+        if (lane == 31) ends[it * warps + (threadIdx.x >> 5)] = end_of_run<T>(f[it]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it) {
+        uint4 n = end_of_run<T>(f[it]);
+        n.x = __shfl_up_sync(0xffffffffu, n.x, 1);
+        n.y = __shfl_up_sync(0xffffffffu, n.y, 1);
+        n.z = __shfl_up_sync(0xffffffffu, n.z, 1);
+        n.w = __shfl_up_sync(0xffffffffu, n.w, 1);
+        const int col = (it * threads + (int)threadIdx.x) * 8;
+        if (lane == 0 && col > 0) n = ends[it * warps + (int)(threadIdx.x >> 5) - 1];
+        store_shifted<T>(row, col, C, f[it], n, col > 0, true);
+    }
 }
 // Columns [col, col + 8) of a row: whole words where rows are ALIGNED (C is then a multiple of 8), as above elsewhere.
 template <typename T, bool ALIGNED> __device__ __forceinline__ Frag<T, 8> load_cols(const T *row, int col, int C) {
