@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(256, ALIGNED ? 8 : 6) pack_kernel(const T *__r
         const uint32_t top = group_top<T>(f);
         float v[8];
         to_floats<T, 8>(f, v);
-        store_held(q, e, at.col, C, v, top);
+        store_held<ALIGNED>(q, e, at.col, C, v, top);
         x += at.step * ldx;
         q += at.step * ldq;
         e += at.step * lde;
@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(256, ALIGNED ? 5 : 4) gated_forward_kernel(con
         float g[8], u[8];
         to_floats<T, 8>(fg, g);
         to_floats<T, 8>(fu, u);
-        if (a.gate_q) store_held(a.gate_q + at_q, a.gate_e + at_e, at.col, F, g, group_top<T>(fg));
-        if (a.up_q) store_held(a.up_q + at_q, a.up_e + at_e, at.col, F, u, group_top<T>(fu));
+        if (a.gate_q) store_held<ALIGNED>(a.gate_q + at_q, a.gate_e + at_e, at.col, F, g, group_top<T>(fg));
+        if (a.up_q) store_held<ALIGNED>(a.up_q + at_q, a.up_e + at_e, at.col, F, u, group_top<T>(fu));
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = g[i] * sigmoid<T>(g[i]) * u[i];
         store_cols<T, ALIGNED>(out, at.col, F, g);
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(256, ALIGNED && sizeof(T) == 2 ? 5 : 4) gated_
         if (a.h_q) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = at.col + i < F ? to_float<T>(from_float<T>(h[i])) : 0.f;     // the values h_out holds
-            store_held(a.h_q + at_q - at.col, a.h_e + t * a.lde, at.col, F, h);
+            store_held<ALIGNED>(a.h_q + at_q - at.col, a.h_e + t * a.lde, at.col, F, h);
         }
         dh += at.step * a.lddh;
         dgate += at.step * a.lddg;

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(MOST) norm_forward_kernel(const NormForward a)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
                     const int col = (it * threads + (int)threadIdx.x) * 8;
-                    store_held(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
+                    store_held<ALIGNED>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
                 }
             sum = cta_sum(sum, scratch[0]);
             const float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(MOST) norm_forward_kernel(const NormForward a)
                     float x[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));   // h' as stored
-                    store_held(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, x);
+                    store_held<ALIGNED>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, x);
                 }
         } else {
 #pragma unroll
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(MOST) norm_forward_kernel(const NormForward a)
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
                     const int col = (it * threads + (int)threadIdx.x) * 8;
-                    store_held(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, h[it]);
+                    store_held<ALIGNED>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, h[it]);
                 }
         }
         sum = cta_sum(sum, scratch[1]);
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(MOST) norm_forward_kernel(const NormForward a)
             if (a.hn.q) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) n[i] = to_float<T>(from_float<T>(n[i]));           // n as stored
-                store_held(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, n);
+                store_held<ALIGNED>(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, n);
             }
         }
         if (!a.b) __syncthreads();   // one sum per row: scratch[1] is rewritten by the next
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
     __shared__ uint64_t full[kMaxStages];
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
-    const int threads = ALIGNED ? MOST : (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
+    const int threads = ALIGNED ? MOST : (int)blockDim.x, C = (int)a.C, Cp = ALIGNED ? C : (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), stage_bytes = a.b ? 2 * row_bytes : row_bytes;
     float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
     uint8_t *ring = dynamic + (a.b ? 8 : 4) * Cp;
     const Slice slice(a.rows_per_group, a.parts_per_group);
@@ -397,8 +397,8 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
     }
     for (int i = threadIdx.x; i < Cp; i += threads) {
         const int at = param_place(i, Cp);
-        w_pre[at] = i < C ? a.w_pre[i] : 0.f;
-        if (a.b) w_post[at] = i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+        w_pre[at] = ALIGNED || i < C ? a.w_pre[i] : 0.f;
+        if (a.b) w_post[at] = !ALIGNED && i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
     }
     __syncthreads();
     int s = 0;
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
                     const int col = (it * threads + (int)threadIdx.x) * 8;
-                    store_held(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
+                    store_held<ALIGNED>(a.hb.q + t * a.ldq, a.hb.e + t * a.lde, col, C, b[it]);
                 }
             sum = 0.f;
 #pragma unroll
@@ -450,8 +450,8 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
                     shared_params(w_post, col, Cp, w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[it][i] = fmaf(b[it][i] * r, w[i], a.res_scale * h[it][i]);
+                    if constexpr (ALIGNED) store_floats<T, 8>((T *)a.h_out + t * a.ldho + col, h[it]);
                 }
-                if (ALIGNED && col < C) store_floats<T, 8>((T *)a.h_out + t * a.ldho + col, h[it]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fmaf(h[it][i], h[it][i], sum);
             }
@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));       // h' as stored
-                store_held(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, x);
+                store_held<ALIGNED>(a.hh.q + t * a.ldq, a.hh.e + t * a.lde, col, C, x);
             }
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
@@ -479,13 +479,13 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
                 shared_params(w_pre, col, Cp, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[it][i] = h[it][i] * r * w[i];
+                if constexpr (ALIGNED) store_floats<T, 8>((T *)a.n_out + t * a.ldn + col, h[it]);
             }
-            if (ALIGNED && col < C) store_floats<T, 8>((T *)a.n_out + t * a.ldn + col, h[it]);
             if (a.hn.q) {
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = to_float<T>(from_float<T>(h[it][i]));       // n as stored
-                store_held(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, x);
+                store_held<ALIGNED>(a.hn.q + t * a.ldq, a.hn.e + t * a.lde, col, C, x);
             }
         }
         if constexpr (!ALIGNED) store_row<T, ITERS>((T *)a.n_out + t * a.ldn, threads, C, h, ends[1]);
@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
     volatile int *failed = &failed_flag;
     const bool has_b = HELD ? a.hb.q != nullptr : a.b != nullptr;
     const bool ring_e = a.lde % 16 == 0;                             // exponents come with the ring where their rows can
-    const int threads = ALIGNED ? MOST : (int)blockDim.x, C = (int)a.C, Cp = (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
+    const int threads = ALIGNED ? MOST : (int)blockDim.x, C = (int)a.C, Cp = ALIGNED ? C : (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
     const int saved_bytes = HELD ? held_bytes : row_bytes;
     const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + saved_bytes, stage_bytes = at_b + (has_b ? saved_bytes : 0);
     float *w_pre = (float *)dynamic, *w_post = w_pre + Cp;           // w_post times the group's gate
@@ -571,8 +571,8 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
     }
     for (int i = threadIdx.x; i < Cp; i += threads) {
         const int at = param_place(i, Cp);
-        w_pre[at] = i < C ? a.w_pre[i] : 0.f;
-        if (has_b) w_post[at] = i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
+        w_pre[at] = ALIGNED || i < C ? a.w_pre[i] : 0.f;
+        if (has_b) w_post[at] = !ALIGNED && i >= C ? 0.f : a.gate ? a.w_post[i] * a.gate[slice.group * C + i] : a.w_post[i];
     }
     __syncthreads();
     float sum_x[ITERS][8], sum_y[ITERS][8];

@@ -335,17 +335,17 @@ template <bool ALIGNED> __device__ __forceinline__ void held_cols(const RawQ &q,
 
 // Writes the checkpoint of columns [col, min(col + 8, C)); every lane of the warp calls it, with zeros for columns that do
 // not exist.  `top`: group_top of the same values.
-__device__ __forceinline__ void store_held(int8_t *q, uint8_t *e, int col, int C, const float (&x)[8], uint32_t top) {
+template <bool ALIGNED> __device__ __forceinline__ void store_held(int8_t *q, uint8_t *e, int col, int C, const float (&x)[8], uint32_t top) {
     const uint32_t ex = group_exponent(top);
     uint32_t v[8];
     quantise(x, top, ex, v);
     if (col < C) {
-        store_q(q + col, C - col, v);
+        store_q(q + col, ALIGNED ? 8 : C - col, v);
         if (col % kGroup == 0) e[(unsigned)col / kGroup] = (uint8_t)ex;
     }
 }
-__device__ __forceinline__ void store_held(int8_t *q, uint8_t *e, int col, int C, const float (&x)[8]) {
-    store_held(q, e, col, C, x, group_top(x));
+template <bool ALIGNED> __device__ __forceinline__ void store_held(int8_t *q, uint8_t *e, int col, int C, const float (&x)[8]) {
+    store_held<ALIGNED>(q, e, col, C, x, group_top(x));
 }
 
 // ---------------------------------------------------------------------------
