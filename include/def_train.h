@@ -12,10 +12,11 @@
  * Conventions (beyond those of def.h)
  *   - Activations are rows [T, C]: T tokens, C consecutive elements of type `dtype` (DEF_DTYPE_*), row stride ld >= C
  *     in ELEMENTS.  Parameters, statistics and parameter gradients are fp32.  Any T >= 0 (0 is a no-op unless a call
- *     says otherwise); sizes and strides are 64-bit.
+ *     says otherwise); offsets are 64-bit, and widths (C, F, O, I, V) are at most 2^30.
  *   - Arithmetic and sums are fp32 (the weight gradient: exact products, fp32 sums), rounded once when an output is
  *     stored.  Sums over tokens are taken in a fixed order: repeated calls give identical bits.
- *   - Rows whose base and stride are multiples of 16 bytes run on 128-bit accesses; others run on element accesses.
+ *   - Rows whose base and stride are multiples of 16 bytes (and whose width is one of 8) run on 128-bit accesses; others on
+ *     the aligned words around them, at a third to two thirds of that speed.
  *   - There is no context.  Work is enqueued on `cuda_stream` (a cudaStream_t, NULL = legacy default stream) of the
  *     current device; nothing is allocated or synchronised.  A workspace is device memory, 16-byte aligned, that the
  *     call may overwrite; calls that overlap on the GPU need one each.
@@ -145,9 +146,9 @@ int def_norm_backward_workspace(int64_t T, int64_t C, int64_t groups, int64_t *b
  * where the logits are large.  0 <= top <= min(V, DEF_LOGPROB_MAX_TOP); top_ids and top_logp are NULL if and only if top = 0.
  * targets y [T] int64.  y < 0: the token is ignored (logp 0, and no gradient through logp).  y >= V: logp is NaN.
  * Logits at or below -1e30 (-infinity, and the lowest values of bf16 and fp32) are masked: in a row with others, p = 0 and
- * they add nothing to the entropy.  A row that is masked throughout: lse is (-infinity, 0),
- * logp (0 <= y < V) and top_logp are -infinity, the entropy is 0.  A NaN or a logit above 2^127 makes l, logp (y >= 0), entropy and top_logp NaN; a NaN ranks with -infinity
- * among the alternatives.  V < 2^31.
+ * they add nothing to the entropy.  A row that is masked throughout: lse is (-infinity, 0), logp (0 <= y < V) and top_logp
+ * are -infinity, the entropy is 0.  A NaN or a logit above 2^127 makes l, logp (y >= 0), entropy and top_logp NaN; a NaN
+ * ranks with -infinity among the alternatives.
  */
 int def_logprob_forward(int32_t dtype, int64_t T, int64_t V, const void *logits, int64_t ldx, const int64_t *targets,
                         float *logp, float *entropy, float *lse, int32_t top, int64_t *top_ids, float *top_logp,

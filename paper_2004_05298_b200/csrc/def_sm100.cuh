@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
 // Shared memory of CTA `rank` of the cluster, at the same place as `address` in this one.
 __device__ __forceinline__ uint32_t cluster_address(uint32_t address, uint32_t rank) {

@@ -85,11 +85,12 @@ int check_rows(int32_t dtype, int64_t T, int64_t C, const char *width) {
     if (!element_size(dtype)) return fail(DEF_ERR_ARG, "dtype must be one of DEF_DTYPE_F32, _BF16, _F16 (got %d)", dtype);
     if (T < 0) return fail(DEF_ERR_ARG, "T must not be negative (got %lld)", (long long)T);
     if (C < 1) return fail(DEF_ERR_ARG, "%s must be at least 1 (got %lld)", width, (long long)C);
-    if (T > ((int64_t)1 << 40) || C > ((int64_t)1 << 31) - 64) return fail(DEF_ERR_ARG, "T or %s is too large", width);
+    if (T > ((int64_t)1 << 40) || C > (int64_t)1 << 30) return fail(DEF_ERR_ARG, "T or %s is too large", width);
     return DEF_OK;
 }
-int check_stride(const void *p, int64_t ld, int64_t C, const char *name) {
-    if (p && (ld < C || ld > (int64_t)1 << 40)) return fail(DEF_ERR_ARG, "the row stride of %s must be at least its width (got %lld)", name, (long long)ld);
+int check_stride(const void *p, int64_t ld, int64_t C, int64_t T, const char *name) {
+    if (p && ld < C) return fail(DEF_ERR_ARG, "the row stride of %s must be at least its width (got %lld)", name, (long long)ld);
+    if (p && ld > ((int64_t)1 << 60) / (T > 0 ? T : 1)) return fail(DEF_ERR_ARG, "the rows of %s reach too far", name);
     return DEF_OK;
 }
 int check_pair(const void *q, const void *e, const char *name) {
@@ -149,7 +150,7 @@ template <typename F> void on_plane(bool aligned, int64_t T, int64_t C, F f) {
 
 extern "C" int def_checkpoint_layout(int64_t C, int64_t *ldq_out, int64_t *lde_out) {
     if (!ldq_out || !lde_out) return fail(DEF_ERR_NULL, "ldq_out and lde_out must not be NULL");
-    if (C < 1 || C > ((int64_t)1 << 31) - 64) return fail(DEF_ERR_ARG, "C must be in [1, 2^31 - 64] (got %lld)", (long long)C);
+    if (C < 1 || C > (int64_t)1 << 30) return fail(DEF_ERR_ARG, "C must be in [1, 2^30] (got %lld)", (long long)C);
     *ldq_out = q_stride(C);
     *lde_out = e_stride(C);
     return DEF_OK;
@@ -160,7 +161,7 @@ extern "C" int def_checkpoint_pack(int32_t dtype, int64_t T, int64_t C, const vo
     DEF_TRY(check_rows(dtype, T, C, "C"));
     if (T == 0) return DEF_OK;
     if (!x || !q || !e) return fail(DEF_ERR_NULL, "x, q and e must not be NULL");
-    DEF_TRY(check_stride(x, ldx, C, "x"));
+    DEF_TRY(check_stride(x, ldx, C, T, "x"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(x, "x", T, C, ldx, es, false), q_view(q, "q", T, C, true), e_view(e, "e", T, C, true)};
     DEF_TRY(check_views(views));
@@ -180,7 +181,7 @@ extern "C" int def_checkpoint_unpack(int32_t dtype, int64_t T, int64_t C, const 
     DEF_TRY(check_rows(dtype, T, C, "C"));
     if (T == 0) return DEF_OK;
     if (!out || !q || !e) return fail(DEF_ERR_NULL, "q, e and out must not be NULL");
-    DEF_TRY(check_stride(out, ldout, C, "out"));
+    DEF_TRY(check_stride(out, ldout, C, T, "out"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(out, "out", T, C, ldout, es, true), q_view(q, "q", T, C, false), e_view(e, "e", T, C, false)};
     DEF_TRY(check_views(views));
@@ -203,9 +204,9 @@ extern "C" int def_gated_forward(int32_t dtype, int64_t T, int64_t F, const void
     if (!gate || !up || !h) return fail(DEF_ERR_NULL, "gate, up and h must not be NULL");
     DEF_TRY(check_pair(gate_q, gate_e, "gate"));
     DEF_TRY(check_pair(up_q, up_e, "up"));
-    DEF_TRY(check_stride(gate, ldg, F, "gate"));
-    DEF_TRY(check_stride(up, ldu, F, "up"));
-    DEF_TRY(check_stride(h, ldh, F, "h"));
+    DEF_TRY(check_stride(gate, ldg, F, T, "gate"));
+    DEF_TRY(check_stride(up, ldu, F, T, "up"));
+    DEF_TRY(check_stride(h, ldh, F, T, "h"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(gate, "gate", T, F, ldg, es, false), rows_view(up, "up", T, F, ldu, es, false),
                           rows_view(h, "h", T, F, ldh, es, true), q_view(gate_q, "gate_q", T, F, true), e_view(gate_e, "gate_e", T, F, true),
@@ -230,10 +231,10 @@ extern "C" int def_gated_backward(int32_t dtype, int64_t T, int64_t F, const voi
     if (!dh || !gate_q || !gate_e || !up_q || !up_e || !dgate || !dup)
         return fail(DEF_ERR_NULL, "dh, the checkpoints of gate and up, dgate and dup must not be NULL");
     DEF_TRY(check_pair(h_q, h_e, "h"));
-    DEF_TRY(check_stride(dh, lddh, F, "dh"));
-    DEF_TRY(check_stride(dgate, lddg, F, "dgate"));
-    DEF_TRY(check_stride(dup, lddu, F, "dup"));
-    DEF_TRY(check_stride(h_out, ldh, F, "h_out"));
+    DEF_TRY(check_stride(dh, lddh, F, T, "dh"));
+    DEF_TRY(check_stride(dgate, lddg, F, T, "dgate"));
+    DEF_TRY(check_stride(dup, lddu, F, T, "dup"));
+    DEF_TRY(check_stride(h_out, ldh, F, T, "h_out"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(dh, "dh", T, F, lddh, es, false), q_view(gate_q, "gate_q", T, F, false), e_view(gate_e, "gate_e", T, F, false),
                           q_view(up_q, "up_q", T, F, false), e_view(up_e, "up_e", T, F, false), rows_view(dgate, "dgate", T, F, lddg, es, true),
@@ -324,10 +325,10 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
     DEF_TRY(check_pair(n_q, n_e, "n"));
     DEF_TRY(check_groups(T, groups));
     if (!(eps >= 0.f) || !(eps <= 1e30f)) return fail(DEF_ERR_ARG, "eps must be a finite number that is not negative");
-    DEF_TRY(check_stride(h, ldh, C, "h"));
-    DEF_TRY(check_stride(b, ldb, C, "b"));
-    DEF_TRY(check_stride(h_out, ldho, C, "h_out"));
-    DEF_TRY(check_stride(n_out, ldn, C, "n_out"));
+    DEF_TRY(check_stride(h, ldh, C, T, "h"));
+    DEF_TRY(check_stride(b, ldb, C, T, "b"));
+    DEF_TRY(check_stride(h_out, ldho, C, T, "h_out"));
+    DEF_TRY(check_stride(n_out, ldn, C, T, "n_out"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(h, "h", T, C, ldh, es, false), rows_view(b, "b", T, C, ldb, es, false),
                           floats_view(w_post, "w_post", C, false), floats_view(gate, "gate", groups * C, false), floats_view(w_pre, "w_pre", C, false),
@@ -413,12 +414,12 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
         return fail(DEF_ERR_ARG, "w_post, gate, rstd_post, db, dw_post and dgate must be NULL where b is");
     if (T > 0 && !workspace) return fail(DEF_ERR_NULL, "workspace must not be NULL");
     if (workspace_bytes < need) return fail(DEF_ERR_ARG, "the workspace must have %lld bytes (got %lld)", (long long)need, (long long)workspace_bytes);
-    DEF_TRY(check_stride(dn, lddn, C, "dn"));
-    DEF_TRY(check_stride(dh_in, lddhi, C, "dh_in"));
-    DEF_TRY(check_stride(h, ldh, C, "h"));
-    DEF_TRY(check_stride(b, ldb, C, "b"));
-    DEF_TRY(check_stride(dh, lddh, C, "dh"));
-    DEF_TRY(check_stride(db, lddb, C, "db"));
+    DEF_TRY(check_stride(dn, lddn, C, T, "dn"));
+    DEF_TRY(check_stride(dh_in, lddhi, C, T, "dh_in"));
+    DEF_TRY(check_stride(h, ldh, C, T, "h"));
+    DEF_TRY(check_stride(b, ldb, C, T, "b"));
+    DEF_TRY(check_stride(dh, lddh, C, T, "dh"));
+    DEF_TRY(check_stride(db, lddb, C, T, "db"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(dn, "dn", T, C, lddn, es, false), rows_view(dh_in, "dh_in", T, C, lddhi, es, false),
                           rows_view(h, "h", T, C, ldh, es, false), rows_view(b, "b", T, C, ldb, es, false),
@@ -570,7 +571,7 @@ extern "C" int def_checkpoint_weight_grad_workspace(int32_t dtype, int64_t T, in
     if (!bytes_out) return fail(DEF_ERR_NULL, "bytes_out must not be NULL");
     DEF_TRY(check_rows(dtype, T, O, "O"));
     DEF_TRY(check_rows(dtype, T, I, "I"));
-    DEF_TRY(check_stride(dy, lddy, O, "dy"));
+    DEF_TRY(check_stride(dy, lddy, O, T, "dy"));
     if (T >= (int64_t)1 << 31) return fail(DEF_ERR_ARG, "T must be below 2^31 (got %lld)", (long long)T);
     const GradPlan p = grad_plan(dtype, T, O, I, dy, lddy, kUsualSms);
     *bytes_out = p.partial_bytes + p.plane_bytes + p.x_bytes;
@@ -604,13 +605,11 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
     const void *rows = dy;
     int64_t ld = lddy;
     if (p.copy_dy) {
-        void *planes = (char *)workspace + p.partial_bytes;
-        const int64_t want = ceil_div(T * O, 256);
-        const unsigned grid = (unsigned)(want < 148 * 32 ? want : 148 * 32);
-        if (es == 4)
-            deft::weight_grad_planes_kernel<float, __nv_bfloat16><<<grid, 256, 0, stream>>>((const float *)dy, lddy, T, O, (__nv_bfloat16 *)planes, p.ld_planes);
-        else
-            deft::weight_grad_planes_kernel<uint16_t, uint16_t><<<grid, 256, 0, stream>>>((const uint16_t *)dy, lddy, T, O, (uint16_t *)planes, p.ld_planes);
+        uint4 *planes = (uint4 *)((char *)workspace + p.partial_bytes);
+        on_plane(false, T, O, [&](auto, dim3 grid, dim3 block) {
+            if (es == 4) deft::weight_grad_planes_kernel<float><<<grid, block, 0, stream>>>((const float *)dy, lddy, T, (int)O, planes, p.ld_planes);
+            else deft::weight_grad_planes_kernel<__half><<<grid, block, 0, stream>>>((const __half *)dy, lddy, T, (int)O, planes, p.ld_planes);
+        });
         DEF_TRY(launched("def_checkpoint_weight_grad (copy)"));
         rows = planes;
         ld = p.ld_planes;
@@ -714,7 +713,7 @@ extern "C" int def_logprob_forward(int32_t dtype, int64_t T, int64_t V, const vo
     if (T == 0) return DEF_OK;
     if (!logits || !targets || !logp || !entropy || !lse) return fail(DEF_ERR_NULL, "logits, targets, logp, entropy and lse must not be NULL");
     if ((top > 0) != (top_ids != nullptr) || (top > 0) != (top_logp != nullptr)) return fail(DEF_ERR_NULL, "top_ids and top_logp must be given if and only if top > 0");
-    DEF_TRY(check_stride(logits, ldx, V, "logits"));
+    DEF_TRY(check_stride(logits, ldx, V, T, "logits"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(logits, "logits", T, V, ldx, es, false), {targets, "targets", 1, T * 8, T * 8, 8, false},
                           floats_view(logp, "logp", T, true), floats_view(entropy, "entropy", T, true), floats_view(lse, "lse", 2 * T, true),
@@ -757,8 +756,8 @@ extern "C" int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const v
     if (T == 0) return DEF_OK;
     if (!logits || !targets || !lse || !entropy || !dlogits) return fail(DEF_ERR_NULL, "logits, targets, lse, entropy and dlogits must not be NULL");
     if ((top > 0) != (top_ids != nullptr) || (top > 0) != (dtop_logp != nullptr)) return fail(DEF_ERR_NULL, "top_ids and dtop_logp must be given if and only if top > 0");
-    DEF_TRY(check_stride(logits, ldx, V, "logits"));
-    DEF_TRY(check_stride(dlogits, lddx, V, "dlogits"));
+    DEF_TRY(check_stride(logits, ldx, V, T, "logits"));
+    DEF_TRY(check_stride(dlogits, lddx, V, T, "dlogits"));
     const int es = element_size(dtype);
     const View views[] = {rows_view(logits, "logits", T, V, ldx, es, false), rows_view(dlogits, "dlogits", T, V, lddx, es, true),
                           {targets, "targets", 1, T * 8, T * 8, 8, false}, floats_view(lse, "lse", 2 * T, false), floats_view(entropy, "entropy", T, false),

@@ -392,24 +392,38 @@ __global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad 
         if (i0 + i + j < a.I) out[j] = a.accumulate ? out[j] + v[j] : v[j];
 }
 
-// dy as the tensor cores take it, where it is not already: 16-bit pieces in rows of ld elements (a multiple of 8).
-// 16-bit types: a copy.  fp32: three bf16 numbers of 8 bits each, by truncation, whose sum is dy exactly.
-template <typename T, typename U>
-__global__ void __launch_bounds__(256) weight_grad_planes_kernel(const T *__restrict__ dy, int64_t lddy, int64_t tokens, int64_t O,
-                                                                 U *__restrict__ out, int64_t ld) {
-    const int64_t n = tokens * O;
-    for (int64_t j = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; j < n; j += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t t = j / O, o = j - t * O;
+// dy as the tensor cores take it, where it is not already: 16-bit pieces in rows of ld elements (a multiple of 8, the last
+// ones 0).  16-bit types: a copy, of either type as bits.  fp32: three bf16 numbers of 8 bits each, by truncation, whose
+// sum is dy exactly.  A thread takes 8 columns.
+template <typename T>
+__global__ void __launch_bounds__(256) weight_grad_planes_kernel(const T *__restrict__ dy, int64_t lddy, int64_t tokens, int O,
+                                                                 uint4 *__restrict__ out, int64_t ld) {
+    const int col = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 8;
+    if (col >= O) return;
+    for (int64_t t = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; t < tokens; t += (int64_t)gridDim.y * blockDim.y) {
+        const Frag<T, 8> f = load_run<T>(dy + t * lddy, col, O);
         if constexpr (sizeof(T) == 2) {
-            out[t * ld + o] = dy[t * lddy + o];
+            uint4 w;
+            memcpy(&w, &f, sizeof(w));
+            out[(t * ld + col) / 8] = w;
         } else {
-            const float x = dy[t * lddy + o];
-            const bool finite = fabsf(x) <= 3.402823466e38f;
-            const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u), rest = x - hi;
-            const float mid = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
-            out[t * ld + o] = from_float<__nv_bfloat16>(finite ? hi : x);
-            out[(tokens + t) * ld + o] = from_float<__nv_bfloat16>(finite ? mid : 0.f);
-            out[(2 * tokens + t) * ld + o] = from_float<__nv_bfloat16>(finite ? rest - mid : 0.f);
+            Frag<__nv_bfloat16, 8> piece[3];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = f.v[i];
+                const bool finite = fabsf(x) <= 3.402823466e38f;
+                const float hi = __uint_as_float(__float_as_uint(x) & 0xffff0000u), rest = x - hi;
+                const float mid = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+                piece[0].v[i] = from_float<__nv_bfloat16>(finite ? hi : x);
+                piece[1].v[i] = from_float<__nv_bfloat16>(finite ? mid : 0.f);
+                piece[2].v[i] = from_float<__nv_bfloat16>(finite ? rest - mid : 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                uint4 w;
+                memcpy(&w, &piece[k], sizeof(w));
+                out[((k * tokens + t) * ld + col) / 8] = w;
+            }
         }
     }
 }

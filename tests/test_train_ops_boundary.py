@@ -47,6 +47,7 @@ def test_pack_and_unpack_refuse():
     assert rc(_3=None) == B.DEF_ERR_NULL and rc(_5=None) == B.DEF_ERR_NULL and rc(_6=None) == B.DEF_ERR_NULL
     assert rc(_4=63) == B.DEF_ERR_ARG and "stride" in B.def_last_error()
     assert rc(_3=at(0, 1)) == B.DEF_ERR_ALIGN and rc(_5=at(1, 8)) == B.DEF_ERR_ALIGN and rc(_6=at(2, 2)) == B.DEF_ERR_ALIGN
+    assert rc(_4=1 << 59) == B.DEF_ERR_ARG and rc(_2=(1 << 30) + 1, _4=1 << 31) == B.DEF_ERR_ARG
     assert rc(_5=at(0, 128)) == B.DEF_ERR_ALIAS and "overlap" in B.def_last_error()
     assert rc(_1=0, _3=None, _5=None, _6=None) == B.DEF_OK            # no rows: a no-op
     if not HAS_GPU:
