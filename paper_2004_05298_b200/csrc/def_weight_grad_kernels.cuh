@@ -369,7 +369,8 @@ __global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad 
     const int64_t half_tile = blockIdx.x / (kTileO / 8), tile = half_tile / 2;       // of the tiles that were cut
     const int rank = (int)(half_tile % 2);
     const int col = (int)(blockIdx.x % (kTileO / 8)) * 8 + threadIdx.x / 32;
-    // pair c holds blocks [all c / pairs, all (c + 1) / pairs); none is empty
+    // pair c holds blocks [all c / pairs, all (c + 1) / pairs): the last pair that starts at or before a block holds it; with
+    // fewer blocks than pairs some hold none
     const int64_t begin = tile * per_tile, end = begin + per_tile;
     const int first = (int)(((begin + 1) * pairs - 1) / all), last = (int)((end * pairs - 1) / all);
     asm volatile("griddepcontrol.wait;" ::: "memory");                                // the parts are those of the kernel before
@@ -382,6 +383,7 @@ __global__ void __launch_bounds__(256) weight_grad_join_kernel(const WeightGrad 
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int c = first; c <= last; ++c) {                                             // the first holds the tile's first block
+        if (all < pairs && all * c / pairs == all * (c + 1) / pairs) continue;
         const float4 v = *reinterpret_cast<const float4 *>(a.partial + (((int64_t)c * 2 + rank) * 2 + (c == first)) * (kTileO * kTileI) + col * kTileI + i);
         sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
     }

@@ -136,6 +136,55 @@ def test_weight_grad(B, dtype, T, O, I):
         assert float(buf[0]) == 7.0 and bool((buf[1 + O * I:] == 7.0).all())
 
 
+@pytest.mark.parametrize("dtype,T,O,I", [
+    (BF16, 130, 4100, 1300),        # rounds of whole tiles and tiles that are cut; x^ widened once
+    (F16, 130, 4100, 1300),
+    (BF16, 1100, 2560, 2048),       # widened in shared memory, exponents by wide copies; more than one accumulator hand-over
+    (F16, 200, 2500, 2100),         # the same with small copies of exponents
+    (F32, 200, 1100, 2500),         # three pieces of dy
+    (BF16, 40, 4608, 4224),         # one block of tokens: nothing to cut
+    (F32, 70, 300, 2500),
+    (BF16, 5000, 40, 8),
+])
+def test_weight_grad_many_tiles(B, dtype, T, O, I):
+    dy = _normal((T, O), dtype, 1, std=0.1)
+    ck = _checkpoint(B, _normal((T, I), BF16, 2))
+    work = torch.empty(max(1, B.def_checkpoint_weight_grad_workspace(dy, I)), dtype=torch.uint8, device=DEV)
+    assert work.numel() <= (68 << 20) + 8 * O * I + 6 * T * (O + 7)
+    dw = torch.full((O, I), float("nan"), device=DEV)
+    B.def_checkpoint_weight_grad(dy, ck, dw, work)
+    x = R.read(ck, I).to(DEV)
+    x = x.to(F16).double() if dtype == F16 else x
+    want, mag = dy.double().t() @ x, dy.double().abs().t() @ x.abs()
+    _close(dw, want, mag, F32, n=2 * (T + 16))
+    first = dw.clone()
+    B.def_checkpoint_weight_grad(dy, ck, dw, work, accumulate=True)
+    _close(dw, 2 * want, 2 * mag, F32, n=2 * (T + 16))
+    B.def_checkpoint_weight_grad(dy, ck, dw, work)
+    assert torch.equal(first, dw)
+
+
+def test_weight_grad_overlapping_calls(B):
+    """Calls back to back on one stream and one workspace, without waiting, of shapes that use it differently."""
+    shapes = [(300, 520, 264, BF16), (64, 136, 1000, F16), (700, 3400, 72, BF16), (129, 257, 333, F32)]
+    runs = []
+    for i, (T, O, I, dt) in enumerate(shapes):
+        dy, ck = _normal((T, O), dt, 3 * i, std=0.1), _checkpoint(B, _normal((T, I), BF16, 3 * i + 1))
+        runs.append((dy, ck, torch.empty(O, I, device=DEV)))
+    work = torch.empty(max(B.def_checkpoint_weight_grad_workspace(dy, dw.shape[1]) for dy, _, dw in runs), dtype=torch.uint8, device=DEV)
+    alone = []
+    for dy, ck, dw in runs:
+        B.def_checkpoint_weight_grad(dy, ck, dw, work)
+        torch.cuda.synchronize()
+        alone.append(dw.clone())
+        dw.fill_(float("nan"))
+    for _ in range(5):
+        for dy, ck, dw in runs:
+            B.def_checkpoint_weight_grad(dy, ck, dw, work)
+    for (_, _, dw), want in zip(runs, alone):
+        assert torch.equal(dw, want)
+
+
 def test_weight_grad_no_tokens_and_nan(B):
     dw = torch.full((24, 40), 3.0, device=DEV)
     none = (torch.empty((0, 48), dtype=torch.int8, device=DEV), torch.empty((0, 4), dtype=torch.uint8, device=DEV))
@@ -424,6 +473,21 @@ def test_logprob(B, dtype, layout):
         for parts in ("all", "logp", "entropy", "top"):
             _check_gradient(B, x, y, top, o, f, dtype, i, parts=parts)
         _check_gradient(B, x, y, top, o, f, dtype, i, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logprob_gradient_with_other_alignment(B, dtype):
+    """Logits and their gradient that do not start alike within 16 bytes."""
+    for T, V in ((5, 777), (3, 30011)):
+        x, y = _logit_inputs(T, V, dtype, 3)
+        o = _run_logprob(B, x, y, 8)
+        f = _check_logprob(x, y, 8, o)
+        dl = _normal((T,), F32, 9)
+        want, mag = R.logprob_backward(f, y, dl, None, f["top_ids"], None)
+        dx = _out(T, V, dtype, "off")
+        B.def_logprob_backward(x, y, o["lse"], o["entropy"], dx, dl)
+        off = (f["lp"].nan_to_num(0, 0, 0).abs() + f["lse"].sum(1).abs()[:, None]).clamp(max=200)
+        _close(dx, want, mag * (1 + off), dtype, n=V / 64 + 128 + 33)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
