@@ -483,7 +483,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
             by_alignment(aligned_rows, [&](auto aligned) {
                 by_row_shape(C, [&](auto shape) {
                     using S = decltype(shape);
-                    a.parts_per_group = norm_parts(T, groups, S::threads(C) <= 128 ? 4 * kUsualSms : S::threads(C) <= 256 ? 2 * kUsualSms : kUsualSms);
+                    a.parts_per_group = norm_parts(T, groups, S::threads(C) <= 128 ? 4 * kUsualSms : S::threads(C) <= 256 ? 3 * kUsualSms : kUsualSms);
                     deft::norm_backward_kernel<decltype(type), aligned.value, S::most, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads(C), 0, stream>>>(a);
                 });
             });
