@@ -129,6 +129,7 @@ struct NormBackward {
     float *partial;                      // [parts][2][C]: sums of dn x and of D y over a part's rows
     int64_t T, C, rows_per_group, ldq, lde;
     int64_t parts_per_group;
+    int ring_e;                          // the stream kernel's ring brings rows of exponents: they are whole 16-byte words
     float res_scale, inv_C;
 };
 
@@ -538,7 +539,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
     const bool has_b = HELD ? a.hb.q != nullptr : a.b != nullptr;
-    const bool ring_e = a.lde % 16 == 0;                             // exponents come with the ring where their rows can
+    const bool ring_e = a.ring_e;                                    // else exponents are read one by one
     const int threads = ALIGNED ? MOST : (int)blockDim.x, C = (int)a.C, Cp = ALIGNED ? C : (C + 7) & ~7, row_bytes = slot_bytes<T, ALIGNED>(C), e_bytes = ring_e ? (int)a.lde : 0, held_bytes = (int)a.ldq + e_bytes;
     const int saved_bytes = HELD ? held_bytes : row_bytes;
     const int at_in = row_bytes, at_h = at_in + (a.dh_in ? row_bytes : 0), at_b = at_h + saved_bytes, stage_bytes = at_b + (has_b ? saved_bytes : 0);

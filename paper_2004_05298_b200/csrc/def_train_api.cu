@@ -449,6 +449,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     a.T = T; a.C = C; a.rows_per_group = T / groups; a.ldq = q_stride(C); a.lde = e_stride(C);
     a.res_scale = res_scale; a.inv_C = 1.f / (float)C;
     const bool aligned_rows = C % 8 == 0 && wide(dn, lddn, es) && wide(dh_in, lddhi, es) && wide(h, ldh, es) && wide(b, ldb, es) && wide(dh, lddh, es) && wide(db, lddb, es);
+    a.ring_e = wide(h_e, a.lde, 1) && wide(b_e, a.lde, 1);           // bulk copies start on 16-byte boundaries
     if (groups > 0x7fffffff / 2) return fail(DEF_ERR_ARG, "groups is too large (got %lld)", (long long)groups);
     cudaError_t err = cudaSuccess;
     bool streamed = false;
@@ -456,7 +457,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     by_stream_shape(C, [&](auto shape) {
             using S = decltype(shape);
             const int64_t params = (has_b ? 8 : 4) * padded;
-            const int64_t held = q_stride(C) + (e_stride(C) % 16 == 0 ? e_stride(C) : 0);
+            const int64_t held = a.ldq + (a.ring_e ? a.lde : 0);
             const int64_t stage = slot * (dh_in ? 2 : 1) + (h_q ? held : slot) + (!has_b ? 0 : b_q ? held : slot);
             const int threads = aligned_rows ? S::most : S::threads(C);
             int ctas = stream_ctas<S>(threads), stages = 0;
