@@ -147,7 +147,7 @@ int def_norm_backward_workspace(int64_t T, int64_t C, int64_t groups, int64_t *b
  * targets y [T] int64.  y < 0: the token is ignored (logp 0, and no gradient through logp).  y >= V: logp is NaN.
  * Logits at or below -1e30 (-infinity, and the lowest values of bf16 and fp32) are masked: in a row with others, p = 0 and
  * they add nothing to the entropy.  A row that is masked throughout: lse is (-infinity, 0), logp (0 <= y < V) and top_logp
- * are -infinity, the entropy is 0.  A NaN or a logit above 2^127 makes l, logp (y >= 0), entropy and top_logp NaN; a NaN
+ * are -infinity, the entropy is 0.  A NaN or +infinity makes l, logp (y >= 0), entropy and top_logp NaN; a NaN
  * ranks with -infinity among the alternatives.
  */
 int def_logprob_forward(int32_t dtype, int64_t T, int64_t V, const void *logits, int64_t ldx, const int64_t *targets,

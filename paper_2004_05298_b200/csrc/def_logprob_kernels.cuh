@@ -16,17 +16,23 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // A logit at or below this (about -1e30, and exact in bf16) is masked; -infinity and the lowest value of bf16 and fp32 are.
 constexpr float kMasked = -0x1.92p+99f;
 
-// Running statistics of part of a row:  s = sum 2^y,  u = sum y 2^y with y = x log2(e) - r.  The reference r is m log2(e)
-// rounded to an integer, m the maximum so far: the product is not rounded before r is taken from it, so that y is as good
-// as if m had been subtracted first, in one operation.
+// Exponents are taken relative to the maximum m:  y = (x - base) log2(e) - r.  Where |m| < kFar, base is 0 and r is m log2(e)
+// rounded to an integer: the product is not rounded before r is taken from it, so that y is as good as if m had been
+// subtracted first, in one operation.  A larger product is itself too coarse to be rounded to an integer (2^-24 of it
+// reaches 128 at 1.5e9), so there base is m and r is 0: x - m is exact where x is near m, and where it is not, 2^y is 0.
+constexpr float kFar = 0x1p20f;
+__device__ __forceinline__ bool is_far(float m) { return !(fabsf(m) < kFar); }
+__device__ __forceinline__ float base_of(float m) { return is_far(m) ? m : 0.f; }
+__device__ __forceinline__ float reference_of(float m) { return is_far(m) ? 0.f : rintf(m * kLog2e); }
+
+// Running statistics of part of a row:  s = sum 2^y,  u = sum y 2^y, m the maximum so far and r = reference_of(m).
 struct Stats {
     float m, r, s, u;
 };
-__device__ __forceinline__ Stats empty_stats() { return {kMasked, kMasked, 0.f, 0.f}; }
+__device__ __forceinline__ Stats empty_stats() { return {kMasked, 0.f, 0.f, 0.f}; }
 // y is held at -1e4, where 2^y is 0 and 0 times y still is.
-__device__ __forceinline__ float exponent(float x, float r) { return max_nan(fmaf(x, kLog2e, -r), -1e4f); }
-__device__ __forceinline__ void rebase(Stats &a, float m, float r) {     // m >= a.m
-    const float d = max_nan(a.r - r, -1e4f), f = exp2_fast(d);
+__device__ __forceinline__ void rebase(Stats &a, float m, float r) {     // m >= a.m: exponents shrink, or grow by less than 1
+    const float d = max_nan(fmaf(base_of(a.m) - base_of(m), kLog2e, a.r - r), -1e4f), f = exp2_fast(d);
     a.u = fmaf(d, a.s, a.u) * f;
     a.s *= f;
     a.m = m;
@@ -167,7 +173,7 @@ template <int N, typename T> __device__ __forceinline__ float largest(const Frag
 
 // A thread's running statistics, the sums in two halves.
 struct Running {
-    float m = kMasked, r = kMasked;
+    float m = kMasked, r = 0.f;
     Pair s = {0}, u = {0};
     __device__ __forceinline__ void reach(float top) {            // before adding elements of which `top` is the largest
         if (top > m) {
@@ -177,7 +183,7 @@ struct Running {
             split_pair(s, a.s, b.s);
             split_pair(u, a.u, b.u);
             m = top;
-            r = rintf(top * kLog2e);
+            r = reference_of(top);
             rebase(a, m, r);
             rebase(b, m, r);
             s = make_pair(a.s, b.s);
@@ -185,23 +191,22 @@ struct Running {
         }
     }
     __device__ __forceinline__ void add(const float (&v)[8]) {
-        if (m == kMasked) {                                       // nothing but masked logits, or NaN, so far
+        const Pair l = make_pair(kLog2e, kLog2e), minus_r = make_pair(-r, -r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (v[i] != v[i]) s = u = make_pair(NAN, NAN);
-        } else {
-            const Pair l = make_pair(kLog2e, kLog2e), minus_r = make_pair(-r, -r);
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                float y0, y1;
-                split_pair(pair_fma(make_pair(v[i], v[i + 1]), l, minus_r), y0, y1);
-                y0 = max_nan(y0, -1e4f);
-                y1 = max_nan(y1, -1e4f);
-                const Pair p = make_pair(exp2_fast(y0), exp2_fast(y1));
-                s = pair_add(s, p);
-                u = pair_fma(p, make_pair(y0, y1), u);
-            }
+        for (int i = 0; i < 8; i += 2) {
+            float y0, y1;
+            split_pair(pair_fma(make_pair(v[i], v[i + 1]), l, minus_r), y0, y1);
+            y0 = max_nan(y0, -1e4f);
+            y1 = max_nan(y1, -1e4f);
+            const Pair p = make_pair(exp2_fast(y0), exp2_fast(y1));
+            s = pair_add(s, p);
+            u = pair_fma(p, make_pair(y0, y1), u);
         }
+    }
+    // What add() takes where m is far (r is 0 there).  m == kMasked: nothing but masked logits, or NaN, so far.
+    __device__ __forceinline__ void from_base(float (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = m != kMasked ? v[i] - m : v[i] == v[i] ? -INFINITY : v[i];
     }
     __device__ __forceinline__ Stats total() const {
         float s0, s1, u0, u1;
@@ -261,6 +266,7 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) logprob_forward_kerne
     auto add_any = [&](int chunk) {
         row.any(chunk, v);
         run.reach(largest(v));
+        if (is_far(run.m)) run.from_base(v);
         run.add(v);
     };
     int c = g;
@@ -269,10 +275,19 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) logprob_forward_kerne
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) f[k] = row.wide(c + k * G);
         run.reach(largest<kAhead>(f));
+        if (is_far(run.m)) {
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            to_floats<T, 8>(f[k], v);
-            run.add(v);
+            for (int k = 0; k < kAhead; ++k) {
+                to_floats<T, 8>(f[k], v);
+                run.from_base(v);
+                run.add(v);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                to_floats<T, 8>(f[k], v);
+                run.add(v);
+            }
         }
     }
     for (; c < row.body; c += G) add_any(c);
@@ -399,7 +414,7 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) logprob_forward_kerne
     if (warp != 0) return;
     const bool none = st.m == kMasked && st.s == 0.f;                // the row is masked throughout
     const float m = none ? INFINITY : st.m;                          // log p = (x - m) - log_s
-    const float log2_s = log2f(st.s), shift = fmaf(-st.m, kLog2e, st.r);          // of the sum relative to 2^r; r - m log2(e)
+    const float log2_s = log2f(st.s), shift = is_far(st.m) ? 0.f : fmaf(-st.m, kLog2e, st.r);   // of the sum as kept; what m's exponent lacks to 0
     const float log_s = none ? 0.f : (log2_s + shift) * kLn2;
     if (threadIdx.x == 0) {
         a.lse[2 * t] = none ? -INFINITY : st.m;
@@ -439,11 +454,11 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) logprob_backward_kern
     const float dl = a.dlogp && y >= 0 ? (y < a.V ? a.dlogp[t] : NAN) : 0.f;
     const float dt = lane < a.top ? a.dtop[t * a.top + lane] : 0.f;
     const bool none = m == -INFINITY;
-    // log2 p = (x log2(e) - r) - shift, r = m log2(e) rounded to an integer; G + dH (log p + H) = slope log2 p + rise
-    const float r = rintf(m * kLog2e), shift = fmaf(m, kLog2e, -r) + log_s * kLog2e;
+    // log2 p = ((x - base) log2(e) - r) - shift; G + dH (log p + H) = slope log2 p + rise
+    const float base = base_of(m), r = reference_of(m), shift = fmaf(m - base, kLog2e, -r) + log_s * kLog2e;
     const float slope = dH * kLn2, rise = fmaf(dH, H, dl + warp_sum(dt));
     auto spread = [&](float x) {
-        const float z = max_nan(fmaf(x, kLog2e, -r) - shift, -1e4f);      // p is 0 there, and 0 times the rest
+        const float z = max_nan(fmaf(x - base, kLog2e, -r) - shift, -1e4f);      // p is 0 there, and 0 times the rest
         return none ? 0.f : -exp2_fast(z) * fmaf(slope, z, rise);
     };
     // Thread k < top owns alternative k, thread `top` the target; the first owner of an index sums its terms.

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import train_ref as R
-from test_train_ops_gpu import B, BF16, DEV, F16, F32, _checkpoint, _close, _norm_inputs, _normal, _out  # noqa: F401
+from test_train_ops_gpu import (B, BF16, DEV, F16, F32, _check_gradient, _check_logprob, _checkpoint, _close, _norm_inputs, _normal,  # noqa: F401
+                                _out, _run_logprob)
 
 
 def _moved(ck, off):
@@ -54,3 +55,51 @@ def test_exponents_at_any_multiple_of_4(B, dtype, T, C, off_h, off_b):  # noqa: 
     work = torch.empty(max(1, B.def_checkpoint_weight_grad_workspace(dy, C)), dtype=torch.uint8, device=DEV)
     B.def_checkpoint_weight_grad(dy, hs, grad, work)
     _close(grad, dy.double().t() @ hv, dy.double().abs().t() @ hv.abs(), F32, n=2 * (T + 16))
+
+
+FILLS = [-1e9, -1e10, -1e12, -1e15, -1e20, -7e29, -8e29, -9e29]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [40, 264, 4099, 33000])
+@pytest.mark.parametrize("target", ["given", "ignored"])
+def test_logits_of_any_size(B, dtype, V, target):  # noqa: F811
+    """Rows filled, or partly filled, with finite masks; maxima far from 0; differences that count beside a large maximum."""
+    few = torch.randperm(V, generator=torch.Generator().manual_seed(V))[:5].to(DEV)
+    step = {F32: 2.0 ** -24, BF16: 2.0 ** -8}[dtype]
+    rows = []
+
+    def row(fill=None, where=slice(None)):
+        r = _normal((V,), F32, V + len(rows), std=2.0)
+        if fill is not None:
+            r[where] = fill
+        rows.append(r)
+        return r
+
+    for f in FILLS:
+        row(f)                                                          # nothing else
+        row(f, slice(0, V // 2))                                        # what the first threads read
+        row(f, slice(V - V // 2, V))
+        row(f, slice(0, V, 2))
+        keep = row()
+        rows[-1] = torch.full_like(keep, f).index_copy(0, few, keep[few])   # five left
+        r = row(f)
+        r[:8] = 2 * f if f > -4e29 else f                               # two masks
+        r[V // 2] = f / 2
+    for m in (1e10, 1e20, -1e10, 3e38):
+        row(m, V - 1)
+        row(m, slice(0, V, 3))                                          # equal maxima
+        row(m, slice(0, V))
+    for m in (2.0 ** 17, 1e6, 2.0 ** 20 - 1, 2.0 ** 20, 1.1e6, 2.0 ** 22, -2.0 ** 20, -2.0 ** 20 + 1, -1e6, 1e9):
+        r = row()                                                       # neighbours of the type around a large number
+        r.mul_(4).round_().mul_(max(2 * abs(m) * step, 0.25)).add_(m)
+    x = torch.stack(rows).to(dtype)
+    T = x.shape[0]
+    y = torch.full((T,), -1, device=DEV) if target == "ignored" else (torch.arange(T, device=DEV) * 7) % V
+    top = min(V, 32)
+    o = _run_logprob(B, x, y, top)
+    f = _check_logprob(x, y, top, o)
+    assert bool(torch.isfinite(o["entropy"]).all()) and bool(torch.isfinite(o["lse"]).all())
+    for parts in ("all", "logp"):
+        _check_gradient(B, x, y, top, o, f, dtype, V, parts=parts)
