@@ -286,9 +286,15 @@ template <typename S> int stream_ctas(int threads) {
     return n < 13 ? n : 13;
 }
 // Stages of a stream kernel's ring: as many as fit beside the parameters with `ctas` on an SM (below 2: not for it).
+constexpr int kStreamSmem = 224 * 1024, kStreamOwn = 2048;            // shared memory of an SM; what a CTA needs besides
 int stream_stages(int64_t params, int64_t stage, int ctas) {
-    const int64_t n = ((int64_t)224 * 1024 / ctas - 2048 - params) / stage;
+    const int64_t n = ((int64_t)kStreamSmem / ctas - kStreamOwn - params) / stage;
     return (int)(n < deft::kMaxStages ? n : deft::kMaxStages);
+}
+// The limit belongs to the kernel, not to the launch: every call sets the same one, the most that any call needs, so that
+// no thread lowers it under another's launch.
+template <typename K> cudaError_t allow_stream_smem(K kernel) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem - kStreamOwn);
 }
 
 int check_groups(int64_t T, int64_t groups) {
@@ -366,7 +372,7 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
                 using E = decltype(type);
                 const auto kernel = aligned_rows ? deft::norm_forward_stream_kernel<E, true, S::most, S::iters, S::min_ctas>
                                                  : deft::norm_forward_stream_kernel<E, false, S::most, S::iters, S::min_ctas>;
-                if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
+                if ((err = allow_stream_smem(kernel)) != cudaSuccess) return;
                 kernel<<<grid, threads, smem, (cudaStream_t)cuda_stream>>>(a, stages);
             });
         });
@@ -474,7 +480,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
                                : deft::norm_backward_stream_kernel<E, aligned.value, S::most, S::iters, S::min_ctas, false>;
                 };
                 const auto kernel = aligned_rows ? pick(Is<true>()) : pick(Is<false>());
-                if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return;
+                if ((err = allow_stream_smem(kernel)) != cudaSuccess) return;
                 kernel<<<(unsigned)(groups * a.parts_per_group), threads, smem, stream>>>(a, stages);
             });
         });

@@ -1,5 +1,8 @@
 """Limits that include/def_train.h promises: the least aligned checkpoints, the largest magnitudes, calls from several
 host threads, the longest runs of rows and of tokens.  Bounds as in test_train_ops_gpu.py."""
+import threading
+import time
+
 import pytest
 import torch
 
@@ -103,3 +106,54 @@ def test_logits_of_any_size(B, dtype, V, target):  # noqa: F811
     assert bool(torch.isfinite(o["entropy"]).all()) and bool(torch.isfinite(o["lse"]).all())
     for parts in ("all", "logp"):
         _check_gradient(B, x, y, top, o, f, dtype, V, parts=parts)
+
+
+@pytest.mark.gpu
+def test_norms_from_many_host_threads(B):  # noqa: F811
+    """Threads with a stream each call the same kernels on rows of different length, three seconds long: as if each were alone."""
+    T, failures, calls = 900, [], []
+
+    def work(C):
+        h, b, w_post, _, w_pre = _norm_inputs(T, C, BF16, "rows", 0, C)
+        ho, n, r2, r1 = _out(T, C, BF16), _out(T, C, BF16), torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+        dh, db, dwp, dw = _out(T, C, BF16), _out(T, C, BF16), torch.empty(C, device=DEV), torch.empty(C, device=DEV)
+        space = torch.empty(B.def_norm_backward_workspace(T, C), dtype=torch.uint8, device=DEV)
+        p = [v.data_ptr() for v in (h, b, w_post, w_pre, ho, n, r2, r1, dh, db, dwp, dw, space)]
+
+        def both(stream):                                               # the library's own calls: no lock is held inside them
+            rc = B.lib.def_norm_forward(1, T, C, p[0], C, p[1], C, p[2], None, 1, p[3], 1.0, 1e-6, p[4], C, p[5], C, p[6], p[7], None, None, None,
+                                        None, None, None, stream)
+            return rc or B.lib.def_norm_backward(1, T, C, p[5], C, None, 0, p[4], C, None, None, p[1], C, None, None, p[2], None, 1, p[3], 1.0,
+                                                 p[6], p[7], p[8], C, p[9], C, p[10], None, p[11], 0, p[12], space.numel(), stream)
+        return both, (ho, n, r2, r1, dh, db, dwp, dw), (h, b, w_post, w_pre, space)
+
+    jobs = [work(C) for C in (4096, 2056, 4088, 2064) for _ in (0, 1)]
+    alone = []
+    for both, outs, _ in jobs:
+        assert both(0) == B.DEF_OK
+        torch.cuda.synchronize()
+        alone.append([o.clone() for o in outs])
+    streams = [torch.cuda.Stream() for _ in jobs]
+    stop = time.monotonic() + 3
+
+    def loop(both, stream):
+        done = 0
+        while time.monotonic() < stop and not failures:
+            for _ in range(50):
+                if both(stream.cuda_stream) != B.DEF_OK:
+                    failures.append(B.def_last_error())
+                    return
+            done += 50
+            stream.synchronize()
+        calls.append(done)
+
+    threads = [threading.Thread(target=loop, args=(job[0], stream)) for job, stream in zip(jobs, streams)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failures, failures[0]
+    assert len(calls) == len(jobs) and min(calls) > 0
+    for (_, outs, _), want in zip(jobs, alone):
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
