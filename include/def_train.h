@@ -126,7 +126,7 @@ int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void *h, int64_t
  * is.  res_scale is a constant.  dh may be dh_in itself (same stride).
  * b absent (no pointer, no checkpoint): the backward pass of n = norm(h); w_post, gate, rstd_post, db, dw_post, dgate
  * must be NULL.  T = 0 writes zeros to the parameter gradients unless accumulate is set.
- * The workspace holds partial sums; the second call says how much is needed.
+ * groups is below 2^31.  The workspace holds partial sums; the second call says how much is needed.
  */
 int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void *dn, int64_t lddn, const void *dh_in,
                       int64_t lddhi, const void *h, int64_t ldh, const int8_t *h_q, const uint8_t *h_e, const void *b,

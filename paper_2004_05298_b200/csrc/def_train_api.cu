@@ -305,6 +305,7 @@ int check_groups(int64_t T, int64_t groups) {
 // Slices per group that rows are cut into (each: one CTA, and in the backward pass one row of partial sums): about `want`
 // in all, at most one per row.
 constexpr int64_t kNormParts = 13 * kUsualSms;    // the most in all, which the workspace is sized for
+constexpr int64_t kMostCtas = 0x7fffffff;         // of a grid
 int64_t norm_parts(int64_t T, int64_t groups, int64_t want) {
     const int64_t rows = T / groups, each = ceil_div(want, groups);
     return rows < each ? rows : each;
@@ -363,9 +364,9 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
             int ctas = stream_ctas<S>(threads), stages = 0;
             while ((stages = stream_stages(params, stage, ctas)) < 2 && ctas > 1) --ctas;
             const int64_t want = (int64_t)ctas * kUsualSms;
-            if (stages < 2 || T < want * kStreamRows) return;
-            streamed = true;
             a.parts_per_group = norm_parts(T, groups, want);
+            if (stages < 2 || T < want * kStreamRows || groups * a.parts_per_group > kMostCtas) return;
+            streamed = true;
             const unsigned grid = (unsigned)(groups * a.parts_per_group);
             const int smem = (int)(params + stages * stage);
             by_dtype(dtype, [&](auto type) {
@@ -382,7 +383,7 @@ extern "C" int def_norm_forward(int32_t dtype, int64_t T, int64_t C, const void 
         by_alignment(aligned_rows, [&](auto aligned) {
             by_row_shape(C, [&](auto shape) {
                 using S = decltype(shape);
-                const unsigned grid = (unsigned)(T < 0x7fffffff ? T : 0x7fffffff);
+                const unsigned grid = (unsigned)(T < kMostCtas ? T : kMostCtas);
                 deft::norm_forward_kernel<decltype(type), aligned.value, S::most, S::iters><<<grid, S::threads(C), 0, (cudaStream_t)cuda_stream>>>(a);
             });
         });
@@ -408,6 +409,7 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     int64_t need = 0;
     if (!element_size(dtype)) return fail(DEF_ERR_ARG, "dtype must be one of DEF_DTYPE_F32, _BF16, _F16 (got %d)", dtype);
     DEF_TRY(def_norm_backward_workspace(T, C, groups, &need));
+    if (T > 0 && groups * norm_parts(T, groups, kNormParts) > kMostCtas) return fail(DEF_ERR_ARG, "groups must be below 2^31 (got %lld)", (long long)groups);
     DEF_TRY(check_pair(h_q, h_e, "h"));
     DEF_TRY(check_pair(b_q, b_e, "b"));
     const bool has_b = b || b_q;
@@ -456,7 +458,6 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
     a.res_scale = res_scale; a.inv_C = 1.f / (float)C;
     const bool aligned_rows = C % 8 == 0 && wide(dn, lddn, es) && wide(dh_in, lddhi, es) && wide(h, ldh, es) && wide(b, ldb, es) && wide(dh, lddh, es) && wide(db, lddb, es);
     a.ring_e = wide(h_e, a.lde, 1) && wide(b_e, a.lde, 1);           // bulk copies start on 16-byte boundaries
-    if (groups > 0x7fffffff / 2) return fail(DEF_ERR_ARG, "groups is too large (got %lld)", (long long)groups);
     cudaError_t err = cudaSuccess;
     bool streamed = false;
     const int64_t slot = aligned_rows ? C * es : ceil_div(C * es, 32) * 32 + 16, padded = ceil_div(C, 8) * 8;

@@ -1,5 +1,6 @@
 """Limits that include/def_train.h promises: the least aligned checkpoints, the largest magnitudes, calls from several
 host threads, the longest runs of rows and of tokens.  Bounds as in test_train_ops_gpu.py."""
+import ctypes
 import threading
 import time
 
@@ -157,3 +158,39 @@ def test_norms_from_many_host_threads(B):  # noqa: F811
     assert len(calls) == len(jobs) and min(calls) > 0
     for (_, outs, _), want in zip(jobs, alone):
         assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+@pytest.mark.gpu
+def test_norm_of_more_groups_than_a_grid_holds(B):  # noqa: F811
+    """More than 2^32 rows, each a group of its own."""
+    T = (1 << 32) + 5
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of free device memory")
+    h = torch.empty((T, 1), dtype=BF16, device=DEV)
+    h.normal_(generator=torch.Generator(device=DEV).manual_seed(1))
+    n = torch.full((T, 1), float("nan"), dtype=BF16, device=DEV)
+    r1, w = torch.full((T,), float("nan"), device=DEV), torch.full((1,), 1.5, device=DEV)
+    rc = B.lib.def_norm_forward(B.DEF_DTYPE_BF16, T, 1, h.data_ptr(), 1, None, 0, None, None, T, w.data_ptr(), 1.0, 1e-5, None, 0,
+                                n.data_ptr(), 1, None, r1.data_ptr(), None, None, None, None, None, None, None)
+    assert rc == B.DEF_OK, B.def_last_error()
+    for at in range(0, T, 1 << 28):
+        x = h[at:at + (1 << 28), 0].float()
+        want = torch.rsqrt(x * x + 1e-5)
+        got = r1[at:at + (1 << 28)]
+        assert bool(((got - want).abs() <= 8 * R.U32 * want).all())
+        want = want.mul_(x).mul_(1.5)
+        assert bool(((n[at:at + (1 << 28), 0].float() - want).abs() <= 1.01 * R.UNIT[BF16] * want.abs()).all())
+
+
+def test_norm_backward_refuses_more_groups_than_a_grid_holds():
+    from paper_2004_05298_b200 import binding
+
+    def at(i):
+        return 0x1000_0000_0000 + i * (1 << 36)                           # made up, never dereferenced
+
+    T = 1 << 32
+    need = ctypes.c_int64(0)
+    assert binding.lib.def_norm_backward_workspace(T, 1, T, ctypes.byref(need)) == binding.DEF_OK
+    rc = binding.lib.def_norm_backward(1, T, 1, at(0), 1, None, 0, at(1), 1, None, None, None, 0, None, None, None, None, T, at(2), 1.0, None,
+                                       at(3), at(4), 1, None, 0, None, None, at(5), 0, at(6), need.value, None)
+    assert rc == binding.DEF_ERR_ARG and "groups" in binding.def_last_error()
