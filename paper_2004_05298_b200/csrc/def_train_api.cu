@@ -526,13 +526,15 @@ namespace {
 struct GradPlan {
     bool copy_dy, copy_x;
     int planes, pairs;
-    int64_t ld_planes, ld_x, partial_bytes, plane_bytes, x_bytes;
+    int64_t ld_dy, ld_planes, ld_x, partial_bytes, plane_bytes, x_bytes;
     int64_t tiles_i, tiles_o, blocks, whole;
 };
 GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *dy, int64_t lddy, int sms) {
     GradPlan p;
     const int es = element_size(dtype);
-    p.copy_dy = es == 4 || !wide(dy, lddy, es);
+    // One row has no stride; rows that a tensor map cannot reach (its strides end at 2^40 bytes) are copied like unaligned ones.
+    p.ld_dy = T > 1 ? lddy : ceil_div(O, 8) * 8;
+    p.copy_dy = es == 4 || !wide(dy, p.ld_dy, es) || p.ld_dy >= ((int64_t)1 << 40) / es;
     p.planes = es == 4 ? 3 : 1;
     p.ld_planes = ceil_div(O, 8) * 8;
     p.ld_x = ceil_div(I, 8) * 8;
@@ -610,32 +612,13 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
     // The plan the workspace was sized by, on as many CTAs.
     GradPlan p = grad_plan(dtype, T, O, I, dy, lddy, kUsualSms);
     const bool half = dtype == DEF_DTYPE_F16;
-    const void *rows = dy;
-    int64_t ld = lddy;
-    if (p.copy_dy) {
-        uint4 *planes = (uint4 *)((char *)workspace + p.partial_bytes);
-        on_plane(false, T, O, [&](auto, dim3 grid, dim3 block) {
-            if (es == 4) deft::weight_grad_planes_kernel<float><<<grid, block, 0, stream>>>((const float *)dy, lddy, T, (int)O, planes, p.ld_planes);
-            else deft::weight_grad_planes_kernel<__half><<<grid, block, 0, stream>>>((const __half *)dy, lddy, T, (int)O, planes, p.ld_planes);
-        });
-        DEF_TRY(launched("def_checkpoint_weight_grad (copy)"));
-        rows = planes;
-        ld = p.ld_planes;
-    }
-    const void *xs = q;
-    if (p.copy_x) {
-        void *wide_x = (char *)workspace + p.partial_bytes + p.plane_bytes;
-        on_plane(I % 8 == 0, T, I, [&](auto v, dim3 grid, dim3 block) {
-            if (half)
-                deft::unpack_kernel<__half, v.value><<<grid, block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, (int)I, (__half *)wide_x, p.ld_x);
-            else
-                deft::unpack_kernel<__nv_bfloat16, v.value><<<grid, block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, (int)I, (__nv_bfloat16 *)wide_x, p.ld_x);
-        });
-        DEF_TRY(launched("def_checkpoint_weight_grad (widen)"));
-        xs = wide_x;
-    }
+    uint4 *planes = (uint4 *)((char *)workspace + p.partial_bytes);
+    void *wide_x = (char *)workspace + p.partial_bytes + p.plane_bytes;
+    const void *rows = p.copy_dy ? planes : dy, *xs = p.copy_x ? wide_x : (const void *)q;
+    const int64_t ld = p.copy_dy ? p.ld_planes : p.ld_dy;
+    // The maps first: nothing is launched where the driver refuses one.
     CUtensorMap map_y, map_x, map_e = {};
-    const cuuint64_t dim_y[3] = {(cuuint64_t)O, (cuuint64_t)T, (cuuint64_t)p.planes}, stride_y[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)T};
+    const cuuint64_t dim_y[3] = {(cuuint64_t)O, (cuuint64_t)T, (cuuint64_t)p.planes}, stride_y[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)(p.planes > 1 ? T : 1)};
     const cuuint32_t box_y[3] = {64, deft::kTileT, 1}, one[3] = {1, 1, 1};
     const cuuint64_t dim_x[2] = {(cuuint64_t)I, (cuuint64_t)T}, stride_x[1] = {(cuuint64_t)(p.copy_x ? p.ld_x * 2 : q_stride(I))};
     const cuuint32_t box_x[2] = {p.copy_x ? 64u : (cuuint32_t)deft::kTileI, deft::kTileT};
@@ -653,6 +636,22 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
         if (encode(&map_e, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(e), dim_e, stride_e, box_e, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return fail(DEF_ERR_CUDA, "the driver refused a tensor map of e");
+    }
+    if (p.copy_dy) {
+        on_plane(false, T, O, [&](auto, dim3 grid, dim3 block) {
+            if (es == 4) deft::weight_grad_planes_kernel<float><<<grid, block, 0, stream>>>((const float *)dy, lddy, T, (int)O, planes, p.ld_planes);
+            else deft::weight_grad_planes_kernel<__half><<<grid, block, 0, stream>>>((const __half *)dy, lddy, T, (int)O, planes, p.ld_planes);
+        });
+        DEF_TRY(launched("def_checkpoint_weight_grad (copy)"));
+    }
+    if (p.copy_x) {
+        on_plane(I % 8 == 0, T, I, [&](auto v, dim3 grid, dim3 block) {
+            if (half)
+                deft::unpack_kernel<__half, v.value><<<grid, block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, (int)I, (__half *)wide_x, p.ld_x);
+            else
+                deft::unpack_kernel<__nv_bfloat16, v.value><<<grid, block, 0, stream>>>(q, e, q_stride(I), e_stride(I), T, (int)I, (__nv_bfloat16 *)wide_x, p.ld_x);
+        });
+        DEF_TRY(launched("def_checkpoint_weight_grad (widen)"));
     }
     deft::WeightGrad a = {e, dw, (float *)workspace, T, O, I, e_stride(I), (int)p.tiles_i, (int)p.tiles_o, (int)p.blocks, p.planes, accumulate, p.whole};
     cudaError_t err = cudaSuccess;

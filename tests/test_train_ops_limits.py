@@ -194,3 +194,20 @@ def test_norm_backward_refuses_more_groups_than_a_grid_holds():
     rc = binding.lib.def_norm_backward(1, T, 1, at(0), 1, None, 0, at(1), 1, None, None, None, 0, None, None, None, None, T, at(2), 1.0, None,
                                        at(3), at(4), 1, None, 0, None, None, at(5), 0, at(6), need.value, None)
     assert rc == binding.DEF_ERR_ARG and "groups" in binding.def_last_error()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("O", [40, 4000])
+def test_weight_grad_of_one_row_of_any_stride(B, O):  # noqa: F811
+    """One token's row stride means nothing, not even to a tensor map (whose strides end at 2^40 bytes)."""
+    I = 520
+    dy, ck = _normal((1, O), BF16, 1), _checkpoint(B, _normal((1, I), BF16, 2))
+    want = torch.empty((O, I), device=DEV)
+    space = torch.empty((68 << 20) + 8 * O * I + 6 * (O + 7), dtype=torch.uint8, device=DEV)
+    B.def_checkpoint_weight_grad(dy, ck, want, space)
+    for ld in (O, 1 << 39, (1 << 59) + 8):
+        dw = torch.full((O, I), 5.0, device=DEV)
+        rc = B.lib.def_checkpoint_weight_grad(B.DEF_DTYPE_BF16, 1, O, I, dy.data_ptr(), ld, ck[0].data_ptr(), ck[1].data_ptr(), dw.data_ptr(), 0,
+                                              space.data_ptr(), space.numel(), None)
+        assert rc == B.DEF_OK, B.def_last_error()
+        assert torch.equal(dw, want)
