@@ -211,3 +211,26 @@ def test_weight_grad_of_one_row_of_any_stride(B, O):  # noqa: F811
                                               space.data_ptr(), space.numel(), None)
         assert rc == B.DEF_OK, B.def_last_error()
         assert torch.equal(dw, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_weight_grad_of_many_tokens_of_one_sign(B, dtype):  # noqa: F811
+    """16384 tokens in whole tiles, all products positive: nothing cancels, and a chain of sums is as long as they get.
+
+    The matrix unit may drop up to a unit, 2^-23 of the running sum, each time it adds 16 products: 64 times until the
+    accumulator is handed over, to a sum that grows linearly, 32.5 2^-23 = 3.9e-6 of the whole at most.  The 16 (fp32: 48)
+    hand-overs round to nearest, 2^-24 each: 8.5 (40.5) more of those.  One chain over all tokens drops up to 6e-5; an fp32
+    dy without its third piece is off by 2e-5, since here every number's last 8 bits are ones."""
+    T, O, I = 16384, 2048, 2304                                          # 72 tiles, one for (nearly) each pair of CTAs
+    dy = torch.empty((T, O), device=DEV).uniform_(1, 2, generator=torch.Generator(device=DEV).manual_seed(1))
+    if dtype == F32:
+        dy = (dy.view(torch.int32) | 0x80ff).view(F32)
+    dy = dy.to(dtype)
+    ck = _checkpoint(B, torch.empty((T, I), device=DEV).uniform_(1, 2, generator=torch.Generator(device=DEV).manual_seed(2)).to(BF16))
+    space = torch.empty(B.def_checkpoint_weight_grad_workspace(dy, I), dtype=torch.uint8, device=DEV)
+    dw = torch.empty((O, I), device=DEV)
+    B.def_checkpoint_weight_grad(dy, ck, dw, space)
+    want = dy.double().t() @ R.read(ck, I).to(DEV)
+    bound = 32.5 * 2.0 ** -23 + (40.5 if dtype == F32 else 8.5) * R.U32 + R.U32
+    assert float(((dw.double() - want) / want).abs().max()) <= bound
