@@ -357,11 +357,15 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int s = 16; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
     return v;
 }
+// What the CTA's threads accessed before is behind all of them afterwards, also where they are one warp.
 // THREADS: those of the CTA, or 0 where only the launch knows.
 template <int THREADS = 0> __device__ __forceinline__ float cta_sum(float v, float *scratch) {
     const int warps = (THREADS ? THREADS : (int)blockDim.x) >> 5, lane = threadIdx.x & 31;
     v = warp_sum(v);
-    if (warps == 1) return v;
+    if (warps == 1) {
+        __syncwarp();
+        return v;
+    }
     if (lane == 0) scratch[threadIdx.x >> 5] = v;
     __syncthreads();
     v = lane < warps ? scratch[lane] : 0.f;
