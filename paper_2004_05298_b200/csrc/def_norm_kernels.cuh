@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_forward_stream_kernel(const N
             }
         }
         sum = cta_sum<ALIGNED ? MOST : 0>(sum, scratch[0]);
-        if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);       // every thread has read the stage
+        if (threadIdx.x == 0 && ok && t + stages < slice.last) fetch(t + stages, s);       // every thread has read the stage
         float r = rsqrtf(fmaf(sum, a.inv_C, a.eps));
         if (!ok) r = NAN;                                             // the wait ran out: no numbers rather than wrong ones
         if (a.b) {
@@ -679,7 +679,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
         out_h += a.lddh;
         if (has_b) {
             const float minus_dot_b = -cta_sum<ALIGNED ? MOST : 0>(dot, scratch[1]) * a.inv_C;
-            if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);   // every thread has read the stage
+            if (threadIdx.x == 0 && ok && t + stages < slice.last) fetch(t + stages, s);   // every thread has read the stage
 #pragma unroll
             for (int it = 0; it < ITERS; ++it) {
 #pragma unroll
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const 
             out_b += a.lddb;
         } else {
             __syncthreads();                                          // one sum per row: scratch[0] is rewritten by the next
-            if (threadIdx.x == 0 && t + stages < slice.last) fetch(t + stages, s);
+            if (threadIdx.x == 0 && ok && t + stages < slice.last) fetch(t + stages, s);
         }
         if (++s == stages) {
             s = 0;

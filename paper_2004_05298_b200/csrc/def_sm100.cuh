@@ -38,8 +38,9 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
         : "memory");
     return done != 0;
 }
-// Waits are bounded: a thread that has waited kWaitLimit raises *failed and gives up, and so does then every other
-// wait of the CTA.  No wait of a healthy kernel lasts a thousandth of that.
+// Waits are bounded: a thread that has waited kWaitLimit raises *failed, waits as long again for what is still on its way
+// (a late copy must not land in another CTA's memory) and gives up, and so does then every other wait of the CTA.  No wait
+// of a healthy kernel lasts a thousandth of that.
 constexpr uint64_t kWaitLimit = 2000000000;               // ns
 __device__ __forceinline__ uint64_t nanoseconds() {
     uint64_t t;
@@ -57,6 +58,7 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
         }
     }
     *failed = 1;
+    while (!barrier_try(bar, parity) && nanoseconds() - start < 2 * kWaitLimit) {}
     return false;
 }
 
