@@ -547,9 +547,12 @@ def def_logprob_forward(logits, targets, logp, entropy, lse, top_ids=None, top_l
 
 
 def def_logprob_backward(logits, targets, lse, entropy, dlogits, dlogp=None, dentropy=None, top_ids=None, dtop_logp=None, stream=None):
+    """dtop_logp needs top_ids; top_ids without it is not looked at."""
     a = _act(logits, "logits")
     dt, T, V, p, ld = a
-    top = 0 if top_ids is None or dtop_logp is None else top_ids.shape[1]
+    if top_ids is None and dtop_logp is not None:
+        raise DefError(DEF_ERR_NULL, "top_ids is None, but dtop_logp is given")
+    top = 0 if dtop_logp is None else top_ids.shape[1]
     if top == 0:
         top_ids = dtop_logp = None
     _check(lib.def_logprob_backward(dt, T, V, p, ld, _need(targets, "targets", (T,), torch.int64), _need(lse, "lse", (T, 2)),

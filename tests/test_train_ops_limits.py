@@ -234,3 +234,18 @@ def test_weight_grad_of_many_tokens_of_one_sign(B, dtype):  # noqa: F811
     want = dy.double().t() @ R.read(ck, I).to(DEV)
     bound = 32.5 * 2.0 ** -23 + (40.5 if dtype == F32 else 8.5) * R.U32 + R.U32
     assert float(((dw.double() - want) / want).abs().max()) <= bound
+
+
+@pytest.mark.gpu
+def test_alternatives_gradient_needs_their_ids(B):  # noqa: F811
+    x = _normal((3, 40), F32, 1)
+    y = torch.zeros(3, dtype=torch.int64, device=DEV)
+    o = _run_logprob(B, x, y, 4)
+    dx = torch.full_like(x, 9.0)
+    with pytest.raises(B.DefError):
+        B.def_logprob_backward(x, y, o["lse"], o["entropy"], dx, dtop_logp=torch.ones(3, 4, device=DEV))
+    with pytest.raises(ValueError):
+        B.def_logprob_backward(x, y, o["lse"], o["entropy"], dx, top_ids=o["top_ids"], dtop_logp=torch.ones(3, 5, device=DEV))
+    assert bool((dx == 9).all())
+    B.def_logprob_backward(x, y, o["lse"], o["entropy"], dx, top_ids=o["top_ids"])
+    assert bool((dx == 0).all())
