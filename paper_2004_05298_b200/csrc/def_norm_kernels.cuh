@@ -308,7 +308,6 @@ template <typename T, bool ALIGNED> struct RowCopy {
         if constexpr (ALIGNED) run_load(slot, p, bytes(), bar);
         else if (bytes()) run_load(slot + (uint32_t)(from - ((uintptr_t)p & ~(uintptr_t)15)), (const void *)from, bytes(), bar);
     }
-    __device__ bool whole() const { return ALIGNED || (from <= (uintptr_t)p && to >= (uintptr_t)(p + C)); }
     // The elements that copy() left out, fewer than 16 bytes at either end; by the first threads of the CTA.
     __device__ void patch(uint8_t *slot) const {
         const T *a = to > from ? (const T *)from : p + C, *b = to > from ? (const T *)to : p + C;

@@ -227,12 +227,6 @@ __device__ __forceinline__ Pair pair_add(Pair a, Pair b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits));
     return d;
 }
-__device__ __forceinline__ Pair pair_mul(Pair a, Pair b) {
-    Pair d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits));
-    return d;
-}
-__device__ __forceinline__ Pair both(float a) { return make_pair(a, a); }
 // ---------------------------------------------------------------------------
 // Checkpoint group: 32 consecutive columns of a row, held by 4 consecutive lanes of a warp (8 columns each).
 // k = max(floor(log2 amax) - 6, -126) is read off the exponent bits of amax: the steps are powers of two, so x 2^-k
