@@ -12,12 +12,13 @@
  * Conventions (beyond those of def.h)
  *   - Activations are rows [T, C]: T tokens, C consecutive elements of type `dtype` (DEF_DTYPE_*), row stride ld >= C
  *     in ELEMENTS.  Parameters, statistics and parameter gradients are fp32.  Any T >= 0 (0 is a no-op unless a call
- *     says otherwise); offsets are 64-bit, and widths (C, F, O, I, V) are at most 2^30.
+ *     says otherwise; below 2^31 for weight gradients and log probabilities); offsets are 64-bit, and widths (C, F, O, I, V) are
+ *     at most 2^30.
  *   - Arithmetic and sums are fp32 (the weight gradient: exact products, fp32 sums), rounded once when an output is
  *     stored.  Sums over tokens are taken in a fixed order: repeated calls give identical bits.
  *   - Rows whose base and stride are multiples of 16 bytes (and whose width is one of 8) run on 128-bit accesses; others on
  *     the aligned words around them, at a third to two thirds of that speed.
- *   - There is no context.  Work is enqueued on `cuda_stream` (a cudaStream_t, NULL = legacy default stream) of the
+ *   - There is no context; calls may come from any host threads at the same time.  Work is enqueued on `cuda_stream` (a cudaStream_t, NULL = legacy default stream) of the
  *     current device; nothing is allocated or synchronised.  A workspace is device memory, 16-byte aligned, that the
  *     call may overwrite; calls that overlap on the GPU need one each.
  *   - Outputs must overlap no other argument (DEF_ERR_ALIAS) except where a call allows it.  Column halves of one

@@ -9,7 +9,7 @@ namespace deft {
 // and the lanes that share an exponent are neighbours.  These kernels move bytes and little else: what counts is that
 // few instructions go into an element and that an SM holds enough threads (32 registers: 2048 of them) to keep enough
 // loads in flight.  Several rows per thread with all loads first cost more in registers than they gave.
-// 16384 x 8192 bf16: pack 68 us (407 MB), unpack 72; 8192 x 10240 gated: forward 119 us (676 MB), backward 142 (844 MB).
+// 16384 x 8192 bf16: pack 73 us (407 MB), unpack 76; 8192 x 10240 gated: forward 122 us (676 MB), backward 145 (844 MB).
 struct Place {
     int col;
     int64_t row, step;

@@ -243,7 +243,7 @@ __device__ __forceinline__ uint32_t kth_of_64(const uint32_t *x, int k) {
 // that reach the bound are ranked by counting.  Where that does not settle it -- too many ties at the bound, too few
 // logits above the masked ones -- the exact way does: an element among the `top` largest lies in the list of a thread whose
 // own largest is among them too, so the threads' largest elements are ranked and the `top` best threads' elements merged.
-// (4096 rows of 128000 bf16, top = 8: 332 us with the exact way alone, 213 like this, 193 without alternatives; the bytes
+// (4096 rows of 128000 bf16, top = 8: 332 us with the exact way alone, 217 like this, 205 without alternatives; the bytes
 // take 162.  2048 threads per SM with two chunks ahead each: 254 us with 1024 threads and four.)
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS, 2048 / THREADS) logprob_forward_kernel(const LogprobForward a, const int split) {

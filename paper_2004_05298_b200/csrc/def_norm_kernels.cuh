@@ -260,8 +260,8 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(const NormBackward 
 // Stream kernels: the same rows where there are many.  A CTA walks a slice of a group's rows; the next rows are on their way
 // to shared memory by bulk copies while one is worked on, and the parameters stay there in fp32.  What bounds these
 // kernels otherwise is the latency of a row: its loads, then two sums over the CTA that each wait for all of it.
-// 16384 x 4096 bf16 in 8 groups: forward 93 us (537 MB), backward from 8-bit saves 136 (676 MB); one row per CTA without
-// copies ahead: 132 and 367.
+// 16384 x 4096 bf16 in 8 groups: forward 94 us (537 MB), backward from 8-bit saves 144 with 12 for the parts' sums (676 MB);
+// one row per CTA without copies ahead: 132 and 367.
 //
 // Rows that are not ALIGNED are copied with the 16-byte words around them, shifted into place when they are read, and
 // written as store_run does.
@@ -527,8 +527,8 @@ template <bool NOTHING> __device__ __forceinline__ void clear_past(float (&x)[8]
 }
 // The backward pass is bound by instructions and registers as much as by bytes: addresses advance from row to row, the step
 // of a checkpoint's group and the row's statistic, both factors, are multiplied first, and what the second half of a row
-// needs stays in shared memory until then (two registers too many cost 20 us in spills that miss the L1).  HELD: h' and b
-// are checkpoints (else both are values).
+// needs stays in shared memory until then (two registers too many cost 20 us in spills that miss the L1; rows wider than 8192
+// columns still spill).  HELD: h' and b are checkpoints (else both are values).
 template <typename T, bool ALIGNED, int MOST, int ITERS, int MINB, bool HELD>
 __global__ void __launch_bounds__(MOST, MINB) norm_backward_stream_kernel(const NormBackward a, const int stages) {
     extern __shared__ __align__(128) uint8_t dynamic[];

@@ -131,6 +131,9 @@ template <typename F> void by_alignment(bool aligned, F f) {
     else f(Is<false>());
 }
 
+// Rows of its columns that a CTA of these kernels walks, where that leaves enough CTAs.  1, 2, 4, 8 of them, us: 16384 x 8192
+// bf16 pack 85, 76, 73, 73, unpack 96, 79, 76, 76, gated backward 239, 216, 208, 208; 16384 x 4097 bf16 pack 80, 68, 63, 62;
+// 8192 x 4096 fp32 pack 27 each, gated forward 76, 76, 78, 78.
 constexpr int kPlaneRows = 4;
 // Launch of a kernel that works on rows by columns without sums: a warp lies in one row.  f(aligned, grid, block).
 template <typename F> void on_plane(bool aligned, int64_t T, int64_t C, F f) {
@@ -138,7 +141,7 @@ template <typename F> void on_plane(bool aligned, int64_t T, int64_t C, F f) {
     unsigned bx = 32;
     while (bx < 256 && bx < lanes) bx *= 2;
     const dim3 block(bx, 256 / bx);
-    // A CTA walks kPlaneRows rows of its columns where that leaves enough CTAs: fewer instructions go into addresses.
+    // Several rows per CTA: fewer instructions go into addresses.
     const int64_t gx = ceil_div(lanes, bx), all = ceil_div(T, block.y);
     int64_t gy = ceil_div(all, kPlaneRows);
     if (gx * gy < 32 * kUsualSms) gy = ceil_div(32 * kUsualSms, gx) < all ? ceil_div(32 * kUsualSms, gx) : all;
@@ -271,6 +274,9 @@ template <typename F> void by_row_shape(int64_t C, F f) {
     else if (n <= 1024) f(Shape<512, 2>());
     else f(Shape<1024, 2>());
 }
+// 288 threads rather than 512 for the widths that 256 just miss, us: 16384 x 4352 bf16 forward 99 against 158, backward 148
+// against 193 (8-bit saves 194 against 282); 4097 forward 199 against 288, backward 370 against 402; fp32 4352 196 against
+// 232, 267 against 271.  The other way round in fp32 off alignment, backward: 4097, 559 against 475.
 template <typename F> void by_stream_shape(int64_t C, F f) {
     const int64_t n = ceil_div(C, 8);
     if (n <= 128) f(StreamShape<128, 1, 6>());
@@ -310,8 +316,13 @@ int64_t norm_parts(int64_t T, int64_t groups, int64_t want) {
     const int64_t rows = T / groups, each = ceil_div(want, groups);
     return rows < each ? rows : each;
 }
-// A stream kernel pays off from this many rows per slice on (backward, 600 x 4096 bf16, two rows: 22 us against 39;
-// 1533 x 1111 fp16, rows not aligned, two: 35 against 32).
+// A stream kernel pays off from this many rows per slice on.  It against one row per CTA at 1, 2, 3, 4 and 6 rows, us:
+//   forward   2048 bf16   11, 11, 11.2, 11.8, 15 against 11, 11, 12.8, 14.9, 21     4096 fp32  11, 13, 15, 19, 27 against 11, 13, 17, 21, 27
+//             4097 bf16   12, 15, 19, 22, 29 against 11, 13, 19, 23, 33             1111 fp16  14, 17, 22, 25, 34 against 11, 13, 17, 21, 29
+//   backward  512 bf16    21, 21, 23, 26, 27 against 19, 21, 26, 28, 34             4096 bf16  17, 19, 21, 22, 28 against 30, 52, 58, 70, 87
+//             4097 bf16   38, 44, 49, 54, 68 against 34, 52, 71, 83, 146            1111 fp16  30, 34, 41, 46, 58 against 25, 33, 40, 50, 79
+// Short unaligned rows would rather have a higher bound forward (513 to 1111 columns lose up to 5 us), long ones a lower one
+// backward.
 constexpr int64_t kStreamRows = 3, kStreamRowsAlignedBackward = 1;
 
 }  // namespace
@@ -491,6 +502,10 @@ extern "C" int def_norm_backward(int32_t dtype, int64_t T, int64_t C, const void
             by_alignment(aligned_rows, [&](auto aligned) {
                 by_row_shape(C, [&](auto shape) {
                     using S = decltype(shape);
+                    // 4, 3 or 1 CTAs per SM.  At 1, 2, 3, 4, 6 of them, us: 1500 x 513 fp16 (96 threads) 40, 28, 25, 23, 26; 1000 x 257
+                    // bf16 (64) 28, 21, 20, 19, 21; 1533 x 1111 fp16 (160) 46, 32, 30, 40, 38; 1533 x 1001 bf16 (128) 44, 32,
+                    // 28, 28, 36; 400 x 4097 bf16 (288) 42, 58, 58, 58, 58; 300 x 8191 bf16 (512) 61, 88, 84, 85, 85.  The
+                    // exception: 800 x 2047 bf16 (256) 34, 30, 40, 42, 48.
                     a.parts_per_group = norm_parts(T, groups, S::threads(C) <= 128 ? 4 * kUsualSms : S::threads(C) <= 256 ? 3 * kUsualSms : kUsualSms);
                     deft::norm_backward_kernel<decltype(type), aligned.value, S::most, S::iters><<<(unsigned)(groups * a.parts_per_group), S::threads(C), 0, stream>>>(a);
                 });
@@ -543,7 +558,10 @@ GradPlan grad_plan(int32_t dtype, int64_t T, int64_t O, int64_t I, const void *d
     p.tiles_o = ceil_div(O, deft::kTileO);
     p.blocks = ceil_div(T, deft::kTileT);
     // A pair of CTAs per pair of SMs.  Rounds of whole tiles; the tiles of a last round that would leave a tenth of the
-    // pairs idle or more are cut by tokens into equal runs instead, which costs a pass over their partial sums.
+    // pairs idle or more are cut by tokens into equal runs instead, which costs a pass over their partial sums.  Whole against
+    // cut, 8192 tokens, I = 4096, bf16, us: 16 tiles of a round of 74 66 against 29, 32 67 against 44, 48 67 against 58, 64
+    // 68 against 73; a round and 6 tiles 131 against 82, one and 54 129 against 128, two and 12 223 against 171.  The partial sums
+    // weigh more where tokens are few, and a tenth is then too little: 64 tiles of 512 tokens 19 against 33.
     const int64_t tiles = p.tiles_i * p.tiles_o, workers = sms / 2, rest = tiles % workers, per_tile = p.blocks * p.planes;
     p.whole = rest * 10 >= workers * 9 || per_tile == 1 ? tiles : tiles - rest;
     const int64_t most = p.whole == 0 ? tiles * per_tile : tiles;
@@ -709,6 +727,9 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
 namespace {
 constexpr int64_t kLogprobNarrow = 24576;  // rows up to this go to CTAs of 128 threads, longer ones to CTAs of 512 (8192 rows of 20000:
                                            // 68 against 99 us; of 32000 fp32, top = 8: 203 against 186)
+// Least columns per CTA of a row that is cut, and what cutting gives, us: one row of 128000 bf16 forward 11.2 against 15.1 whole,
+// backward 8.2 against 12.3; 64 such rows 14.4 against 16.6, 8.3 against 14.4; one row of 20000 10.3 and 8.1 either way; 16
+// rows of 50001 bf16 12.3 against 10.3, 8.2 either way.
 constexpr int64_t kLogprobLeast = 4096;
 }  // namespace
 

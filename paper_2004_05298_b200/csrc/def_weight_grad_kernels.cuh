@@ -9,8 +9,8 @@
 // when it accumulates (16384 tokens in one chain are 7e-6 off), and a chain of 1024 keeps that at 2e-7.
 //
 // A pair of CTAs works on a 256 x 256 tile (cta_group::2): each brings half of either operand, which halves the reads of
-// shared memory per product.  8192 tokens, 8192 x 4096, bf16: 390 us in a burst (1.4 PFLOP/s, tensor pipe 81 % busy), 468
-// in a loop of seconds under the power cap; the same with 128 x 256 tiles of single CTAs: 530.
+// shared memory per product.  8192 tokens, 8192 x 4096, bf16: 390 to 413 us in a burst (1.3 to 1.4 PFLOP/s, tensor pipe 81 %
+// busy), 470 in a loop of seconds under the power cap; the same with 128 x 256 tiles of single CTAs: 530 in a burst.
 #pragma once
 
 #include <cuda.h>
