@@ -19,29 +19,29 @@ EPS = 1e-7
 def listed():
     return [
         # Recurrence over tokens.  One token of each of 64 sequences, states kept between calls: sampling while training.
-        {"name": "recurrence, 64 single tokens", "op": "rec_fwd", "dtype": "bfloat16", "T": 64, "C": 2048, "sequences": 64, "ragged": False, "state": True},
+        {"name": "recurrence 64 single tokens", "op": "rec_fwd", "dtype": "bfloat16", "T": 64, "C": 2048, "sequences": 64, "ragged": False, "state": True},
         # A training forward pass over a packed batch: eight documents of different lengths, padding at the end.
-        {"name": "recurrence, packed batch", "op": "rec_fwd", "dtype": "bfloat16", "T": 16384, "C": 4096, "sequences": 8, "ragged": True, "state": False},
+        {"name": "recurrence packed batch", "op": "rec_fwd", "dtype": "bfloat16", "T": 16384, "C": 4096, "sequences": 8, "ragged": True, "state": False},
         # One long document through a narrow fp32 model: few channels, so time itself has to be cut.
-        {"name": "recurrence, narrow and long", "op": "rec_fwd", "dtype": "float32", "T": 16384, "C": 512, "sequences": 1, "ragged": False, "state": True},
+        {"name": "recurrence narrow and long", "op": "rec_fwd", "dtype": "float32", "T": 16384, "C": 512, "sequences": 1, "ragged": False, "state": True},
         # Backward of a short ragged batch of odd width (rows are not aligned), with states carried in and out.
-        {"name": "recurrence back, odd", "op": "rec_bwd", "dtype": "float16", "T": 1533, "C": 1111, "sequences": 13, "ragged": True, "state": True},
+        {"name": "recurrence back odd", "op": "rec_bwd", "dtype": "float16", "T": 1533, "C": 1111, "sequences": 13, "ragged": True, "state": True},
         # Backward of the packed training batch.
-        {"name": "recurrence back, packed batch", "op": "rec_bwd", "dtype": "bfloat16", "T": 16384, "C": 4096, "sequences": 8, "ragged": True, "state": False},
+        {"name": "recurrence back packed batch", "op": "rec_bwd", "dtype": "bfloat16", "T": 16384, "C": 4096, "sequences": 8, "ragged": True, "state": False},
         # Feed-forward block.  One token: the weights are what has to be read.
-        {"name": "feed-forward, 1 token", "op": "ffn_fwd", "dtype": "bfloat16", "T": 1, "C": 2048, "F": 5632},
+        {"name": "feed-forward 1 token", "op": "ffn_fwd", "dtype": "bfloat16", "T": 1, "C": 2048, "F": 5632},
         # Evaluation of a small fp32 model.
-        {"name": "feed-forward, fp32", "op": "ffn_fwd", "dtype": "float32", "T": 1024, "C": 1024, "F": 2816},
+        {"name": "feed-forward fp32", "op": "ffn_fwd", "dtype": "float32", "T": 1024, "C": 1024, "F": 2816},
         # A training step's forward and backward pass through a small layer, ragged on all sides.
-        {"name": "feed-forward train, ragged", "op": "ffn_train", "dtype": "float16", "T": 1501, "C": 777, "F": 1000},
+        {"name": "feed-forward train ragged", "op": "ffn_train", "dtype": "float16", "T": 1501, "C": 777, "F": 1000},
         # The same for a large block and a whole batch: where the matrix products count.
-        {"name": "feed-forward train, large", "op": "ffn_train", "dtype": "bfloat16", "T": 8192, "C": 4096, "F": 10240},
+        {"name": "feed-forward train large", "op": "ffn_train", "dtype": "bfloat16", "T": 8192, "C": 4096, "F": 10240},
         # Orthogonalised updates.  One small weight of a language model in the gradient rows of four workers.
-        {"name": "orthogonalize, 4 small", "op": "ortho", "dtype": "float32", "batch": 4, "rows": 256, "cols": 640, "steps": 5},
+        {"name": "orthogonalize 4 small", "op": "ortho", "dtype": "float32", "batch": 4, "rows": 256, "cols": 640, "steps": 5},
         # A tall 16-bit momentum of odd sizes.
-        {"name": "orthogonalize, odd bf16", "op": "ortho", "dtype": "bfloat16", "batch": 1, "rows": 1000, "cols": 777, "steps": 5},
+        {"name": "orthogonalize odd bf16", "op": "ortho", "dtype": "bfloat16", "batch": 1, "rows": 1000, "cols": 777, "steps": 5},
         # The large projection of a block.
-        {"name": "orthogonalize, large", "op": "ortho", "dtype": "float32", "batch": 1, "rows": 4096, "cols": 10240, "steps": 5},
+        {"name": "orthogonalize large", "op": "ortho", "dtype": "float32", "batch": 1, "rows": 4096, "cols": 10240, "steps": 5},
     ]
 
 
