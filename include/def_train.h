@@ -168,6 +168,36 @@ int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const void *logits
                          int32_t top, const int64_t *top_ids, const float *dtop_logp, void *dlogits, int64_t lddx,
                          void *cuda_stream);
 
+/*
+ * Gated linear recurrence over the tokens of packed sequences, channel by channel:
+ *     c_t = 1 / (1 + exp(g_t)),  a_t = 1 - c_t,     h_t = a_t h_{t-1} + c_t x_t,     y_t = h_t
+ * x, gate (the logits g), y: [T, C], T <= 2^30.  Sequence s holds rows [offsets[s], offsets[s + 1]) (offsets: sequences + 1
+ * numbers in device memory, 8-byte aligned, not decreasing; sequences may be empty), or, with offsets NULL, the s-th of
+ * `sequences` equally long runs (T must be a multiple).  Rows of no sequence are neither read nor written.  Offsets that
+ * decrease or leave [0, T] do no harm outside the arguments, but what is computed then is not specified.
+ * h0, h_last [sequences, C] fp32: the state before a sequence's first token (NULL: 0) and behind its last one (NULL: not
+ * written; a sequence without tokens hands on its h0).  y may be x itself (same stride) where no backward pass will need x.
+ * One token of each sequence: T = sequences, offsets NULL, h_last of one call is the next one's h0.
+ * The state is fp32; an infinity or a NaN stays within its sequence and channel.
+ * The workspace holds maps of parts of long narrow calls; def_recurrence_workspace says how much is needed (at most
+ * 4096 C bytes; the same forward and backward).
+ */
+int def_recurrence_forward(int32_t dtype, int64_t T, int64_t C, int64_t sequences, const int64_t *offsets, const void *x,
+                           int64_t ldx, const void *gate, int64_t ldg, const float *h0, void *y, int64_t ldy, float *h_last,
+                           void *workspace, int64_t workspace_bytes, void *cuda_stream);
+int def_recurrence_workspace(int32_t dtype, int64_t T, int64_t C, int64_t *bytes_out);
+
+/*
+ * Its backward pass, from y as stored by the forward call.  With h_{t-1} = y_{t-1} (h0 or 0 before the first token):
+ *     lambda_t = dy_t + a_{t+1} lambda_{t+1}   (the last token: dy_t + dh_last, dh_last NULL: 0)
+ *     dx_t = c_t lambda_t,   dgate_t = lambda_t a_t c_t (h_{t-1} - x_t),   dh0 = a_1 lambda_1 of the first token
+ * dh0 [sequences, C] may be NULL; without tokens it is dh_last.  dx and dgate overlap no input.
+ */
+int def_recurrence_backward(int32_t dtype, int64_t T, int64_t C, int64_t sequences, const int64_t *offsets, const void *dy,
+                            int64_t lddy, const float *dh_last, const void *x, int64_t ldx, const void *gate, int64_t ldg,
+                            const void *y, int64_t ldy, const float *h0, void *dx, int64_t lddx, void *dgate, int64_t lddg,
+                            float *dh0, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -70,6 +70,10 @@ SIGNATURES = {
     "def_norm_backward_workspace": (ctypes.c_int, [_i64, _i64, _i64, _ptr]),
     "def_logprob_forward": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _i64] + [_ptr] * 4 + [_i32] + [_ptr] * 3),
     "def_logprob_backward": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _i64] + [_ptr] * 5 + [_i32] + [_ptr] * 3 + [_i64, _ptr]),
+    "def_recurrence_workspace": (ctypes.c_int, [_i32, _i64, _i64, _ptr]),
+    "def_recurrence_forward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _ptr] + [_ptr, _i64] * 2 + [_ptr, _ptr, _i64, _ptr, _ptr, _i64, _ptr]),
+    "def_recurrence_backward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _ptr, _ptr, _i64, _ptr] + [_ptr, _i64] * 3 + [_ptr] + [_ptr, _i64] * 2
+                                + [_ptr, _ptr, _i64, _ptr]),
 }
 
 
@@ -559,3 +563,53 @@ def def_logprob_backward(logits, targets, lse, entropy, dlogits, dlogp=None, den
                                     _need(entropy, "entropy", (T,)), _param(dlogp, "dlogp", (T,)), _param(dentropy, "dentropy", (T,)), top,
                                     _param(top_ids, "top_ids", (T, top), torch.int64), _param(dtop_logp, "dtop_logp", (T, top)),
                                     *_act(dlogits, "dlogits", a)[3:], _stream(stream)))
+
+
+def _same_device(first, *others):
+    """All on one GPU, the current one (where work is enqueued)."""
+    at = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != at:
+            raise ValueError("the tensors must live on one GPU")
+    if at != torch.cuda.current_device():
+        raise ValueError("the tensors live on GPU %d, but GPU %d is the current device" % (at, torch.cuda.current_device()))
+
+
+def _sequences(offsets, sequences, T):
+    """(offsets pointer, number of sequences)."""
+    if offsets is None:
+        return None, int(sequences)
+    n = offsets.numel() - 1 if isinstance(offsets, torch.Tensor) else 0
+    if sequences not in (1, n):
+        raise ValueError("offsets tells of %d sequences, expected %d" % (n, sequences))
+    return _need(offsets, "offsets", (n + 1,), torch.int64), n
+
+
+def def_recurrence_workspace(T, C, dtype=torch.float32):
+    out = ctypes.c_int64(0)
+    _check(lib.def_recurrence_workspace(_DTYPES[dtype], int(T), int(C), ctypes.byref(out)))
+    return int(out.value)
+
+
+def def_recurrence_forward(x, gate, y, h0=None, h_last=None, sequences=1, offsets=None, workspace=None, stream=None):
+    """y_t = h_t = a_t h_{t-1} + (1 - a_t) x_t, a = sigmoid(gate), along the rows of each sequence.  offsets: int64
+    [sequences + 1], or None for equally long ones; h0, h_last: float32 [sequences, C]."""
+    a = _act(x, "x")
+    dt, T, C = a[:3]
+    o, S = _sequences(offsets, sequences, T)
+    w, nw = _work(workspace, "workspace")
+    args = (dt, T, C, S, o, *a[3:], *_act(gate, "gate", a)[3:], _param(h0, "h0", (S, C)), *_act(y, "y", a)[3:], _param(h_last, "h_last", (S, C)), w, nw)
+    _same_device(x, gate, y, h0, h_last, offsets, workspace)
+    _check(lib.def_recurrence_forward(*args, _stream(stream)))
+
+
+def def_recurrence_backward(dy, x, gate, y, dx, dgate, h0=None, dh_last=None, dh0=None, sequences=1, offsets=None, workspace=None, stream=None):
+    """Gradients of x, gate and h0 from those of y and h_last; y as the forward call stored it."""
+    a = _act(x, "x")
+    dt, T, C = a[:3]
+    o, S = _sequences(offsets, sequences, T)
+    w, nw = _work(workspace, "workspace")
+    args = (dt, T, C, S, o, *_act(dy, "dy", a)[3:], _param(dh_last, "dh_last", (S, C)), *a[3:], *_act(gate, "gate", a)[3:], *_act(y, "y", a)[3:],
+            _param(h0, "h0", (S, C)), *_act(dx, "dx", a)[3:], *_act(dgate, "dgate", a)[3:], _param(dh0, "dh0", (S, C)), w, nw)
+    _same_device(x, dy, gate, y, dx, dgate, h0, dh_last, dh0, offsets, workspace)
+    _check(lib.def_recurrence_backward(*args, _stream(stream)))
