@@ -198,6 +198,42 @@ int def_recurrence_backward(int32_t dtype, int64_t T, int64_t C, int64_t sequenc
                             const void *y, int64_t ldy, const float *h0, void *dx, int64_t lddx, void *dgate, int64_t lddg,
                             float *dh0, void *workspace, int64_t workspace_bytes, void *cuda_stream);
 
+/*
+ * Gated feed-forward block, one kernel per product, with the activation in the first one's epilogue:
+ *     [g | u] = x w_in^T,   h = silu(g) u,   out = h w_down^T
+ * x [T, C], h [T, F], out [T, O]; w_in [2F, C]: the gate's F rows, then those of u, and w_down [O, F], both contiguous, of
+ * type dtype.  g and u stay in fp32; h is rounded to dtype once, and the second product takes it so.  w_down and out NULL:
+ * h only.  gate_q/gate_e, up_q/up_e: checkpoints of g and u (of the fp32 values) for the backward pass; all NULL or all given.
+ * 16-bit types: exact products, summed in fp32.  fp32: operands in three bf16 pieces of 8 bits, the six products of pieces
+ * that reach 2^-24 (an infinity may give NaN).  T <= 2^30, F <= 2^29.
+ * The workspace holds the pieces of fp32 operands, and aligned copies of operands whose rows are not multiples of 16 bytes
+ * or do not start on them; the second call says how much is needed for the same arguments: at most, with r(n) = n + 7 and
+ * P = 3 for fp32, 1 else, 2 P (T r(C) + 2F r(C) + T r(F) + O r(F)) bytes.
+ */
+int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *x, int64_t ldx, const void *w_in,
+                     const void *w_down, void *h, int64_t ldh, void *out, int64_t ldout, int8_t *gate_q, uint8_t *gate_e,
+                     int8_t *up_q, uint8_t *up_e, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+int def_feed_forward_workspace(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *x, int64_t ldx,
+                               const void *w_in, const void *w_down, const void *h, int64_t ldh, int64_t *bytes_out);
+
+/*
+ * Its backward pass from the checkpoints (g^, u^), s = 1 / (1 + exp(-g^)):
+ *     dh = dout w_down,   dgate = dh u^ s (1 + g^ (1 - s)),   dup = dh g^ s,   dx = [dgate | dup] w_in,   h^ = g^ s u^
+ * dout [T, O]; dboth [T, 2F]: dgate in its first F columns, dup in the others; dx [T, C] (w_in and dx NULL: not computed).
+ * dh stays in fp32; dboth is rounded to dtype once, and the product for dx takes it so.  h^ is written as values (h_out
+ * [T, F]) and / or as a checkpoint of those values (h_q, h_e); NULL skips either.  The weights' gradients are
+ * def_checkpoint_weight_grad of dboth with the checkpoint of x, and of dout with that of h^.
+ * The workspace is as above, for dout, w_down, dboth and w_in.
+ */
+int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *dout, int64_t lddout,
+                              const void *w_in, const void *w_down, const int8_t *gate_q, const uint8_t *gate_e,
+                              const int8_t *up_q, const uint8_t *up_e, void *dboth, int64_t lddb, void *dx, int64_t lddx,
+                              void *h_out, int64_t ldh, int8_t *h_q, uint8_t *h_e, void *workspace,
+                              int64_t workspace_bytes, void *cuda_stream);
+int def_feed_forward_backward_workspace(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *dout,
+                                        int64_t lddout, const void *w_in, const void *w_down, const void *dboth, int64_t lddb,
+                                        int64_t *bytes_out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -72,6 +72,10 @@ SIGNATURES = {
     "def_logprob_backward": (ctypes.c_int, [_i32, _i64, _i64, _ptr, _i64] + [_ptr] * 5 + [_i32] + [_ptr] * 3 + [_i64, _ptr]),
     "def_recurrence_workspace": (ctypes.c_int, [_i32, _i64, _i64, _ptr]),
     "def_recurrence_forward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _ptr] + [_ptr, _i64] * 2 + [_ptr, _ptr, _i64, _ptr, _ptr, _i64, _ptr]),
+    "def_feed_forward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _i64, _ptr, _i64, _ptr, _ptr] + [_ptr, _i64] * 2 + [_ptr] * 5 + [_i64, _ptr]),
+    "def_feed_forward_workspace": (ctypes.c_int, [_i32, _i64, _i64, _i64, _i64, _ptr, _i64, _ptr, _ptr, _ptr, _i64, _ptr]),
+    "def_feed_forward_backward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _i64, _ptr, _i64] + [_ptr] * 6 + [_ptr, _i64] * 3 + [_ptr] * 3 + [_i64, _ptr]),
+    "def_feed_forward_backward_workspace": (ctypes.c_int, [_i32, _i64, _i64, _i64, _i64, _ptr, _i64, _ptr, _ptr, _ptr, _i64, _ptr]),
     "def_recurrence_backward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _ptr, _ptr, _i64, _ptr] + [_ptr, _i64] * 3 + [_ptr] + [_ptr, _i64] * 2
                                 + [_ptr, _ptr, _i64, _ptr]),
 }
@@ -613,3 +617,79 @@ def def_recurrence_backward(dy, x, gate, y, dx, dgate, h0=None, dh_last=None, dh
             _param(h0, "h0", (S, C)), *_act(dx, "dx", a)[3:], *_act(dgate, "dgate", a)[3:], _param(dh0, "dh0", (S, C)), w, nw)
     _same_device(x, dy, gate, y, dx, dgate, h0, dh_last, dh0, offsets, workspace)
     _check(lib.def_recurrence_backward(*args, _stream(stream)))
+
+
+def _weights(t, name, like, shape=None):
+    """Pointer of a contiguous matrix of the activations' type, and its shape."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise TypeError("%s must be a two-dimensional torch tensor" % name)
+    shape = tuple(t.shape) if shape is None else shape
+    return _param(t, name, shape, like.dtype), shape
+
+
+def _feed_shapes(x, w_in, w_down):
+    """(pointer of w_in, pointer of w_down or None, F, O) for activations x [T, C]."""
+    wi, (rows, C) = _weights(w_in, "w_in", x)
+    if rows % 2 or C != x.shape[1]:
+        raise ValueError("w_in has shape %s, expected (2F, %d)" % ((rows, C), x.shape[1]))
+    F = rows // 2
+    if w_down is None:
+        return wi, None, F, 1
+    wd, (O, cols) = _weights(w_down, "w_down", x)
+    if cols != F:
+        raise ValueError("w_down has shape %s, expected (O, %d)" % ((O, cols), F))
+    return wi, wd, F, O
+
+
+def def_feed_forward_workspace(x, w_in, w_down, h):
+    dt, T, C, p, ld = _act(x, "x")
+    wi, wd, F, O = _feed_shapes(x, w_in, w_down)
+    out = ctypes.c_int64(0)
+    _check(lib.def_feed_forward_workspace(dt, T, C, F, O, p, ld, wi, wd, *_act(h, "h", (dt, T, F))[3:], ctypes.byref(out)))
+    return int(out.value)
+
+
+def def_feed_forward(x, w_in, w_down, h, out, gate_ck=None, up_ck=None, workspace=None, stream=None):
+    """h = silu(x w_in[:F]^T) (x w_in[F:]^T), out = h w_down^T; w_down and out None: h only.  gate_ck, up_ck: checkpoints of
+    the two products for the backward pass."""
+    dt, T, C, p, ld = _act(x, "x")
+    wi, wd, F, O = _feed_shapes(x, w_in, w_down)
+    gq, ge = _held(gate_ck, "gate checkpoint", T, F)
+    uq, ue = _held(up_ck, "up checkpoint", T, F)
+    w, nw = _work(workspace, "workspace")
+    args = (dt, T, C, F, O, p, ld, wi, wd, *_act(h, "h", (dt, T, F))[3:], *_opt_act(out, "out", (dt, T, O)), gq, ge, uq, ue, w, nw)
+    _same_device(x, w_in, w_down, h, out, workspace, *(gate_ck or ()), *(up_ck or ()))
+    _check(lib.def_feed_forward(*args, _stream(stream)))
+
+
+def def_feed_forward_backward_workspace(dout, w_in, w_down, dboth):
+    dt, T, O, p, ld = _act(dout, "dout")
+    wd, (_, F) = _weights(w_down, "w_down", dout)
+    wi, C = (None, 1) if w_in is None else (_weights(w_in, "w_in", dout)[0], w_in.shape[1])
+    out = ctypes.c_int64(0)
+    _check(lib.def_feed_forward_backward_workspace(dt, T, C, F, O, p, ld, wi, wd, *_act(dboth, "dboth", (dt, T, 2 * F))[3:], ctypes.byref(out)))
+    return int(out.value)
+
+
+def def_feed_forward_backward(dout, w_in, w_down, gate_ck, up_ck, dboth, dx, h_out=None, h_ck=None, workspace=None, stream=None):
+    """dboth [T, 2F]: the gradients of the two products of def_feed_forward, side by side; dx = dboth w_in (w_in and dx None:
+    not computed); h_out, h_ck: the recomputed h as values and as a checkpoint."""
+    dt, T, O, p, ld = _act(dout, "dout")
+    wd, (rows, F) = _weights(w_down, "w_down", dout)
+    if rows != O:
+        raise ValueError("w_down has shape %s, expected (%d, F)" % ((rows, F), O))
+    wi, C = None, 1
+    if w_in is not None:
+        wi, (rows, C) = _weights(w_in, "w_in", dout)
+        if rows != 2 * F:
+            raise ValueError("w_in has shape %s, expected (%d, C)" % ((rows, C), 2 * F))
+    if gate_ck is None or up_ck is None:
+        raise DefError(DEF_ERR_NULL, "the checkpoints of gate and up must not be None")
+    gq, ge = _held(gate_ck, "gate checkpoint", T, F)
+    uq, ue = _held(up_ck, "up checkpoint", T, F)
+    hq, he = _held(h_ck, "h checkpoint", T, F)
+    w, nw = _work(workspace, "workspace")
+    args = (dt, T, C, F, O, p, ld, wi, wd, gq, ge, uq, ue, *_act(dboth, "dboth", (dt, T, 2 * F))[3:], *_opt_act(dx, "dx", (dt, T, C)),
+            *_opt_act(h_out, "h_out", (dt, T, F)), hq, he, w, nw)
+    _same_device(dout, w_in, w_down, dboth, dx, h_out, workspace, *gate_ck, *up_ck, *(h_ck or ()))
+    _check(lib.def_feed_forward_backward(*args, _stream(stream)))

@@ -1,0 +1,168 @@
+// C boundary of the gated feed-forward block (see include/def_train.h).
+#include "def_feed_kernels.cuh"
+#include "def_product_launch.cuh"
+
+namespace {
+
+struct FeedPlan {
+    Operand x, w_in, h, w_down;
+    int64_t bytes() const { return x.bytes + w_in.bytes + h.bytes + w_down.bytes; }
+};
+// x [T, C] and w_in [2F, C]; h [T, F] and w_down [O, F] (w_down NULL: without the second product).
+FeedPlan feed_plan(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *x, int64_t ldx, const void *w_in, const void *w_down, const void *h,
+                   int64_t ldh) {
+    FeedPlan p = {operand(dtype, x, T, C, ldx), operand(dtype, w_in, 2 * F, C, C), {}, {}};
+    if (w_down) {
+        p.h = operand(dtype, h, T, F, ldh);
+        p.w_down = operand(dtype, w_down, O, F, F);
+    }
+    return p;
+}
+int check_feed(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O) {
+    DEF_TRY(check_rows(dtype, T, C, "C"));
+    DEF_TRY(check_rows(dtype, T, F, "F"));
+    DEF_TRY(check_rows(dtype, T, O, "O"));
+    if (T > (int64_t)1 << 30 || F > (int64_t)1 << 29) return fail(DEF_ERR_ARG, "T must be at most 2^30 and F at most 2^29");
+    return DEF_OK;
+}
+int check_workspace(const void *workspace, int64_t bytes, int64_t need) {
+    if (need > 0 && !workspace) return fail(DEF_ERR_NULL, "workspace must not be NULL");
+    if (bytes < need) return fail(DEF_ERR_ARG, "the workspace must have %lld bytes (got %lld)", (long long)need, (long long)bytes);
+    return DEF_OK;
+}
+View weights_view(const void *p, const char *name, int64_t rows, int64_t cols, int64_t es) { return rows_view(p, name, p ? 1 : 0, rows * cols, rows * cols, es, false); }
+
+}  // namespace
+
+extern "C" int def_feed_forward_workspace(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *x, int64_t ldx, const void *w_in,
+                                          const void *w_down, const void *h, int64_t ldh, int64_t *bytes_out) {
+    if (!bytes_out) return fail(DEF_ERR_NULL, "bytes_out must not be NULL");
+    DEF_TRY(check_feed(dtype, T, C, F, O));
+    DEF_TRY(check_stride(x, ldx, C, T, "x"));
+    DEF_TRY(check_stride(h, ldh, F, T, "h"));
+    *bytes_out = feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh).bytes();
+    return DEF_OK;
+}
+
+extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *x, int64_t ldx, const void *w_in, const void *w_down,
+                                void *h, int64_t ldh, void *out, int64_t ldout, int8_t *gate_q, uint8_t *gate_e, int8_t *up_q, uint8_t *up_e,
+                                void *workspace, int64_t workspace_bytes, void *cuda_stream) {
+    int64_t need = 0;
+    DEF_TRY(def_feed_forward_workspace(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh, &need));
+    if (T == 0) return DEF_OK;
+    if (!x || !w_in || !h) return fail(DEF_ERR_NULL, "x, w_in and h must not be NULL");
+    if (!w_down != !out) return fail(DEF_ERR_NULL, "w_down and out must both be given or both be NULL");
+    DEF_TRY(check_pair(gate_q, gate_e, "gate"));
+    DEF_TRY(check_pair(up_q, up_e, "up"));
+    if (!gate_q != !up_q) return fail(DEF_ERR_NULL, "the checkpoints of gate and up must both be given or both be NULL");
+    DEF_TRY(check_stride(out, ldout, O, T, "out"));
+    DEF_TRY(check_workspace(workspace, workspace_bytes, need));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(x, "x", T, C, ldx, es, false), weights_view(w_in, "w_in", 2 * F, C, es), weights_view(w_down, "w_down", O, F, es),
+                          rows_view(h, "h", T, F, ldh, es, true), rows_view(out, "out", T, O, ldout, es, true), q_view(gate_q, "gate_q", T, F, true),
+                          e_view(gate_e, "gate_e", T, F, true), q_view(up_q, "up_q", T, F, true), e_view(up_e, "up_e", T, F, true),
+                          {workspace, "workspace", need > 0 ? 1 : 0, need, need, 16, true}};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    FeedPlan p = feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh);
+    char *at = (char *)workspace;
+    for (Operand *o : {&p.x, &p.w_in, &p.h, &p.w_down}) place(*o, at);
+    // The maps first: nothing is launched where the driver refuses one.
+    CUtensorMap map_x, map_in, map_h, map_down;
+    DEF_TRY(operand_map(map_x, dtype, p.x, false));
+    DEF_TRY(operand_map(map_in, dtype, p.w_in, false));
+    if (w_down) {
+        DEF_TRY(operand_map(map_h, dtype, p.h, false));
+        DEF_TRY(operand_map(map_down, dtype, p.w_down, false));
+    }
+    DEF_TRY(fill(p.x, dtype, x, ldx, stream, "def_feed_forward (x)"));
+    DEF_TRY(fill(p.w_in, dtype, w_in, C, stream, "def_feed_forward (w_in)"));
+    int rc = DEF_OK;
+    by_dtype(dtype, [&](auto type) {
+        using E = decltype(type);
+        const deft::StoreGated<E> store = {(E *)h, ldh, T, F, q_stride(F), e_stride(F), gate_q, up_q, gate_e, up_e, wide(h, ldh, es)};
+        rc = launch_product<false>(product_of(dtype, T, ceil_div(F, deft::kTileRows), C, deft::kTileRows, (int)F), store, map_x, map_in, stream, "def_feed_forward");
+    });
+    if (rc != DEF_OK || !w_down) return rc;
+    DEF_TRY(fill(p.h, dtype, h, ldh, stream, "def_feed_forward (h)"));
+    DEF_TRY(fill(p.w_down, dtype, w_down, F, stream, "def_feed_forward (w_down)"));
+    by_dtype(dtype, [&](auto type) {
+        using E = decltype(type);
+        const deft::StoreRows<E> store = {(E *)out, ldout, T, O, wide(out, ldout, es)};
+        rc = launch_product<false>(product_of(dtype, T, ceil_div(O, deft::kTileCols), F, deft::kTileCols, deft::kTileRows), store, map_h, map_down, stream,
+                                   "def_feed_forward (out)");
+    });
+    return rc;
+}
+
+extern "C" int def_feed_forward_backward_workspace(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *dout, int64_t lddout, const void *w_in,
+                                                   const void *w_down, const void *dboth, int64_t lddb, int64_t *bytes_out) {
+    if (!bytes_out) return fail(DEF_ERR_NULL, "bytes_out must not be NULL");
+    DEF_TRY(check_feed(dtype, T, C, F, O));
+    DEF_TRY(check_stride(dout, lddout, O, T, "dout"));
+    DEF_TRY(check_stride(dboth, lddb, 2 * F, T, "dboth"));
+    *bytes_out = operand(dtype, dout, T, O, lddout).bytes + operand(dtype, w_down, O, F, F).bytes +
+                 (w_in ? operand(dtype, dboth, T, 2 * F, lddb).bytes + operand(dtype, w_in, 2 * F, C, C).bytes : 0);
+    return DEF_OK;
+}
+
+extern "C" int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *dout, int64_t lddout, const void *w_in,
+                                         const void *w_down, const int8_t *gate_q, const uint8_t *gate_e, const int8_t *up_q, const uint8_t *up_e,
+                                         void *dboth, int64_t lddb, void *dx, int64_t lddx, void *h_out, int64_t ldh, int8_t *h_q, uint8_t *h_e,
+                                         void *workspace, int64_t workspace_bytes, void *cuda_stream) {
+    int64_t need = 0;
+    DEF_TRY(def_feed_forward_backward_workspace(dtype, T, C, F, O, dout, lddout, w_in, w_down, dboth, lddb, &need));
+    if (T == 0) return DEF_OK;
+    if (!dout || !w_down || !gate_q || !gate_e || !up_q || !up_e || !dboth)
+        return fail(DEF_ERR_NULL, "dout, w_down, the checkpoints of gate and up, and dboth must not be NULL");
+    if (!w_in != !dx) return fail(DEF_ERR_NULL, "w_in and dx must both be given or both be NULL");
+    DEF_TRY(check_pair(h_q, h_e, "h"));
+    DEF_TRY(check_stride(dx, lddx, C, T, "dx"));
+    DEF_TRY(check_stride(h_out, ldh, F, T, "h_out"));
+    DEF_TRY(check_workspace(workspace, workspace_bytes, need));
+    const int es = element_size(dtype);
+    const View views[] = {rows_view(dout, "dout", T, O, lddout, es, false), weights_view(w_in, "w_in", 2 * F, C, es), weights_view(w_down, "w_down", O, F, es),
+                          q_view(gate_q, "gate_q", T, F, false), e_view(gate_e, "gate_e", T, F, false), q_view(up_q, "up_q", T, F, false),
+                          e_view(up_e, "up_e", T, F, false), rows_view(dboth, "dboth", T, 2 * F, lddb, es, true), rows_view(dx, "dx", T, C, lddx, es, true),
+                          rows_view(h_out, "h_out", T, F, ldh, es, true), q_view(h_q, "h_q", T, F, true), e_view(h_e, "h_e", T, F, true),
+                          {workspace, "workspace", need > 0 ? 1 : 0, need, need, 16, true}};
+    DEF_TRY(check_views(views));
+    if (const int sms = sm_count(); sms < 0) return sms;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    Operand a = operand(dtype, dout, T, O, lddout), down = operand(dtype, w_down, O, F, F), both = {}, in = {};
+    if (dx) {
+        both = operand(dtype, dboth, T, 2 * F, lddb);
+        in = operand(dtype, w_in, 2 * F, C, C);
+    }
+    char *at = (char *)workspace;
+    for (Operand *o : {&a, &down, &both, &in}) place(*o, at);
+    CUtensorMap map_a, map_down, map_both, map_in;
+    DEF_TRY(operand_map(map_a, dtype, a, false));
+    DEF_TRY(operand_map(map_down, dtype, down, true));
+    if (dx) {
+        DEF_TRY(operand_map(map_both, dtype, both, false));
+        DEF_TRY(operand_map(map_in, dtype, in, true));
+    }
+    DEF_TRY(fill(a, dtype, dout, lddout, stream, "def_feed_forward_backward (dout)"));
+    DEF_TRY(fill(down, dtype, w_down, F, stream, "def_feed_forward_backward (w_down)"));
+    int rc = DEF_OK;
+    by_dtype(dtype, [&](auto type) {
+        using E = decltype(type);
+        E *dgate = (E *)dboth, *dup = dgate + F;
+        const deft::StoreGatedBack<E> store = {dgate, dup, (E *)h_out, lddb, ldh, T, F, q_stride(F), e_stride(F), gate_q, up_q, gate_e, up_e, h_q, h_e,
+                                               wide(dgate, lddb, es), wide(dup, lddb, es), wide(h_out, ldh, es)};
+        rc = launch_product<true>(product_of(dtype, T, ceil_div(F, deft::kTileCols), O, deft::kTileCols, deft::kTileRows), store, map_a, map_down, stream,
+                                  "def_feed_forward_backward");
+    });
+    if (rc != DEF_OK || !dx) return rc;
+    DEF_TRY(fill(both, dtype, dboth, lddb, stream, "def_feed_forward_backward (dboth)"));
+    DEF_TRY(fill(in, dtype, w_in, C, stream, "def_feed_forward_backward (w_in)"));
+    by_dtype(dtype, [&](auto type) {
+        using E = decltype(type);
+        const deft::StoreRows<E> store = {(E *)dx, lddx, T, C, wide(dx, lddx, es)};
+        rc = launch_product<true>(product_of(dtype, T, ceil_div(C, deft::kTileCols), 2 * F, deft::kTileCols, deft::kTileRows), store, map_both, map_in, stream,
+                                  "def_feed_forward_backward (dx)");
+    });
+    return rc;
+}

@@ -1,0 +1,108 @@
+// Host side of the products on tensor cores: operands, their tensor maps, the launch.
+#pragma once
+
+#include "def_planes_kernels.cuh"
+#include "def_product_kernels.cuh"
+#include "def_train_checks.cuh"
+
+namespace {
+
+// An operand [rows, cols] as the kernels take it: where it lies, or the 16-bit pieces that a copy of it is cut into.
+struct Operand {
+    const void *p;
+    int64_t rows, cols, ld;
+    bool copy;
+    int planes;
+    int64_t bytes;                          // of the copy
+};
+Operand operand(int32_t dtype, const void *p, int64_t rows, int64_t cols, int64_t ld) {
+    const int es = element_size(dtype);
+    Operand o = {p, rows, cols, rows > 1 ? ld : ceil_div(cols, 8) * 8, false, es == 4 ? 3 : 1, 0};
+    o.copy = es == 4 || !wide(p, o.ld, es) || o.ld >= ((int64_t)1 << 40) / es;
+    if (o.copy) {
+        o.ld = ceil_div(cols, 8) * 8;
+        o.bytes = o.planes * rows * o.ld * 2;
+    }
+    return o;
+}
+// Where the copy goes in the workspace; `at` moves on behind it.
+void place(Operand &o, char *&at) {
+    if (!o.copy) return;
+    o.p = at;
+    at += o.bytes;
+}
+int fill(const Operand &o, int32_t dtype, const void *from, int64_t ld, cudaStream_t stream, const char *what) {
+    if (!o.copy) return DEF_OK;
+    on_plane(false, o.rows, o.cols, [&](auto, dim3 grid, dim3 block) {
+        uint4 *out = (uint4 *)const_cast<void *>(o.p);
+        if (dtype == DEF_DTYPE_F32) deft::planes_kernel<float><<<grid, block, 0, stream>>>((const float *)from, ld, o.rows, (int)o.cols, out, o.ld);
+        else deft::planes_kernel<__half><<<grid, block, 0, stream>>>((const __half *)from, ld, o.rows, (int)o.cols, out, o.ld);
+    });
+    return launched(what);
+}
+
+// Map of [z][rows][cols] 16-bit elements in boxes of 64 columns and `box_rows` rows.
+int operand_map(CUtensorMap &map, bool half, const void *p, int64_t cols, int64_t rows, int64_t z, int64_t ld, int box_rows) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return fail(DEF_ERR_CUDA, "the driver does not offer tensor maps");
+    const cuuint64_t dim[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)z}, stride[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)(z > 1 ? rows : 1)};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+    if (encode(&map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dim, stride, box, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return fail(DEF_ERR_CUDA, "the driver refused a tensor map");
+    return DEF_OK;
+}
+int operand_map(CUtensorMap &map, int32_t dtype, const Operand &o, bool k_rows) {
+    return operand_map(map, dtype == DEF_DTYPE_F16, o.p, o.cols, o.rows, o.planes, o.ld, k_rows ? deft::kTileK : deft::kTileRows);
+}
+
+// fp32 values in three bf16 pieces of 8 bits each: the six products above 2^-24, small ones first.
+deft::Product product_of(int32_t dtype, int64_t m, int64_t tiles_n, int64_t k, int step_n, int second) {
+    deft::Product p = {};
+    p.tiles_m = (int)ceil_div(m, 2 * deft::kTileRows);
+    p.tiles_n = (int)tiles_n;
+    p.batch = 1;
+    p.blocks = (int)ceil_div(k, deft::kTileK);
+    const bool pieces = dtype == DEF_DTYPE_F32;
+    p.pairs = pieces ? 6 : 1;
+    p.planes_a = p.planes_b = pieces ? 3 : 1;
+    p.order_a = pieces ? 0x001102u : 0u;
+    p.order_b = pieces ? 0x010120u : 0u;
+    p.chunk = deft::kShortChain;
+    p.step_n = step_n;
+    p.second = second;
+    p.bf16 = dtype != DEF_DTYPE_F16;
+    return p;
+}
+
+template <bool BN, typename EPILOGUE>
+int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t stream, const char *what) {
+    const auto kernel = deft::product_kernel<EPILOGUE, BN>;
+    // The epilogue's warps take over registers that the others give up: those have to be there.
+    cudaFuncAttributes at;
+    cudaError_t err = cudaFuncGetAttributes(&at, kernel);
+    if (err == cudaSuccess && at.numRegs * deft::kProductThreads < 128 * 56 + 256 * 224) return fail(DEF_ERR_CUDA, "%s: built with too few registers", what);
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, deft::kProductSmem);
+    if (err == cudaSuccess) {
+        const int64_t n = p.triangle ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n, tiles = n * p.batch;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)((tiles < kUsualSms / 2 ? tiles : kUsualSms / 2) * 2));
+        cfg.blockDim = dim3(deft::kProductThreads);
+        cfg.dynamicSmemBytes = deft::kProductSmem;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        err = cudaLaunchKernelEx(&cfg, kernel, p, epilogue, map_a, map_b);
+    }
+    if (err == cudaSuccess) return DEF_OK;
+    cudaGetLastError();
+    return cuda_fail(err, what);
+}
+
+}  // namespace

@@ -72,3 +72,49 @@ def within(got, want, err, dtype):
     assert torch.equal(torch.isnan(got), torch.isnan(want))
     over = torch.nan_to_num((got - want).abs() - tol, nan=0.0)
     assert over.numel() == 0 or float(over.max()) <= 0, "off by %g beyond the bound" % float(over.max())
+
+
+def chain(n, pieces):
+    """What fp32 sums of n exact products on tensor cores may be off, relative to the magnitudes summed: 1024 terms in a chain that
+    truncates, 16 at a time, to a unit in the last place (64 u of 2 each), chains added in fp32, and, in pieces, the products that are
+    left out (mid lo, lo mid, lo lo: 3 times 2^-24)."""
+    return (2 * min(64, -(-n // 16)) + -(-n // 1024) + (3 + 6 if pieces else 0)) * U32
+
+
+def feed_forward(x, w_in, w_down=None, h_dtype=None):
+    """(g, u, h, out) in 64 bits and bounds for (g, u, h, out) before their rounding; out from h rounded to its type."""
+    dtype, x, w_in = x.dtype, x.double(), w_in.double()
+    F, pieces = w_in.shape[0] // 2, dtype == torch.float32
+    both, mag = x @ w_in.t(), x.abs() @ w_in.abs().t()
+    err = chain(x.shape[1], pieces) * mag
+    g, u, eg, eu = both[:, :F], both[:, F:], err[:, :F], err[:, F:]
+    h = g * torch.sigmoid(g) * u
+    # silu's slope is at most 1.1; the gate's own error is that of the logistic function, and three roundings
+    eh = 1.1 * eg * u.abs() + (g.abs() * eu + eg * eu) * torch.sigmoid(g).clamp(min=0) * 1.1 + h.abs() * (gate_error(g, dtype) + 4 * U32)
+    if w_down is None:
+        return (g, u, h, None), (eg, eu, eh, None)
+    w = w_down.double()
+    out = h @ w.t()
+    eo = (eh + h.abs() * (0 if pieces else UNIT[dtype])) @ w.abs().t() * 1.01 + chain(F, pieces) * (h.abs() @ w.abs().t())
+    return (g, u, h, out), (eg, eu, eh, eo)
+
+
+def feed_backward(dout, w_in, w_down, g, u):
+    """(dgate, dup, h^, dx) in 64 bits from the values g^, u^ that the checkpoints hold, and bounds before their rounding."""
+    dtype = dout.dtype
+    dout, w_in, w, g, u = (v.double() for v in (dout, w_in, w_down, g, u))
+    F, pieces = g.shape[1], dtype == torch.float32
+    dh, mag = dout @ w, dout.abs() @ w.abs()
+    edh = chain(dout.shape[1], pieces) * mag
+    s, e = torch.sigmoid(g), gate_error(g, dtype)
+    slope = s * (1 + g * (1 - s))
+    dg, du, h = dh * u * slope, dh * g * s, g * s * u
+    # s (1 + g (1 - s)): s is off by s e; 1 - s by s e + U32 absolutely; a few roundings of terms of at most s (1 + |g|)
+    e_slope = s * (1 + g.abs()) * (2 * e + 6 * U32)
+    edg = u.abs() * (edh * slope.abs() + (dh.abs() + edh) * e_slope) + 3 * U32 * dg.abs()
+    edu = (g * s).abs() * edh + du.abs() * (e + 4 * U32)
+    eh = h.abs() * (e + 4 * U32)
+    both, eboth = torch.cat([dg, du], 1), torch.cat([edg, edu], 1)
+    dx = both @ w_in
+    edx = (eboth + both.abs() * (0 if pieces else UNIT[dtype])) @ w_in.abs() * 1.01 + chain(2 * F, pieces) * (both.abs() @ w_in.abs())
+    return (dg, du, h, dx), (edg, edu, eh, edx)
