@@ -206,9 +206,9 @@ int def_recurrence_backward(int32_t dtype, int64_t T, int64_t C, int64_t sequenc
  * h only.  gate_q/gate_e, up_q/up_e: checkpoints of g and u (of the fp32 values) for the backward pass; all NULL or all given.
  * 16-bit types: exact products, summed in fp32.  fp32: operands in three bf16 pieces of 8 bits, the six products of pieces
  * that reach 2^-24 (an infinity may give NaN).  T <= 2^30, F <= 2^29.
- * The workspace holds the pieces of fp32 operands, and aligned copies of operands whose rows are not multiples of 16 bytes
- * or do not start on them; the second call says how much is needed for the same arguments: at most, with r(n) = n + 7 and
- * P = 3 for fp32, 1 else, 2 P (T r(C) + 2F r(C) + T r(F) + O r(F)) bytes.
+ * The workspace holds partial products where k is cut over CTAs, the pieces of fp32 operands, and aligned copies of operands
+ * whose rows are not multiples of 16 bytes or do not start on them; the second call says how much is needed for the same
+ * arguments: at most, with r(n) = n + 7 and P = 3 for fp32, 1 else, 20 MiB + 2 P (T r(C) + 2F r(C) + T r(F) + O r(F)) bytes.
  */
 int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *x, int64_t ldx, const void *w_in,
                      const void *w_down, void *h, int64_t ldh, void *out, int64_t ldout, int8_t *gate_q, uint8_t *gate_e,

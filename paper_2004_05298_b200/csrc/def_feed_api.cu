@@ -1,20 +1,48 @@
 // C boundary of the gated feed-forward block (see include/def_train.h).
+#include <algorithm>
+
 #include "def_feed_kernels.cuh"
 #include "def_product_launch.cuh"
 
 namespace {
 
+// Two products, one after the other, and their operands; the parts of cut tiles come first in the workspace.
 struct FeedPlan {
-    Operand x, w_in, h, w_down;
-    int64_t bytes() const { return x.bytes + w_in.bytes + h.bytes + w_down.bytes; }
+    Operand a1, b1, a2, b2;
+    deft::Product first, second;
+    int64_t parts;
+    int64_t bytes() const { return parts + a1.bytes + b1.bytes + a2.bytes + b2.bytes; }
+    void put(void *workspace) {
+        first.parts = second.parts = (float *)workspace;
+        char *at = (char *)workspace + parts;
+        for (Operand *o : {&a1, &b1, &a2, &b2}) place(*o, at);
+    }
 };
 // x [T, C] and w_in [2F, C]; h [T, F] and w_down [O, F] (w_down NULL: without the second product).
 FeedPlan feed_plan(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *x, int64_t ldx, const void *w_in, const void *w_down, const void *h,
                    int64_t ldh) {
-    FeedPlan p = {operand(dtype, x, T, C, ldx), operand(dtype, w_in, 2 * F, C, C), {}, {}};
+    FeedPlan p = {operand(dtype, x, T, C, ldx), operand(dtype, w_in, 2 * F, C, C)};
+    p.first = product_of(dtype, T, ceil_div(F, deft::kTileRows), C, deft::kTileRows, (int)F);
+    p.parts = plan_cuts(p.first);
     if (w_down) {
-        p.h = operand(dtype, h, T, F, ldh);
-        p.w_down = operand(dtype, w_down, O, F, F);
+        p.a2 = operand(dtype, h, T, F, ldh);
+        p.b2 = operand(dtype, w_down, O, F, F);
+        p.second = product_of(dtype, T, ceil_div(O, deft::kTileCols), F, deft::kTileCols, deft::kTileRows);
+        p.parts = std::max(p.parts, plan_cuts(p.second));
+    }
+    return p;
+}
+// dout [T, O] and w_down [O, F]; dboth [T, 2F] and w_in [2F, C] (w_in NULL: without the second product).
+FeedPlan back_plan(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *dout, int64_t lddout, const void *w_in, const void *w_down,
+                   const void *dboth, int64_t lddb) {
+    FeedPlan p = {operand(dtype, dout, T, O, lddout), operand(dtype, w_down, O, F, F)};
+    p.first = product_of(dtype, T, ceil_div(F, deft::kTileCols), O, deft::kTileCols, deft::kTileRows);
+    p.parts = plan_cuts(p.first);
+    if (w_in) {
+        p.a2 = operand(dtype, dboth, T, 2 * F, lddb);
+        p.b2 = operand(dtype, w_in, 2 * F, C, C);
+        p.second = product_of(dtype, T, ceil_div(C, deft::kTileCols), 2 * F, deft::kTileCols, deft::kTileRows);
+        p.parts = std::max(p.parts, plan_cuts(p.second));
     }
     return p;
 }
@@ -66,32 +94,30 @@ extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, 
     if (const int sms = sm_count(); sms < 0) return sms;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
     FeedPlan p = feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh);
-    char *at = (char *)workspace;
-    for (Operand *o : {&p.x, &p.w_in, &p.h, &p.w_down}) place(*o, at);
+    p.put(workspace);
     // The maps first: nothing is launched where the driver refuses one.
     CUtensorMap map_x, map_in, map_h, map_down;
-    DEF_TRY(operand_map(map_x, dtype, p.x, false));
-    DEF_TRY(operand_map(map_in, dtype, p.w_in, false));
+    DEF_TRY(operand_map(map_x, dtype, p.a1, false));
+    DEF_TRY(operand_map(map_in, dtype, p.b1, false));
     if (w_down) {
-        DEF_TRY(operand_map(map_h, dtype, p.h, false));
-        DEF_TRY(operand_map(map_down, dtype, p.w_down, false));
+        DEF_TRY(operand_map(map_h, dtype, p.a2, false));
+        DEF_TRY(operand_map(map_down, dtype, p.b2, false));
     }
-    DEF_TRY(fill(p.x, dtype, x, ldx, stream, "def_feed_forward (x)"));
-    DEF_TRY(fill(p.w_in, dtype, w_in, C, stream, "def_feed_forward (w_in)"));
+    DEF_TRY(fill(p.a1, dtype, x, ldx, stream, "def_feed_forward (x)"));
+    DEF_TRY(fill(p.b1, dtype, w_in, C, stream, "def_feed_forward (w_in)"));
     int rc = DEF_OK;
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreGated<E> store = {(E *)h, ldh, T, F, q_stride(F), e_stride(F), gate_q, up_q, gate_e, up_e, wide(h, ldh, es)};
-        rc = launch_product<false>(product_of(dtype, T, ceil_div(F, deft::kTileRows), C, deft::kTileRows, (int)F), store, map_x, map_in, stream, "def_feed_forward");
+        rc = launch_product<false, true>(p.first, store, map_x, map_in, stream, "def_feed_forward");
     });
     if (rc != DEF_OK || !w_down) return rc;
-    DEF_TRY(fill(p.h, dtype, h, ldh, stream, "def_feed_forward (h)"));
-    DEF_TRY(fill(p.w_down, dtype, w_down, F, stream, "def_feed_forward (w_down)"));
+    DEF_TRY(fill(p.a2, dtype, h, ldh, stream, "def_feed_forward (h)"));
+    DEF_TRY(fill(p.b2, dtype, w_down, F, stream, "def_feed_forward (w_down)"));
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreRows<E> store = {(E *)out, ldout, T, O, wide(out, ldout, es)};
-        rc = launch_product<false>(product_of(dtype, T, ceil_div(O, deft::kTileCols), F, deft::kTileCols, deft::kTileRows), store, map_h, map_down, stream,
-                                   "def_feed_forward (out)");
+        rc = launch_product<false, sizeof(E) == 4>(p.second, store, map_h, map_down, stream, "def_feed_forward (out)");
     });
     return rc;
 }
@@ -102,8 +128,7 @@ extern "C" int def_feed_forward_backward_workspace(int32_t dtype, int64_t T, int
     DEF_TRY(check_feed(dtype, T, C, F, O));
     DEF_TRY(check_stride(dout, lddout, O, T, "dout"));
     DEF_TRY(check_stride(dboth, lddb, 2 * F, T, "dboth"));
-    *bytes_out = operand(dtype, dout, T, O, lddout).bytes + operand(dtype, w_down, O, F, F).bytes +
-                 (w_in ? operand(dtype, dboth, T, 2 * F, lddb).bytes + operand(dtype, w_in, 2 * F, C, C).bytes : 0);
+    *bytes_out = back_plan(dtype, T, C, F, O, dout, lddout, w_in, w_down, dboth, lddb).bytes();
     return DEF_OK;
 }
 
@@ -130,39 +155,32 @@ extern "C" int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, in
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
-    Operand a = operand(dtype, dout, T, O, lddout), down = operand(dtype, w_down, O, F, F), both = {}, in = {};
-    if (dx) {
-        both = operand(dtype, dboth, T, 2 * F, lddb);
-        in = operand(dtype, w_in, 2 * F, C, C);
-    }
-    char *at = (char *)workspace;
-    for (Operand *o : {&a, &down, &both, &in}) place(*o, at);
+    FeedPlan p = back_plan(dtype, T, C, F, O, dout, lddout, w_in, w_down, dboth, lddb);
+    p.put(workspace);
     CUtensorMap map_a, map_down, map_both, map_in;
-    DEF_TRY(operand_map(map_a, dtype, a, false));
-    DEF_TRY(operand_map(map_down, dtype, down, true));
+    DEF_TRY(operand_map(map_a, dtype, p.a1, false));
+    DEF_TRY(operand_map(map_down, dtype, p.b1, true));
     if (dx) {
-        DEF_TRY(operand_map(map_both, dtype, both, false));
-        DEF_TRY(operand_map(map_in, dtype, in, true));
+        DEF_TRY(operand_map(map_both, dtype, p.a2, false));
+        DEF_TRY(operand_map(map_in, dtype, p.b2, true));
     }
-    DEF_TRY(fill(a, dtype, dout, lddout, stream, "def_feed_forward_backward (dout)"));
-    DEF_TRY(fill(down, dtype, w_down, F, stream, "def_feed_forward_backward (w_down)"));
+    DEF_TRY(fill(p.a1, dtype, dout, lddout, stream, "def_feed_forward_backward (dout)"));
+    DEF_TRY(fill(p.b1, dtype, w_down, F, stream, "def_feed_forward_backward (w_down)"));
     int rc = DEF_OK;
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         E *dgate = (E *)dboth, *dup = dgate + F;
         const deft::StoreGatedBack<E> store = {dgate, dup, (E *)h_out, lddb, ldh, T, F, q_stride(F), e_stride(F), gate_q, up_q, gate_e, up_e, h_q, h_e,
-                                               wide(dgate, lddb, es), wide(dup, lddb, es), wide(h_out, ldh, es)};
-        rc = launch_product<true>(product_of(dtype, T, ceil_div(F, deft::kTileCols), O, deft::kTileCols, deft::kTileRows), store, map_a, map_down, stream,
-                                  "def_feed_forward_backward");
+                                               wide(dgate, lddb, es) && wide(dup, lddb, es), wide(h_out, ldh, es)};
+        rc = launch_product<true, sizeof(E) == 4>(p.first, store, map_a, map_down, stream, "def_feed_forward_backward");
     });
     if (rc != DEF_OK || !dx) return rc;
-    DEF_TRY(fill(both, dtype, dboth, lddb, stream, "def_feed_forward_backward (dboth)"));
-    DEF_TRY(fill(in, dtype, w_in, C, stream, "def_feed_forward_backward (w_in)"));
+    DEF_TRY(fill(p.a2, dtype, dboth, lddb, stream, "def_feed_forward_backward (dboth)"));
+    DEF_TRY(fill(p.b2, dtype, w_in, C, stream, "def_feed_forward_backward (w_in)"));
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreRows<E> store = {(E *)dx, lddx, T, C, wide(dx, lddx, es)};
-        rc = launch_product<true>(product_of(dtype, T, ceil_div(C, deft::kTileCols), 2 * F, deft::kTileCols, deft::kTileRows), store, map_both, map_in, stream,
-                                  "def_feed_forward_backward (dx)");
+        rc = launch_product<true, sizeof(E) == 4>(p.second, store, map_both, map_in, stream, "def_feed_forward_backward (dx)");
     });
     return rc;
 }

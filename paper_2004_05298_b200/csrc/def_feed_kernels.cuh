@@ -4,23 +4,20 @@
 //     backward   dh = dout W_down,     dg = dh u s (1 + g (1 - s)),  du = dh g s,  h^ = g s u  from the checkpoints
 //
 // The first product's tile is 128 columns of g beside the same 128 of u: the two CTAs of a pair bring one each, and a thread
-// holds 64 of either, two groups of a checkpoint.  Nothing but h (or dg, du and h^) goes to memory in more than 8 bits.
+// holds 32 of either, a group of a checkpoint.  Nothing but h (or dg, du and h^) goes to memory in more than 8 bits.
 #pragma once
 
 #include "def_product_kernels.cuh"
 
 namespace deft {
 
-// A group of 32 columns that one thread holds, the first n of which exist.
-__device__ __forceinline__ uint32_t held_top(const float (&x)[32], int n) {
-    float top = 0.f;
+// Checkpoint of a group of 32 columns that one thread holds, the first n of which exist.
+template <typename V> __device__ __forceinline__ void store_group(int8_t *q, uint8_t *e, const V (&x)[32], int n) {
+    float most = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-        if (i < n) top = max_nan(top, fabsf(x[i]));
-    return __float_as_uint(top);
-}
-__device__ __forceinline__ void store_group(int8_t *q, uint8_t *e, const float (&x)[32], int n) {
-    const uint32_t top = held_top(x, n), ex = group_exponent(top);
+        if (i < n) most = max_nan(most, fabsf(to_float<V>(x[i])));
+    const uint32_t top = __float_as_uint(most), ex = group_exponent(top);
 #pragma unroll
     for (int p = 0; p < 4; p += 2) {
         uint32_t w[4];
@@ -29,7 +26,7 @@ __device__ __forceinline__ void store_group(int8_t *q, uint8_t *e, const float (
             float part[8];
             uint32_t v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) part[i] = x[8 * (p + r) + i];
+            for (int i = 0; i < 8; ++i) part[i] = to_float<V>(x[8 * (p + r) + i]);
             quantise(part, top, ex, v);
             if (n >= 32) {
                 w[2 * r] = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
@@ -44,99 +41,108 @@ __device__ __forceinline__ void store_group(int8_t *q, uint8_t *e, const float (
     }
     *e = (uint8_t)ex;
 }
-// The values of a group (rows of q are padded to 16 bytes: words that begin inside a row lie inside it).
-__device__ __forceinline__ void load_group(const int8_t *q, const uint8_t *e, float (&x)[32], int n) {
-    uint4 w[2];
-    w[0] = *reinterpret_cast<const uint4 *>(q);
-    w[1] = n > 16 ? *reinterpret_cast<const uint4 *>(q + 16) : make_uint4(0, 0, 0, 0);
-    const uint32_t ex = *e;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        RawQ r;
-        r.w[0] = p % 2 ? w[p / 2].z : w[p / 2].x;
-        r.w[1] = p % 2 ? w[p / 2].w : w[p / 2].y;
-        float part[8];
-        held_values(r, ex, part);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[8 * p + i] = part[i];
-    }
-}
 
 template <typename T> __device__ __forceinline__ float logistic(float g) {
-    if constexpr (sizeof(T) == 2) return __fdividef(1.f, 1.f + __expf(-g));
+    if constexpr (sizeof(T) == 2) return __fdividef(1.f, 1.f + expf(-g));
     else return 1.f / (1.f + expf(-g));
 }
 
 template <typename T> struct StoreGated {
+    static constexpr bool kBoth = true;
     T *h;
     int64_t ldh, rows, F, ldq, lde;
     int8_t *gate_q, *up_q;
     uint8_t *gate_e, *up_e;
     int wide;
-    static __device__ __forceinline__ uint32_t first(int half) { return half * 64; }
-    static __device__ __forceinline__ uint32_t second(int half) { return 128 + half * 64; }
-    __device__ __forceinline__ void store(const float (&acc)[128], int, int64_t row, int64_t col, int half, bool) const {
-        if (row >= rows) return;
-        col += half * 64;
+    static __device__ __forceinline__ uint32_t first(int group) { return group * 32; }
+    static __device__ __forceinline__ uint32_t second(int group) { return 128 + group * 32; }
+    __device__ __forceinline__ void store(const float (&g)[32], const float (&u)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
+        if (c >= F) return;
+        const int n = F - c < 32 ? (int)(F - c) : 32;
+        const bool there = row < rows;
+        if (gate_q && there) {
+            store_group(gate_q + row * ldq + c, gate_e + row * lde + c / kGroup, g, n);
+            store_group(up_q + row * ldq + c, up_e + row * lde + c / kGroup, u, n);
+        }
+        T *p = h + row * ldh + c;
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const int64_t c = col + 32 * part;
-            if (c >= F) break;
-            const int n = F - c < 32 ? (int)(F - c) : 32;
-            float g[32], u[32];
+        for (int f = 0; f < 32; f += 8) {                          // 8 columns at a time, so that little is held at once
+            float v[8];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                g[i] = acc[32 * part + i];
-                u[i] = acc[64 + 32 * part + i];
+            for (int i = 0; i < 8; ++i) v[i] = g[f + i] * logistic<T>(g[f + i]) * u[f + i];
+            if (wide && n >= 32) {
+                if (there) store_floats<T, 8>(p + f, v);
+            } else {
+                constexpr int W = kTurn<T>;
+                const int at = f % W;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) turn_put<T, W>(turn, at + i, v[i]);
+                if (at + 8 == W && f - at < n) turn_store<T, W>(turn, p + f - at, ldh, there, n - (f - at));
             }
-            if (gate_q) {
-                store_group(gate_q + row * ldq + c, gate_e + row * lde + c / kGroup, g, n);
-                store_group(up_q + row * ldq + c, up_e + row * lde + c / kGroup, u, n);
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) g[i] = g[i] * logistic<T>(g[i]) * u[i];
-            store_32<T>(h + row * ldh + c, n, wide, g);
         }
     }
 };
 
 template <typename T> struct StoreGatedBack {
+    static constexpr bool kBoth = false;
     T *dgate, *dup, *h;
     int64_t ldd, ldh, rows, F, ldq, lde;
     const int8_t *gate_q, *up_q;
     const uint8_t *gate_e, *up_e;
     int8_t *h_q;
     uint8_t *h_e;
-    int wide, wide_up, wide_h;
-    static __device__ __forceinline__ uint32_t first(int half) { return half * 128; }
-    static __device__ __forceinline__ uint32_t second(int half) { return half * 128 + 64; }
-    __device__ __forceinline__ void store(const float (&acc)[128], int, int64_t row, int64_t col, int half, bool) const {
-        if (row >= rows) return;
-        col += half * 128;
+    int wide, wide_h;                     // of dgate and dup; of h
+    static __device__ __forceinline__ uint32_t first(int group) { return group * 64; }
+    static __device__ __forceinline__ uint32_t second(int group) { return group * 64 + 32; }
+    // 8 columns at a time, so that little is held at once; only h^ is needed for the whole group.
+    __device__ __forceinline__ void store(const float (&dh)[32], const float (&)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
+        if (c >= F) return;
+        const int n = F - c < 32 ? (int)(F - c) : 32;
+        const bool there = row < rows, direct = wide && n >= 32;
+        const int8_t *q = gate_q + row * ldq + c, *r = up_q + row * ldq + c;
+        const uint32_t eg = there ? gate_e[row * lde + c / kGroup] : 1u, eu = there ? up_e[row * lde + c / kGroup] : 1u;
+        uint4 wg = {}, wu = {};                                    // 16 columns
+        T *pg = dgate + row * ldd + c, *pu = dup + row * ldd + c;
+        uint8_t *turn_up = turn + kTurnBytes / 2;
+        T hv[32];
 #pragma unroll
-        for (int part = 0; part < 4; ++part) {
-            const int64_t c = col + 32 * part;
-            if (c >= F) break;
-            const int n = F - c < 32 ? (int)(F - c) : 32;
-            float g[32], u[32], d[32];
-            load_group(gate_q + row * ldq + c, gate_e + row * lde + c / kGroup, g, n);
-            load_group(up_q + row * ldq + c, up_e + row * lde + c / kGroup, u, n);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const float s = logistic<T>(g[i]), dh = acc[32 * part + i], gs = g[i] * s;
-                d[i] = dh * u[i] * (s * (1.f + g[i] * (1.f - s)));
-                u[i] = gs * u[i];                                   // h^
-                g[i] = dh * gs;
+        for (int p = 0; p < 4; ++p) {
+            if (p % 2 == 0 && there && 8 * p < n) {                // rows of q are padded to 16 bytes
+                wg = *reinterpret_cast<const uint4 *>(q + 8 * p);
+                wu = *reinterpret_cast<const uint4 *>(r + 8 * p);
             }
-            store_32<T>(dgate + row * ldd + c, n, wide, d);
-            store_32<T>(dup + row * ldd + c, n, wide_up, g);
-            if (h) store_32<T>(h + row * ldh + c, n, wide_h, u);
-            if (h_q) {
+            const RawQ qg = {{p % 2 ? wg.z : wg.x, p % 2 ? wg.w : wg.y}}, qu = {{p % 2 ? wu.z : wu.x, p % 2 ? wu.w : wu.y}};
+            float g[8], u[8], d[8];
+            held_values(qg, eg, g);
+            held_values(qu, eu, u);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) u[i] = to_float<T>(from_float<T>(u[i]));
-                store_group(h_q + row * ldq + c, h_e + row * lde + c / kGroup, u, n);
+            for (int i = 0; i < 8; ++i) {
+                const float s = logistic<T>(g[i]), gs = g[i] * s, x = dh[8 * p + i];
+                hv[8 * p + i] = from_float<T>(gs * u[i]);
+                d[i] = x * u[i] * (s * fmaf(g[i], 1.f - s, 1.f));
+                u[i] = x * gs;
+            }
+            if (direct) {
+                if (there) {
+                    store_floats<T, 8>(pg + 8 * p, d);
+                    store_floats<T, 8>(pu + 8 * p, u);
+                }
+            } else {
+                constexpr int W = kTurn<T> / 2;                    // of either
+                const int at = 8 * p % W, f = 8 * p - at;          // f: first column of the run that is put there
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    turn_put<T, W>(turn, at + i, d[i]);
+                    turn_put<T, W>(turn_up, at + i, u[i]);
+                }
+                if (at + 8 == W && f < n) {
+                    turn_store<T, W>(turn, pg + f, ldd, there, n - f);
+                    turn_store<T, W>(turn_up, pu + f, ldd, there, n - f);
+                }
             }
         }
+        if (h) store_32<T>(h + row * ldh + c, ldh, there, n, wide_h, hv, turn);
+        if (h_q && there) store_group(h_q + row * ldq + c, h_e + row * lde + c / kGroup, hv, n);
     }
 };
 

@@ -6,11 +6,11 @@
 //
 // A pair of CTAs works on a 256 x 256 tile (cta_group::2): each brings half of either operand, 64 deep, in a ring of kStages,
 // and holds half of D's rows in tensor memory, two tiles of them, so that the epilogue of one runs under the products of the
-// next.  The accumulator is emptied into fp32 registers every `chunk` stages (the matrix unit truncates when it accumulates:
-// 1024 terms in a chain keep that at 2e-7 of the magnitudes, 16384 at 7e-6).
+// next.  The matrix unit truncates when it accumulates, so where a result keeps more than 16 bits (LONG) the accumulator is
+// emptied into fp32 registers every kChain stages, 256 terms.
 //
 // Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread of the even CTA), 2 reports to it what has
-// landed, the last 8 empty accumulators and store.
+// landed, the last 16 empty accumulators and store, 64 columns of a row per thread.
 #pragma once
 
 #include <cuda.h>
@@ -22,26 +22,51 @@ namespace deft {
 
 constexpr int kTileRows = 128, kTileCols = 256, kTileK = 64;           // of one CTA's accumulator; k per stage
 constexpr int kHalfBytes = kTileRows * kTileK * 2;                     // of either operand's half in a stage
-constexpr int kStages = 7;
-constexpr int kProductThreads = 384;
-constexpr int kProductSmem = 1024 + kStages * 2 * kHalfBytes + 256;
-constexpr int kShortChain = 16;                                        // stages per accumulator hand-over
+constexpr int kStages = 6;
+constexpr int kStoreWarps = 16;
+constexpr int kProductThreads = 128 + 32 * kStoreWarps;
+constexpr int kControlRegisters = 56, kStoreRegisters = 104;           // a thread's, of the first 4 warps and of the others
+constexpr int kTurnBytes = 2048;                                       // per storing warp: rows that are turned before they are stored
+constexpr int kProductSmem = 1024 + kStages * 2 * kHalfBytes + kStoreWarps * kTurnBytes + 256;
+constexpr int kChain = 4;                                              // stages per accumulator hand-over
+constexpr int64_t kPartFloats = (int64_t)kTileRows * kTileCols;        // of a CTA's part of a tile
 
 struct Product {
     int tiles_m, tiles_n, batch;          // tiles of 256 rows; of 256 columns (gated: 128 of either half)
     int blocks, pairs;                    // stages along k; pairs of planes
-    int chunk;
     int planes_a, planes_b;               // of each batch's operands
     uint32_t order_a, order_b;            // plane of each pair, 4 bits each
     int triangle;                         // tiles with n <= m only (tiles_m = tiles_n)
     int step_n, second;                   // columns between tiles; where the second CTA's half of B starts, behind the first's
     int bf16;
+    int64_t whole;                        // tiles [0, whole) are worked on whole, of the others each k in `cuts` parts
+    int cuts;
+    float *parts;                         // [(tile - whole) * cuts + cut][CTA of the pair][column][row]
 };
 
-__device__ __forceinline__ int64_t product_tiles(const Product &p) {
+__host__ __device__ inline int64_t product_tiles(const Product &p) {
     const int64_t n = p.triangle ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
     return n * p.batch;
 }
+// Pieces of work, dealt to the pairs of CTAs in turn: first whole tiles, then the cuts of the others.
+__host__ __device__ inline int64_t product_pieces(const Product &p) { return p.whole + (product_tiles(p) - p.whole) * p.cuts; }
+struct Piece {
+    int64_t tile;
+    int k0, k1;                           // stages
+    __device__ Piece(const Product &p, int64_t i) {
+        const int per_tile = p.blocks * p.pairs;
+        if (i < p.whole) {
+            tile = i;
+            k0 = 0;
+            k1 = per_tile;
+        } else {
+            const int64_t j = i - p.whole, cut = j % p.cuts;
+            tile = p.whole + j / p.cuts;
+            k0 = (int)(per_tile * cut / p.cuts);
+            k1 = (int)(per_tile * (cut + 1) / p.cuts);
+        }
+    }
+};
 // Tiles in bands of 8 along m, so that the CTAs at work at one time share rows of A and of B in the L2.
 __device__ __forceinline__ void product_place(const Product &p, int64_t tile, int &batch, int &m, int &n) {
     if (p.triangle) {
@@ -66,15 +91,41 @@ __device__ __forceinline__ uint32_t product_descriptor(bool bf16, bool b_n) {
            (uint32_t)(2 * kTileRows >> 4) << 24;
 }
 
-// Epilogue: `cols` of each thread's 128 columns start at first(half) and, for the second 64 of them, at second(half);
-// store() gets them with the thread's row and its first column, of every row and column of the tile.
-template <typename EPILOGUE, bool BN>
+// 32 columns of the accumulator: as they are, or added to what there is, two at a time.
+__device__ __forceinline__ void take_columns(uint32_t from, float (&x)[32]) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        uint32_t v[16];
+        tmem_load_16(from + 16 * q, v);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[16 * q + j] = __uint_as_float(v[j]);
+    }
+}
+__device__ __forceinline__ void add_columns(uint32_t from, Pair (&x)[16]) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        uint32_t v[16];
+        tmem_load_16(from + 16 * q, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[8 * q + j] = pair_add(x[8 * q + j], make_pair(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+    }
+}
+__device__ __forceinline__ void split_columns(const Pair (&x)[16], float (&out)[32]) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) split_pair(x[j], out[2 * j], out[2 * j + 1]);
+}
+
+// Epilogue: a thread has 64 columns of one row, 32 from first(group) on and 32 from second(group), the group one of four.
+// store() gets 32 of them at a time, or (kBoth) all at once, with the row and the column they belong to; whole warps call it,
+// with rows and columns that may lie outside the result.
+template <typename EPILOGUE, bool BN, bool LONG>
 __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const Product p, const EPILOGUE epilogue, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
     extern __shared__ uint8_t raw[];
     uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sa = base, *sb = sa + kStages * kHalfBytes;
-    uint64_t *bars = (uint64_t *)(sb + kStages * kHalfBytes);
+    uint8_t *turns = sb + kStages * kHalfBytes;
+    uint64_t *bars = (uint64_t *)(turns + kStoreWarps * kTurnBytes);
     const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, acc_full = ready + 8 * kStages,
                    acc_empty = acc_full + 16, drained = acc_empty + 16;
     uint32_t *tmem_slot = (uint32_t *)(bars + 3 * kStages + 5);
@@ -89,7 +140,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(acc_full + 8 * b, 1);
-            barrier_init(acc_empty + 8 * b, 2 * 8);
+            barrier_init(acc_empty + 8 * b, 2 * kStoreWarps);
         }
         barrier_init(drained, 1);
         *failed = 0;
@@ -105,34 +156,33 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     tmem_fence_after();
     const uint32_t tmem = *tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the set-up above may overlap the kernel before
-    const int64_t tiles = product_tiles(p), step = gridDim.x / 2;
-    const int per_tile = p.blocks * p.pairs;
+    const int64_t pieces = product_pieces(p), step = gridDim.x / 2;
     int batch, tm, tn;
 
     if (warp < 4) {
-        registers_down<56>();
+        registers_down<kControlRegisters>();
         if (warp == 0 && lane == 0) {
             prefetch_map(&map_a);
             prefetch_map(&map_b);
             uint32_t n = 0;
             bool ok = true;
-            for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += step) {
-                product_place(p, tile, batch, tm, tn);
+            for (int64_t i = blockIdx.x / 2; ok && i < pieces; i += step) {
+                const Piece w(p, i);
+                product_place(p, w.tile, batch, tm, tn);
                 const int m0 = tm * 2 * kTileRows + rank * kTileRows, n0 = tn * p.step_n + (rank ? p.second : 0);
-                for (int q = 0; ok && q < p.pairs; ++q) {
+                for (int k = w.k0; k < w.k1; ++k, ++n) {
+                    const uint32_t s = n % kStages, round = n / kStages, bar = full + 8 * s;
+                    if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
+                    const int q = k / p.blocks, at = (k - q * p.blocks) * kTileK;
                     const int za = batch * p.planes_a + (int)(p.order_a >> 4 * q & 15u), zb = batch * p.planes_b + (int)(p.order_b >> 4 * q & 15u);
-                    for (int k = 0; k < p.blocks; ++k, ++n) {
-                        const uint32_t s = n % kStages, round = n / kStages, bar = full + 8 * s;
-                        if (!(ok = barrier_wait(empty + 8 * s, (round & 1) ^ 1, failed))) break;
-                        barrier_expect(bar, 2 * kHalfBytes);
-                        tensor_load_3d(smem_address(sa + s * kHalfBytes), &map_a, k * kTileK, m0, za, bar);
-                        if constexpr (BN) {
+                    barrier_expect(bar, 2 * kHalfBytes);
+                    tensor_load_3d(smem_address(sa + s * kHalfBytes), &map_a, at, m0, za, bar);
+                    if constexpr (BN) {
 #pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                tensor_load_3d(smem_address(sb + s * kHalfBytes + j * (kTileK * 128)), &map_b, n0 + 64 * j, k * kTileK, zb, bar);
-                        } else {
-                            tensor_load_3d(smem_address(sb + s * kHalfBytes), &map_b, k * kTileK, n0, zb, bar);
-                        }
+                        for (int j = 0; j < 2; ++j)
+                            tensor_load_3d(smem_address(sb + s * kHalfBytes + j * (kTileK * 128)), &map_b, n0 + 64 * j, at, zb, bar);
+                    } else {
+                        tensor_load_3d(smem_address(sb + s * kHalfBytes), &map_b, at, n0, zb, bar);
                     }
                 }
             }
@@ -147,12 +197,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const uint32_t idesc = product_descriptor(p.bf16 != 0, BN);
             uint32_t n = 0, chunk = 0;
             bool ok = true;
-            for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += step) {
-                for (int k = 0; k < per_tile && ok; ++chunk) {
+            for (int64_t i = blockIdx.x / 2; ok && i < pieces; i += step) {
+                const Piece w(p, i);
+                for (int k = w.k0; k < w.k1 && ok; ++chunk) {
                     const uint32_t buf = chunk & 1, round = chunk >> 1;
                     if (!(ok = barrier_wait(acc_empty + 8 * buf, (round & 1) ^ 1, failed))) break;
                     tmem_fence_after();
-                    const int stop = k + p.chunk < per_tile ? k + p.chunk : per_tile;
+                    const int stop = LONG && k + kChain < w.k1 ? k + kChain : w.k1;
                     for (int first = k; k < stop; ++k, ++n) {
                         const uint32_t s = n % kStages;
                         if (!(ok = barrier_wait(ready + 8 * s, (n / kStages) & 1, failed))) break;   // in both CTAs
@@ -174,45 +225,89 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         } else if (warp == 2 && lane == 0) {
             uint32_t n = 0;
             bool ok = true;
-            for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += step)
-                for (int k = 0; k < per_tile; ++k, ++n) {
+            for (int64_t i = blockIdx.x / 2; ok && i < pieces; i += step) {
+                const Piece w(p, i);
+                for (int k = w.k0; k < w.k1; ++k, ++n) {
                     if (!(ok = barrier_wait(full + 8 * (n % kStages), (n / kStages) & 1, failed))) break;
                     barrier_arrive_at(ready + 8 * (n % kStages), 0);
                 }
+            }
         }
     } else {
-        registers_up<224>();
-        const int half = (warp & 7) >> 2, quarter = warp & 3;       // lanes quarter * 32..
+        registers_up<kStoreRegisters>();
+        const int group = (warp - 4) >> 2, quarter = warp & 3;      // lanes quarter * 32..
         const int row = quarter * 32 + lane;
         const uint32_t source = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t c0 = EPILOGUE::first(half), c1 = EPILOGUE::second(half);
+        const uint32_t c0 = EPILOGUE::first(group), c1 = EPILOGUE::second(group);
+        uint8_t *turn = turns + (warp - 4) * kTurnBytes;
         uint32_t chunk = 0;
         bool ok = true;
-        for (int64_t tile = blockIdx.x / 2; tile < tiles; tile += step) {
-            product_place(p, tile, batch, tm, tn);
-            float acc[128];
-            for (int k = 0; k < per_tile; k += p.chunk, ++chunk) {
-                const uint32_t buf = chunk & 1, round = chunk >> 1;
-                ok = ok && barrier_wait(acc_full + 8 * buf, round & 1, failed);
-                if (__any_sync(0xffffffffu, !ok)) break;
-                tmem_fence_after();
+        for (int64_t i = blockIdx.x / 2; i < pieces; i += step) {
+            const Piece w(p, i);
+            product_place(p, w.tile, batch, tm, tn);
+            const int64_t r0 = (int64_t)tm * 2 * kTileRows + rank * kTileRows + row, n0 = (int64_t)tn * p.step_n;
+            const bool cut = i >= p.whole && p.cuts > 1;
+            float *parts = p.parts + ((i - p.whole) * 2 + rank) * kPartFloats + row;
+            float a[32], b[32];
+            constexpr int kTurns = EPILOGUE::kBoth ? 1 : 2;
+            const auto put = [&](int t) {                           // a (and b), columns of turn t
+                if (__any_sync(0xffffffffu, !ok || *failed)) {      // a wait ran out: no numbers rather than wrong ones
+                    ok = false;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    uint32_t v[16];
-                    tmem_load_16(source + buf * kTileCols + (q < 4 ? c0 + q * 16 : c1 + (q - 4) * 16), v);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[q * 16 + i] = (k > 0 ? acc[q * 16 + i] : 0.f) + __uint_as_float(v[i]);
+                    for (int j = 0; j < 32; ++j) a[j] = b[j] = NAN;
                 }
+                const uint32_t c = t ? c1 : c0;
+                if (!cut) {
+                    epilogue.store(a, b, batch, r0, n0 + c, turn);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        parts[(c + j) * kTileRows] = a[j];
+                        if (EPILOGUE::kBoth) parts[(c1 + j) * kTileRows] = b[j];
+                    }
+                }
+            };
+            const auto release = [&](uint32_t buf) {
                 tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) barrier_arrive_at(acc_empty + 8 * buf, 0);
-            }
-            if (*failed) {                                          // a wait ran out: no numbers rather than wrong ones
-                ok = false;
+            };
+            if constexpr (LONG) {
+                Pair sa[16], sb[16];
 #pragma unroll
-                for (int i = 0; i < 128; ++i) acc[i] = NAN;
+                for (int j = 0; j < 16; ++j) sa[j] = sb[j] = make_pair(0.f, 0.f);
+                for (int k = w.k0; k < w.k1; k += kChain, ++chunk) {
+                    const uint32_t buf = chunk & 1, round = chunk >> 1;
+                    ok = ok && barrier_wait(acc_full + 8 * buf, round & 1, failed);
+                    if (__any_sync(0xffffffffu, !ok)) break;
+                    tmem_fence_after();
+                    add_columns(source + buf * kTileCols + c0, sa);
+                    add_columns(source + buf * kTileCols + c1, sb);
+                    release(buf);
+                }
+                split_columns(sa, a);
+                if (EPILOGUE::kBoth) split_columns(sb, b);
+#pragma unroll 1
+                for (int t = 0; t < kTurns; ++t) {
+                    put(t);
+                    split_columns(sb, a);
+                }
+            } else {
+                const uint32_t buf = chunk & 1, round = chunk >> 1;
+                ++chunk;
+                ok = ok && barrier_wait(acc_full + 8 * buf, round & 1, failed);
+                ok = __all_sync(0xffffffffu, ok);
+                tmem_fence_after();
+#pragma unroll 1
+                for (int t = 0; t < kTurns; ++t) {                  // the accumulator holds the second turn's columns meanwhile
+                    if (ok) {
+                        take_columns(source + buf * kTileCols + (t ? c1 : c0), a);
+                        if (EPILOGUE::kBoth) take_columns(source + buf * kTileCols + c1, b);
+                        if (t == kTurns - 1) release(buf);
+                    }
+                    put(t);
+                }
             }
-            epilogue.store(acc, batch, (int64_t)tm * 2 * kTileRows + rank * kTileRows + row, (int64_t)tn * p.step_n, half, tm == tn);
         }
     }
     tmem_fence_before();
@@ -224,44 +319,92 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     }
 }
 
-// ---------------------------------------------------------------------------
-// Epilogues.  A thread has 128 columns of one row: runs of 32 of them are stored in 16-byte words where the rows allow it.
-// ---------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ void store_32(T *p, int n, bool wide, const float (&v)[32]) {
-    if (wide && n >= 32) {
+// The tiles whose k was cut: their parts, added in order, and the same epilogue.  Threads: 128 rows by 2 runs of columns.
+template <typename EPILOGUE>
+__global__ void __launch_bounds__(256) product_join_kernel(const Product p, const EPILOGUE epilogue) {
+    __shared__ uint4 turns[8][kTurnBytes / 16];
+    constexpr int kRuns = EPILOGUE::kBoth ? 4 : 8;
+    const int64_t half_tile = blockIdx.x / (kRuns / 2), tile = half_tile / 2;
+    const int rank = (int)(half_tile % 2), run = (int)(blockIdx.x % (kRuns / 2)) * 2 + threadIdx.x / 128, row = threadIdx.x % 128;
+    const int group = EPILOGUE::kBoth ? run : run / 2;
+    const uint32_t ca = EPILOGUE::kBoth || run % 2 == 0 ? EPILOGUE::first(group) : EPILOGUE::second(group), cb = EPILOGUE::second(group);
+    asm volatile("griddepcontrol.wait;" ::: "memory");             // the parts are those of the kernel before
+    float a[32], b[32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float part[8];
+    for (int j = 0; j < 32; ++j) a[j] = b[j] = 0.f;
+    for (int c = 0; c < p.cuts; ++c) {
+        const float *in = p.parts + ((tile * p.cuts + c) * 2 + rank) * kPartFloats + row;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) part[j] = v[8 * i + j];
-            store_floats<T, 8>(p + 8 * i, part);
+        for (int j = 0; j < 32; ++j) {
+            a[j] += in[(ca + j) * kTileRows];
+            if (EPILOGUE::kBoth) b[j] += in[(cb + j) * kTileRows];
         }
-    } else {
+    }
+    int batch, tm, tn;
+    product_place(p, p.whole + tile, batch, tm, tn);
+    epilogue.store(a, b, batch, (int64_t)tm * 2 * kTileRows + rank * kTileRows + row, (int64_t)tn * p.step_n + ca, (uint8_t *)turns[threadIdx.x / 32]);
+}
+
+// ---------------------------------------------------------------------------
+// Stores of a warp's 32 rows by 32 columns, a row per thread.  Whole runs of 32 on 16-byte boundaries go out as they are
+// held, in 16-byte words.  All others are turned in shared memory first, so that the lanes of a warp store consecutive
+// elements: W columns of a row at a time.  (Elements stored as they are held, one sector each: four times as long for a
+// 1501 x 777 result.)
+// ---------------------------------------------------------------------------
+template <typename T> constexpr int kTurn = 64 / (int)sizeof(T);                       // columns that kTurnBytes hold
+template <typename T, int W> __device__ __forceinline__ int turn_place(int row, int c) {
+    // no two lanes of a warp that puts (one column, all rows) or takes in one bank, but for the narrowest
+    return row * W + (c ^ (sizeof(T) == 4 ? row >> (W == 16 ? 1 : 2) & (W - 1) : W == 32 ? row & 30 : row >> 1 & 14));
+}
+template <typename T, int W> __device__ __forceinline__ void turn_put(uint8_t *turn, int c, float v) {
+    reinterpret_cast<T *>(turn)[turn_place<T, W>(threadIdx.x & 31, c)] = from_float<T>(v);
+}
+// The first n <= W columns put there by all lanes go to p (this lane's row and the first column); `there`: the row exists.
+template <typename T, int W> __device__ __forceinline__ void turn_store(const uint8_t *turn, T *p, int64_t ld, bool there, int n) {
+    constexpr int kRows = 32 / W;                                  // rows that a warp stores at a time
+    const int lane = threadIdx.x & 31, rows = __popc(__ballot_sync(0xffffffffu, there)), sub = lane / W, c = lane % W;
+    T *out = p + (sub - lane) * ld + c;                            // rows that exist come first
+    __syncwarp();
+    if (c < n) {
+#pragma unroll 8
+        for (int r = sub; r < rows; r += kRows, out += kRows * ld) *out = reinterpret_cast<const T *>(turn)[turn_place<T, W>(r, c)];
+    }
+    __syncwarp();
+}
+template <typename T, typename V> __device__ __forceinline__ void store_32(T *p, int64_t ld, bool there, int n, bool wide, const V (&v)[32], uint8_t *turn) {
+    if (wide && n >= 32) {
+        if (there)
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < n) p[i] = from_float<T>(v[i]);
+            for (int i = 0; i < 4; ++i) {
+                float part[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) part[j] = to_float<V>(v[8 * i + j]);
+                store_floats<T, 8>(p + 8 * i, part);
+            }
+    } else {
+        constexpr int W = kTurn<T>;
+#pragma unroll
+        for (int f = 0; f < 32; f += W) {
+            if (f >= n) break;
+#pragma unroll
+            for (int j = 0; j < W; ++j) turn_put<T, W>(turn, j, to_float<V>(v[f + j]));
+            turn_store<T, W>(turn, p + f, ld, there, n - f);
+        }
     }
 }
 
 // out [rows, cols] <- D.
 template <typename T> struct StoreRows {
+    static constexpr bool kBoth = false;
     T *out;
     int64_t ld, rows, cols;
     int wide;
-    static __device__ __forceinline__ uint32_t first(int half) { return half * 128; }
-    static __device__ __forceinline__ uint32_t second(int half) { return half * 128 + 64; }
-    __device__ __forceinline__ void store(const float (&acc)[128], int, int64_t row, int64_t col, int half, bool) const {
-        if (row >= rows) return;
-        col += half * 128;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            if (col + 32 * g >= cols) break;
-            float v[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = acc[32 * g + i];
-            const int64_t left = cols - col - 32 * g;
-            store_32<T>(out + row * ld + col + 32 * g, left < 32 ? (int)left : 32, wide, v);
-        }
+    static __device__ __forceinline__ uint32_t first(int group) { return group * 64; }
+    static __device__ __forceinline__ uint32_t second(int group) { return group * 64 + 32; }
+    __device__ __forceinline__ void store(const float (&a)[32], const float (&)[32], int, int64_t row, int64_t col, uint8_t *turn) const {
+        if (col >= cols) return;
+        const int64_t left = cols - col;
+        store_32<T>(out + row * ld + col, ld, row < rows, left < 32 ? (int)left : 32, wide, a, turn);
     }
 };
 

@@ -68,25 +68,43 @@ deft::Product product_of(int32_t dtype, int64_t m, int64_t tiles_n, int64_t k, i
     p.planes_a = p.planes_b = pieces ? 3 : 1;
     p.order_a = pieces ? 0x001102u : 0u;
     p.order_b = pieces ? 0x010120u : 0u;
-    p.chunk = deft::kShortChain;
     p.step_n = step_n;
     p.second = second;
     p.bf16 = dtype != DEF_DTYPE_F16;
     return p;
 }
 
-template <bool BN, typename EPILOGUE>
+// How tiles that do not fill a round of the pairs are cut along k.  Each part has kLeastStages, and the cut has to save
+// kJoinStages more than the join, a launch and a pass over the parts, takes.
+constexpr int kLeastStages = 4, kJoinStages = 16;
+constexpr int64_t kMostPartBytes = (int64_t)kUsualSms * deft::kPartFloats * 4;
+int64_t plan_cuts(deft::Product &p, int64_t most_bytes = kMostPartBytes) {
+    const int64_t tiles = deft::product_tiles(p), workers = kUsualSms / 2, rest = tiles % workers, each = 2 * deft::kPartFloats * 4;
+    const int per_tile = p.blocks * p.pairs;
+    p.whole = tiles;
+    p.cuts = 1;
+    if (rest == 0) return 0;
+    int64_t cuts = workers / rest;
+    if (cuts > per_tile / kLeastStages) cuts = per_tile / kLeastStages;
+    if (cuts > most_bytes / (rest * each)) cuts = most_bytes / (rest * each);
+    if (cuts < 2 || per_tile - per_tile / cuts < kJoinStages) return 0;
+    p.whole = tiles - rest;
+    p.cuts = (int)cuts;
+    return rest * cuts * each;
+}
+
+template <bool BN, bool LONG, typename EPILOGUE>
 int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t stream, const char *what) {
-    const auto kernel = deft::product_kernel<EPILOGUE, BN>;
+    const auto kernel = deft::product_kernel<EPILOGUE, BN, LONG>;
     // The epilogue's warps take over registers that the others give up: those have to be there.
     cudaFuncAttributes at;
     cudaError_t err = cudaFuncGetAttributes(&at, kernel);
-    if (err == cudaSuccess && at.numRegs * deft::kProductThreads < 128 * 56 + 256 * 224) return fail(DEF_ERR_CUDA, "%s: built with too few registers", what);
+    if (err == cudaSuccess && at.numRegs * deft::kProductThreads < 128 * deft::kControlRegisters + 32 * deft::kStoreWarps * deft::kStoreRegisters) return fail(DEF_ERR_CUDA, "%s: built with too few registers", what);
     if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, deft::kProductSmem);
     if (err == cudaSuccess) {
-        const int64_t n = p.triangle ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n, tiles = n * p.batch;
+        const int64_t pieces = deft::product_pieces(p);
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)((tiles < kUsualSms / 2 ? tiles : kUsualSms / 2) * 2));
+        cfg.gridDim = dim3((unsigned)((pieces < kUsualSms / 2 ? pieces : kUsualSms / 2) * 2));
         cfg.blockDim = dim3(deft::kProductThreads);
         cfg.dynamicSmemBytes = deft::kProductSmem;
         cfg.stream = stream;
@@ -99,6 +117,14 @@ int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUten
         cfg.attrs = attr;
         cfg.numAttrs = 2;
         err = cudaLaunchKernelEx(&cfg, kernel, p, epilogue, map_a, map_b);
+        if (const int64_t cut = deft::product_tiles(p) - p.whole; cut > 0 && err == cudaSuccess) {
+            cfg.gridDim = dim3((unsigned)(cut * (EPILOGUE::kBoth ? 4 : 8)));
+            cfg.blockDim = dim3(256);
+            cfg.dynamicSmemBytes = 0;
+            cfg.attrs = attr + 1;
+            cfg.numAttrs = 1;
+            err = cudaLaunchKernelEx(&cfg, deft::product_join_kernel<EPILOGUE>, p, epilogue);
+        }
     }
     if (err == cudaSuccess) return DEF_OK;
     cudaGetLastError();

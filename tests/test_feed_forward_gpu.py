@@ -107,7 +107,7 @@ def test_sizes(B, dtype, layout):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("T,C,F,O", [(5000, 64, 300, 64), (300, 1111, 2000, 777), (64, 2048, 1408, 2048), (700, 96, 9000, 32)])
+@pytest.mark.parametrize("T,C,F,O", [(5000, 64, 300, 64), (300, 1111, 2000, 777), (64, 2048, 1408, 2048), (700, 96, 9000, 32), (2500, 40, 1999, 33), (3000, 33, 5001, 70)])
 def test_more_tiles_than_pairs_and_long_sums(B, dtype, T, C, F, O):
     _check(B, T, C, F, O, dtype, 5)
 
@@ -126,12 +126,12 @@ def test_parts_alone(B):
     x, w_in, w_down = _normal((T, C), BF16, 1), _normal((2 * F, C), BF16, 2, 0.1), _normal((C, F), BF16, 3, 0.1)
     h, h2, out = torch.empty(T, F, dtype=BF16, device=DEV), torch.empty(T, F, dtype=BF16, device=DEV), torch.empty(T, C, dtype=BF16, device=DEV)
     cks = [_held(B, T, F) for _ in range(2)]
-    B.def_feed_forward(x, w_in, w_down, h, out, *cks)
-    B.def_feed_forward(x, w_in, None, h2, None)
+    B.def_feed_forward(x, w_in, w_down, h, out, *cks, workspace=_work(32 << 20))
+    B.def_feed_forward(x, w_in, None, h2, None, workspace=_work(32 << 20))
     assert torch.equal(h, h2)
     dout, both, both2, dx = _normal((T, C), BF16, 4), *(torch.empty(T, 2 * F, dtype=BF16, device=DEV) for _ in range(2)), torch.empty(T, C, dtype=BF16, device=DEV)
-    B.def_feed_forward_backward(dout, w_in, w_down, *cks, both, dx)
-    B.def_feed_forward_backward(dout, None, w_down, *cks, both2, None)
+    B.def_feed_forward_backward(dout, w_in, w_down, *cks, both, dx, workspace=_work(32 << 20))
+    B.def_feed_forward_backward(dout, None, w_down, *cks, both2, None, workspace=_work(32 << 20))
     assert torch.equal(both, both2)
     empty = x[:0]
     B.def_feed_forward(empty, w_in, w_down, h[:0], out[:0])
@@ -144,7 +144,7 @@ def test_large_values_and_specials(B):
     x[5], x[7, 3], x[9, 1] = 0, math.nan, math.inf
     h, out = torch.empty(T, F, dtype=BF16, device=DEV), torch.empty(T, C, dtype=BF16, device=DEV)
     cks = [_held(B, T, F) for _ in range(2)]
-    B.def_feed_forward(x, w_in, w_down, h, out, *cks)
+    B.def_feed_forward(x, w_in, w_down, h, out, *cks, workspace=_work(32 << 20))
     assert bool((h[5] == 0).all()) and bool((out[5] == 0).all())
     assert bool(torch.isnan(h[7]).all()) and bool(torch.isnan(out[7]).all()) and not bool(torch.isfinite(out[9]).any())
     rest = [i for i in range(T) if i not in (7, 9)]
@@ -201,8 +201,8 @@ def test_a_whole_training_pass(B):
     both, dx = torch.empty(T, 2 * F, dtype=BF16, device=DEV), torch.empty(T, C, dtype=BF16, device=DEV)
     dwi, dwd = torch.empty(2 * F, C, device=DEV), torch.empty(C, F, device=DEV)
     B.def_checkpoint_pack(x, x_ck)
-    B.def_feed_forward(x, w_in, w_down, h, out, gate_ck, up_ck)
-    B.def_feed_forward_backward(dout, w_in, w_down, gate_ck, up_ck, both, dx, h_ck=h_ck)
+    B.def_feed_forward(x, w_in, w_down, h, out, gate_ck, up_ck, workspace=_work(32 << 20))
+    B.def_feed_forward_backward(dout, w_in, w_down, gate_ck, up_ck, both, dx, h_ck=h_ck, workspace=_work(32 << 20))
     for dy, ck, dw in ((both, x_ck, dwi), (dout, h_ck, dwd)):
         B.def_checkpoint_weight_grad(dy, ck, dw, _work(B.def_checkpoint_weight_grad_workspace(dy, dw.shape[1])))
     leaves = [v.double().requires_grad_() for v in (x, w_in, w_down)]
