@@ -11,8 +11,10 @@
 
 namespace deft {
 
-// Checkpoint of a group of 32 columns that one thread holds, the first n of which exist.
-template <typename V> __device__ __forceinline__ void store_group(int8_t *q, uint8_t *e, const V (&x)[32], int n) {
+// Checkpoint of a group of 32 columns that one thread holds, the first n of which exist; whole groups are turned (32 bytes a
+// row).  Whole warps call it.
+template <typename V>
+__device__ __forceinline__ void store_group(int8_t *q, int64_t ldq, uint8_t *e, const V (&x)[32], int n, bool there, uint8_t *turn) {
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
@@ -34,12 +36,13 @@ template <typename V> __device__ __forceinline__ void store_group(int8_t *q, uin
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (8 * (p + r) + i < n) q[8 * (p + r) + i] = (int8_t)v[i];
+                    if (8 * (p + r) + i < n && there) q[8 * (p + r) + i] = (int8_t)v[i];
             }
         }
-        if (n >= 32) *reinterpret_cast<uint4 *>(q + 8 * p) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (n >= 32) turn_put_word<32>(turn, p / 2, make_uint4(w[0], w[1], w[2], w[3]));
     }
-    *e = (uint8_t)ex;
+    if (n >= 32) turn_store_words<32>(turn, q, ldq, there);
+    if (there) *e = (uint8_t)ex;
 }
 
 template <typename T> __device__ __forceinline__ float logistic(float g) {
@@ -56,13 +59,14 @@ template <typename T> struct StoreGated {
     int wide;
     static __device__ __forceinline__ uint32_t first(int group) { return group * 32; }
     static __device__ __forceinline__ uint32_t second(int group) { return 128 + group * 32; }
+    __device__ __forceinline__ void fetch(int64_t, int64_t) const {}
     __device__ __forceinline__ void store(const float (&g)[32], const float (&u)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
         if (c >= F) return;
         const int n = F - c < 32 ? (int)(F - c) : 32;
         const bool there = row < rows;
-        if (gate_q && there) {
-            store_group(gate_q + row * ldq + c, gate_e + row * lde + c / kGroup, g, n);
-            store_group(up_q + row * ldq + c, up_e + row * lde + c / kGroup, u, n);
+        if (gate_q) {
+            store_group(gate_q + row * ldq + c, ldq, gate_e + row * lde + c / kGroup, g, n, there, turn);
+            store_group(up_q + row * ldq + c, ldq, up_e + row * lde + c / kGroup, u, n, there, turn);
         }
         T *p = h + row * ldh + c;
 #pragma unroll
@@ -71,7 +75,9 @@ template <typename T> struct StoreGated {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = g[f + i] * logistic<T>(g[f + i]) * u[f + i];
             if (wide && n >= 32) {
-                if (there) store_floats<T, 8>(p + f, v);
+                constexpr int W = kTurn<T>;
+                turn_put_8<64, T>(turn, f % W, v);
+                if (f % W + 8 == W) turn_store_words<64>(turn, p + f + 8 - W, ldh * (int64_t)sizeof(T), there);
             } else {
                 constexpr int W = kTurn<T>;
                 const int at = f % W;
@@ -94,6 +100,11 @@ template <typename T> struct StoreGatedBack {
     int wide, wide_h;                     // of dgate and dup; of h
     static __device__ __forceinline__ uint32_t first(int group) { return group * 64; }
     static __device__ __forceinline__ uint32_t second(int group) { return group * 64 + 32; }
+    __device__ __forceinline__ void fetch(int64_t row, int64_t c) const {
+        if (row >= rows || c >= F) return;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(gate_q + row * ldq + c));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(up_q + row * ldq + c));
+    }
     // 8 columns at a time, so that little is held at once; only h^ is needed for the whole group.
     __device__ __forceinline__ void store(const float (&dh)[32], const float (&)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
         if (c >= F) return;
@@ -122,14 +133,16 @@ template <typename T> struct StoreGatedBack {
                 d[i] = x * u[i] * (s * fmaf(g[i], 1.f - s, 1.f));
                 u[i] = x * gs;
             }
+            constexpr int W = kTurn<T> / 2;                        // of either
+            const int at = 8 * p % W, f = 8 * p - at;              // f: first column of the run that is put there
             if (direct) {
-                if (there) {
-                    store_floats<T, 8>(pg + 8 * p, d);
-                    store_floats<T, 8>(pu + 8 * p, u);
+                turn_put_8<32, T>(turn, at, d);
+                turn_put_8<32, T>(turn_up, at, u);
+                if (at + 8 == W) {
+                    turn_store_words<32>(turn, pg + f, ldd * (int64_t)sizeof(T), there);
+                    turn_store_words<32>(turn_up, pu + f, ldd * (int64_t)sizeof(T), there);
                 }
             } else {
-                constexpr int W = kTurn<T> / 2;                    // of either
-                const int at = 8 * p % W, f = 8 * p - at;          // f: first column of the run that is put there
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     turn_put<T, W>(turn, at + i, d[i]);
@@ -142,7 +155,7 @@ template <typename T> struct StoreGatedBack {
             }
         }
         if (h) store_32<T>(h + row * ldh + c, ldh, there, n, wide_h, hv, turn);
-        if (h_q && there) store_group(h_q + row * ldq + c, h_e + row * lde + c / kGroup, hv, n);
+        if (h_q) store_group(h_q + row * ldq + c, ldq, h_e + row * lde + c / kGroup, hv, n, there, turn);
     }
 };
 

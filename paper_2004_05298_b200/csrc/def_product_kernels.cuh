@@ -7,7 +7,7 @@
 // A pair of CTAs works on a 256 x 256 tile (cta_group::2): each brings half of either operand, 64 deep, in a ring of kStages,
 // and holds half of D's rows in tensor memory, two tiles of them, so that the epilogue of one runs under the products of the
 // next.  The matrix unit truncates when it accumulates, so where a result keeps more than 16 bits (LONG) the accumulator is
-// emptied into fp32 registers every kChain stages, 256 terms.
+// emptied into fp32 registers every kChain stages, 512 terms.
 //
 // Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread of the even CTA), 2 reports to it what has
 // landed, the last 16 empty accumulators and store, 64 columns of a row per thread.
@@ -28,7 +28,7 @@ constexpr int kProductThreads = 128 + 32 * kStoreWarps;
 constexpr int kControlRegisters = 56, kStoreRegisters = 104;           // a thread's, of the first 4 warps and of the others
 constexpr int kTurnBytes = 2048;                                       // per storing warp: rows that are turned before they are stored
 constexpr int kProductSmem = 1024 + kStages * 2 * kHalfBytes + kStoreWarps * kTurnBytes + 256;
-constexpr int kChain = 4;                                              // stages per accumulator hand-over
+constexpr int kChain = 8;                                              // stages per accumulator hand-over
 constexpr int64_t kPartFloats = (int64_t)kTileRows * kTileCols;        // of a CTA's part of a tile
 
 struct Product {
@@ -117,7 +117,7 @@ __device__ __forceinline__ void split_columns(const Pair (&x)[16], float (&out)[
 
 // Epilogue: a thread has 64 columns of one row, 32 from first(group) on and 32 from second(group), the group one of four.
 // store() gets 32 of them at a time, or (kBoth) all at once, with the row and the column they belong to; whole warps call it,
-// with rows and columns that may lie outside the result.
+// with rows and columns that may lie outside the result.  fetch() comes long before it, for what store() will read.
 template <typename EPILOGUE, bool BN, bool LONG>
 __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const Product p, const EPILOGUE epilogue, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
@@ -248,6 +248,10 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const int64_t r0 = (int64_t)tm * 2 * kTileRows + rank * kTileRows + row, n0 = (int64_t)tn * p.step_n;
             const bool cut = i >= p.whole && p.cuts > 1;
             float *parts = p.parts + ((i - p.whole) * 2 + rank) * kPartFloats + row;
+            if (!cut) {
+                epilogue.fetch(r0, n0 + c0);
+                epilogue.fetch(r0, n0 + c1);
+            }
             float a[32], b[32];
             constexpr int kTurns = EPILOGUE::kBoth ? 1 : 2;
             const auto put = [&](int t) {                           // a (and b), columns of turn t
@@ -346,11 +350,36 @@ __global__ void __launch_bounds__(256) product_join_kernel(const Product p, cons
 }
 
 // ---------------------------------------------------------------------------
-// Stores of a warp's 32 rows by 32 columns, a row per thread.  Whole runs of 32 on 16-byte boundaries go out as they are
-// held, in 16-byte words.  All others are turned in shared memory first, so that the lanes of a warp store consecutive
-// elements: W columns of a row at a time.  (Elements stored as they are held, one sector each: four times as long for a
-// 1501 x 777 result.)
+// Stores of a warp's 32 rows by 32 columns, a row per thread.  They are turned in shared memory first, so that a store
+// instruction writes whole sectors of few rows rather than 16 bytes of 32 rows: words of 16 bytes where the rows allow it,
+// kTurn elements of a row at a time elsewhere.
 // ---------------------------------------------------------------------------
+
+// 32 rows of P bytes (64 or 32) in words of 16; no two lanes of a quarter warp in one bank, putting or taking.
+template <int P> __device__ __forceinline__ uint4 *turn_word(uint8_t *turn, int row, int word) {
+    return reinterpret_cast<uint4 *>(turn + row * P + (P == 64 ? word ^ (row >> 1 & 3) : word ^ (row >> 2 & 1)) * 16);
+}
+template <int P> __device__ __forceinline__ void turn_put_word(uint8_t *turn, int word, const uint4 &v) { *turn_word<P>(turn, threadIdx.x & 31, word) = v; }
+// 8 elements from column c (a multiple of 8) of those P bytes on.
+template <int P, typename T> __device__ __forceinline__ void turn_put_8(uint8_t *turn, int c, const float (&x)[8]) {
+    const Frag<T, 8> f = round_run<T>(x);
+    uint4 w[sizeof(T) / 2];
+    memcpy(w, &f, sizeof(f));
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) turn_put_word<P>(turn, c * (int)sizeof(T) / 16 + i, w[i]);
+}
+// What all lanes put there goes to p (this lane's row); `there`: the row exists.  Rows that exist come first.
+template <int P> __device__ __forceinline__ void turn_store_words(uint8_t *turn, void *p, int64_t pitch, bool there) {
+    constexpr int kWords = P / 16, kRows = 32 / kWords;             // rows that a warp stores at a time
+    const int lane = threadIdx.x & 31, rows = __popc(__ballot_sync(0xffffffffu, there)), sub = lane / kWords, word = lane % kWords;
+    char *out = (char *)p + (sub - lane) * pitch + word * 16;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kWords; ++i, out += kRows * pitch)
+        if (sub + i * kRows < rows) *reinterpret_cast<uint4 *>(out) = *turn_word<P>(turn, sub + i * kRows, word);
+    __syncwarp();
+}
+
 template <typename T> constexpr int kTurn = 64 / (int)sizeof(T);                       // columns that kTurnBytes hold
 template <typename T, int W> __device__ __forceinline__ int turn_place(int row, int c) {
     // no two lanes of a warp that puts (one column, all rows) or takes in one bank, but for the narrowest
@@ -373,14 +402,14 @@ template <typename T, int W> __device__ __forceinline__ void turn_store(const ui
 }
 template <typename T, typename V> __device__ __forceinline__ void store_32(T *p, int64_t ld, bool there, int n, bool wide, const V (&v)[32], uint8_t *turn) {
     if (wide && n >= 32) {
-        if (there)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float part[8];
+        for (int f = 0; f < 32; f += 8) {
+            float part[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) part[j] = to_float<V>(v[8 * i + j]);
-                store_floats<T, 8>(p + 8 * i, part);
-            }
+            for (int j = 0; j < 8; ++j) part[j] = to_float<V>(v[f + j]);
+            turn_put_8<64, T>(turn, f % kTurn<T>, part);
+            if (f % kTurn<T> + 8 == kTurn<T>) turn_store_words<64>(turn, p + f + 8 - kTurn<T>, ld * (int64_t)sizeof(T), there);
+        }
     } else {
         constexpr int W = kTurn<T>;
 #pragma unroll
@@ -401,6 +430,7 @@ template <typename T> struct StoreRows {
     int wide;
     static __device__ __forceinline__ uint32_t first(int group) { return group * 64; }
     static __device__ __forceinline__ uint32_t second(int group) { return group * 64 + 32; }
+    __device__ __forceinline__ void fetch(int64_t, int64_t) const {}
     __device__ __forceinline__ void store(const float (&a)[32], const float (&)[32], int, int64_t row, int64_t col, uint8_t *turn) const {
         if (col >= cols) return;
         const int64_t left = cols - col;
