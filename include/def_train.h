@@ -41,6 +41,7 @@ enum { DEF_DTYPE_F32 = 0, DEF_DTYPE_BF16 = 1, DEF_DTYPE_F16 = 2 };
 #define DEF_CHECKPOINT_GROUP 32   /* columns of a row that share one exponent            */
 #define DEF_NORM_MAX_C 16384      /* widest row of def_norm_*                            */
 #define DEF_LOGPROB_MAX_TOP 32    /* most alternatives def_logprob_* returns             */
+#define DEF_ORTHOGONALIZE_MAX_STEPS 32
 
 /*
  * The 8-bit checkpoint of X [T, C] (the OCP microscaling layout for 8-bit integers): each run of 32 consecutive
@@ -233,6 +234,26 @@ int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, int64_t F, in
 int def_feed_forward_backward_workspace(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *dout,
                                         int64_t lddout, const void *w_in, const void *w_down, const void *dboth, int64_t lddb,
                                         int64_t *bytes_out);
+
+/*
+ * Orthogonalises updates: for each matrix x [rows, cols] of the batch, with X = x / (|x|_F + eps) (transposed if tall) and the
+ * steps' coefficients (a, b, c) in turn,
+ *     A = X X^T,   X <- (a I + b A + c A A) X,        out = scale X
+ * which takes each singular value s to s (a + b s^2 + c s^4) and leaves the singular vectors.  coeffs: 3 * steps numbers in HOST
+ * memory, each within 8 of 0, read before the call returns; 1 <= steps <= DEF_ORTHOGONALIZE_MAX_STEPS.
+ * Matrix i of x starts at element i * stride_x and has rows of ldx; out likewise.  So one call serves a weight in all W rows of
+ * def_step's gradients (stride d), at any 4-byte address, and in place: out may be x itself (same strides).
+ * rows, cols and batch are at most 2^16; batch = 0 is a no-op.
+ * The norm is summed in 64 bits.  X, A and B are held in 22 bits (two fp16 pieces each), products are exact and summed in
+ * fp32.  Singular values have to stay below 4 and the entries of B below 16 (larger ones give infinities and NaN), as they do
+ * for polynomials that converge on [0, 1]; the 22 bits are relative to 1, so a matrix whose norm is far below eps loses
+ * digits.  A matrix of zeros gives zeros; a NaN or an infinity makes its whole matrix NaN, and no other.
+ * The workspace is at most batch (16 (m + 8) (n + m + 16) + 8192) bytes, m <= n the sides; the second call says how much.
+ */
+int def_orthogonalize(int32_t dtype, int64_t batch, int64_t rows, int64_t cols, const void *x, int64_t ldx,
+                      int64_t stride_x, void *out, int64_t ldo, int64_t stride_o, const float *coeffs, int32_t steps,
+                      float eps, float scale, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+int def_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int64_t *bytes_out);
 
 #ifdef __cplusplus
 }

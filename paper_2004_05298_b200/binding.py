@@ -76,6 +76,8 @@ SIGNATURES = {
     "def_feed_forward_workspace": (ctypes.c_int, [_i32, _i64, _i64, _i64, _i64, _ptr, _i64, _ptr, _ptr, _ptr, _i64, _ptr]),
     "def_feed_forward_backward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _i64, _ptr, _i64] + [_ptr] * 6 + [_ptr, _i64] * 3 + [_ptr] * 3 + [_i64, _ptr]),
     "def_feed_forward_backward_workspace": (ctypes.c_int, [_i32, _i64, _i64, _i64, _i64, _ptr, _i64, _ptr, _ptr, _ptr, _i64, _ptr]),
+    "def_orthogonalize": (ctypes.c_int, [_i32, _i64, _i64, _i64] + [_ptr, _i64, _i64] * 2 + [_ptr, _i32, _f32, _f32, _ptr, _i64, _ptr]),
+    "def_orthogonalize_workspace": (ctypes.c_int, [_i64, _i64, _i64, _ptr]),
     "def_recurrence_backward": (ctypes.c_int, [_i32, _i64, _i64, _i64, _ptr, _ptr, _i64, _ptr] + [_ptr, _i64] * 3 + [_ptr] + [_ptr, _i64] * 2
                                 + [_ptr, _ptr, _i64, _ptr]),
 }
@@ -693,3 +695,40 @@ def def_feed_forward_backward(dout, w_in, w_down, gate_ck, up_ck, dboth, dx, h_o
             *_opt_act(h_out, "h_out", (dt, T, F)), hq, he, w, nw)
     _same_device(dout, w_in, w_down, dboth, dx, h_out, workspace, *gate_ck, *up_ck, *(h_ck or ()))
     _check(lib.def_feed_forward_backward(*args, _stream(stream)))
+
+
+DEF_ORTHOGONALIZE_MAX_STEPS = 32
+DEF_ORTHOGONALIZE_COEFFS = ((3.4445, -4.7750, 2.0315),) * 5    # takes singular values from 0.002 on to within 0.68 .. 1.13
+
+
+def _matrices(t, name):
+    """(dtype code, batch, rows, cols, pointer, row stride, matrix stride) of [rows, cols] or [batch, rows, cols]."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or t.dim() not in (2, 3):
+        raise TypeError("%s must be a float32, bfloat16 or float16 torch tensor of two or three dimensions" % name)
+    if not t.is_cuda:
+        raise TypeError("%s must live on the GPU" % name)
+    rows, cols = t.shape[-2:]
+    batch, stride = (t.shape[0], t.stride(0)) if t.dim() == 3 else (1, 0)
+    if t.stride(-1) != 1 and cols > 1:
+        raise ValueError("the columns of %s must be consecutive" % name)
+    return _DTYPES[t.dtype], batch, rows, cols, t.data_ptr(), t.stride(-2) if rows > 1 else cols, stride
+
+
+def def_orthogonalize_workspace(rows, cols, batch=1):
+    out = ctypes.c_int64(0)
+    _check(lib.def_orthogonalize_workspace(int(batch), int(rows), int(cols), ctypes.byref(out)))
+    return int(out.value)
+
+
+def def_orthogonalize(x, out, coeffs=DEF_ORTHOGONALIZE_COEFFS, eps=1e-7, scale=1.0, workspace=None, stream=None):
+    """out = scale X after the Newton-Schulz steps of `coeffs` (an (a, b, c) for each) from X = x / (|x| + eps); x, out: [rows,
+    cols] or [batch, rows, cols] with any strides of rows and matrices; out may be x."""
+    a, o = _matrices(x, "x"), _matrices(out, "out")
+    if a[:4] != o[:4] or x.dim() != out.dim():
+        raise ValueError("out is %s of %s, expected %s of %s" % (out.dtype, tuple(out.shape), x.dtype, tuple(x.shape)))
+    flat = [float(v) for step in coeffs for v in step]
+    if len(flat) != 3 * len(coeffs):
+        raise ValueError("coeffs must hold three numbers for each step")
+    w, nw = _work(workspace, "workspace")
+    _same_device(x, out, workspace)
+    _check(lib.def_orthogonalize(*a, *o[4:], (ctypes.c_float * len(flat))(*flat), len(coeffs), float(eps), float(scale), w, nw, _stream(stream)))

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libdef_b200.so")
-SOURCES = ["def_api.cu", "def_train_api.cu", "def_block_api.cu", "def_feed_api.cu"]
+SOURCES = ["def_api.cu", "def_train_api.cu", "def_block_api.cu", "def_feed_api.cu", "def_orthogonal_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-shared", "-Xcompiler", "-fPIC", "-cudart", "static",

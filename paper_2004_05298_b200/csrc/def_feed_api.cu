@@ -109,7 +109,7 @@ extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, 
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreGated<E> store = {(E *)h, ldh, T, F, q_stride(F), e_stride(F), gate_q, up_q, gate_e, up_e, wide(h, ldh, es)};
-        rc = launch_product<false, true>(p.first, store, map_x, map_in, stream, "def_feed_forward");
+        rc = launch_product<false, 8>(p.first, store, map_x, map_in, stream, "def_feed_forward");
     });
     if (rc != DEF_OK || !w_down) return rc;
     DEF_TRY(fill(p.a2, dtype, h, ldh, stream, "def_feed_forward (h)"));
@@ -117,7 +117,7 @@ extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, 
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreRows<E> store = {(E *)out, ldout, T, O, wide(out, ldout, es)};
-        rc = launch_product<false, sizeof(E) == 4>(p.second, store, map_h, map_down, stream, "def_feed_forward (out)");
+        rc = launch_product<false, sizeof(E) == 4 ? 8 : 0>(p.second, store, map_h, map_down, stream, "def_feed_forward (out)");
     });
     return rc;
 }
@@ -172,7 +172,7 @@ extern "C" int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, in
         E *dgate = (E *)dboth, *dup = dgate + F;
         const deft::StoreGatedBack<E> store = {dgate, dup, (E *)h_out, lddb, ldh, T, F, q_stride(F), e_stride(F), gate_q, up_q, gate_e, up_e, h_q, h_e,
                                                wide(dgate, lddb, es) && wide(dup, lddb, es), wide(h_out, ldh, es)};
-        rc = launch_product<true, sizeof(E) == 4>(p.first, store, map_a, map_down, stream, "def_feed_forward_backward");
+        rc = launch_product<true, sizeof(E) == 4 ? 8 : 0>(p.first, store, map_a, map_down, stream, "def_feed_forward_backward");
     });
     if (rc != DEF_OK || !dx) return rc;
     DEF_TRY(fill(p.a2, dtype, dboth, lddb, stream, "def_feed_forward_backward (dboth)"));
@@ -180,7 +180,7 @@ extern "C" int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, in
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreRows<E> store = {(E *)dx, lddx, T, C, wide(dx, lddx, es)};
-        rc = launch_product<true, sizeof(E) == 4>(p.second, store, map_both, map_in, stream, "def_feed_forward_backward (dx)");
+        rc = launch_product<true, sizeof(E) == 4 ? 8 : 0>(p.second, store, map_both, map_in, stream, "def_feed_forward_backward (dx)");
     });
     return rc;
 }

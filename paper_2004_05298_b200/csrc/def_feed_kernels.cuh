@@ -57,10 +57,7 @@ template <typename T> struct StoreGated {
     int8_t *gate_q, *up_q;
     uint8_t *gate_e, *up_e;
     int wide;
-    static __device__ __forceinline__ uint32_t first(int group) { return group * 32; }
-    static __device__ __forceinline__ uint32_t second(int group) { return 128 + group * 32; }
-    __device__ __forceinline__ void fetch(int64_t, int64_t) const {}
-    __device__ __forceinline__ void store(const float (&g)[32], const float (&u)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
+    __device__ __forceinline__ void store(float (&g)[32], float (&u)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
         if (c >= F) return;
         const int n = F - c < 32 ? (int)(F - c) : 32;
         const bool there = row < rows;
@@ -98,15 +95,8 @@ template <typename T> struct StoreGatedBack {
     int8_t *h_q;
     uint8_t *h_e;
     int wide, wide_h;                     // of dgate and dup; of h
-    static __device__ __forceinline__ uint32_t first(int group) { return group * 64; }
-    static __device__ __forceinline__ uint32_t second(int group) { return group * 64 + 32; }
-    __device__ __forceinline__ void fetch(int64_t row, int64_t c) const {
-        if (row >= rows || c >= F) return;
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(gate_q + row * ldq + c));
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(up_q + row * ldq + c));
-    }
     // 8 columns at a time, so that little is held at once; only h^ is needed for the whole group.
-    __device__ __forceinline__ void store(const float (&dh)[32], const float (&)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
+    __device__ __forceinline__ void store(float (&dh)[32], float (&)[32], int, int64_t row, int64_t c, uint8_t *turn) const {
         if (c >= F) return;
         const int n = F - c < 32 ? (int)(F - c) : 32;
         const bool there = row < rows, direct = wide && n >= 32;

@@ -6,11 +6,11 @@
 //
 // A pair of CTAs works on a 256 x 256 tile (cta_group::2): each brings half of either operand, 64 deep, in a ring of kStages,
 // and holds half of D's rows in tensor memory, two tiles of them, so that the epilogue of one runs under the products of the
-// next.  The matrix unit truncates when it accumulates, so where a result keeps more than 16 bits (LONG) the accumulator is
-// emptied into fp32 registers every kChain stages, 512 terms.
+// next.  The matrix unit truncates when it accumulates, so where a result keeps more than 16 bits the accumulator is
+// emptied into fp32 registers every CHAIN stages of 64 terms (0: at the end only).
 //
 // Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread of the even CTA), 2 reports to it what has
-// landed, the last 16 empty accumulators and store, 64 columns of a row per thread.
+// landed, the last 8 or 16 empty accumulators and store, 128 or 64 columns of a row per thread.
 #pragma once
 
 #include <cuda.h>
@@ -23,12 +23,13 @@ namespace deft {
 constexpr int kTileRows = 128, kTileCols = 256, kTileK = 64;           // of one CTA's accumulator; k per stage
 constexpr int kHalfBytes = kTileRows * kTileK * 2;                     // of either operand's half in a stage
 constexpr int kStages = 6;
-constexpr int kStoreWarps = 16;
-constexpr int kProductThreads = 128 + 32 * kStoreWarps;
-constexpr int kControlRegisters = 56, kStoreRegisters = 104;           // a thread's, of the first 4 warps and of the others
 constexpr int kTurnBytes = 2048;                                       // per storing warp: rows that are turned before they are stored
-constexpr int kProductSmem = 1024 + kStages * 2 * kHalfBytes + kStoreWarps * kTurnBytes + 256;
-constexpr int kChain = 8;                                              // stages per accumulator hand-over
+// Sums in registers need them for 128 columns a thread, of 8 warps; else 16 warps keep up with more at a time.
+template <int CHAIN> struct ProductShape {
+    static constexpr int store_warps = CHAIN ? 8 : 16, threads = 128 + 32 * store_warps;
+    static constexpr int control_registers = 56, store_registers = CHAIN ? 224 : 104;     // a thread's, of the first 4 warps and of the others
+    static constexpr int smem = 1024 + kStages * 2 * kHalfBytes + store_warps * kTurnBytes + 256;
+};
 constexpr int64_t kPartFloats = (int64_t)kTileRows * kTileCols;        // of a CTA's part of a tile
 
 struct Product {
@@ -53,7 +54,7 @@ __host__ __device__ inline int64_t product_pieces(const Product &p) { return p.w
 struct Piece {
     int64_t tile;
     int k0, k1;                           // stages
-    __device__ Piece(const Product &p, int64_t i) {
+    __device__ Piece(const Product &p, int i) {
         const int per_tile = p.blocks * p.pairs;
         if (i < p.whole) {
             tile = i;
@@ -115,17 +116,17 @@ __device__ __forceinline__ void split_columns(const Pair (&x)[16], float (&out)[
     for (int j = 0; j < 16; ++j) split_pair(x[j], out[2 * j], out[2 * j + 1]);
 }
 
-// Epilogue: a thread has 64 columns of one row, 32 from first(group) on and 32 from second(group), the group one of four.
-// store() gets 32 of them at a time, or (kBoth) all at once, with the row and the column they belong to; whole warps call it,
-// with rows and columns that may lie outside the result.  fetch() comes long before it, for what store() will read.
-template <typename EPILOGUE, bool BN, bool LONG>
-__global__ void __launch_bounds__(kProductThreads, 1)
-    product_kernel(const Product p, const EPILOGUE epilogue, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+// Epilogue: store() gets 32 columns of a row per thread at a time, columns 32 u of the tile on for u < 8, or (kBoth) for u < 4
+// those and 32 columns from 128 + 32 u on; whole warps call it, with rows and columns that may lie outside the result.
+template <typename EPILOGUE, bool BN, int CHAIN>
+__global__ void __launch_bounds__(ProductShape<CHAIN>::threads, 1)
+    product_kernel(const __grid_constant__ Product p, const __grid_constant__ EPILOGUE epilogue, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+    using S = ProductShape<CHAIN>;
     extern __shared__ uint8_t raw[];
     uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sa = base, *sb = sa + kStages * kHalfBytes;
     uint8_t *turns = sb + kStages * kHalfBytes;
-    uint64_t *bars = (uint64_t *)(turns + kStoreWarps * kTurnBytes);
+    uint64_t *bars = (uint64_t *)(turns + S::store_warps * kTurnBytes);
     const uint32_t full = smem_address(bars), empty = full + 8 * kStages, ready = empty + 8 * kStages, acc_full = ready + 8 * kStages,
                    acc_empty = acc_full + 16, drained = acc_empty + 16;
     uint32_t *tmem_slot = (uint32_t *)(bars + 3 * kStages + 5);
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(acc_full + 8 * b, 1);
-            barrier_init(acc_empty + 8 * b, 2 * kStoreWarps);
+            barrier_init(acc_empty + 8 * b, 2 * S::store_warps);
         }
         barrier_init(drained, 1);
         *failed = 0;
@@ -156,17 +157,17 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     tmem_fence_after();
     const uint32_t tmem = *tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the set-up above may overlap the kernel before
-    const int64_t pieces = product_pieces(p), step = gridDim.x / 2;
+    const int pieces = (int)product_pieces(p), step = (int)gridDim.x / 2;   // the host keeps them below 2^30
     int batch, tm, tn;
 
     if (warp < 4) {
-        registers_down<kControlRegisters>();
+        registers_down<S::control_registers>();
         if (warp == 0 && lane == 0) {
             prefetch_map(&map_a);
             prefetch_map(&map_b);
             uint32_t n = 0;
             bool ok = true;
-            for (int64_t i = blockIdx.x / 2; ok && i < pieces; i += step) {
+            for (int i = (int)blockIdx.x / 2; ok && i < pieces; i += step) {
                 const Piece w(p, i);
                 product_place(p, w.tile, batch, tm, tn);
                 const int m0 = tm * 2 * kTileRows + rank * kTileRows, n0 = tn * p.step_n + (rank ? p.second : 0);
@@ -197,13 +198,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const uint32_t idesc = product_descriptor(p.bf16 != 0, BN);
             uint32_t n = 0, chunk = 0;
             bool ok = true;
-            for (int64_t i = blockIdx.x / 2; ok && i < pieces; i += step) {
+            for (int i = (int)blockIdx.x / 2; ok && i < pieces; i += step) {
                 const Piece w(p, i);
                 for (int k = w.k0; k < w.k1 && ok; ++chunk) {
                     const uint32_t buf = chunk & 1, round = chunk >> 1;
                     if (!(ok = barrier_wait(acc_empty + 8 * buf, (round & 1) ^ 1, failed))) break;
                     tmem_fence_after();
-                    const int stop = LONG && k + kChain < w.k1 ? k + kChain : w.k1;
+                    const int stop = CHAIN && k + CHAIN < w.k1 ? k + CHAIN : w.k1;
                     for (int first = k; k < stop; ++k, ++n) {
                         const uint32_t s = n % kStages;
                         if (!(ok = barrier_wait(ready + 8 * s, (n / kStages) & 1, failed))) break;   // in both CTAs
@@ -225,7 +226,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         } else if (warp == 2 && lane == 0) {
             uint32_t n = 0;
             bool ok = true;
-            for (int64_t i = blockIdx.x / 2; ok && i < pieces; i += step) {
+            for (int i = (int)blockIdx.x / 2; ok && i < pieces; i += step) {
                 const Piece w(p, i);
                 for (int k = w.k0; k < w.k1; ++k, ++n) {
                     if (!(ok = barrier_wait(full + 8 * (n % kStages), (n / kStages) & 1, failed))) break;
@@ -234,40 +235,41 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             }
         }
     } else {
-        registers_up<kStoreRegisters>();
-        const int group = (warp - 4) >> 2, quarter = warp & 3;      // lanes quarter * 32..
+        registers_up<S::store_registers>();
+        // a warp's columns, in units of 32: kUnits from its group's first on
+        constexpr int kAll = EPILOGUE::kBoth ? 4 : 8, kUnits = kAll * 4 / S::store_warps, kSums = EPILOGUE::kBoth ? 2 * kUnits : kUnits;
+        const int unit = ((warp - 4) >> 2) * kUnits, quarter = warp & 3;      // lanes quarter * 32..
         const int row = quarter * 32 + lane;
         const uint32_t source = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t c0 = EPILOGUE::first(group), c1 = EPILOGUE::second(group);
         uint8_t *turn = turns + (warp - 4) * kTurnBytes;
         uint32_t chunk = 0;
         bool ok = true;
-        for (int64_t i = blockIdx.x / 2; i < pieces; i += step) {
+        for (int i = (int)blockIdx.x / 2; i < pieces; i += step) {
             const Piece w(p, i);
-            product_place(p, w.tile, batch, tm, tn);
-            const int64_t r0 = (int64_t)tm * 2 * kTileRows + rank * kTileRows + row, n0 = (int64_t)tn * p.step_n;
             const bool cut = i >= p.whole && p.cuts > 1;
-            float *parts = p.parts + ((i - p.whole) * 2 + rank) * kPartFloats + row;
-            if (!cut) {
-                epilogue.fetch(r0, n0 + c0);
-                epilogue.fetch(r0, n0 + c1);
-            }
+            // where this thread's columns belong
+            const auto place = [&](int64_t &r0, int64_t &n0) {
+                product_place(p, w.tile, batch, tm, tn);
+                r0 = (int64_t)tm * 2 * kTileRows + rank * kTileRows + row;
+                n0 = (int64_t)tn * p.step_n;
+            };
             float a[32], b[32];
-            constexpr int kTurns = EPILOGUE::kBoth ? 1 : 2;
-            const auto put = [&](int t) {                           // a (and b), columns of turn t
+            const auto put = [&](int u) {                           // a (and b), the columns of unit u
                 if (__any_sync(0xffffffffu, !ok || *failed)) {      // a wait ran out: no numbers rather than wrong ones
                     ok = false;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) a[j] = b[j] = NAN;
                 }
-                const uint32_t c = t ? c1 : c0;
                 if (!cut) {
-                    epilogue.store(a, b, batch, r0, n0 + c, turn);
+                    int64_t r0, n0;
+                    place(r0, n0);
+                    epilogue.store(a, b, batch, r0, n0 + 32 * u, turn);
                 } else {
+                    float *parts = p.parts + ((i - p.whole) * 2 + rank) * kPartFloats + 32 * u * kTileRows + row;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        parts[(c + j) * kTileRows] = a[j];
-                        if (EPILOGUE::kBoth) parts[(c1 + j) * kTileRows] = b[j];
+                        parts[j * kTileRows] = a[j];
+                        if (EPILOGUE::kBoth) parts[(128 + j) * kTileRows] = b[j];
                     }
                 }
             };
@@ -276,25 +278,33 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 __syncwarp();
                 if (lane == 0) barrier_arrive_at(acc_empty + 8 * buf, 0);
             };
-            if constexpr (LONG) {
-                Pair sa[16], sb[16];
+            if constexpr (CHAIN > 0) {
+                Pair sum[kSums][16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sa[j] = sb[j] = make_pair(0.f, 0.f);
-                for (int k = w.k0; k < w.k1; k += kChain, ++chunk) {
+                for (int u = 0; u < kSums; ++u)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[u][j] = make_pair(0.f, 0.f);
+                for (int k = w.k0; k < w.k1; k += CHAIN, ++chunk) {
                     const uint32_t buf = chunk & 1, round = chunk >> 1;
                     ok = ok && barrier_wait(acc_full + 8 * buf, round & 1, failed);
                     if (__any_sync(0xffffffffu, !ok)) break;
                     tmem_fence_after();
-                    add_columns(source + buf * kTileCols + c0, sa);
-                    add_columns(source + buf * kTileCols + c1, sb);
+#pragma unroll
+                    for (int u = 0; u < kUnits; ++u) {
+                        add_columns(source + buf * kTileCols + 32 * (unit + u), sum[u]);
+                        if constexpr (EPILOGUE::kBoth) add_columns(source + buf * kTileCols + 128 + 32 * (unit + u), sum[kUnits + u]);
+                    }
                     release(buf);
                 }
-                split_columns(sa, a);
-                if (EPILOGUE::kBoth) split_columns(sb, b);
 #pragma unroll 1
-                for (int t = 0; t < kTurns; ++t) {
-                    put(t);
-                    split_columns(sb, a);
+                for (int u = 0; u < kUnits; ++u) {                  // one copy of the epilogue's code: the sums move up
+                    split_columns(sum[0], a);
+                    if constexpr (EPILOGUE::kBoth) split_columns(sum[kUnits], b);
+                    put(unit + u);
+#pragma unroll
+                    for (int v = 0; v + 1 < kSums; ++v)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[v][j] = sum[v + 1][j];
                 }
             } else {
                 const uint32_t buf = chunk & 1, round = chunk >> 1;
@@ -303,13 +313,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 ok = __all_sync(0xffffffffu, ok);
                 tmem_fence_after();
 #pragma unroll 1
-                for (int t = 0; t < kTurns; ++t) {                  // the accumulator holds the second turn's columns meanwhile
+                for (int u = 0; u < kUnits; ++u) {                  // the accumulator holds the later units' columns meanwhile
                     if (ok) {
-                        take_columns(source + buf * kTileCols + (t ? c1 : c0), a);
-                        if (EPILOGUE::kBoth) take_columns(source + buf * kTileCols + c1, b);
-                        if (t == kTurns - 1) release(buf);
+                        take_columns(source + buf * kTileCols + 32 * (unit + u), a);
+                        if (EPILOGUE::kBoth) take_columns(source + buf * kTileCols + 128 + 32 * (unit + u), b);
+                        if (u == kUnits - 1) release(buf);
                     }
-                    put(t);
+                    put(unit + u);
                 }
             }
         }
@@ -330,8 +340,7 @@ __global__ void __launch_bounds__(256) product_join_kernel(const Product p, cons
     constexpr int kRuns = EPILOGUE::kBoth ? 4 : 8;
     const int64_t half_tile = blockIdx.x / (kRuns / 2), tile = half_tile / 2;
     const int rank = (int)(half_tile % 2), run = (int)(blockIdx.x % (kRuns / 2)) * 2 + threadIdx.x / 128, row = threadIdx.x % 128;
-    const int group = EPILOGUE::kBoth ? run : run / 2;
-    const uint32_t ca = EPILOGUE::kBoth || run % 2 == 0 ? EPILOGUE::first(group) : EPILOGUE::second(group), cb = EPILOGUE::second(group);
+    const int ca = 32 * run, cb = 128 + 32 * run;
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the parts are those of the kernel before
     float a[32], b[32];
 #pragma unroll
@@ -428,10 +437,7 @@ template <typename T> struct StoreRows {
     T *out;
     int64_t ld, rows, cols;
     int wide;
-    static __device__ __forceinline__ uint32_t first(int group) { return group * 64; }
-    static __device__ __forceinline__ uint32_t second(int group) { return group * 64 + 32; }
-    __device__ __forceinline__ void fetch(int64_t, int64_t) const {}
-    __device__ __forceinline__ void store(const float (&a)[32], const float (&)[32], int, int64_t row, int64_t col, uint8_t *turn) const {
+    __device__ __forceinline__ void store(float (&a)[32], float (&)[32], int, int64_t row, int64_t col, uint8_t *turn) const {
         if (col >= cols) return;
         const int64_t left = cols - col;
         store_32<T>(out + row * ld + col, ld, row < rows, left < 32 ? (int)left : 32, wide, a, turn);

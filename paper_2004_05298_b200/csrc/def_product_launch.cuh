@@ -93,20 +93,23 @@ int64_t plan_cuts(deft::Product &p, int64_t most_bytes = kMostPartBytes) {
     return rest * cuts * each;
 }
 
-template <bool BN, bool LONG, typename EPILOGUE>
+template <bool BN, int CHAIN, typename EPILOGUE>
 int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t stream, const char *what) {
-    const auto kernel = deft::product_kernel<EPILOGUE, BN, LONG>;
-    // The epilogue's warps take over registers that the others give up: those have to be there.
+    using S = deft::ProductShape<CHAIN>;
+    const auto kernel = deft::product_kernel<EPILOGUE, BN, CHAIN>;
+    if (deft::product_pieces(p) >= (int64_t)1 << 30) return fail(DEF_ERR_ARG, "%s: the result is too large", what);
+    // The storing warps take over registers that the others give up: those have to be there.
     cudaFuncAttributes at;
     cudaError_t err = cudaFuncGetAttributes(&at, kernel);
-    if (err == cudaSuccess && at.numRegs * deft::kProductThreads < 128 * deft::kControlRegisters + 32 * deft::kStoreWarps * deft::kStoreRegisters) return fail(DEF_ERR_CUDA, "%s: built with too few registers", what);
-    if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, deft::kProductSmem);
+    if (err == cudaSuccess && at.numRegs * S::threads < 128 * S::control_registers + 32 * S::store_warps * S::store_registers)
+        return fail(DEF_ERR_CUDA, "%s: built with too few registers", what);
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
     if (err == cudaSuccess) {
         const int64_t pieces = deft::product_pieces(p);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)((pieces < kUsualSms / 2 ? pieces : kUsualSms / 2) * 2));
-        cfg.blockDim = dim3(deft::kProductThreads);
-        cfg.dynamicSmemBytes = deft::kProductSmem;
+        cfg.blockDim = dim3(S::threads);
+        cfg.dynamicSmemBytes = S::smem;
         cfg.stream = stream;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -118,3 +118,36 @@ def feed_backward(dout, w_in, w_down, g, u):
     dx = both @ w_in
     edx = (eboth + both.abs() * (0 if pieces else UNIT[dtype])) @ w_in.abs() * 1.01 + chain(2 * F, pieces) * (both.abs() @ w_in.abs())
     return (dg, du, h, dx), (edg, edu, eh, edx)
+
+
+MUON = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def orthogonalize(x, coeffs=MUON, eps=1e-7, scale=1.0):
+    """(out, bound of the error's Frobenius norm) of one matrix in 64 bits.  f(s) = s (a + b s^2 + c s^4) takes an error of X to at
+    most max |f'| times its Frobenius norm (divided differences of an odd function); a step adds what its three products and
+    the 22 bits of A, B and X leave: 2^-22 of a value, 3 2^-22 for the product of the lower pieces, and the chains' truncation
+    (512 terms, 16 at a time, two units each)."""
+    x = x.double()
+    tall = x.shape[0] > x.shape[1]
+    X = x.t() if tall else x
+    X = X / (X.norm() + eps)
+    bits = 2.0 ** -22
+
+    def chain(k, mags):
+        return (2 * min(32, -(-k // 16)) * U32 + 3 * bits + -(-3 * k // 512) * U32) * float(mags.norm())
+
+    err = bits * float(X.norm())
+    for a, b, c in coeffs:
+        m, n = X.shape
+        A = X @ X.t()
+        B = a * torch.eye(m, dtype=X.dtype, device=X.device) + b * A + c * A @ A
+        sx, sa = float(torch.linalg.matrix_norm(X, 2)), float(torch.linalg.matrix_norm(A, 2))
+        s = torch.linspace(0, sx, 1001, dtype=torch.float64)
+        slope = float((a + 3 * b * s ** 2 + 5 * c * s ** 4).abs().max())
+        eA = chain(n, X.abs() @ X.abs().t()) + bits * float(A.norm())
+        eB = (abs(b) + 2 * abs(c) * sa) * eA + abs(c) * chain(m, A.abs() @ A.abs()) + bits * float(B.norm())
+        Y = B @ X
+        err = slope * err + sx * eB + chain(m, B.abs() @ X.abs()) + bits * float(Y.norm())
+        X = Y
+    return scale * (X.t() if tall else X), abs(scale) * err
