@@ -1,4 +1,6 @@
 // C boundary of the operators between a model's input and its gradient rows (see include/def_train.h): recurrence over tokens.
+#include <algorithm>
+
 #include "def_recurrence_kernels.cuh"
 #include "def_train_checks.cuh"
 
@@ -9,48 +11,92 @@ namespace {
 
 constexpr int64_t kMostSteps = (int64_t)1 << 30;
 
+// Where even clusters leave SMs idle, long calls are cut into parts, whose maps a first kernel finds, reading the gate and x (or
+// dy) once more.  Clusters against parts, forward and back, us: 16384 x 1024 bf16 70 against 44, 100 against 60; 65536 x 1024 210
+// against 162, 339 against 250; 16384 x 2048 74 against 86, 109 against 123; few rounds: 2048 x 1024 15 against 18, 21 each.
+constexpr int kFewRounds = 4;
 // How a call is cut: channels per CTA, CTAs of a cluster along time, parts of time.
 struct RecurrencePlan {
-    int lanes, tiles, ranks, parts, part_steps;
+    int tiles, ranks, parts, part_steps;
 };
-RecurrencePlan recurrence_plan(int64_t T, int64_t C, int lanes) {
+RecurrencePlan recurrence_plan(int64_t T, int64_t C, int lanes, int steps, int ctas) {
     RecurrencePlan p;
-    p.lanes = lanes;
     p.tiles = (int)ceil_div(C, 32 * lanes);
-    const int64_t blocks = ceil_div(T, deft::kRecSteps);
+    const int64_t blocks = ceil_div(T, steps);
     p.ranks = 1;
     p.parts = 1;
-    while (p.ranks < deft::kMostCluster && p.ranks * 2 <= blocks && (int64_t)p.tiles * p.ranks < 2 * kUsualSms) p.ranks *= 2;
+    while (p.ranks < deft::kMostCluster && p.ranks * 2 <= blocks && (int64_t)p.tiles * p.ranks * 2 <= ctas * kUsualSms) p.ranks *= 2;
     int64_t each = blocks;
-    if ((int64_t)p.tiles * p.ranks < kUsualSms / 2 && blocks > p.ranks) {
+    if ((int64_t)p.tiles * p.ranks < kUsualSms && blocks > kFewRounds * p.ranks) {
         p.ranks = 1;
-        const int64_t want = ceil_div(3 * kUsualSms, p.tiles), most = want < deft::kMostParts ? want : (int64_t)deft::kMostParts;
+        const int64_t space = 1 + 4096 * C / (ceil_div(C, 64) * 64 * 8);      // parts that the documented workspace has room for
+        const int64_t want = std::min(ceil_div(ctas * kUsualSms, p.tiles), space), most = std::min<int64_t>(want, deft::kMostParts);
         each = ceil_div(blocks, blocks < most ? blocks : most);
         p.parts = (int)ceil_div(blocks, each);
     }
-    p.part_steps = (int)((each > 0 ? each : 1) * deft::kRecSteps);
+    p.part_steps = (int)((each > 0 ? each : 1) * steps);
     return p;
 }
-int64_t recurrence_bytes(const RecurrencePlan &p, int64_t C) { return p.parts > 1 ? (int64_t)p.parts * C * 8 : 0; }
-
-// Two 16-bit elements at a time need even strides, an even width and 4-byte bases; the workspace is sized for either way.
+constexpr int kMostCtas = 4, kShortBlock = 64, kLongBlock = 128;
+// The workspace is sized for every form a call of this size may take.
 int64_t recurrence_need(int32_t dtype, int64_t T, int64_t C) {
-    const int64_t one = recurrence_bytes(recurrence_plan(T, C, 1), C), two = recurrence_bytes(recurrence_plan(T, C, 2), C);
-    return element_size(dtype) == 2 && two > one ? two : one;
+    int64_t parts = 1;
+    for (int lanes = 1; lanes <= 2; ++lanes)
+        for (int steps : {kShortBlock, kLongBlock})
+            for (int ctas = 2; ctas <= kMostCtas; ++ctas) {
+                const int64_t n = recurrence_plan(T, C, lanes, steps, ctas).parts;
+                if (n > parts) parts = n;
+            }
+    return parts > 1 ? (parts - 1) * ceil_div(C, 64) * 64 * 8 : 0;
 }
 
-template <bool BACK> int recurrence(int32_t dtype, deft::Recurrence a, bool pairs, cudaStream_t stream, const char *what) {
-    const RecurrencePlan p = recurrence_plan(a.T, a.C, pairs ? 2 : 1);
+// Rows that a tensor map takes, in boxes of 64 columns by the steps of a block.
+bool mapped(const void *p, int64_t ld, int64_t T, int64_t es) { return ((uintptr_t)p & 15u) == 0 && (T == 1 || (ld * es % 16 == 0 && ld * es < (int64_t)1 << 40)); }
+int rows_map(CUtensorMap &map, int32_t dtype, const void *p, int64_t T, int64_t C, int64_t ld, int steps) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return fail(DEF_ERR_CUDA, "the driver does not offer tensor maps");
+    const cuuint64_t es = element_size(dtype), dim[2] = {(cuuint64_t)C, (cuuint64_t)T}, stride[1] = {T > 1 ? (cuuint64_t)ld * es : (cuuint64_t)ceil_div(C * es, 16) * 16};
+    const cuuint32_t box[2] = {64, (cuuint32_t)steps}, one[2] = {1, 1};
+    const CUtensorMapDataType type = dtype == DEF_DTYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == DEF_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    if (encode(&map, type, 2, const_cast<void *>(p), dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return fail(DEF_ERR_CUDA, "the driver refused a tensor map");
+    return DEF_OK;
+}
+
+// `pairs`: 16-bit rows can be read two elements at a time; `streamed`: rows can be copied by tensor maps, too.
+template <bool BACK> int recurrence(int32_t dtype, deft::Recurrence a, bool pairs, bool streamed, cudaStream_t stream, const char *what) {
+    int ctas = kMostCtas, steps = deft::kRecSteps;
+    if (streamed)
+        by_dtype(dtype, [&](auto type) {
+            using B = deft::StreamBlock<decltype(type), BACK>;
+            static_assert(B::steps == kLongBlock || B::steps == kShortBlock);
+            static_assert(B::ctas >= 2 && B::ctas <= kMostCtas && (deft::kRecSteps == kLongBlock || deft::kRecSteps == kShortBlock));
+            ctas = B::ctas;
+            steps = B::steps;
+        });
+    const RecurrencePlan p = recurrence_plan(a.T, a.C, streamed || pairs ? 2 : 1, steps, ctas);
     a.tiles = p.tiles;
     a.parts = p.parts;
     a.part_steps = p.part_steps;
+    deft::RecurrenceMaps maps = {};
+    if (streamed) {
+        DEF_TRY(rows_map(maps.gate, dtype, a.gate, a.T, a.C, a.ldg, steps));
+        DEF_TRY(rows_map(maps.first, dtype, BACK ? a.dy : a.x, a.T, a.C, BACK ? a.lddy : a.ldx, steps));
+        if (BACK) {
+            DEF_TRY(rows_map(maps.x, dtype, a.x, a.T, a.C, a.ldx, steps));
+            DEF_TRY(rows_map(maps.y, dtype, a.y, a.T, a.C, a.ldy, steps));
+        }
+    }
     cudaError_t err = cudaSuccess;
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
-        auto launch = [&](auto kernel, int ranks, int parts) {
+        auto launch = [&](auto kernel, int smem, int ranks, int parts, auto... args) {
+            if (err == cudaSuccess && smem > 0) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3((unsigned)(p.tiles * ranks), (unsigned)parts);
             cfg.blockDim = dim3(32 * deft::kRecWarps);
+            cfg.dynamicSmemBytes = (size_t)smem;
             cfg.stream = stream;
             cudaLaunchAttribute attr[1];
             attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -58,12 +104,18 @@ template <bool BACK> int recurrence(int32_t dtype, deft::Recurrence a, bool pair
             attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
             cfg.attrs = attr;
             cfg.numAttrs = ranks > 1 ? 1 : 0;
-            if (err == cudaSuccess) err = cudaLaunchKernelEx(&cfg, kernel, a, ranks);
+            if (err == cudaSuccess) err = cudaLaunchKernelEx(&cfg, kernel, a, ranks, args...);
         };
+        if (streamed) {
+            constexpr int smem = deft::StreamBlock<E, BACK>::smem;
+            if (p.parts > 1) launch(deft::recurrence_stream_kernel<E, BACK, true>, smem, 1, p.parts - 1, maps);
+            launch(deft::recurrence_stream_kernel<E, BACK, false>, smem, p.ranks, p.parts, maps);
+            return;
+        }
         auto both = [&](auto v) {
             constexpr int V = decltype(v)::value ? 2 : 1;
-            if (p.parts > 1) launch(deft::recurrence_kernel<E, V, BACK, true>, 1, p.parts - 1);
-            launch(deft::recurrence_kernel<E, V, BACK, false>, p.ranks, p.parts);
+            if (p.parts > 1) launch(deft::recurrence_kernel<E, V, BACK, true>, 0, 1, p.parts - 1);
+            launch(deft::recurrence_kernel<E, V, BACK, false>, 0, p.ranks, p.parts);
         };
         if constexpr (sizeof(E) == 2) by_alignment(pairs, both);
         else both(Is<false>());
@@ -75,7 +127,8 @@ template <bool BACK> int recurrence(int32_t dtype, deft::Recurrence a, bool pair
     return DEF_OK;
 }
 
-bool even(const void *p, int64_t ld) { return ((uintptr_t)p & 3u) == 0 && ld % 2 == 0; }
+// Whether two elements at a time can be read and written.
+bool even(const void *p, int64_t ld, int64_t es) { return ((uintptr_t)p & (unsigned)(2 * es - 1)) == 0 && ld % 2 == 0; }
 
 int check_sequences(int64_t T, int64_t sequences, const int64_t *offsets) {
     if (T > kMostSteps) return fail(DEF_ERR_ARG, "T must be at most 2^30 (got %lld)", (long long)T);
@@ -118,8 +171,9 @@ extern "C" int def_recurrence_forward(int32_t dtype, int64_t T, int64_t C, int64
     a.ldx = ldx; a.ldg = ldg; a.ldy = ldy;
     a.h0 = h0; a.h_last = h_last; a.offsets = offsets; a.sequences = sequences;
     a.T = (int)T; a.C = (int)C; a.each = (int)(T / sequences); a.summary = (float2 *)workspace;
-    const bool pairs = es == 2 && C % 2 == 0 && even(x, ldx) && even(gate, ldg) && even(y, ldy);
-    return recurrence<false>(dtype, a, pairs, (cudaStream_t)cuda_stream, "def_recurrence_forward");
+    const bool pairs = C % 2 == 0 && even(x, ldx, es) && even(gate, ldg, es) && even(y, ldy, es);
+    const bool streamed = T > 0 && pairs && mapped(x, ldx, T, es) && mapped(gate, ldg, T, es);
+    return recurrence<false>(dtype, a, pairs && es == 2, streamed, (cudaStream_t)cuda_stream, "def_recurrence_forward");
 }
 
 extern "C" int def_recurrence_backward(int32_t dtype, int64_t T, int64_t C, int64_t sequences, const int64_t *offsets, const void *dy,
@@ -152,6 +206,7 @@ extern "C" int def_recurrence_backward(int32_t dtype, int64_t T, int64_t C, int6
     a.ldx = ldx; a.ldg = ldg; a.ldy = ldy; a.lddy = lddy; a.lddx = lddx; a.lddg = lddg;
     a.h0 = h0; a.dh_last = dh_last; a.dh0 = dh0; a.offsets = offsets; a.sequences = sequences;
     a.T = (int)T; a.C = (int)C; a.each = (int)(T / sequences); a.summary = (float2 *)workspace;
-    const bool pairs = es == 2 && C % 2 == 0 && even(dy, lddy) && even(x, ldx) && even(gate, ldg) && even(y, ldy) && even(dx, lddx) && even(dgate, lddg);
-    return recurrence<true>(dtype, a, pairs, (cudaStream_t)cuda_stream, "def_recurrence_backward");
+    const bool pairs = C % 2 == 0 && even(dy, lddy, es) && even(x, ldx, es) && even(gate, ldg, es) && even(y, ldy, es) && even(dx, lddx, es) && even(dgate, lddg, es);
+    const bool streamed = T > 0 && pairs && mapped(dy, lddy, T, es) && mapped(x, ldx, T, es) && mapped(gate, ldg, T, es) && mapped(y, ldy, T, es);
+    return recurrence<true>(dtype, a, pairs && es == 2, streamed, (cudaStream_t)cuda_stream, "def_recurrence_backward");
 }

@@ -14,12 +14,14 @@
 // with a zero of that sign no infinity or NaN of another sequence gets in).
 #pragma once
 
+#include <cuda.h>
+
 #include "def_sm100.cuh"
 #include "def_train_common.cuh"
 
 namespace deft {
 
-constexpr int kRun = 16, kRecWarps = 8, kRecSteps = kRun * kRecWarps;   // steps of a warp; of a CTA's block
+constexpr int kRun = 8, kRecWarps = 8, kRecSteps = kRun * kRecWarps;   // steps of a warp; of a CTA's block
 constexpr int kMostCluster = 8, kMostParts = 256;                       // CTAs in a cluster; parts that time is cut into
 constexpr int kKeptOffsets = 1024;                                      // offsets that fit in shared memory
 
@@ -33,18 +35,16 @@ struct Recurrence {
     int64_t sequences;
     int T, C, each, tiles;
     int parts, part_steps;                      // time is cut into parts of so many steps, each worked on by itself
-    float2 *summary;                            // [parts][C]: (P, L) of each part
+    float2 *summary;                            // (P, L) of each part and channel: [parts][C], or of pairs of channels (P, P, L, L)
 };
 
-template <typename T> __device__ __forceinline__ float fast_exp(float v) {   // two units in the last place and |v| 2^-24
-    return __expf(v);
-}
-template <> __device__ __forceinline__ float fast_exp<float>(float v) { return expf(v); }
-
-__device__ __forceinline__ float min_nan(float a, float b) {       // keeps a NaN
-    float y;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
+// 1 / (1 + exp(g)).  16-bit types: exp is off by two units in the last place and |g| 2^-24.  Results below 2^-126 become 0.
+template <typename T> __device__ __forceinline__ float logistic_back(float g) {
+    float e, c;
+    if constexpr (sizeof(T) == 4) e = expf(g);
+    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * 1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(c) : "f"(1.f + e));
+    return c;
 }
 
 // One lane's V consecutive elements, as they lie in memory.
@@ -118,7 +118,7 @@ struct Places {
 // BACK: steps count from the last token.  PART: only (P, L) of each part.
 // Grid: tiles of channels x CTAs of a cluster, parts.
 template <typename T, int V, bool BACK, bool PART>
-__global__ void __launch_bounds__(32 * kRecWarps) recurrence_kernel(const Recurrence a, int ranks) {
+__global__ void __launch_bounds__(32 * kRecWarps, BACK ? 4 : 1) recurrence_kernel(const Recurrence a, int ranks) {
     __shared__ float2 runs[2][kRecWarps][32 * V];
     __shared__ float2 blocks[2][kMostCluster][32 * V];
     __shared__ int kept[kKeptOffsets];
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(32 * kRecWarps) recurrence_kernel(const Recurr
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 // a step that is not there leaves the state as it is
-                c[j][v] = is_there >> j & 1u ? min_nan(__fdividef(1.f, 1.f + fast_exp<T>(to_float<T>(in_g[j].v[v]))), 1.f) : 0.f;
+                c[j][v] = is_there >> j & 1u ? logistic_back<T>(to_float<T>(in_g[j].v[v])) : 0.f;
                 const float b = to_float<T>(in_b[j].v[v]), keep = 1.f - c[j][v];
                 L[v] = BACK ? keep * (L[v] + b) : fmaf(keep, L[v], c[j][v] * b);
                 P[v] *= keep;
@@ -343,6 +343,341 @@ __global__ void __launch_bounds__(32 * kRecWarps) recurrence_kernel(const Recurr
             if (a.each == 0 && !a.offsets || a.offsets && at.bound(q + 1) <= at.bound(q))
 #pragma unroll
                 for (int v = 0; v < V; ++v) leave_to[(int64_t)q * a.C + col + v] = entered(q, v);
+}
+
+// ---------------------------------------------------------------------------
+// The same for rows on 16-byte boundaries: blocks of steps by 64 channels come by tensor copies into a ring, so that loads run
+// on under the two passes over a block and registers hold little.  Small blocks, so that several CTAs share an SM: one
+// computes while others wait for a barrier.  Pass one leaves 1 - c and c x of a step in registers (backward: c; what else
+// pass two needs it reads from the ring again).  A thread has two channels and works on both in one instruction.
+// ---------------------------------------------------------------------------
+template <typename T, bool BACK> struct StreamBlock {
+    static constexpr int run = sizeof(T) == 2 && !BACK ? 16 : 8, steps = run * kRecWarps;
+    static constexpr int tensors = BACK ? 4 : 2, row = 64 * (int)sizeof(T), bytes = steps * row;
+    static constexpr int ctas = 2, stages = 3;
+    static constexpr int smem = stages * tensors * bytes + 128;
+};
+constexpr int kStreamOffsets = 128;             // offsets that are kept in shared memory
+struct RecurrenceMaps {
+    CUtensorMap gate, first, x, y;              // first: x forward, dy backward; x and y: backward only
+};
+
+template <typename T> __device__ __forceinline__ Pair two_channels(const uint8_t *p) {
+    if constexpr (sizeof(T) == 4) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        return make_pair(v.x, v.y);
+    } else {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
+        Few<T, 2> f;
+        memcpy(&f, &w, 4);
+        return make_pair(to_float<T>(f.v[0]), to_float<T>(f.v[1]));
+    }
+}
+template <typename T> __device__ __forceinline__ void store_channels(T *p, Pair v) {
+    float a, b;
+    split_pair(v, a, b);
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float2 *>(p) = make_float2(a, b);
+    } else {
+        Few<T, 2> f;
+        f.v[0] = from_float<T>(a);
+        f.v[1] = from_float<T>(b);
+        uint32_t w;
+        memcpy(&w, &f, 4);
+        *reinterpret_cast<uint32_t *>(p) = w;
+    }
+}
+__device__ __forceinline__ Pair pair_mul(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.bits) : "l"(a.bits), "l"(b.bits));
+    return d;
+}
+__device__ __forceinline__ bool is_nan(Pair p) {
+    float a, b;
+    split_pair(p, a, b);
+    return isnan(a) || isnan(b);
+}
+template <typename T> __device__ __forceinline__ Pair logistic_back(Pair g) {
+    float a, b;
+    if constexpr (sizeof(T) == 4) {
+        split_pair(g, a, b);
+        return make_pair(logistic_back<T>(a), logistic_back<T>(b));
+    } else {
+        split_pair(pair_mul(g, make_pair(1.44269504f, 1.44269504f)), a, b);
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+        split_pair(pair_add(make_pair(a, b), make_pair(1.f, 1.f)), a, b);
+        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+        return make_pair(a, b);
+    }
+}
+struct alignas(16) Map2 { Pair P, L; };          // (P, L) of two channels
+// `calm`: no sequence starts there.
+template <bool CALM> __device__ __forceinline__ Pair advance2(const Map2 &m, Pair s) {
+    if constexpr (CALM) {
+        return pair_fma(m.P, s, m.L);
+    } else {
+        float p0, p1, l0, l1, s0, s1;
+        split_pair(m.P, p0, p1);
+        split_pair(m.L, l0, l1);
+        split_pair(s, s0, s1);
+        return make_pair(advance(make_float2(p0, l0), s0), advance(make_float2(p1, l1), s1));
+    }
+}
+template <bool CALM> __device__ __forceinline__ Map2 join2(const Map2 &first, const Map2 &then) {
+    if constexpr (CALM) {
+        return {pair_mul(then.P, first.P), pair_fma(then.P, first.L, then.L)};
+    } else {
+        float a0, a1, b0, b1, c0, c1, d0, d1;
+        split_pair(first.P, a0, a1);
+        split_pair(first.L, b0, b1);
+        split_pair(then.P, c0, c1);
+        split_pair(then.L, d0, d1);
+        const float2 x = join(make_float2(a0, b0), make_float2(c0, d0)), y = join(make_float2(a1, b1), make_float2(c1, d1));
+        return {make_pair(x.x, y.x), make_pair(x.y, y.y)};
+    }
+}
+// A CTA's block as one, from its warps' runs; the state before a warp's run and behind the cluster's blocks.
+using Runs = const Map2 (&)[kRecWarps][32];
+using Blocks = const Map2 (&)[kMostCluster][32];
+template <bool CALM> __device__ __forceinline__ Map2 join_runs(Runs runs, int lane) {
+    Map2 all = runs[0][lane];
+#pragma unroll
+    for (int w = 1; w < kRecWarps; ++w) all = join2<CALM>(all, runs[w][lane]);
+    return all;
+}
+template <bool CALM> __device__ __forceinline__ Pair advance_all(Runs runs, Blocks blocks, int ranks, int rank, int warp, int lane, Pair &behind) {
+    Pair s = behind;
+    if (ranks > 1) {
+        for (int r = 0; r < ranks; ++r) {
+            if (r == rank) s = behind;
+            behind = advance2<CALM>(blocks[r][lane], behind);
+        }
+        for (int w = 0; w < warp; ++w) s = advance2<CALM>(runs[w][lane], s);
+    } else {
+#pragma unroll
+        for (int w = 0; w < kRecWarps; ++w) {
+            if (w == warp) s = behind;
+            behind = advance2<CALM>(runs[w][lane], behind);
+        }
+    }
+    return s;
+}
+// 16 bytes to another CTA's shared memory, counted there on `bar`.
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map2 &m) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(to), "l"(m.P.bits), "l"(m.L.bits), "r"(bar) : "memory");
+}
+
+template <typename T, bool BACK, bool PART>
+__global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
+    recurrence_stream_kernel(const Recurrence a, int ranks, const __grid_constant__ RecurrenceMaps maps) {
+    using B = StreamBlock<T, BACK>;
+    constexpr int R = B::run, kSteps = B::steps, kUsed = PART ? 2 : B::tensors;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ Map2 runs[2][kRecWarps][32];
+    __shared__ Map2 blocks[2][kMostCluster][32];
+    __shared__ int kept[kStreamOffsets];
+    __shared__ uint64_t bars[B::stages + 2];
+    __shared__ volatile int failed;
+    uint8_t *stages = (uint8_t *)(((uintptr_t)ring + 127) & ~(uintptr_t)127);
+    const uint32_t full = smem_address(bars), got = full + 8 * B::stages;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = ranks > 1 ? (int)cluster_rank() : 0, tile = (int)blockIdx.x / ranks;
+    const int col = tile * 64 + lane * 2;
+    const bool mine = col < a.C;                                 // C is even
+    Places at = {a.offsets, nullptr, (int)a.sequences, a.each, a.T};
+    if (a.offsets && a.sequences < kStreamOffsets) {
+        for (int s = threadIdx.x; s <= at.sequences; s += blockDim.x) {
+            const int64_t o = a.offsets[s];
+            kept[s] = o < 0 ? 0 : o > a.T ? a.T : (int)o;
+        }
+        at.kept = kept;
+    }
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < B::stages + 2; ++s) barrier_init(full + 8 * s, 1);
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (ranks > 1) cluster_sync();                               // all have started before one writes to another
+    const int begin = (int)blockIdx.y * a.part_steps;            // of this part
+    const int end = min(a.T, begin + a.part_steps);
+    const int stride = ranks * kSteps, rounds = (end - begin + stride - 1) / stride;
+    const auto load = [&](int i) {                               // one thread: the block of round i
+        const int s = i % B::stages, run = begin + i * stride + rank * kSteps;
+        const int t0 = BACK ? a.T - run - kSteps : run;          // may lie before the first or behind the last row: zeros there
+        const uint32_t bar = full + 8 * s, to = smem_address(stages + s * B::tensors * B::bytes);
+        barrier_expect(bar, kUsed * B::bytes);
+        tensor_load_2d(to, &maps.gate, tile * 64, t0, bar);
+        tensor_load_2d(to + B::bytes, &maps.first, tile * 64, t0, bar);
+        if constexpr (BACK && !PART) {
+            tensor_load_2d(to + 2 * B::bytes, &maps.x, tile * 64, t0, bar);
+            tensor_load_2d(to + 3 * B::bytes, &maps.y, tile * 64, t0 - 1, bar);
+        }
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < B::stages && i < rounds; ++i) load(i);
+
+    const float *enter_with = BACK ? a.dh_last : a.h0;
+    float *leave_to = BACK ? a.dh0 : a.h_last;
+    const auto entered = [&](int s) {
+        const float *p = enter_with + (int64_t)s * a.C + col;
+        return enter_with && mine ? make_pair(p[0], p[1]) : make_pair(0.f, 0.f);
+    };
+    const auto left = [&](int s, Pair v) {
+        if (!mine) return;
+        float *p = leave_to + (int64_t)s * a.C + col;
+        split_pair(v, p[0], p[1]);
+    };
+    const Pair zero = make_pair(0.f, 0.f), one = make_pair(1.f, 1.f), minus = make_pair(-1.f, -1.f);
+    Map2 whole = {one, zero};                                    // PART: of the part so far; else L is the state before the block
+    if (!PART && mine) {
+#pragma unroll 4
+        for (int p = 0; p < (int)blockIdx.y; ++p)
+            whole.L = advance2<false>(*reinterpret_cast<const Map2 *>(a.summary + ((int64_t)p * a.tiles * 64 + col)), whole.L);
+    }
+    int first = 0, behind = 0;                                   // tokens of a sequence this CTA has come to
+    bool ok = true;
+    int stage = 0, turn = 0;                                     // of the ring: round i is stage i mod stages, in its turn-th use
+    for (int i = 0; i < rounds; ++i, turn ^= stage == B::stages - 1, stage = stage == B::stages - 1 ? 0 : stage + 1) {
+        const int buf = i & 1, base = begin + i * stride, run = base + rank * kSteps + warp * R;
+        // Calm: all of the cluster's blocks of this round lie inside one sequence, its first and last token elsewhere.
+        const int t_lo = BACK ? a.T - base - stride : base, t_hi = t_lo + stride - 1;
+        bool calm = t_lo > first && t_hi < behind - 1 && base + stride <= end;
+        uint32_t is_there = (1u << R) - 1u, enters = 0, leaves = 0;
+        int seq = 0;
+        if (!calm) {
+            bool there = false, enter = false, leave = false;
+            if (base < end) at.find(BACK ? a.T - 1 - min(base + stride, end) + 1 : min(base + stride, end) - 1, first, behind);     // where the round ends
+            if (lane < R && run + lane < end) {
+                const int t = BACK ? a.T - 1 - (run + lane) : run + lane;
+                int lo, hi;
+                seq = at.find(t, lo, hi);
+                there = lo <= t && t < hi;
+                enter = there && t == (BACK ? hi - 1 : lo);
+                leave = there && t == (BACK ? lo : hi - 1);
+            }
+            is_there = __ballot_sync(0xffffffffu, there);
+            enters = __ballot_sync(0xffffffffu, enter);
+            leaves = __ballot_sync(0xffffffffu, leave);
+        }
+        if (!BACK && !leave_to) leaves = 0;                      // nothing happens there
+        const bool plain = is_there == (1u << R) - 1u && (enters | leaves) == 0;
+        ok = ok && barrier_wait(full + 8 * stage, turn, &failed);
+        // row j of the run; backward a block's rows lie in the order of time
+        const uint8_t *rows = stages + stage * (B::tensors * B::bytes) + (BACK ? kSteps - 1 - warp * R : warp * R) * B::row + lane * (B::row / 32);
+        constexpr int kStep = BACK ? -B::row : B::row;
+        Pair keep[R], in[R];                                     // 1 - c, c x (backward: c)
+        Map2 m = {one, zero};
+        const auto pass_one = [&](int j, Pair &keep_j, Pair &in_j) {
+            const Pair c = logistic_back<T>(two_channels<T>(rows + j * kStep)), b = two_channels<T>(rows + j * kStep + B::bytes);
+            keep_j = pair_fma(c, minus, one);
+            if constexpr (BACK) {
+                in_j = c;
+                m.L = pair_mul(keep_j, pair_add(m.L, b));
+            } else {
+                in_j = pair_mul(c, b);
+                m.L = pair_fma(keep_j, m.L, in_j);
+            }
+            m.P = pair_mul(m.P, keep_j);
+        };
+        if (plain) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) pass_one(j, keep[j], in[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                if (enters >> j & 1u) m = {make_pair(-0.f, -0.f), entered(__shfl_sync(0xffffffffu, seq, j))};
+                if (is_there >> j & 1u) pass_one(j, keep[j], in[j]);
+            }
+        }
+        runs[buf][warp][lane] = m;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            // forward all are done with this block, backward with the one before
+            if (!BACK || PART) {
+                if (i + B::stages < rounds) load(i + B::stages);
+            } else if (i > 0 && i - 1 + B::stages < rounds) {
+                load(i - 1 + B::stages);
+            }
+        }
+        if (ranks > 1) {
+            if (warp == 0) {
+                const Map2 all = calm ? join_runs<true>(runs[buf], lane) : join_runs<false>(runs[buf], lane);
+                if (lane == 0) barrier_expect(got + 8 * buf, (uint32_t)ranks * sizeof(blocks[0][0]));
+                const uint32_t to = smem_address(&blocks[buf][rank][lane]);
+                for (int r = 0; r < ranks; ++r) send(cluster_address(to, r), cluster_address(got + 8 * buf, r), all);
+            }
+            ok = ok && barrier_wait(got + 8 * buf, i >> 1 & 1, &failed);
+        }
+        if constexpr (PART) {
+            whole = calm ? join2<true>(whole, join_runs<true>(runs[buf], lane)) : join2<false>(whole, join_runs<false>(runs[buf], lane));
+            continue;
+        }
+        // Before this warp's run.  A start's -0 takes a finite state away in the plain product as well; others need the look.
+        Pair next = whole.L, s = advance_all<true>(runs[buf], blocks[buf], ranks, rank, warp, lane, next);
+        if (!calm && __any_sync(0xffffffffu, is_nan(s) || is_nan(next))) {
+            next = whole.L;
+            s = advance_all<false>(runs[buf], blocks[buf], ranks, rank, warp, lane, next);
+        }
+        whole.L = next;
+        if (__any_sync(0xffffffffu, !ok || failed)) {            // a wait ran out: no numbers rather than wrong ones
+            ok = false;
+            s = whole.L = make_pair(NAN, NAN);
+        }
+        const int64_t t0 = BACK ? a.T - 1 - run : run;
+        T *out = BACK ? (T *)a.dx + t0 * a.lddx + col : (T *)a.y + t0 * a.ldy + col, *out_g = (T *)a.dgate + t0 * a.lddg + col;
+        const auto pass_two = [&](int j, Pair keep_j, Pair in_j, Pair before) {
+            if constexpr (!BACK) {
+                s = pair_fma(keep_j, s, in_j);
+                if (mine) store_channels<T>(out, s);
+                out += a.ldy;
+            } else {
+                const Pair b = two_channels<T>(rows + j * kStep + B::bytes), x = two_channels<T>(rows + j * kStep + 2 * B::bytes);
+                const Pair lambda = pair_add(b, s), dx = pair_mul(in_j, lambda);
+                s = pair_mul(keep_j, lambda);
+                const Pair dg = pair_mul(pair_mul(dx, keep_j), pair_fma(x, minus, before));
+                if (mine) {
+                    store_channels<T>(out, dx);
+                    store_channels<T>(out_g, dg);
+                }
+                out -= a.lddx;
+                out_g -= a.lddg;
+            }
+        };
+        const auto earlier = [&](int j) { return BACK ? two_channels<T>(rows + j * kStep + 3 * B::bytes) : zero; };
+        if (plain) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) pass_two(j, keep[j], in[j], earlier(j));
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const int q = __shfl_sync(0xffffffffu, seq, j);
+                if (enters >> j & 1u) s = ok ? entered(q) : make_pair(NAN, NAN);
+                if (is_there >> j & 1u) {
+                    Pair before = earlier(j);
+                    if (BACK && (leaves >> j & 1u)) {
+                        const float *p = a.h0 + (int64_t)q * a.C + col;
+                        before = a.h0 && mine ? make_pair(p[0], p[1]) : zero;
+                    }
+                    pass_two(j, keep[j], in[j], before);
+                } else {
+                    out += BACK ? -a.lddx : a.ldy;
+                    out_g -= a.lddg;
+                }
+                if (leave_to && (leaves >> j & 1u)) left(q, s);
+            }
+        }
+    }
+    if (PART) {
+        if (warp == 0) *reinterpret_cast<Map2 *>(a.summary + ((int64_t)blockIdx.y * a.tiles * 64 + col)) = whole;
+        return;
+    }
+    // A sequence without tokens hands on what it was given.
+    if (leave_to && blockIdx.y == 0 && rank == 0 && mine && a.offsets)
+        for (int q = warp; q < at.sequences; q += kRecWarps)
+            if (at.bound(q + 1) <= at.bound(q)) left(q, entered(q));
 }
 
 }  // namespace deft
