@@ -1,5 +1,6 @@
 // C boundary of the gated feed-forward block (see include/def_train.h).
 #include <algorithm>
+#include <type_traits>
 
 #include "def_feed_kernels.cuh"
 #include "def_product_launch.cuh"
@@ -32,6 +33,15 @@ FeedPlan feed_plan(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, co
     }
     return p;
 }
+// How few tokens without checkpoints are worked on: as columns of products whose rows are the weights (16 bits, in place), or
+// against rows of the weights read by warps (fp32, or rows off 16-byte boundaries).
+enum class Few { no, columns, rows };
+Few few_tokens(int32_t dtype, int64_t T, bool checkpoints, const FeedPlan &p) {
+    const bool copied = p.a1.copy || p.b1.copy || p.a2.copy || p.b2.copy;
+    if (checkpoints) return Few::no;
+    if (element_size(dtype) == 2 && !copied && T <= deft::kMostTokens) return Few::columns;
+    return T <= deft::kFewTokens ? Few::rows : Few::no;
+}
 // dout [T, O] and w_down [O, F]; dboth [T, 2F] and w_in [2F, C] (w_in NULL: without the second product).
 FeedPlan back_plan(int32_t dtype, int64_t T, int64_t C, int64_t F, int64_t O, const void *dout, int64_t lddout, const void *w_in, const void *w_down,
                    const void *dboth, int64_t lddb) {
@@ -57,6 +67,56 @@ int check_workspace(const void *workspace, int64_t bytes, int64_t need) {
     if (need > 0 && !workspace) return fail(DEF_ERR_NULL, "workspace must not be NULL");
     if (bytes < need) return fail(DEF_ERR_ARG, "the workspace must have %lld bytes (got %lld)", (long long)need, (long long)bytes);
     return DEF_OK;
+}
+// Tokens as N: k is cut so that there are about two CTAs per SM.
+template <typename E, bool GATED>
+cudaError_t launch_tokens(int64_t T, int64_t rows, int64_t k, E *out, int64_t ldo, const CUtensorMap &map_w, const CUtensorMap &map_x, bool after, cudaStream_t stream) {
+    const int64_t tiles = ceil_div(rows, deft::kTileRows), blocks = ceil_div(k, deft::kTileK);
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({deft::kMostSplit, 2 * kUsualSms / tiles, blocks / 2}));
+    const deft::TokenProduct p = {(int)T, (int)blocks, std::is_same_v<E, __nv_bfloat16>, rows, ldo};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)tiles, (unsigned)splits);
+    cfg.blockDim = dim3(192);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.y = (unsigned)splits;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = after ? 2 : 1;
+    auto launch = [&](auto kernel, int smem) {
+        cfg.dynamicSmemBytes = (size_t)smem;
+        const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        return err == cudaSuccess ? cudaLaunchKernelEx(&cfg, kernel, p, out, map_w, map_x) : err;
+    };
+    return T <= 16 ? launch(deft::token_product_kernel<E, GATED, 16>, deft::TokenShape<GATED, 16>::smem)
+                   : launch(deft::token_product_kernel<E, GATED, 32>, deft::TokenShape<GATED, 32>::smem);
+}
+int token_box(int64_t T) { return T <= 16 ? 16 : 32; }
+template <typename E, bool GATED>
+cudaError_t launch_rows(const deft::FewTokens<E> &a, bool after, cudaStream_t stream) {
+    const bool aligned = a.cols % 8 == 0 && wide(a.x, a.tokens > 1 ? a.ldx : 8, sizeof(E)) && wide(a.w, 8, sizeof(E));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ceil_div(a.rows, deft::kFewWarps));
+    cfg.blockDim = dim3(32 * deft::kFewWarps);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = after ? 1 : 0;
+    cudaError_t err = cudaSuccess;
+    auto launch = [&](auto tokens) {
+        constexpr int N = decltype(tokens)::value;
+        err = aligned ? cudaLaunchKernelEx(&cfg, deft::few_tokens_kernel<E, N, GATED, true>, a) : cudaLaunchKernelEx(&cfg, deft::few_tokens_kernel<E, N, GATED, false>, a);
+    };
+    if (a.tokens <= 1) launch(std::integral_constant<int, 1>());
+    else if (a.tokens <= 2) launch(std::integral_constant<int, 2>());
+    else if (a.tokens <= 4) launch(std::integral_constant<int, 4>());
+    else launch(std::integral_constant<int, 8>());
+    return err;
 }
 View weights_view(const void *p, const char *name, int64_t rows, int64_t cols, int64_t es) { return rows_view(p, name, p ? 1 : 0, rows * cols, rows * cols, es, false); }
 
@@ -93,6 +153,39 @@ extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, 
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    const Few few = few_tokens(dtype, T, gate_q != nullptr, feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh));
+    if (few == Few::columns) {
+        const bool half = dtype == DEF_DTYPE_F16;
+        CUtensorMap map_x, map_in, map_h, map_down;
+        DEF_TRY(operand_map(map_x, half, x, C, T, 1, T > 1 ? ldx : ceil_div(C, 8) * 8, token_box(T)));
+        DEF_TRY(operand_map(map_in, half, w_in, C, 2 * F, 1, C, deft::kTileRows));
+        if (out) {
+            DEF_TRY(operand_map(map_h, half, h, F, T, 1, T > 1 ? ldh : ceil_div(F, 8) * 8, token_box(T)));
+            DEF_TRY(operand_map(map_down, half, w_down, F, O, 1, F, deft::kTileRows));
+        }
+        cudaError_t err = cudaSuccess;
+        by_dtype(dtype, [&](auto type) {
+            using E = decltype(type);
+            if constexpr (sizeof(E) == 2) {
+                err = launch_tokens<E, true>(T, F, C, (E *)h, ldh, map_in, map_x, false, stream);
+                if (err == cudaSuccess && out) err = launch_tokens<E, false>(T, O, F, (E *)out, ldout, map_down, map_h, true, stream);
+            }
+        });
+        if (err == cudaSuccess) return DEF_OK;
+        cudaGetLastError();
+        return cuda_fail(err, "def_feed_forward");
+    }
+    if (few == Few::rows) {
+        cudaError_t err = cudaSuccess;
+        by_dtype(dtype, [&](auto type) {
+            using E = decltype(type);
+            err = launch_rows<E, true>({(const E *)x, (const E *)w_in, (E *)h, ldx, ldh, F, C, (int)T}, false, stream);
+            if (err == cudaSuccess && out) err = launch_rows<E, false>({(const E *)h, (const E *)w_down, (E *)out, ldh, ldout, O, F, (int)T}, true, stream);
+        });
+        if (err == cudaSuccess) return DEF_OK;
+        cudaGetLastError();
+        return cuda_fail(err, "def_feed_forward");
+    }
     FeedPlan p = feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh);
     p.put(workspace);
     // The maps first: nothing is launched where the driver refuses one.

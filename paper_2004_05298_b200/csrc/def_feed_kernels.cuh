@@ -149,4 +149,236 @@ template <typename T> struct StoreGatedBack {
     }
 };
 
+// ---------------------------------------------------------------------------
+// Few tokens: every weight is read once and there is little else to do, so a warp takes one row of w_in's gate and the same of
+// its other half (or one row of w_down), in runs of 8 elements per lane, several of them ahead, and multiplies them by all tokens'
+// elements in fp32.  The weights of the second product are on their way before the first one is done.
+// ---------------------------------------------------------------------------
+constexpr int kFewTokens = 8, kFewWarps = 8;
+
+template <typename T> struct FewTokens {
+    const T *x, *w;
+    T *out;
+    int64_t ldx, ldo, rows, cols;             // of w (gated: of either half)
+    int tokens;
+};
+
+template <typename T, int TOKENS, bool GATED, bool ALIGNED>
+__global__ void __launch_bounds__(32 * kFewWarps) few_tokens_kernel(const FewTokens<T> a) {
+    constexpr int kRows = GATED ? 2 : 1, kAhead = (sizeof(T) == 2 ? 8 : 4) / kRows;
+    const int lane = threadIdx.x & 31, C = (int)a.cols;
+    const int64_t row = (int64_t)blockIdx.x * kFewWarps + threadIdx.x / 32;
+    const bool there = row < a.rows;
+    const T *w[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) w[r] = a.w + ((there ? row : 0) + r * a.rows) * a.cols;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    Frag<T, 8> f[kAhead][kRows];
+    const auto fetch = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const int c = c0 + (i * 32 + lane) * 8;
+                f[i][r] = there && c < C ? load_cols<T, ALIGNED>(w[r], c, C) : zeros<T, 8>();
+            }
+    };
+    fetch(0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");             // x may come from the kernel before
+    float sum[kRows][TOKENS];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) sum[r][t] = 0.f;
+    for (int c0 = 0; c0 < C; c0 += kAhead * 256) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int c = c0 + (i * 32 + lane) * 8;
+            float v[kRows][8];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) to_floats<T, 8>(f[i][r], v[r]);
+            if (c < C) {
+#pragma unroll
+                for (int t = 0; t < TOKENS; ++t) {
+                    const T *x = a.x + (t < a.tokens ? t : a.tokens - 1) * a.ldx;
+                    Frag<T, 8> g;
+                    if constexpr (ALIGNED) g = *reinterpret_cast<const Frag<T, 8> *>(x + c);
+                    else g = load_run<T>(x, c, C);
+                    float u[8];
+                    to_floats<T, 8>(g, u);
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum[r][t] = fmaf(v[r][j], u[j], sum[r][t]);
+                }
+            }
+        }
+        if (c0 + kAhead * 256 < C) fetch(c0 + kAhead * 256);
+    }
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+        float y = warp_sum(sum[0][t]);
+        if constexpr (GATED) y = y * logistic<T>(y) * warp_sum(sum[1][t]);
+        if (lane == 0 && there && t < a.tokens) a.out[t * a.ldo + row] = from_float<T>(y);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Up to 32 tokens in 16 bits on tensor cores: 128 rows of the weights (gated: of either half) are M, the tokens N, so that the
+// weights stream through two rings per SM and nothing else is moved.  k is cut over the CTAs of a cluster, which leave their sums in
+// shared memory and add a share of them each, in the order of k.
+//
+// Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread), the last 4 take the sums.
+// ---------------------------------------------------------------------------
+constexpr int kMostTokens = 32, kMostSplit = 8;
+template <bool GATED, int N> struct TokenShape {
+    static constexpr int tiles = GATED ? 2 : 1, stages = GATED ? 3 : 5;
+    static constexpr int bytes_w = kTileRows * kTileK * 2, bytes_x = N * kTileK * 2, bytes = tiles * bytes_w + bytes_x;
+    static constexpr int columns = tiles * N < 32 ? 32 : tiles * N;                          // of tensor memory
+    static constexpr int smem = 1024 + stages * bytes + 128;
+    static_assert(tiles * N * kTileRows * 4 <= stages * bytes);                              // the sums take the ring's place
+};
+struct TokenProduct {
+    int tokens, blocks, bf16;             // blocks: of k
+    int64_t rows, ldo;                    // rows of the weights (gated: of either half)
+};
+
+__device__ __forceinline__ void mma_single(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit_single(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+template <typename T, bool GATED, int N>
+__global__ void __launch_bounds__(192, 2) token_product_kernel(const TokenProduct p, T *__restrict__ out, const __grid_constant__ CUtensorMap map_w,
+                                                               const __grid_constant__ CUtensorMap map_x) {
+    using S = TokenShape<GATED, N>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[2 * S::stages + 1];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int failed;
+    uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t full = smem_address(bars), empty = full + 8 * S::stages, done = empty + 8 * S::stages;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, splits = (int)gridDim.y, rank = (int)blockIdx.y;      // a cluster lies along y
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < 2 * S::stages + 1; ++s) barrier_init(full + 8 * s, 1);
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int k0 = (int)((int64_t)p.blocks * rank / splits), k1 = (int)((int64_t)p.blocks * (rank + 1) / splits);
+    const int row0 = (int)blockIdx.x * kTileRows;
+
+    if (warp == 0 && lane == 0) {
+        const auto weights = [&](int i) {
+            const uint32_t s = i % S::stages, bar = full + 8 * s;
+            barrier_expect(bar, S::bytes);
+            tensor_load_3d(smem_address(base + s * S::bytes), &map_w, (k0 + i) * kTileK, row0, 0, bar);
+            if (GATED) tensor_load_3d(smem_address(base + s * S::bytes + S::bytes_w), &map_w, (k0 + i) * kTileK, (int)p.rows + row0, 0, bar);
+        };
+        const auto tokens = [&](int i) {
+            const uint32_t s = i % S::stages;
+            tensor_load_3d(smem_address(base + s * S::bytes + S::tiles * S::bytes_w), &map_x, (k0 + i) * kTileK, 0, 0, full + 8 * s);
+        };
+        const int n = k1 - k0, first = n < S::stages ? n : S::stages;
+        for (int i = 0; i < first; ++i) weights(i);
+        asm volatile("griddepcontrol.wait;" ::: "memory");         // the tokens may come from the kernel before, the weights do not
+        for (int i = 0; i < first; ++i) tokens(i);
+        bool ok = true;
+        int loaded = first;
+        for (; loaded < n; ++loaded) {
+            if (!(ok = barrier_wait(empty + 8 * (loaded % S::stages), (loaded / S::stages & 1) ^ 1, &failed))) break;
+            weights(loaded);
+            tokens(loaded);
+        }
+        // the copies in flight end before the CTA does
+        const uint64_t start = nanoseconds();
+        for (int m = loaded > S::stages ? loaded - S::stages : 0; m < loaded; ++m)
+            while (!barrier_try(full + 8 * (m % S::stages), m / S::stages & 1) && nanoseconds() - start < kWaitLimit) {}
+    } else if (warp == 1 && lane == 0) {
+        const uint32_t idesc = 1u << 4 | (p.bf16 ? 1u : 0u) << 7 | (p.bf16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17 | (uint32_t)(kTileRows >> 4) << 24;
+        for (int i = 0; i < k1 - k0; ++i) {
+            const uint32_t s = i % S::stages;
+            if (!barrier_wait(full + 8 * s, i / S::stages & 1, &failed)) break;
+            tmem_fence_after();
+            const uint8_t *at = base + s * S::bytes;
+            const uint64_t db = operand_descriptor(smem_address(at + S::tiles * S::bytes_w), kTileK * 128);
+#pragma unroll
+            for (int t = 0; t < S::tiles; ++t) {
+                const uint64_t da = operand_descriptor(smem_address(at + t * S::bytes_w), kTileK * 128);
+#pragma unroll
+                for (int j = 0; j < kTileK / 16; ++j) mma_single(tmem + t * N, da + j * (32 >> 4), db + j * (32 >> 4), idesc, i > 0 || j > 0);
+            }
+            mma_commit_single(empty + 8 * s);
+        }
+        mma_commit_single(done);
+        const uint64_t start = nanoseconds();
+        while (!barrier_try(done, 0) && nanoseconds() - start < kWaitLimit) {}
+    }
+    const int row = (warp & 3) * 32 + lane;                        // of the tile, warps 2 to 5
+    float sum[S::tiles][N];
+    if (warp >= 2) {
+        const bool ok = barrier_wait(done, 0, &failed);
+        tmem_fence_after();
+#pragma unroll
+        for (int t = 0; t < S::tiles; ++t)
+#pragma unroll
+            for (int q = 0; q < N / 16; ++q) {
+                uint32_t v[16];
+                __syncwarp();
+                tmem_load_16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * N + 16 * q, v);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sum[t][16 * q + j] = ok && !failed ? __uint_as_float(v[j]) : NAN;
+            }
+        tmem_fence_before();
+    }
+    const auto store = [&](int t, float a, float b) {
+        if (t < p.tokens && row0 + row < p.rows) out[t * p.ldo + row0 + row] = from_float<T>(GATED ? a * logistic<T>(a) * b : a);
+    };
+    if (splits == 1) {
+        if (warp >= 2)
+#pragma unroll
+            for (int t = 0; t < N; ++t) store(t, sum[0][t], sum[S::tiles - 1][t]);
+        __syncthreads();
+    } else {
+        __syncthreads();                                           // every copy has landed and been used
+        float *mine = (float *)base;
+        if (warp >= 2)
+#pragma unroll
+            for (int t = 0; t < S::tiles; ++t)
+#pragma unroll
+                for (int j = 0; j < N; ++j) mine[(t * N + j) * kTileRows + row] = sum[t][j];
+        cluster_sync();
+        if (warp >= 2)
+            for (int t = rank; t < p.tokens; t += splits) {
+                float a = 0.f, b = 0.f;
+                for (int r = 0; r < splits; ++r) {
+                    a += cluster_load(cluster_address(smem_address(mine + t * kTileRows + row), r));
+                    if (GATED) b += cluster_load(cluster_address(smem_address(mine + (N + t) * kTileRows + row), r));
+                }
+                store(t, a, b);
+            }
+        cluster_sync();                                            // nobody reads this CTA's sums any more
+    }
+    if (warp == 1) {
+        __syncwarp();
+        tmem_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::columns));
+    }
+}
+
 }  // namespace deft
