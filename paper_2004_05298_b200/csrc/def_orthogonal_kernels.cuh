@@ -146,16 +146,13 @@ struct StoreSymmetric {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= alpha;
         if (add) {
-            if (there)
+            Frag<__half, 8> x[8];                                  // all on their way at once
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 8; ++k) x[k] = there ? load_frag<__half, 8>(add + at + k / 4 * plane + k % 4 * 8) : zeros<__half, 8>();
 #pragma unroll
-                    for (int f = 0; f < 32; f += 8) {
-                        float x[8];
-                        to_floats<__half, 8>(*reinterpret_cast<const Frag<__half, 8> *>(add + at + k * plane + f), x);
+            for (int k = 0; k < 8; ++k)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[f + i] = fmaf(beta, x[i], v[f + i]);
-                    }
+                for (int i = 0; i < 8; ++i) v[k % 4 * 8 + i] = fmaf(beta, to_float<__half>(x[k].v[i]), v[k % 4 * 8 + i]);
             const int at_diagonal = row - col >= 0 && row - col < 32 ? (int)(row - col) : -1;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
