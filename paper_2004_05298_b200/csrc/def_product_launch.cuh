@@ -76,7 +76,7 @@ deft::Product product_of(int32_t dtype, int64_t m, int64_t tiles_n, int64_t k, i
 
 // How tiles that do not fill a round of the pairs are cut along k.  Each part has kLeastStages, and the cut has to save
 // kJoinStages more than the join, a launch and a pass over the parts, takes.
-constexpr int kLeastStages = 4, kJoinStages = 16;
+constexpr int kLeastStages = 4, kJoinStages = 4;
 constexpr int64_t kMostPartBytes = (int64_t)kUsualSms * deft::kPartFloats * 4;
 int64_t plan_cuts(deft::Product &p, int64_t most_bytes = kMostPartBytes) {
     const int64_t tiles = deft::product_tiles(p), workers = kUsualSms / 2, rest = tiles % workers, each = 2 * deft::kPartFloats * 4;
