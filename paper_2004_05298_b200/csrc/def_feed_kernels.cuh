@@ -45,11 +45,6 @@ __device__ __forceinline__ void store_group(int8_t *q, int64_t ldq, uint8_t *e, 
     if (there) *e = (uint8_t)ex;
 }
 
-template <typename T> __device__ __forceinline__ float logistic(float g) {
-    if constexpr (sizeof(T) == 2) return __fdividef(1.f, 1.f + expf(-g));
-    else return 1.f / (1.f + expf(-g));
-}
-
 template <typename T> struct StoreGated {
     static constexpr bool kBoth = true;
     T *h;

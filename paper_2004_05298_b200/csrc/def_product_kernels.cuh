@@ -26,8 +26,8 @@ constexpr int kStages = 6;
 constexpr int kTurnBytes = 2048;                                       // per storing warp: rows that are turned before they are stored
 // Sums in registers need them for 128 columns a thread, of 8 warps; else 16 warps keep up with more at a time.
 template <int CHAIN> struct ProductShape {
-    static constexpr int store_warps = CHAIN ? 8 : 16, threads = 128 + 32 * store_warps;
-    static constexpr int control_registers = 56, store_registers = CHAIN ? 224 : 104;     // a thread's, of the first 4 warps and of the others
+    static constexpr int store_warps = CHAIN > 0 && CHAIN < 8 ? 8 : 16, threads = 128 + 32 * store_warps;
+    static constexpr int control_registers = 56, store_registers = store_warps == 8 ? 224 : 104;     // a thread's, of the first 4 warps and of the others
     static constexpr int smem = 1024 + kStages * 2 * kHalfBytes + store_warps * kTurnBytes + 256;
 };
 constexpr int64_t kPartFloats = (int64_t)kTileRows * kTileCols;        // of a CTA's part of a tile

@@ -38,14 +38,8 @@ struct Recurrence {
     float2 *summary;                            // (P, L) of each part and channel: [parts][C], or of pairs of channels (P, P, L, L)
 };
 
-// 1 / (1 + exp(g)).  16-bit types: exp is off by two units in the last place and |g| 2^-24.  Results below 2^-126 become 0.
-template <typename T> __device__ __forceinline__ float logistic_back(float g) {
-    float e, c;
-    if constexpr (sizeof(T) == 4) e = expf(g);
-    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * 1.44269504f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(c) : "f"(1.f + e));
-    return c;
-}
+// 1 / (1 + exp(g)) = 1 - a.
+template <typename T> __device__ __forceinline__ float logistic_back(float g) { return logistic<T>(-g); }
 
 // One lane's V consecutive elements, as they lie in memory.
 template <typename T, int V> struct Few { T v[V]; };

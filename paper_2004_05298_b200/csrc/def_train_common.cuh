@@ -209,6 +209,15 @@ template <typename T, bool ALIGNED> __device__ __forceinline__ void store_cols(T
     }
 }
 
+// 1 / (1 + exp(-v)).  16-bit types: exp is off by two units in the last place and |v| 2^-24; results below 2^-126 become 0.
+template <typename T> __device__ __forceinline__ float logistic(float v) {
+    float e, s;
+    if constexpr (sizeof(T) == 4) e = expf(-v);
+    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
+    return s;
+}
+
 // Two fp32 operations in one instruction.
 struct Pair { uint64_t bits; };
 __device__ __forceinline__ Pair make_pair(float a, float b) {
