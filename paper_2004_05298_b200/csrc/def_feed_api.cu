@@ -7,6 +7,8 @@
 
 namespace {
 
+constexpr int64_t kShortSums = 1024;          // terms up to which chains are 4 stages
+
 // Two products, one after the other, and their operands; the parts of cut tiles come first in the workspace.
 struct FeedPlan {
     Operand a1, b1, a2, b2;
@@ -196,17 +198,18 @@ extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, 
         DEF_TRY(operand_map(map_h, dtype, p.a2, false));
         DEF_TRY(operand_map(map_down, dtype, p.b2, false));
     }
-    DEF_TRY(fill(p.a1, dtype, x, ldx, stream, "def_feed_forward (x)"));
-    DEF_TRY(fill(p.b1, dtype, w_in, C, stream, "def_feed_forward (w_in)"));
+    DEF_TRY(fill({p.a1, p.b1, p.b2}, dtype, {x, w_in, w_down}, {ldx, C, F}, stream, "def_feed_forward (copies)"));
     int rc = DEF_OK;
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreGated<E> store = {(E *)h, ldh, T, F, q_stride(F), e_stride(F), gate_q, up_q, gate_e, up_e, wide(h, ldh, es)};
-        rc = launch_product<false, 8>(p.first, store, map_x, map_in, stream, "def_feed_forward");
+        // What a checkpoint keeps goes by the sums' last bits.  A chain of 4 stages against 8, 777 terms: checkpoints in fp16 are
+        // 0.8 against 1.2 10^-4 off (plain fp32 sums: 0.9), 4096 terms: bf16 0.8 against 1.1 (1.2) at 1169 against 1050 us.
+        rc = C <= kShortSums ? launch_product<false, 4>(p.first, store, map_x, map_in, stream, "def_feed_forward")
+                             : launch_product<false, 8>(p.first, store, map_x, map_in, stream, "def_feed_forward");
     });
     if (rc != DEF_OK || !w_down) return rc;
-    DEF_TRY(fill(p.a2, dtype, h, ldh, stream, "def_feed_forward (h)"));
-    DEF_TRY(fill(p.b2, dtype, w_down, F, stream, "def_feed_forward (w_down)"));
+    DEF_TRY(fill({p.a2}, dtype, {h}, {ldh}, stream, "def_feed_forward (h)"));
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreRows<E> store = {(E *)out, ldout, T, O, wide(out, ldout, es)};
@@ -257,8 +260,7 @@ extern "C" int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, in
         DEF_TRY(operand_map(map_both, dtype, p.a2, false));
         DEF_TRY(operand_map(map_in, dtype, p.b2, true));
     }
-    DEF_TRY(fill(p.a1, dtype, dout, lddout, stream, "def_feed_forward_backward (dout)"));
-    DEF_TRY(fill(p.b1, dtype, w_down, F, stream, "def_feed_forward_backward (w_down)"));
+    DEF_TRY(fill({p.a1, p.b1, p.b2}, dtype, {dout, w_down, w_in}, {lddout, F, C}, stream, "def_feed_forward_backward (copies)"));
     int rc = DEF_OK;
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
@@ -268,8 +270,7 @@ extern "C" int def_feed_forward_backward(int32_t dtype, int64_t T, int64_t C, in
         rc = launch_product<true, sizeof(E) == 4 ? 8 : 0>(p.first, store, map_a, map_down, stream, "def_feed_forward_backward");
     });
     if (rc != DEF_OK || !dx) return rc;
-    DEF_TRY(fill(p.a2, dtype, dboth, lddb, stream, "def_feed_forward_backward (dboth)"));
-    DEF_TRY(fill(p.b2, dtype, w_in, C, stream, "def_feed_forward_backward (w_in)"));
+    DEF_TRY(fill({p.a2}, dtype, {dboth}, {lddb}, stream, "def_feed_forward_backward (dboth)"));
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
         const deft::StoreRows<E> store = {(E *)dx, lddx, T, C, wide(dx, lddx, es)};

@@ -5,13 +5,24 @@
 
 namespace deft {
 
-// Rows as the tensor cores take them, where they do not lie like that already: 16-bit pieces in rows of ld elements (a multiple of 8, the last
-// ones 0).  16-bit types: a copy, of either type as bits.  fp32: three bf16 numbers of 8 bits each, by truncation, whose
-// sum is the value exactly.  A thread takes 8 columns.
-template <typename T>
-__global__ void __launch_bounds__(256) planes_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int cols,
-                                                                 uint4 *__restrict__ out, int64_t ld) {
-    const int col = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 8;
+// Rows as the tensor cores take them, where they do not lie like that already: 16-bit pieces in rows of ld elements (a multiple
+// of 8, the last ones 0).  16-bit types: a copy, of either type as bits.  fp32: three bf16 numbers of 8 bits each, by truncation,
+// whose sum is the value exactly.  A thread takes 8 columns; blockIdx.z is the matrix.
+constexpr int kMostPlanes = 4;
+struct Planes {
+    struct Matrix {
+        const void *x;
+        uint4 *out;
+        int64_t ldx, rows, ld;
+        int cols;
+    } of[kMostPlanes];
+};
+template <typename T> __global__ void __launch_bounds__(256) planes_kernel(const __grid_constant__ Planes p) {
+    const Planes::Matrix &m = p.of[blockIdx.z];
+    const T *x = (const T *)m.x;
+    uint4 *out = m.out;
+    const int64_t ldx = m.ldx, rows = m.rows, ld = m.ld;
+    const int cols = m.cols, col = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 8;
     if (col >= cols) return;
     for (int64_t t = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; t < rows; t += (int64_t)gridDim.y * blockDim.y) {
         const Frag<T, 8> f = load_run<T>(x + t * ldx, col, cols);

@@ -24,9 +24,10 @@ constexpr int kTileRows = 128, kTileCols = 256, kTileK = 64;           // of one
 constexpr int kHalfBytes = kTileRows * kTileK * 2;                     // of either operand's half in a stage
 constexpr int kStages = 6;
 constexpr int kTurnBytes = 2048;                                       // per storing warp: rows that are turned before they are stored
-// Sums in registers need them for 128 columns a thread, of 8 warps; else 16 warps keep up with more at a time.
-template <int CHAIN> struct ProductShape {
-    static constexpr int store_warps = CHAIN > 0 && CHAIN < 8 ? 8 : 16, threads = 128 + 32 * store_warps;
+// Sums in registers need them for 128 columns a thread where chains are short, of 8 warps; else 16 warps keep up with more at a
+// time, also where a few of their registers are spilled (64 columns each; gated, 8192 x 1024 x 4096 bf16: 137 us against 166).
+template <typename EPILOGUE, int CHAIN> struct ProductShape {
+    static constexpr int store_warps = CHAIN == 0 || CHAIN >= 8 || EPILOGUE::kBoth ? 16 : 8, threads = 128 + 32 * store_warps;
     static constexpr int control_registers = 56, store_registers = store_warps == 8 ? 224 : 104;     // a thread's, of the first 4 warps and of the others
     static constexpr int smem = 1024 + kStages * 2 * kHalfBytes + store_warps * kTurnBytes + 256;
 };
@@ -119,9 +120,9 @@ __device__ __forceinline__ void split_columns(const Pair (&x)[16], float (&out)[
 // Epilogue: store() gets 32 columns of a row per thread at a time, columns 32 u of the tile on for u < 8, or (kBoth) for u < 4
 // those and 32 columns from 128 + 32 u on; whole warps call it, with rows and columns that may lie outside the result.
 template <typename EPILOGUE, bool BN, int CHAIN>
-__global__ void __launch_bounds__(ProductShape<CHAIN>::threads, 1)
+__global__ void __launch_bounds__(ProductShape<EPILOGUE, CHAIN>::threads, 1)
     product_kernel(const __grid_constant__ Product p, const __grid_constant__ EPILOGUE epilogue, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
-    using S = ProductShape<CHAIN>;
+    using S = ProductShape<EPILOGUE, CHAIN>;
     extern __shared__ uint8_t raw[];
     uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sa = base, *sb = sa + kStages * kHalfBytes;

@@ -31,12 +31,22 @@ void place(Operand &o, char *&at) {
     o.p = at;
     at += o.bytes;
 }
-int fill(const Operand &o, int32_t dtype, const void *from, int64_t ld, cudaStream_t stream, const char *what) {
-    if (!o.copy) return DEF_OK;
-    on_plane(false, o.rows, o.cols, [&](auto, dim3 grid, dim3 block) {
-        uint4 *out = (uint4 *)const_cast<void *>(o.p);
-        if (dtype == DEF_DTYPE_F32) deft::planes_kernel<float><<<grid, block, 0, stream>>>((const float *)from, ld, o.rows, (int)o.cols, out, o.ld);
-        else deft::planes_kernel<__half><<<grid, block, 0, stream>>>((const __half *)from, ld, o.rows, (int)o.cols, out, o.ld);
+// The copies of those of N operands that need one, in one launch.
+template <int N> int fill(const Operand (&o)[N], int32_t dtype, const void *const (&from)[N], const int64_t (&ld)[N], cudaStream_t stream, const char *what) {
+    deft::Planes p = {};
+    int n = 0;
+    int64_t lanes = 0, rows = 0;
+    for (int i = 0; i < N; ++i) {
+        if (!o[i].copy) continue;
+        p.of[n++] = {from[i], (uint4 *)const_cast<void *>(o[i].p), ld[i], o[i].rows, o[i].ld, (int)o[i].cols};
+        lanes = std::max(lanes, ceil_div(o[i].cols, 8));
+        rows = std::max(rows, o[i].rows);
+    }
+    if (n == 0) return DEF_OK;
+    on_plane(false, rows, lanes * 8, [&](auto, dim3 grid, dim3 block) {
+        grid.z = (unsigned)n;
+        if (dtype == DEF_DTYPE_F32) deft::planes_kernel<float><<<grid, block, 0, stream>>>(p);
+        else deft::planes_kernel<__half><<<grid, block, 0, stream>>>(p);
     });
     return launched(what);
 }
@@ -95,7 +105,7 @@ int64_t plan_cuts(deft::Product &p, int64_t most_bytes = kMostPartBytes) {
 
 template <bool BN, int CHAIN, typename EPILOGUE>
 int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t stream, const char *what) {
-    using S = deft::ProductShape<CHAIN>;
+    using S = deft::ProductShape<EPILOGUE, CHAIN>;
     const auto kernel = deft::product_kernel<EPILOGUE, BN, CHAIN>;
     if (deft::product_pieces(p) >= (int64_t)1 << 30) return fail(DEF_ERR_ARG, "%s: the result is too large", what);
     // The storing warps take over registers that the others give up: those have to be there.

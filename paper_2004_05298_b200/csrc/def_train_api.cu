@@ -496,8 +496,9 @@ extern "C" int def_checkpoint_weight_grad(int32_t dtype, int64_t T, int64_t O, i
     }
     if (p.copy_dy) {
         on_plane(false, T, O, [&](auto, dim3 grid, dim3 block) {
-            if (es == 4) deft::planes_kernel<float><<<grid, block, 0, stream>>>((const float *)dy, lddy, T, (int)O, planes, p.ld_planes);
-            else deft::planes_kernel<__half><<<grid, block, 0, stream>>>((const __half *)dy, lddy, T, (int)O, planes, p.ld_planes);
+            const deft::Planes m = {{{dy, planes, lddy, T, p.ld_planes, (int)O}}};
+            if (es == 4) deft::planes_kernel<float><<<grid, block, 0, stream>>>(m);
+            else deft::planes_kernel<__half><<<grid, block, 0, stream>>>(m);
         });
         DEF_TRY(launched("def_checkpoint_weight_grad (copy)"));
     }
