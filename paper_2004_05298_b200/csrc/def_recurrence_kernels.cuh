@@ -112,7 +112,7 @@ struct Places {
 // BACK: steps count from the last token.  PART: only (P, L) of each part.
 // Grid: tiles of channels x CTAs of a cluster, parts.
 template <typename T, int V, bool BACK, bool PART>
-__global__ void __launch_bounds__(32 * kRecWarps, BACK ? 4 : 1) recurrence_kernel(const Recurrence a, int ranks) {
+__global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Recurrence a, int ranks) {
     __shared__ float2 runs[2][kRecWarps][32 * V];
     __shared__ float2 blocks[2][kMostCluster][32 * V];
     __shared__ int kept[kKeptOffsets];
@@ -536,9 +536,10 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
     int stage = 0, turn = 0;                                     // of the ring: round i is stage i mod stages, in its turn-th use
     for (int i = 0; i < rounds; ++i, turn ^= stage == B::stages - 1, stage = stage == B::stages - 1 ? 0 : stage + 1) {
         const int buf = i & 1, base = begin + i * stride, run = base + rank * kSteps + warp * R;
-        // Calm: all of the cluster's blocks of this round lie inside one sequence, its first and last token elsewhere.
+        // Calm: all of the cluster's blocks of this round lie inside one sequence, its first and (where that matters) last token
+        // elsewhere.
         const int t_lo = BACK ? a.T - base - stride : base, t_hi = t_lo + stride - 1;
-        bool calm = t_lo > first && t_hi < behind - 1 && base + stride <= end;
+        const bool calm = t_lo > first && t_hi < behind - (BACK || leave_to ? 1 : 0) && base + stride <= end;
         uint32_t is_there = (1u << R) - 1u, enters = 0, leaves = 0;
         int seq = 0;
         if (!calm) {
