@@ -1,13 +1,16 @@
 /*
  * def_train.h -- operators of a language model's training step around def_step, on one B200 (sm_100a).
  *
- * def_step (def.h) consumes fp32 gradient rows; these calls are the memory-bound parts of the forward and backward
- * passes that produce them, with activations kept between the two in 8 bits:
+ * def_step (def.h) consumes fp32 gradient rows; these calls are parts of the forward and backward passes that produce
+ * them, with activations kept between the two in 8 bits, and of what is done with them before the step:
  *
  *   def_norm_*        root-mean-square norms before and after a block, fused with the block's gate and residual scale
  *   def_checkpoint_*  8-bit activation checkpoints, and the weight gradient taken straight from one
  *   def_gated_*       the gated activation, its checkpoints, and its backward pass from them
  *   def_logprob_*     log probabilities of given tokens with entropy and top alternatives, and their gradient
+ *   def_recurrence_*  a gated linear recurrence over the tokens of packed sequences, with states kept between calls
+ *   def_feed_forward* the gated feed-forward block, activation and checkpoints in the products' own kernels
+ *   def_orthogonalize orthogonalised weight gradients (Newton-Schulz products), of one or of all workers' rows
  *
  * Conventions (beyond those of def.h)
  *   - Activations are rows [T, C]: T tokens, C consecutive elements of type `dtype` (DEF_DTYPE_*), row stride ld >= C
@@ -174,7 +177,7 @@ int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const void *logits
  *     c_t = 1 / (1 + exp(g_t)),  a_t = 1 - c_t,     h_t = a_t h_{t-1} + c_t x_t,     y_t = h_t
  * x, gate (the logits g), y: [T, C], T <= 2^30.  Sequence s holds rows [offsets[s], offsets[s + 1]) (offsets: sequences + 1
  * numbers in device memory, 8-byte aligned, not decreasing; sequences may be empty), or, with offsets NULL, the s-th of
- * `sequences` equally long runs (T must be a multiple).  Rows of no sequence are neither read nor written.  Offsets that
+ * `sequences` equally long runs (T must be a multiple).  Rows of no sequence are not written, and what they hold does not matter.  Offsets that
  * decrease or leave [0, T] do no harm outside the arguments, but what is computed then is not specified.
  * h0, h_last [sequences, C] fp32: the state before a sequence's first token (NULL: 0) and behind its last one (NULL: not
  * written; a sequence without tokens hands on its h0).  y may be x itself (same stride) where no backward pass will need x.
