@@ -93,31 +93,36 @@ template <bool BACK> int recurrence(int32_t dtype, deft::Recurrence a, bool pair
     cudaError_t err = cudaSuccess;
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
-        auto launch = [&](auto kernel, int smem, int ranks, int parts, auto... args) {
-            if (err == cudaSuccess && smem > 0) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        // `after`: the launch may overlap the end of the one before, which finds the parts' maps
+        auto launch = [&](auto kernel, int smem, int ranks, int parts, bool after, auto... args) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3((unsigned)(p.tiles * ranks), (unsigned)parts);
             cfg.blockDim = dim3(32 * deft::kRecWarps);
             cfg.dynamicSmemBytes = (size_t)smem;
             cfg.stream = stream;
-            cudaLaunchAttribute attr[1];
+            cudaLaunchAttribute attr[2];
             attr[0].id = cudaLaunchAttributeClusterDimension;
             attr[0].val.clusterDim.x = (unsigned)ranks;
             attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-            cfg.attrs = attr;
-            cfg.numAttrs = ranks > 1 ? 1 : 0;
+            attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[1].val.programmaticStreamSerializationAllowed = 1;
+            cfg.attrs = ranks > 1 ? attr : attr + 1;
+            cfg.numAttrs = (ranks > 1 ? 1 : 0) + (after ? 1 : 0);
             if (err == cudaSuccess) err = cudaLaunchKernelEx(&cfg, kernel, a, ranks, args...);
         };
         if (streamed) {
             constexpr int smem = deft::StreamBlock<E, BACK>::smem;
-            if (p.parts > 1) launch(deft::recurrence_stream_kernel<E, BACK, true>, smem, 1, p.parts - 1, maps);
-            launch(deft::recurrence_stream_kernel<E, BACK, false>, smem, p.ranks, p.parts, maps);
+            constexpr auto part = deft::recurrence_stream_kernel<E, BACK, true>, whole = deft::recurrence_stream_kernel<E, BACK, false>;
+            if (p.parts > 1 && (err = allow_smem<part>(smem)) != cudaSuccess) return;
+            if ((err = allow_smem<whole>(smem)) != cudaSuccess) return;
+            if (p.parts > 1) launch(part, smem, 1, p.parts - 1, false, maps);
+            launch(whole, smem, p.ranks, p.parts, p.parts > 1, maps);
             return;
         }
         auto both = [&](auto v) {
             constexpr int V = decltype(v)::value ? 2 : 1;
-            if (p.parts > 1) launch(deft::recurrence_kernel<E, V, BACK, true>, 0, 1, p.parts - 1);
-            launch(deft::recurrence_kernel<E, V, BACK, false>, 0, p.ranks, p.parts);
+            if (p.parts > 1) launch(deft::recurrence_kernel<E, V, BACK, true>, 0, 1, p.parts - 1, false);
+            launch(deft::recurrence_kernel<E, V, BACK, false>, 0, p.ranks, p.parts, false);
         };
         if constexpr (sizeof(E) == 2) by_alignment(pairs, both);
         else both(Is<false>());

@@ -88,13 +88,13 @@ cudaError_t launch_tokens(int64_t T, int64_t rows, int64_t k, E *out, int64_t ld
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = after ? 2 : 1;
-    auto launch = [&](auto kernel, int smem) {
-        cfg.dynamicSmemBytes = (size_t)smem;
-        const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        return err == cudaSuccess ? cudaLaunchKernelEx(&cfg, kernel, p, out, map_w, map_x) : err;
+    auto launch = [&](auto columns) {
+        constexpr int N = decltype(columns)::value, smem = deft::TokenShape<GATED, N>::smem;
+        cfg.dynamicSmemBytes = smem;
+        const cudaError_t err = allow_smem<deft::token_product_kernel<E, GATED, N>>(smem);
+        return err == cudaSuccess ? cudaLaunchKernelEx(&cfg, deft::token_product_kernel<E, GATED, N>, p, out, map_w, map_x) : err;
     };
-    return T <= 16 ? launch(deft::token_product_kernel<E, GATED, 16>, deft::TokenShape<GATED, 16>::smem)
-                   : launch(deft::token_product_kernel<E, GATED, 32>, deft::TokenShape<GATED, 32>::smem);
+    return T <= 16 ? launch(std::integral_constant<int, 16>()) : launch(std::integral_constant<int, 32>());
 }
 int token_box(int64_t T) { return T <= 16 ? 16 : 32; }
 template <typename E, bool GATED>

@@ -30,6 +30,8 @@ template <typename EPILOGUE, int CHAIN> struct ProductShape {
     static constexpr int store_warps = CHAIN == 0 || CHAIN >= 8 || EPILOGUE::kBoth ? 16 : 8, threads = 128 + 32 * store_warps;
     static constexpr int control_registers = 56, store_registers = store_warps == 8 ? 224 : 104;     // a thread's, of the first 4 warps and of the others
     static constexpr int smem = 1024 + kStages * 2 * kHalfBytes + store_warps * kTurnBytes + 256;
+    // The storing warps take over registers that the others give up: those have to be there (launch bounds give multiples of 8).
+    static_assert(65536 / threads / 8 * 8 * threads >= 128 * control_registers + 32 * store_warps * store_registers);
 };
 constexpr int64_t kPartFloats = (int64_t)kTileRows * kTileCols;        // of a CTA's part of a tile
 
@@ -43,6 +45,7 @@ struct Product {
     int bf16;
     int64_t whole;                        // tiles [0, whole) are worked on whole, of the others each k in `cuts` parts
     int cuts;
+    int early;                            // the next kernel may be set up while this one runs: where half the SMs are idle
     float *parts;                         // [(tile - whole) * cuts + cut][CTA of the pair][column][row]
 };
 
@@ -158,6 +161,7 @@ __global__ void __launch_bounds__(ProductShape<EPILOGUE, CHAIN>::threads, 1)
     tmem_fence_after();
     const uint32_t tmem = *tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the set-up above may overlap the kernel before
+    if (p.early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int pieces = (int)product_pieces(p), step = (int)gridDim.x / 2;   // the host keeps them below 2^30
     int batch, tm, tn;
 
@@ -343,6 +347,7 @@ __global__ void __launch_bounds__(256) product_join_kernel(const Product p, cons
     const int rank = (int)(half_tile % 2), run = (int)(blockIdx.x % (kRuns / 2)) * 2 + threadIdx.x / 128, row = threadIdx.x % 128;
     const int ca = 32 * run, cb = 128 + 32 * run;
     asm volatile("griddepcontrol.wait;" ::: "memory");             // the parts are those of the kernel before
+    if (p.early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     float a[32], b[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) a[j] = b[j] = 0.f;

@@ -106,18 +106,15 @@ int64_t plan_cuts(deft::Product &p, int64_t most_bytes = kMostPartBytes) {
 template <bool BN, int CHAIN, typename EPILOGUE>
 int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t stream, const char *what) {
     using S = deft::ProductShape<EPILOGUE, CHAIN>;
-    const auto kernel = deft::product_kernel<EPILOGUE, BN, CHAIN>;
+    constexpr auto kernel = deft::product_kernel<EPILOGUE, BN, CHAIN>;
     if (deft::product_pieces(p) >= (int64_t)1 << 30) return fail(DEF_ERR_ARG, "%s: the result is too large", what);
-    // The storing warps take over registers that the others give up: those have to be there.
-    cudaFuncAttributes at;
-    cudaError_t err = cudaFuncGetAttributes(&at, kernel);
-    if (err == cudaSuccess && at.numRegs * S::threads < 128 * S::control_registers + 32 * S::store_warps * S::store_registers)
-        return fail(DEF_ERR_CUDA, "%s: built with too few registers", what);
-    if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
+    cudaError_t err = allow_smem<kernel>(S::smem);
     if (err == cudaSuccess) {
         const int64_t pieces = deft::product_pieces(p);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)((pieces < kUsualSms / 2 ? pieces : kUsualSms / 2) * 2));
+        deft::Product q = p;
+        q.early = pieces <= kUsualSms / 4;
         cfg.blockDim = dim3(S::threads);
         cfg.dynamicSmemBytes = S::smem;
         cfg.stream = stream;
@@ -129,14 +126,14 @@ int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUten
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        err = cudaLaunchKernelEx(&cfg, kernel, p, epilogue, map_a, map_b);
+        err = cudaLaunchKernelEx(&cfg, kernel, q, epilogue, map_a, map_b);
         if (const int64_t cut = deft::product_tiles(p) - p.whole; cut > 0 && err == cudaSuccess) {
             cfg.gridDim = dim3((unsigned)(cut * (EPILOGUE::kBoth ? 4 : 8)));
             cfg.blockDim = dim3(256);
             cfg.dynamicSmemBytes = 0;
             cfg.attrs = attr + 1;
             cfg.numAttrs = 1;
-            err = cudaLaunchKernelEx(&cfg, deft::product_join_kernel<EPILOGUE>, p, epilogue);
+            err = cudaLaunchKernelEx(&cfg, deft::product_join_kernel<EPILOGUE>, q, epilogue);
         }
     }
     if (err == cudaSuccess) return DEF_OK;

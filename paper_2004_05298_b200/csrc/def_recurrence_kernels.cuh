@@ -512,6 +512,8 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
     };
     if (threadIdx.x == 0)
         for (int i = 0; i < B::stages && i < rounds; ++i) load(i);
+    if (PART) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    else asm volatile("griddepcontrol.wait;" ::: "memory");      // the parts' maps are the kernel before's; the copies above are not
 
     const float *enter_with = BACK ? a.dh_last : a.h0;
     float *leave_to = BACK ? a.dh0 : a.h_last;

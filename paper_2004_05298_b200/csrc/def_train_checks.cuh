@@ -115,6 +115,18 @@ int launched(const char *what) {
     return err == cudaSuccess ? DEF_OK : cuda_fail(err, what);
 }
 
+// A kernel's limit of dynamic shared memory, raised once per kernel and device (every call of a kernel asks for the same).  K is the
+// kernel itself, so that each has a record of its own.
+template <auto K> cudaError_t allow_smem(int bytes) {
+    static std::atomic<uint64_t> raised{0};
+    static_assert(kMaxDevices <= 64);
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess || (raised.load(std::memory_order_acquire) >> dev & 1)) return err;
+    if ((err = cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) == cudaSuccess) raised.fetch_or((uint64_t)1 << dev, std::memory_order_release);
+    return err;
+}
+
 // Calls f with a value of the element type.
 template <typename F> void by_dtype(int32_t dtype, F f) {
     if (dtype == DEF_DTYPE_F32) f(float());
