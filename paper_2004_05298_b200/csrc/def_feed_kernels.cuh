@@ -11,14 +11,42 @@
 
 namespace deft {
 
+// 32 values of a row rounded to T, two of 16 bits in a register.
+template <typename T> struct Rounded32 {
+    uint32_t w[8 * sizeof(T)];
+    __device__ __forceinline__ void set(int i, float even, float odd) {       // i: even
+        if constexpr (sizeof(T) == 4) {
+            w[i] = __float_as_uint(even);
+            w[i + 1] = __float_as_uint(odd);
+        } else if constexpr (__is_same(T, __half)) {
+            const __half2 two = __floats2half2_rn(even, odd);
+            memcpy(&w[i / 2], &two, 4);
+        } else {
+            const __nv_bfloat162 two = __floats2bfloat162_rn(even, odd);
+            memcpy(&w[i / 2], &two, 4);
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(w[i]);
+        } else if constexpr (!__is_same(T, __half)) {
+            return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        } else {
+            const uint16_t bits = (uint16_t)(w[i / 2] >> i % 2 * 16);
+            T v;
+            memcpy(&v, &bits, 2);
+            return to_float<T>(v);
+        }
+    }
+};
 // Checkpoint of a group of 32 columns that one thread holds, the first n of which exist; whole groups are turned (32 bytes a
 // row).  Whole warps call it.
 template <typename V>
-__device__ __forceinline__ void store_group(int8_t *q, int64_t ldq, uint8_t *e, const V (&x)[32], int n, bool there, uint8_t *turn) {
+__device__ __forceinline__ void store_group(int8_t *q, int64_t ldq, uint8_t *e, const V &x, int n, bool there, uint8_t *turn) {
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-        if (i < n) most = max_nan(most, fabsf(to_float<V>(x[i])));
+        if (i < n) most = max_nan(most, fabsf(x[i]));
     const uint32_t top = __float_as_uint(most), ex = group_exponent(top);
 #pragma unroll
     for (int p = 0; p < 4; p += 2) {
@@ -28,7 +56,7 @@ __device__ __forceinline__ void store_group(int8_t *q, int64_t ldq, uint8_t *e, 
             float part[8];
             uint32_t v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) part[i] = to_float<V>(x[8 * (p + r) + i]);
+            for (int i = 0; i < 8; ++i) part[i] = x[8 * (p + r) + i];
             quantise(part, top, ex, v);
             if (n >= 32) {
                 w[2 * r] = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
@@ -100,7 +128,7 @@ template <typename T> struct StoreGatedBack {
         uint4 wg = {}, wu = {};                                    // 16 columns
         T *pg = dgate + row * ldd + c, *pu = dup + row * ldd + c;
         uint8_t *turn_up = turn + kTurnBytes / 2;
-        T hv[32];
+        Rounded32<T> hv;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
             if (p % 2 == 0 && there && 8 * p < n) {                // rows of q are padded to 16 bytes
@@ -114,10 +142,13 @@ template <typename T> struct StoreGatedBack {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float s = logistic<T>(g[i]), gs = g[i] * s, x = dh[8 * p + i];
-                hv[8 * p + i] = from_float<T>(gs * u[i]);
+                const float h_back = gs * u[i];
                 d[i] = x * u[i] * (s * fmaf(g[i], 1.f - s, 1.f));
                 u[i] = x * gs;
+                g[i] = h_back;
             }
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) hv.set(8 * p + i, g[i], g[i + 1]);
             constexpr int W = kTurn<T> / 2;                        // of either
             const int at = 8 * p % W, f = 8 * p - at;              // f: first column of the run that is put there
             if (direct) {

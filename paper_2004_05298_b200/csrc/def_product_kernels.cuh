@@ -415,13 +415,13 @@ template <typename T, int W> __device__ __forceinline__ void turn_store(const ui
     }
     __syncwarp();
 }
-template <typename T, typename V> __device__ __forceinline__ void store_32(T *p, int64_t ld, bool there, int n, bool wide, const V (&v)[32], uint8_t *turn) {
+template <typename T, typename V> __device__ __forceinline__ void store_32(T *p, int64_t ld, bool there, int n, bool wide, const V &v, uint8_t *turn) {
     if (wide && n >= 32) {
 #pragma unroll
         for (int f = 0; f < 32; f += 8) {
             float part[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) part[j] = to_float<V>(v[f + j]);
+            for (int j = 0; j < 8; ++j) part[j] = v[f + j];
             turn_put_8<64, T>(turn, f % kTurn<T>, part);
             if (f % kTurn<T> + 8 == kTurn<T>) turn_store_words<64>(turn, p + f + 8 - kTurn<T>, ld * (int64_t)sizeof(T), there);
         }
@@ -431,7 +431,7 @@ template <typename T, typename V> __device__ __forceinline__ void store_32(T *p,
         for (int f = 0; f < 32; f += W) {
             if (f >= n) break;
 #pragma unroll
-            for (int j = 0; j < W; ++j) turn_put<T, W>(turn, j, to_float<V>(v[f + j]));
+            for (int j = 0; j < W; ++j) turn_put<T, W>(turn, j, v[f + j]);
             turn_store<T, W>(turn, p + f, ld, there, n - f);
         }
     }
