@@ -591,7 +591,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         }
         runs[buf][warp][lane] = m;
         __syncthreads();
-        if (threadIdx.x == 0) {
+        if (threadIdx.x == 0 && ok) {
             // forward all are done with this block, backward with the one before
             if (!BACK || PART) {
                 if (i + B::stages < rounds) load(i + B::stages);
@@ -622,6 +622,10 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         if (__any_sync(0xffffffffu, !ok || failed)) {            // a wait ran out: no numbers rather than wrong ones
             ok = false;
             s = whole.L = make_pair(NAN, NAN);
+            // The others may still be sending: this CTA stays until they have given up, too.  (A barrier of the cluster at the end, or this
+            // there, costs 6 us of 114.)
+            if (ranks > 1 && i + 1 == rounds)
+                for (const uint64_t start = nanoseconds(); nanoseconds() - start < 3 * kWaitLimit;) __nanosleep(1000);
         }
         const int64_t t0 = BACK ? a.T - 1 - run : run;
         T *out = BACK ? (T *)a.dx + t0 * a.lddx + col : (T *)a.y + t0 * a.ldy + col, *out_g = (T *)a.dgate + t0 * a.lddg + col;
