@@ -196,10 +196,7 @@ __global__ void __launch_bounds__(ProductShape<EPILOGUE, CHAIN>::threads, 1)
             const uint64_t start = nanoseconds();
             for (uint32_t m = n > kStages ? n - kStages : 0; m < n; ++m)
                 while (!barrier_try(full + 8 * (m % kStages), (m / kStages) & 1) && nanoseconds() - start < kWaitLimit) {}
-        } else if (warp == 1 && lane == 0 && rank != 0) {
-            const uint64_t start = nanoseconds();                  // the other CTA's last commit arrives here too
-            while (!barrier_try(drained, 0) && nanoseconds() - start < 2 * kWaitLimit) {}
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1 && lane == 0 && rank == 0) {
             const uint32_t idesc = product_descriptor(p.bf16 != 0, BN);
             uint32_t n = 0, chunk = 0;
             bool ok = true;
@@ -226,8 +223,6 @@ __global__ void __launch_bounds__(ProductShape<EPILOGUE, CHAIN>::threads, 1)
                 }
             }
             mma_commit(drained);
-            const uint64_t start = nanoseconds();
-            while (!barrier_try(drained, 0) && nanoseconds() - start < kWaitLimit) {}
         } else if (warp == 2 && lane == 0) {
             uint32_t n = 0;
             bool ok = true;
@@ -331,6 +326,11 @@ __global__ void __launch_bounds__(ProductShape<EPILOGUE, CHAIN>::threads, 1)
     }
     tmem_fence_before();
     __syncthreads();
+    if (threadIdx.x == 32) {                                       // the even CTA's last commit arrives in both
+        const uint64_t start = nanoseconds();
+        while (!barrier_try(drained, 0) && nanoseconds() - start < kWaitLimit) {}
+    }
+    __syncwarp();
     cluster_sync();                                                // nothing of this CTA is used by the other any more
     if (warp == 1) {
         __syncwarp();
