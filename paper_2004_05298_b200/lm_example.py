@@ -204,7 +204,7 @@ class Orthogonal:
     def __init__(self, layout, workers, scale):
         self.layout, self.scale = layout, scale
         shapes = [layout.at[n][1] for n in layout.projections()]
-        self.workspace = torch.empty(max(B.def_orthogonalize_workspace(r, c, workers) for r, c in shapes), dtype=torch.uint8, device=DEV)
+        self.workspace = torch.empty(max((B.def_orthogonalize_workspace(r, c, workers) for r, c in shapes), default=0), dtype=torch.uint8, device=DEV)
 
     def __call__(self, grads):
         for name in self.layout.projections():

@@ -89,3 +89,11 @@ def test_training_runs_with_everything(E):
     losses, model, _ = E.train(steps=6, workers=2, ratio=4, vocab=96, width=64, hidden=128, blocks=2, tokens=256, length=64, mixer="recurrence", fused=True,
                                orthogonal=0.01)
     assert len(losses) == 6 and all(math.isfinite(v) for v in losses) and bool(torch.isfinite(model).all())
+
+
+def test_a_model_without_blocks_has_nothing_to_orthogonalise(E):
+    layout = E.Layout(32, 16, 24, 0)
+    grads = torch.randn(2, layout.d, device="cuda")
+    old = grads.clone()
+    E.Orthogonal(layout, 2, 0.5)(grads)
+    assert torch.equal(grads, old)
