@@ -128,8 +128,8 @@ int launch_product(const deft::Product &p, const EPILOGUE &epilogue, const CUten
         cfg.numAttrs = 2;
         err = cudaLaunchKernelEx(&cfg, kernel, q, epilogue, map_a, map_b);
         if (const int64_t cut = deft::product_tiles(p) - p.whole; cut > 0 && err == cudaSuccess) {
-            cfg.gridDim = dim3((unsigned)(cut * (EPILOGUE::kBoth ? 4 : 8)));
-            cfg.blockDim = dim3(256);
+            cfg.gridDim = dim3((unsigned)(cut * (EPILOGUE::kBoth ? 8 : 16)));
+            cfg.blockDim = dim3(deft::kJoinThreads);
             cfg.dynamicSmemBytes = 0;
             cfg.attrs = attr + 1;
             cfg.numAttrs = 1;
