@@ -43,7 +43,7 @@ OrthogonalPlan orthogonal_plan(int64_t batch, int64_t rows, int64_t cols) {
     p.polynomial = piece_product(batch, p.m, p.m, p.m, true);
     p.update = piece_product(batch, p.m, p.n, p.m, false);
     const int64_t most = std::min(kMostPartBytes, batch * (16 * (p.m + 8) * (p.n + p.m + 16) + 8192) - p.bytes());
-    for (deft::Product *q : {&p.gram, &p.polynomial, &p.update}) p.parts = std::max(p.parts, plan_cuts(*q, most));
+    for (deft::Product *q : {&p.gram, &p.polynomial, &p.update}) p.parts = std::max(p.parts, plan_cuts(*q, most, 2));
     return p;
 }
 // Stages in a chain of the matrix unit.  What the chains lose against fp32 sums decides: relative error of five steps with 4, 2
