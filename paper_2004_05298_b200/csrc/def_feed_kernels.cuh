@@ -178,7 +178,8 @@ template <typename T> struct StoreGatedBack {
 // ---------------------------------------------------------------------------
 // Few tokens: every weight is read once and there is little else to do, so a warp takes one row of w_in's gate and the same of
 // its other half (or one row of w_down), in runs of 8 elements per lane, several of them ahead, and multiplies them by all tokens'
-// elements in fp32.  The weights of the second product are on their way before the first one is done.
+// elements in fp32.  The weights of the second product are on their way before the first one is done.  2048 x 5632 fp32, 138 MB of
+// weights: 1 token 33 us (4.2 TB/s), 4 tokens 53, 8 tokens 91 (fp32 multiplications).
 // ---------------------------------------------------------------------------
 constexpr int kFewTokens = 8, kFewWarps = 8;
 
@@ -252,7 +253,8 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_tokens_kernel(const FewTok
 // ---------------------------------------------------------------------------
 // Up to 32 tokens in 16 bits on tensor cores: 128 rows of the weights (gated: of either half) are M, the tokens N, so that the
 // weights stream through two rings per SM and nothing else is moved.  k is cut over the CTAs of a cluster, which leave their sums in
-// shared memory and add a share of them each, in the order of k.
+// shared memory and add a share of them each, in the order of k.  1 token, 2048 x 5632 bf16, 69 MB of weights: both products 20.7 us
+// (3.3 TB/s; two launches), 4096 x 10240, 252 MB: 48 us (5.2 TB/s).
 //
 // Warps: 0 copies (one thread), 1 issues the matrix instructions (one thread), the last 4 take the sums.
 // ---------------------------------------------------------------------------

