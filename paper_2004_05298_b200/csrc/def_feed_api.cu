@@ -155,15 +155,17 @@ extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, 
     DEF_TRY(check_views(views));
     if (const int sms = sm_count(); sms < 0) return sms;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
-    const Few few = few_tokens(dtype, T, gate_q != nullptr, feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh));
+    FeedPlan p = feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh);
+    const Few few = few_tokens(dtype, T, gate_q != nullptr, p);
     if (few == Few::columns) {
         const bool half = dtype == DEF_DTYPE_F16;
         CUtensorMap map_x, map_in, map_h, map_down;
-        DEF_TRY(operand_map(map_x, half, x, C, T, 1, T > 1 ? ldx : ceil_div(C, 8) * 8, token_box(T)));
-        DEF_TRY(operand_map(map_in, half, w_in, C, 2 * F, 1, C, deft::kTileRows));
+        // the plan's strides: those by which it says that nothing has to be copied (a single row has any)
+        DEF_TRY(operand_map(map_x, half, x, C, T, 1, p.a1.ld, token_box(T)));
+        DEF_TRY(operand_map(map_in, half, w_in, C, 2 * F, 1, p.b1.ld, deft::kTileRows));
         if (out) {
-            DEF_TRY(operand_map(map_h, half, h, F, T, 1, T > 1 ? ldh : ceil_div(F, 8) * 8, token_box(T)));
-            DEF_TRY(operand_map(map_down, half, w_down, F, O, 1, F, deft::kTileRows));
+            DEF_TRY(operand_map(map_h, half, h, F, T, 1, p.a2.ld, token_box(T)));
+            DEF_TRY(operand_map(map_down, half, w_down, F, O, 1, p.b2.ld, deft::kTileRows));
         }
         cudaError_t err = cudaSuccess;
         by_dtype(dtype, [&](auto type) {
@@ -188,7 +190,6 @@ extern "C" int def_feed_forward(int32_t dtype, int64_t T, int64_t C, int64_t F, 
         cudaGetLastError();
         return cuda_fail(err, "def_feed_forward");
     }
-    FeedPlan p = feed_plan(dtype, T, C, F, O, x, ldx, w_in, w_down, h, ldh);
     p.put(workspace);
     // The maps first: nothing is launched where the driver refuses one.
     CUtensorMap map_x, map_in, map_h, map_down;
