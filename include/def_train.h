@@ -208,8 +208,9 @@ int def_recurrence_backward(int32_t dtype, int64_t T, int64_t C, int64_t sequenc
  * x [T, C], h [T, F], out [T, O]; w_in [2F, C]: the gate's F rows, then those of u, and w_down [O, F], both contiguous, of
  * type dtype.  g and u stay in fp32; h is rounded to dtype once, and the second product takes it so.  w_down and out NULL:
  * h only.  gate_q/gate_e, up_q/up_e: checkpoints of g and u (of the fp32 values) for the backward pass; all NULL or all given.
- * 16-bit types: exact products, summed in fp32.  fp32: operands in three bf16 pieces of 8 bits, the six products of pieces
- * that reach 2^-24 (an infinity may give NaN).  T <= 2^30, F <= 2^29.
+ * 16-bit types: exact products, summed in fp32 by the matrix unit, which truncates: of sums of one sign at most 3 10^-5 is lost (fp16;
+ * bf16: 3 10^-4), however many terms, less than a tenth of the rounding of the result.  fp32: operands in three bf16 pieces of 8 bits, the
+ * six products of pieces that reach 2^-24 (an infinity may give NaN).  T <= 2^30, F <= 2^29.
  * The workspace holds partial products where k is cut over CTAs, the pieces of fp32 operands, and aligned copies of operands
  * whose rows are not multiples of 16 bytes or do not start on them; the second call says how much is needed for the same
  * arguments: at most, with r(n) = n + 7 and P = 3 for fp32, 1 else, 20 MiB + 2 P (T r(C) + 2F r(C) + T r(F) + O r(F)) bytes.

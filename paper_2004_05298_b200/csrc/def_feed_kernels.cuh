@@ -268,6 +268,7 @@ template <bool GATED, int N> struct TokenShape {
 };
 struct TokenProduct {
     int tokens, blocks, bf16;             // blocks: of k
+    int chain;                            // stages after which the sums move to registers: the matrix unit's truncate
     int64_t rows, ldo;                    // rows of the weights (gated: of either half)
 };
 
@@ -288,15 +289,16 @@ __global__ void __launch_bounds__(192, 2) token_product_kernel(const TokenProduc
                                                                const __grid_constant__ CUtensorMap map_x) {
     using S = TokenShape<GATED, N>;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * S::stages + 1];
+    __shared__ uint64_t bars[2 * S::stages + 2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int failed;
     uint8_t *base = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-    const uint32_t full = smem_address(bars), empty = full + 8 * S::stages, done = empty + 8 * S::stages;
+    const uint32_t full = smem_address(bars), empty = full + 8 * S::stages, done = empty + 8 * S::stages, taken = done + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, splits = (int)gridDim.y, rank = (int)blockIdx.y;      // a cluster lies along y
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2 * S::stages + 1; ++s) barrier_init(full + 8 * s, 1);
+        barrier_init(taken, 4);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -339,7 +341,14 @@ __global__ void __launch_bounds__(192, 2) token_product_kernel(const TokenProduc
             while (!barrier_try(full + 8 * (m % S::stages), m / S::stages & 1) && nanoseconds() - start < kWaitLimit) {}
     } else if (warp == 1 && lane == 0) {
         const uint32_t idesc = 1u << 4 | (p.bf16 ? 1u : 0u) << 7 | (p.bf16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17 | (uint32_t)(kTileRows >> 4) << 24;
-        for (int i = 0; i < k1 - k0; ++i) {
+        uint32_t chunk = 0;
+        for (int i = 0, left = p.chain; i < k1 - k0; ++i, --left) {
+            if (left == 0) {
+                mma_commit_single(done);
+                if (!barrier_wait(taken, chunk++ & 1, &failed)) break;
+                tmem_fence_after();
+                left = p.chain;
+            }
             const uint32_t s = i % S::stages;
             if (!barrier_wait(full + 8 * s, i / S::stages & 1, &failed)) break;
             tmem_fence_after();
@@ -349,30 +358,43 @@ __global__ void __launch_bounds__(192, 2) token_product_kernel(const TokenProduc
             for (int t = 0; t < S::tiles; ++t) {
                 const uint64_t da = operand_descriptor(smem_address(at + t * S::bytes_w), kTileK * 128);
 #pragma unroll
-                for (int j = 0; j < kTileK / 16; ++j) mma_single(tmem + t * N, da + j * (32 >> 4), db + j * (32 >> 4), idesc, i > 0 || j > 0);
+                for (int j = 0; j < kTileK / 16; ++j) mma_single(tmem + t * N, da + j * (32 >> 4), db + j * (32 >> 4), idesc, left < p.chain || j > 0);
             }
             mma_commit_single(empty + 8 * s);
         }
         mma_commit_single(done);
         const uint64_t start = nanoseconds();
-        while (!barrier_try(done, 0) && nanoseconds() - start < kWaitLimit) {}
+        while (!barrier_try(done, chunk & 1) && nanoseconds() - start < kWaitLimit) {}
     }
     const int row = (warp & 3) * 32 + lane;                        // of the tile, warps 2 to 5
     float sum[S::tiles][N];
     if (warp >= 2) {
-        const bool ok = barrier_wait(done, 0, &failed);
-        tmem_fence_after();
 #pragma unroll
         for (int t = 0; t < S::tiles; ++t)
 #pragma unroll
-            for (int q = 0; q < N / 16; ++q) {
-                uint32_t v[16];
-                __syncwarp();
-                tmem_load_16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * N + 16 * q, v);
+            for (int j = 0; j < N; ++j) sum[t][j] = 0.f;
+        uint32_t chunk = 0;
+        const auto take = [&]() {
+            const bool ok = barrier_wait(done, chunk & 1, &failed);
+            tmem_fence_after();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sum[t][16 * q + j] = ok && !failed ? __uint_as_float(v[j]) : NAN;
-            }
-        tmem_fence_before();
+            for (int t = 0; t < S::tiles; ++t)
+#pragma unroll
+                for (int q = 0; q < N / 16; ++q) {
+                    uint32_t v[16];
+                    __syncwarp();
+                    tmem_load_16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * N + 16 * q, v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[t][16 * q + j] += ok && !failed ? __uint_as_float(v[j]) : NAN;
+                }
+            tmem_fence_before();
+        };
+        for (int left = k1 - k0 - p.chain; left > 0; left -= p.chain, ++chunk) {
+            take();
+            __syncwarp();
+            if (lane == 0) barrier_arrive_at(taken, rank);
+        }
+        take();
     }
     const auto store = [&](int t, float a, float b) {
         if (t < p.tokens && row0 + row < p.rows) out[t * p.ldo + row0 + row] = from_float<T>(GATED ? a * logistic<T>(a) * b : a);

@@ -7,7 +7,8 @@
 // A pair of CTAs works on a 256 x 256 tile (cta_group::2): each brings half of either operand, 64 deep, in a ring of kStages,
 // and holds half of D's rows in tensor memory, two tiles of them, so that the epilogue of one runs under the products of the
 // next.  The matrix unit truncates when it accumulates, so where a result keeps more than 16 bits the accumulator is
-// emptied into fp32 registers every CHAIN stages of 64 terms (0: at the end only).
+// emptied into fp32 registers every CHAIN stages of 64 terms (0: at the end only, for sums that are short beside what their
+// rounding takes away).
 //
 // Bound by the matrix unit (measured peak 1.66 PFLOP/s) where the last round of tiles is full: 8192 x 4096 x 10240 bf16 425 us (1.62
 // PFLOP/s), gated with checkpoints 1000 (1.38), backward activation 570 (1.20, its epilogue); small ones by two launches,
