@@ -71,6 +71,11 @@ View matrices_view(const void *p, const char *name, int64_t batch, int64_t rows,
     const int64_t width = ((rows - 1) * ld + cols) * es;
     return {p, name, batch, width, batch > 1 ? stride * es : width, (unsigned)es, written};
 }
+// The same as rows of one pitch, where the distance between matrices allows it: columns of one buffer beside each other are apart.
+View matrix_rows_view(const void *p, const char *name, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int64_t es, bool written) {
+    if (batch > 1 && stride % ld != 0) return matrices_view(p, name, batch, rows, cols, ld, stride, es, written);
+    return rows_view(p, name, batch > 1 ? (batch - 1) * (stride / ld) + rows : rows, cols, ld, es, written);
+}
 int check_layout(const char *name, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
     if (ld < cols) return fail(DEF_ERR_ARG, "the row stride of %s must be at least its width (got %lld)", name, (long long)ld);
     if (ld > ((int64_t)1 << 40)) return fail(DEF_ERR_ARG, "the rows of %s reach too far", name);
@@ -107,10 +112,14 @@ extern "C" int def_orthogonalize(int32_t dtype, int64_t batch, int64_t rows, int
     if (workspace_bytes < p.bytes()) return fail(DEF_ERR_ARG, "the workspace must have %lld bytes (got %lld)", (long long)p.bytes(), (long long)workspace_bytes);
     const int es = element_size(dtype);
     const bool same = x == out && (rows == 1 || ldx == ldo) && (batch == 1 || stride_x == stride_o);
-    const View views[] = {matrices_view(x, "x", batch, rows, cols, ldx, stride_x, es, false), matrices_view(same ? nullptr : out, "out", batch, rows, cols, ldo, stride_o, es, true),
-                          {workspace, "workspace", 1, p.bytes(), p.bytes(), 16, true}};
-    DEF_TRY(check_views(views));
-    if (((uintptr_t)out & (unsigned)(es - 1))) return fail(DEF_ERR_ALIGN, "out is not %d-byte aligned", es);
+    const View in_view = matrices_view(x, "x", batch, rows, cols, ldx, stride_x, es, false), out_view = matrices_view(out, "out", batch, rows, cols, ldo, stride_o, es, true),
+               work_view = {workspace, "workspace", 1, p.bytes(), p.bytes(), 16, true};
+    const View first[] = {in_view, work_view}, second[] = {out_view, work_view};
+    DEF_TRY(check_views(first));
+    DEF_TRY(check_views(second));
+    if (!same && share_bytes(in_view, out_view) &&
+        share_bytes(matrix_rows_view(x, "x", batch, rows, cols, ldx, stride_x, es, false), matrix_rows_view(out, "out", batch, rows, cols, ldo, stride_o, es, true)))
+        return fail(DEF_ERR_ALIAS, "x and out overlap");
     if (const int sms = sm_count(); sms < 0) return sms;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
     char *at = (char *)workspace;
