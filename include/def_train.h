@@ -244,7 +244,8 @@ int def_feed_forward_backward_workspace(int32_t dtype, int64_t T, int64_t C, int
  * steps' coefficients (a, b, c) in turn,
  *     A = X X^T,   X <- (a I + b A + c A A) X,        out = scale X
  * which takes each singular value s to s (a + b s^2 + c s^4) and leaves the singular vectors.  coeffs: 3 * steps numbers in HOST
- * memory, each within 8 of 0, read before the call returns; 1 <= steps <= DEF_ORTHOGONALIZE_MAX_STEPS.
+ * memory, read before the call returns, each within 8 of 0 (within 64 where the polynomials keep singular values that start in
+ * [0, 1] below 4 and a + b s^2 + c s^4 below 16, as far as can be told from the coefficients); 1 <= steps <= DEF_ORTHOGONALIZE_MAX_STEPS.
  * Matrix i of x starts at element i * stride_x and has rows of ldx; out likewise.  So one call serves a weight in all W rows of
  * def_step's gradients (stride d), at any 4-byte address, and in place: out may be x itself (same strides).
  * rows, cols and batch are at most 2^16; batch = 0 is a no-op.

@@ -1,5 +1,6 @@
 // C boundary of the orthogonalised update (see include/def_train.h).
 #include <algorithm>
+#include <cmath>
 
 #include "def_orthogonal_kernels.cuh"
 #include "def_product_launch.cuh"
@@ -66,6 +67,37 @@ int check_matrices(int32_t dtype, int64_t batch, int64_t rows, int64_t cols) {
         return fail(DEF_ERR_ARG, "rows and cols must be in [1, 2^16] (got %lld, %lld)", (long long)rows, (long long)cols);
     return DEF_OK;
 }
+// Whether the steps keep the singular values of X below 4 and those of B below 16, whatever matrix they start from (norm 1 at
+// most): then the entries are, too, which is what the pieces have room for.
+bool polynomials_stay(const float *coeffs, int steps) {
+    double top = 1.;                                       // singular values of X are in [0, top]
+    for (int i = 0; i < steps; ++i, coeffs += 3) {
+        const double a = coeffs[0], b = coeffs[1], c = coeffs[2], most = top * top;
+        const auto factor = [&](double t) { return a + t * (b + t * c); };             // of the singular value whose square is t
+        double largest = 0., next = 0.;
+        const auto look = [&](double t) {
+            if (!(t >= 0.)) t = 0.;
+            if (t > most) t = most;
+            largest = std::max(largest, std::abs(factor(t)));
+            next = std::max(next, std::sqrt(t) * std::abs(factor(t)));
+        };
+        look(0.);
+        look(most);
+        if (c != 0.) {
+            look(-b / (2. * c));                           // extremes of the factor, and of s times it
+            const double root = 9. * b * b - 20. * a * c;
+            if (root >= 0.) {
+                look((-3. * b + std::sqrt(root)) / (10. * c));
+                look((-3. * b - std::sqrt(root)) / (10. * c));
+            }
+        } else if (b != 0.) {
+            look(-a / (3. * b));
+        }
+        top = next * 1.00001;                              // what 22 bits may add
+        if (!(largest * 1.001 < 16.) || !(top < 4.)) return false;
+    }
+    return true;
+}
 // Matrices as a view: `batch` runs that each span a whole matrix.
 View matrices_view(const void *p, const char *name, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int64_t es, bool written) {
     const int64_t width = ((rows - 1) * ld + cols) * es;
@@ -100,7 +132,8 @@ extern "C" int def_orthogonalize(int32_t dtype, int64_t batch, int64_t rows, int
     if (steps < 1 || steps > DEF_ORTHOGONALIZE_MAX_STEPS) return fail(DEF_ERR_ARG, "steps must be in [1, %d] (got %d)", DEF_ORTHOGONALIZE_MAX_STEPS, steps);
     if (!coeffs) return fail(DEF_ERR_NULL, "coeffs must not be NULL");
     for (int i = 0; i < 3 * steps; ++i)
-        if (!(coeffs[i] >= -8.f && coeffs[i] <= 8.f)) return fail(DEF_ERR_ARG, "coefficients must be within 8 of 0 (got %g)", (double)coeffs[i]);
+        if (!(std::abs(coeffs[i]) <= 8.f) && !(std::abs(coeffs[i]) <= 64.f && polynomials_stay(coeffs, steps)))
+            return fail(DEF_ERR_ARG, "coefficients must be within 8 of 0, or within 64 where singular values stay below 4 (got %g)", (double)coeffs[i]);
     if (!(eps >= 0.f) || !(eps <= 1e30f)) return fail(DEF_ERR_ARG, "eps must be a finite number that is not negative");
     if (!(scale >= -1e30f && scale <= 1e30f)) return fail(DEF_ERR_ARG, "scale must be a finite number");
     if (batch == 0) return DEF_OK;

@@ -31,3 +31,12 @@ def test_columns_beside_each_other(B, rows, cols, dtype):
             for i in range(got.shape[0]):
                 _near(got[i], was[i])
         assert torch.equal(big[..., :cols + 3], old[..., :cols + 3]) and torch.equal(big[..., 2 * cols + 3:], old[..., 2 * cols + 3:])
+
+
+def test_steps_that_start_steep(B):
+    """A schedule whose first coefficients are beyond 8."""
+    from test_block_ops_edges import STEEP
+    for rows, cols in ((48, 80), (300, 200), (1300, 700)):
+        x, out = _normal((rows, cols), F32, 1), torch.empty(rows, cols, device=DEV)
+        B.def_orthogonalize(x, out, coeffs=STEEP, workspace=_work(B, rows, cols))
+        _near(out, x, coeffs=STEEP)
