@@ -151,3 +151,34 @@ def orthogonalize(x, coeffs=MUON, eps=1e-7, scale=1.0):
         err = slope * err + sx * eB + chain(m, B.abs() @ X.abs()) + bits * float(Y.norm())
         X = Y
     return scale * (X.t() if tall else X), abs(scale) * err
+
+
+def newton_schulz(x, coeffs=MUON, eps=1e-7, lost=(), mirrored=()):
+    """The steps of one matrix in 64 bits (tall or wide); with X, A and B held in two fp16 pieces where `lost` is given: those it
+    names without their lower piece, A or B of `mirrored` without it in tiles of 256 above the diagonal."""
+    X = x.double().t() if x.shape[0] > x.shape[1] else x.double()
+    pieces = lost is not None
+
+    def hold(v, name):
+        if not pieces:
+            return v
+        hi = (v * 4096).half().double()
+        lo = (v * 4096 - hi).half().double() * (name not in lost)
+        if name in mirrored:
+            tile = torch.arange(v.shape[0]) // 256
+            lo = torch.where(tile[:, None] < tile[None, :], 0.0, lo)
+        return (hi + lo) / 4096
+
+    X = hold(X / (X.norm() + eps), "X")
+    for i, (a, b, c) in enumerate(coeffs):
+        A = hold(X @ X.t(), "A")
+        X = hold(a * torch.eye(len(A), dtype=X.dtype, device=X.device) + b * A + c * A @ A, "B") @ X
+        if i + 1 < len(coeffs):
+            X = hold(X, "X")
+    return X.t() if x.shape[0] > x.shape[1] else X
+
+
+# What fp32 results of five steps may be off, relative in Frobenius norm: plain fp32 sums leave 1 to 2 10^-6 at these sizes, two pieces
+# 2 to 3 10^-7 more, the matrix unit's truncation (1.7 2^-24 for each of the 4 to 16 additions of a chain) somewhat more than the sums.
+# Without the lower piece of X, A or B anywhere 3 10^-4 and more are missing, in mirrored tiles alone 9 10^-5 (600 x 700).
+NEAR = 1e-5

@@ -3,6 +3,7 @@ import ctypes
 
 import torch
 
+import block_ref as R
 from paper_2004_05298_b200 import binding as B
 from test_block_ops_boundary import at, caller
 
@@ -67,3 +68,17 @@ def test_what_polynomials_do_to_singular_values():
         s = s * f
         assert float(f.abs().max()) < 16 and float(s.abs().max()) < 4
     assert float((s[10000:] - 1).abs().max()) < 0.01
+
+
+def test_the_precision_bound_tells_lost_pieces():
+    """R.NEAR is passed by two pieces and missed, by far, where the lower piece of something is lost."""
+    torch.manual_seed(0)
+    for m, n in ((64, 64), (300, 200), (100, 2000), (600, 700)):
+        for direction in (0, 3):
+            x = torch.randn(m, n) + direction * torch.randn(m, 1) * torch.randn(1, n)
+            want = R.newton_schulz(x, lost=None)
+            off = lambda **kw: float((R.newton_schulz(x, **kw) - want).norm() / want.norm())      # noqa: E731
+            assert off() < R.NEAR / 20
+            assert all(off(lost=(k,)) > 20 * R.NEAR for k in "XAB")
+            if m > 512:
+                assert all(off(mirrored=(k,)) > 5 * R.NEAR for k in "AB")
