@@ -81,3 +81,41 @@ def test_packed_sequences_in_parts(B, T, C, layout, dtype):
     _check(B, T, C, dtype, 3, layout, S=9, offsets=_cuts(T, 9, 1, T - 77), mean=4.0)
     _check(B, T, C, dtype, 4, layout, S=200, offsets=_cuts(T, 200, 2, T), mean=4.0, state=False)
     _check(B, T, C, dtype, 5, layout, S=5, offsets=[100, 100, T // 2, T // 2, T - 1, T], mean=6.0)
+
+
+def _scan(a, b):
+    """s_t = a_t s_{t-1} + b_t along the rows, 64 bits: each round joins runs of k rows to runs of 2 k."""
+    k = 1
+    while k < a.shape[0]:
+        b = torch.cat([b[:k], b[k:] + a[k:] * b[:-k]])
+        a = torch.cat([a[:k], a[k:] * a[:-k]])
+        k *= 2
+    return b
+
+
+@pytest.mark.parametrize("T,C,layout", [(1 << 18, 64, "rows"), (1 << 18, 33, "off"), (1 << 16, 1024, "rows"), (1 << 15, 4800, "rows")])
+def test_memories_of_many_tokens(B, T, C, layout):
+    """c = (k + 1/2) 2^-24, which 1 - c in fp32 is off by half a unit from: a state that is folded with it at every step drifts by 2^-25
+    a step, a fraction 1 / (2 k + 1) of what it should lose.  Runs of 8 steps are folded at once here: a rounding of what they keep
+    (2^-25), one where runs are joined, one of the state (2^-24), all at most 2^-26 a step; 2^-20 for what happens within a block."""
+    k = 60 + torch.arange(C, device=DEV, dtype=torch.float64) % 40
+    c = (k + 0.5) * 2.0 ** -24
+    g = torch.log((1 - c) / c).float()
+    exact = torch.sigmoid(-g.double())
+    assert float(((exact * 2 ** 24 - k - 0.5).abs()).max()) < 0.02
+    gate = _laid(g.expand(T, C), layout)
+    x, dy = (_laid(1 + _normal((T, C), F32, i, 0.3), layout) for i in (1, 2))
+    y, dx, dg = (_laid(torch.zeros(T, C, device=DEV), layout) for _ in range(3))
+    last, dh0, work = torch.empty(1, C, device=DEV), torch.empty(1, C, device=DEV), _work(B, T, C, F32)
+    B.def_recurrence_forward(x, gate, y, h_last=last, workspace=work)
+    B.def_recurrence_backward(dy, x, gate, y, dx, dg, dh0=dh0, workspace=work)
+    step = max(1, (1 << 23) // T)
+    for i in range(0, C, step):                                            # some channels at a time
+        part = slice(i, min(C, i + step))
+        e = exact[part].expand(T, -1)
+        for gots, b in (((last[0, part], y[-1, part]), e * x[:, part].double()), ((dh0[0, part],), (1 - e) * dy[:, part].double().flip(0))):
+            want, most = _scan(1 - e, b), _scan(1 - e, b.abs())
+            off = _scan(1 - e, 2.0 ** -26 * most)[-1] + 2.0 ** -20 * most[-1]
+            for got in gots:
+                worst = float(((got.double() - want[-1]).abs() / off).max())
+                assert worst <= 1, worst
