@@ -352,17 +352,20 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
 
 // ---------------------------------------------------------------------------
 // The same for rows on 16-byte boundaries: blocks of steps by 64 channels come by tensor copies into a ring, so that loads run
-// on under the two passes over a block and registers hold little.  Small blocks, so that several CTAs share an SM: one
-// computes while others wait for a barrier.  Pass one leaves 1 - c and c x of a step in registers (backward: c; what else
+// on under the two passes over a block and registers hold little.  Small blocks, so that two CTAs share an SM (fp32 backward:
+// one): one computes while the other waits for a barrier.  Pass one leaves 1 - c and c x of a step in registers (backward: c; what else
 // pass two needs it reads from the ring again).  A thread has two channels and works on both in one instruction.
 // ---------------------------------------------------------------------------
+constexpr int kStreamOffsets = 128;             // offsets that are kept in shared memory
 template <typename T, bool BACK> struct StreamBlock {
     static constexpr int run = sizeof(T) == 2 && !BACK ? 16 : 8, steps = run * kRecWarps;
     static constexpr int tensors = BACK ? 4 : 2, row = 64 * (int)sizeof(T), bytes = steps * row;
-    static constexpr int ctas = 2, stages = 3;
-    static constexpr int smem = stages * tensors * bytes + 128;
+    static constexpr int stages = 3, smem = stages * tensors * bytes + 128, part_smem = stages * 2 * bytes + 128;   // part: gate and x (dy)
+    // CTAs per SM that a call is cut for, and that have room beside each other, but for fp32 backward, whose ring leaves room for one: there a
+    // call runs in two waves.  Cut for one CTA (and parts rounded down), us: 16384 x 256 30 against 37, 16384 x 2048 179 against 217;
+    // but 8192 x 4096 177 against 143, 16384 x 4096 359 against 297.
+    static constexpr int ctas = 2;
 };
-constexpr int kStreamOffsets = 128;             // offsets that are kept in shared memory
 struct RecurrenceMaps {
     CUtensorMap gate, first, x, y;              // first: x forward, dy backward; x and y: backward only
 };
@@ -515,11 +518,12 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
     const int begin = (int)blockIdx.y * a.part_steps;            // of this part
     const int end = min(a.T, begin + a.part_steps);
     const int stride = ranks * kSteps, rounds = (end - begin + stride - 1) / stride;
+    constexpr int kStage = kUsed * B::bytes;
     const auto load = [&](int i) {                               // one thread: the block of round i
         const int s = i % B::stages, run = begin + i * stride + rank * kSteps;
         const int t0 = BACK ? a.T - run - kSteps : run;          // may lie before the first or behind the last row: zeros there
-        const uint32_t bar = full + 8 * s, to = smem_address(stages + s * B::tensors * B::bytes);
-        barrier_expect(bar, kUsed * B::bytes);
+        const uint32_t bar = full + 8 * s, to = smem_address(stages + s * kStage);
+        barrier_expect(bar, kStage);
         tensor_load_2d(to, &maps.gate, tile * 64, t0, bar);
         tensor_load_2d(to + B::bytes, &maps.first, tile * 64, t0, bar);
         if constexpr (BACK && !PART) {
@@ -580,7 +584,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         const bool plain = is_there == (1u << R) - 1u && (enters | leaves) == 0;
         ok = ok && barrier_wait(full + 8 * stage, turn, &failed);
         // row j of the run; backward a block's rows lie in the order of time
-        const uint8_t *rows = stages + stage * (B::tensors * B::bytes) + (BACK ? kSteps - 1 - warp * R : warp * R) * B::row + lane * (B::row / 32);
+        const uint8_t *rows = stages + stage * kStage + (BACK ? kSteps - 1 - warp * R : warp * R) * B::row + lane * (B::row / 32);
         constexpr int kStep = BACK ? -B::row : B::row;
         Pair keep[R], in[R];                                     // 1 - c, c x (backward: c)
         Map2 m = {one, zero};
