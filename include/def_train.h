@@ -180,9 +180,12 @@ int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const void *logits
  * `sequences` equally long runs (T must be a multiple).  Rows of no sequence are not written, and what they hold does not matter.  Offsets that
  * decrease or leave [0, T] do no harm outside the arguments, but what is computed then is not specified.
  * h0, h_last [sequences, C] fp32: the state before a sequence's first token (NULL: 0) and behind its last one (NULL: not
- * written; a sequence without tokens hands on its h0).  y may be x itself (same stride) where no backward pass will need x.
+ * written; a sequence without tokens hands on its h0; h_last is other memory than h0).  y may be x itself (same stride) where no
+ * backward pass will need x.
  * One token of each sequence: T = sequences, offsets NULL, h_last of one call is the next one's h0.
- * The state is fp32; an infinity or a NaN stays within its sequence and channel.
+ * The state is fp32, each step of it one rounding; what runs of 8 or 16 steps keep of it is found without the rounding of 1 - c, so
+ * that within a call memories of many tokens (c down to 2^-18 or so) drift by no more than 2^-26 of the state a step.  In calls of
+ * one token each that rounding stays, 2^-25 a step.  An infinity or a NaN stays within its sequence and channel.
  * The workspace holds maps of parts of long narrow calls; def_recurrence_workspace says how much is needed (at most
  * 4096 C bytes; the same forward and backward).
  */

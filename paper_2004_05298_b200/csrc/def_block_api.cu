@@ -93,6 +93,7 @@ template <bool BACK> int recurrence(int32_t dtype, deft::Recurrence a, bool pair
             DEF_TRY(rows_map(maps.y, dtype, a.y, a.T, a.C, a.ldy, steps));
         }
     }
+    const bool handed = (BACK ? a.dh0 : a.h_last) != nullptr;
     cudaError_t err = cudaSuccess;
     by_dtype(dtype, [&](auto type) {
         using E = decltype(type);
@@ -115,17 +116,21 @@ template <bool BACK> int recurrence(int32_t dtype, deft::Recurrence a, bool pair
         };
         if (streamed) {
             constexpr int smem = deft::StreamBlock<E, BACK>::smem, part_smem = deft::StreamBlock<E, BACK>::part_smem;
-            constexpr auto part = deft::recurrence_stream_kernel<E, BACK, true>, whole = deft::recurrence_stream_kernel<E, BACK, false>;
+            constexpr auto part = deft::recurrence_stream_kernel<E, BACK, true, false>;
             if (p.parts > 1 && (err = allow_smem<part>(part_smem)) != cudaSuccess) return;
-            if ((err = allow_smem<whole>(smem)) != cudaSuccess) return;
-            if (p.parts > 1) launch(part, part_smem, 1, p.parts - 1, false, maps);
-            launch(whole, smem, p.ranks, p.parts, p.parts > 1, maps);
+            const auto both = [&](auto is_handed) {
+                constexpr auto whole = deft::recurrence_stream_kernel<E, BACK, false, decltype(is_handed)::value>;
+                if ((err = allow_smem<whole>(smem)) != cudaSuccess) return;
+                if (p.parts > 1) launch(part, part_smem, 1, p.parts - 1, false, maps);
+                launch(whole, smem, p.ranks, p.parts, p.parts > 1, maps);
+            };
+            by_alignment(handed, both);
             return;
         }
         auto both = [&](auto v) {
             constexpr int V = decltype(v)::value ? 2 : 1;
-            if (p.parts > 1) launch(deft::recurrence_kernel<E, V, BACK, true>, 0, 1, p.parts - 1, false);
-            launch(deft::recurrence_kernel<E, V, BACK, false>, 0, p.ranks, p.parts, false);
+            if (p.parts > 1) launch(deft::recurrence_kernel<E, V, BACK, true, false>, 0, 1, p.parts - 1, false);
+            by_alignment(handed, [&](auto is_handed) { launch(deft::recurrence_kernel<E, V, BACK, false, decltype(is_handed)::value>, 0, p.ranks, p.parts, false); });
         };
         if constexpr (sizeof(E) == 2) by_alignment(pairs, both);
         else both(Is<false>());

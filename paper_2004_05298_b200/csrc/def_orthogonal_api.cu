@@ -51,7 +51,8 @@ OrthogonalPlan orthogonal_plan(int64_t batch, int64_t rows, int64_t cols) {
 // and 1 of them, beside that of the same steps in plain fp32, 10^-6:
 //     128 x 128  2.3, 2.3, 1.6 (1.4)     512 x 512  3.6, 2.5, 1.6 (2.3)     1024 x 1024  4.0, 2.2, 1.4 (2.7)     1500 x 3000  3.5, 2.0, 1.3 (2.7)
 //     2048 x 4096  3.4, 1.9, 1.3 (2.9)   100 x 8000  3.1, 3.4, 2.2 (1.3)    4096 x 10240  3.3, 1.9, 1.4 (3.8)
-// 4096 x 10240 takes 7.9, 9.2 and 10.3 ms, 512 x 512 260, 262 and 270 us.
+// 4096 x 10240 takes 7.9, 9.2 and 10.3 ms (calls back to back, one set of inputs), 512 x 512 260, 262 and 270 us (before joins read
+// several parts at once: 209 with 2 stages now).
 int piece_chain(int64_t m) { return m < 384 ? 1 : m < 1280 ? 2 : 4; }
 template <bool BN, typename EPILOGUE>
 int launch_pieces(int64_t m, const deft::Product &p, const EPILOGUE &epilogue, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t stream, const char *what) {

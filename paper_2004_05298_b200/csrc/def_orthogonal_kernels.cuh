@@ -6,8 +6,9 @@
 // rounded and what that leaves, which carry 22 bits; each product is the three products of pieces above 2^-22.  Singular values
 // stay below 4 where the polynomial is one that converges, so no entry of X or A is larger than 16 and a power of two
 // that puts 16 at the end of fp16's range serves all of them (kPieceScale).  A and A A are symmetric: tiles on and below
-// the diagonal are computed, those below stored twice.  Five steps of 4096 x 10240 fp32 take 8.3 ms, 1.05 PFLOP/s of fp16 products
-// (chains emptied every 4 stages); of 256 x 256 190 us, 15 products one after another.
+// the diagonal are computed, those below stored twice.  Five steps of 4096 x 10240 fp32 take 7.8 to 8.1 ms, 1.1 PFLOP/s of fp16
+// products (calls back to back, one set of inputs; 8.3 ms with three in turn; chains emptied every 4 stages); of 256 x 256 187 us, 15
+// products one after another.
 #pragma once
 
 #include "def_product_kernels.cuh"

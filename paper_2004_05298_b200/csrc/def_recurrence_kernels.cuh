@@ -11,8 +11,8 @@
 // Every sum is taken in one order.
 //
 // It is bound by what a round of a cluster's blocks waits for, not by memory.  Measured, of the copy rate of 6562 GB/s: 16384 x 4096
-// bf16 in 8 sequences forward 115 us (3.5 TB/s), backward 181 (4.4); 8192 x 4096 fp32 85 (4.7) and 177 (4.5); 16384 x 512 fp32 in
-// parts 33; rows off alignment, 16384 x 4097 bf16, 262 and 525.
+// bf16 in 8 sequences forward 117 us (3.4 TB/s), backward 182 (4.4); 8192 x 4096 fp32 84 (4.8) and 172 (4.7); 16384 x 512 fp32 in
+// parts 31 and 51; rows off alignment, 16384 x 4097 bf16, 256 and 523.
 //
 // Sequences lie one behind another; at a sequence's first step the state is replaced, P becomes -0 ("nothing from before":
 // with a zero of that sign no infinity or NaN of another sequence gets in).
@@ -80,8 +80,12 @@ template <typename T, int V> __device__ __forceinline__ void store_few(T *p, con
 // What a run keeps of the state before it: the product of its 1 - c, each of them rounded; or, where that is at least a half, 1 less
 // what it lets go, Q = c + (1 - c) Q', in which nothing is lost.  Only so do memories of many tokens last as long as they should: for c =
 // 2^-17 a state that is multiplied with a rounded 1 - c at every step may be off by a 256th.  (A start sets Q to 1.)  Within a run the
-// rounded 1 - c serves: what 16 steps are off there is not handed on.  It takes 3 % (16384 x 4096 bf16 forward 114.4 to 118.3 us).
+// rounded 1 - c serves, since what its steps are off there is not handed on; but for runs whose state leaves the call (one token of each
+// sequence, say): there what the rounding takes from 1 - c (`lost`, exact) is multiplied, too.  Q takes 3 % (16384 x 4096 bf16 forward 114.4
+// to 118.3 us).
 __device__ __forceinline__ float kept_by(float P, float Q) { return Q < 0.5f ? 1.f - Q : P; }
+__device__ __forceinline__ float lost(float keep, float c) { return (1.f - keep) - c; }
+__device__ __forceinline__ float finite(float s) { return fminf(fmaxf(s, -3.402823466e38f), 3.402823466e38f); }   // 0 times infinity is no number
 __device__ __forceinline__ bool is_reset(float P) { return __float_as_uint(P) == 0x80000000u; }
 __device__ __forceinline__ float advance(float2 m, float s) { return is_reset(m.x) ? m.y : fmaf(m.x, s, m.y); }
 __device__ __forceinline__ float2 join(float2 first, float2 then) {
@@ -118,9 +122,9 @@ struct Places {
     }
 };
 
-// BACK: steps count from the last token.  PART: only (P, L) of each part.
-// Grid: tiles of channels x CTAs of a cluster, parts.
-template <typename T, int V, bool BACK, bool PART>
+// BACK: steps count from the last token.  PART: only (P, L) of each part.  HANDED: the states behind the sequences (dh0) are wanted, which
+// are then found more carefully.  Grid: tiles of channels x CTAs of a cluster, parts.
+template <typename T, int V, bool BACK, bool PART, bool HANDED>
 __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Recurrence a, int ranks) {
     __shared__ float2 runs[2][kRecWarps][32 * V];
     __shared__ float2 blocks[2][kMostCluster][32 * V];
@@ -139,7 +143,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
         __syncthreads();
     }
     const float *enter_with = BACK ? a.dh_last : a.h0;
-    float *leave_to = BACK ? a.dh0 : a.h_last;
+    float *leave_to = BACK ? a.dh0 : a.h_last;                   // HANDED
     const auto entered = [&](int s, int v) { return enter_with && mine ? enter_with[(int64_t)s * a.C + col + v] : 0.f; };
 
     if (ranks > 1) cluster_sync();                               // all have started before one writes to another
@@ -272,6 +276,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
                 }
         }
 
+        const bool handed = HANDED && leaves;
         if constexpr (!BACK) {
             T *py = (T *)a.y + t0 * a.ldy + col;
 #pragma unroll
@@ -282,9 +287,14 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
                     for (int v = 0; v < V; ++v) s[v] = entered(q, v);
                 }
 #pragma unroll
-                for (int v = 0; v < V; ++v) s[v] = fmaf(1.f - c[j][v], s[v], c[j][v] * to_float<T>(in_b[j].v[v]));
+                for (int v = 0; v < V; ++v) {
+                    const float keep = 1.f - c[j][v];
+                    float in = c[j][v] * to_float<T>(in_b[j].v[v]);
+                    if (handed) in = fmaf(lost(keep, c[j][v]), finite(s[v]), in);
+                    s[v] = fmaf(keep, s[v], in);
+                }
                 if (is_there >> j & 1u) store_few<T, V>(py + j * a.ldy, s);
-                if (leave_to && (leaves >> j & 1u)) {
+                if (HANDED && (leaves >> j & 1u)) {
                     const int q = __shfl_sync(0xffffffffu, seq, j);
                     if (mine)
 #pragma unroll
@@ -321,13 +331,13 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
                     const float lambda = to_float<T>(in_b[j].v[v]) + s[v], keep = 1.f - c[j][v];
                     dx[v] = c[j][v] * lambda;
                     dg[v] = lambda * (before[v] - to_float<T>(in_x[j].v[v])) * (keep * c[j][v]);
-                    s[v] = keep * lambda;
+                    s[v] = handed ? fmaf(keep, lambda, lost(keep, c[j][v]) * finite(lambda)) : keep * lambda;
                 }
                 if (is_there >> j & 1u) {
                     store_few<T, V>(pdx - j * a.lddx, dx);
                     store_few<T, V>(pdg - j * a.lddg, dg);
                 }
-                if (leave_to && (leaves >> j & 1u)) {
+                if (HANDED && (leaves >> j & 1u)) {
                     const int q = __shfl_sync(0xffffffffu, seq, j);
                     if (mine)
 #pragma unroll
@@ -343,7 +353,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
         return;
     }
     // A sequence without tokens hands on what it was given.
-    if (leave_to && blockIdx.y == 0 && rank == 0 && mine && (a.offsets || a.each == 0))
+    if (HANDED && blockIdx.y == 0 && rank == 0 && mine && (a.offsets || a.each == 0))
         for (int q = warp; q < at.sequences; q += kRecWarps)
             if (a.each == 0 && !a.offsets || a.offsets && at.bound(q + 1) <= at.bound(q))
 #pragma unroll
@@ -426,6 +436,16 @@ __device__ __forceinline__ Pair kept_by(Pair P, Pair Q) {
     split_pair(Q, q0, q1);
     return make_pair(kept_by(p0, q0), kept_by(p1, q1));
 }
+__device__ __forceinline__ Pair lost(Pair keep, Pair c) {
+    const Pair one = make_pair(1.f, 1.f), minus = make_pair(-1.f, -1.f);
+    return pair_fma(c, minus, pair_fma(keep, minus, one));
+}
+__device__ __forceinline__ Pair finite(Pair s) {
+    float a, b;
+    split_pair(s, a, b);
+    return make_pair(finite(a), finite(b));
+}
+template <bool B> struct Known { static constexpr bool value = B; };
 struct alignas(16) Map2 { Pair P, L; };          // (P, L) of two channels
 // `calm`: no sequence starts there.
 template <bool CALM> __device__ __forceinline__ Pair advance2(const Map2 &m, Pair s) {
@@ -483,7 +503,7 @@ __device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map2 &m) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(to), "l"(m.P.bits), "l"(m.L.bits), "r"(bar) : "memory");
 }
 
-template <typename T, bool BACK, bool PART>
+template <typename T, bool BACK, bool PART, bool HANDED>
 __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
     recurrence_stream_kernel(const Recurrence a, int ranks, const __grid_constant__ RecurrenceMaps maps) {
     using B = StreamBlock<T, BACK>;
@@ -562,7 +582,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         // Calm: all of the cluster's blocks of this round lie inside one sequence, its first and (where that matters) last token
         // elsewhere.
         const int t_lo = BACK ? a.T - base - stride : base, t_hi = t_lo + stride - 1;
-        const bool calm = t_lo > first && t_hi < behind - (BACK || leave_to ? 1 : 0) && base + stride <= end;
+        const bool calm = t_lo > first && t_hi < behind - (BACK || HANDED ? 1 : 0) && base + stride <= end;
         uint32_t is_there = (1u << R) - 1u, enters = 0, leaves = 0;
         int seq = 0;
         if (!calm) {
@@ -580,18 +600,20 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
             enters = __ballot_sync(0xffffffffu, enter);
             leaves = __ballot_sync(0xffffffffu, leave);
         }
-        if (!BACK && !leave_to) leaves = 0;                      // nothing happens there
+        if (!BACK && !HANDED) leaves = 0;                      // nothing happens there
         const bool plain = is_there == (1u << R) - 1u && (enters | leaves) == 0;
         ok = ok && barrier_wait(full + 8 * stage, turn, &failed);
         // row j of the run; backward a block's rows lie in the order of time
         const uint8_t *rows = stages + stage * kStage + (BACK ? kSteps - 1 - warp * R : warp * R) * B::row + lane * (B::row / 32);
         constexpr int kStep = BACK ? -B::row : B::row;
-        Pair keep[R], in[R];                                     // 1 - c, c x (backward: c)
+        Pair keep[R], in[R];                                     // 1 - c (or c, see pass_one), c x (backward: c)
         Map2 m = {one, zero};
         Pair let = zero;                                         // Q
-        const auto pass_one = [&](int j, Pair &keep_j, Pair &in_j) {
+        // first_j: 1 - c; c where the state behind a run that is not plain may be handed on
+        const auto pass_one = [&](int j, Pair &first_j, Pair &in_j, auto is_plain) {
             const Pair c = logistic_back<T>(two_channels<T>(rows + j * kStep)), b = two_channels<T>(rows + j * kStep + B::bytes);
-            keep_j = pair_fma(c, minus, one);
+            const Pair keep_j = pair_fma(c, minus, one);
+            first_j = decltype(is_plain)::value || !HANDED ? keep_j : c;
             if constexpr (BACK) {
                 in_j = c;
                 m.L = pair_mul(keep_j, pair_add(m.L, b));
@@ -604,7 +626,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         };
         if (plain) {
 #pragma unroll
-            for (int j = 0; j < R; ++j) pass_one(j, keep[j], in[j]);
+            for (int j = 0; j < R; ++j) pass_one(j, keep[j], in[j], Known<true>());
         } else {
 #pragma unroll
             for (int j = 0; j < R; ++j) {
@@ -612,7 +634,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
                     m = {make_pair(-0.f, -0.f), entered(__shfl_sync(0xffffffffu, seq, j))};
                     let = one;
                 }
-                if (is_there >> j & 1u) pass_one(j, keep[j], in[j]);
+                if (is_there >> j & 1u) pass_one(j, keep[j], in[j], Known<false>());
             }
         }
         m.P = kept_by(m.P, let);
@@ -656,15 +678,19 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         }
         const int64_t t0 = BACK ? a.T - 1 - run : run;
         T *out = BACK ? (T *)a.dx + t0 * a.lddx + col : (T *)a.y + t0 * a.ldy + col, *out_g = (T *)a.dgate + t0 * a.lddg + col;
-        const auto pass_two = [&](int j, Pair keep_j, Pair in_j, Pair before) {
+        const bool handed = HANDED && leaves;
+        const auto pass_two = [&](int j, Pair first_j, Pair in_j, Pair before, auto is_plain) {
+            constexpr bool kPlain = decltype(is_plain)::value || !HANDED;
+            const Pair keep_j = kPlain ? first_j : pair_fma(first_j, minus, one);
+            const auto rest = [&](Pair v) { return pair_mul(lost(keep_j, first_j), finite(v)); };
             if constexpr (!BACK) {
-                s = pair_fma(keep_j, s, in_j);
+                s = pair_fma(keep_j, s, !kPlain && handed ? pair_add(rest(s), in_j) : in_j);
                 if (mine) store_channels<T>(out, s);
                 out += a.ldy;
             } else {
                 const Pair b = two_channels<T>(rows + j * kStep + B::bytes), x = two_channels<T>(rows + j * kStep + 2 * B::bytes);
                 const Pair lambda = pair_add(b, s), dx = pair_mul(in_j, lambda);
-                s = pair_mul(keep_j, lambda);
+                s = !kPlain && handed ? pair_fma(keep_j, lambda, rest(lambda)) : pair_mul(keep_j, lambda);
                 const Pair dg = pair_mul(pair_mul(dx, keep_j), pair_fma(x, minus, before));
                 if (mine) {
                     store_channels<T>(out, dx);
@@ -677,7 +703,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         const auto earlier = [&](int j) { return BACK ? two_channels<T>(rows + j * kStep + 3 * B::bytes) : zero; };
         if (plain) {
 #pragma unroll
-            for (int j = 0; j < R; ++j) pass_two(j, keep[j], in[j], earlier(j));
+            for (int j = 0; j < R; ++j) pass_two(j, keep[j], in[j], earlier(j), Known<true>());
         } else {
 #pragma unroll
             for (int j = 0; j < R; ++j) {
@@ -689,12 +715,12 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
                         const float *p = a.h0 + (int64_t)q * a.C + col;
                         before = a.h0 && mine ? make_pair(p[0], p[1]) : zero;
                     }
-                    pass_two(j, keep[j], in[j], before);
+                    pass_two(j, keep[j], in[j], before, Known<false>());
                 } else {
                     out += BACK ? -a.lddx : a.ldy;
                     out_g -= a.lddg;
                 }
-                if (leave_to && (leaves >> j & 1u)) left(q, s);
+                if (HANDED && (leaves >> j & 1u)) left(q, s);
             }
         }
     }
@@ -703,7 +729,7 @@ __global__ void __launch_bounds__(32 * kRecWarps, StreamBlock<T, BACK>::ctas)
         return;
     }
     // A sequence without tokens hands on what it was given.
-    if (leave_to && blockIdx.y == 0 && rank == 0 && mine && a.offsets)
+    if (HANDED && blockIdx.y == 0 && rank == 0 && mine && a.offsets)
         for (int q = warp; q < at.sequences; q += kRecWarps)
             if (at.bound(q + 1) <= at.bound(q)) left(q, entered(q));
 }

@@ -119,3 +119,34 @@ def test_memories_of_many_tokens(B, T, C, layout):
             for got in gots:
                 worst = float(((got.double() - want[-1]).abs() / off).max())
                 assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("S,C,layout", [(40, 64, "rows"), (200, 64, "rows"), (40, 33, "off")])
+def test_states_handed_on_from_call_to_call(B, S, C, layout):
+    """One token of each sequence a call, c = (k + 1/2) 2^-24: what a step with a rounded 1 - c drifts, 2^-25, adds up to 6 10^-4 in all channels
+    alike.  The other roundings, of the state by up to half a unit in the last place, 2^-24 / sqrt(12) of it in the mean square, are as
+    random as the tokens.  But 50 tokens recur, and the state moves by a thousandth only, so that what they leave may recur, too: N / 50 times
+    the sum of 50 such errors, N / sqrt(50) 2^-24 / sqrt(12) = 4.9 10^-5 (8 standard deviations allowed), independent from one channel and
+    sequence to another, so that their mean over all S C of them is less by sqrt(S C)."""
+    N = 20000
+    k = 60 + torch.arange(C, device=DEV, dtype=torch.float64) % 40
+    g = torch.log((1 - (k + 0.5) * 2.0 ** -24) / ((k + 0.5) * 2.0 ** -24)).float()
+    c = torch.sigmoid(-g.double())
+    gate = _laid(g.expand(S, C), layout)
+    tokens = [_laid(1 + _normal((S, C), F32, i, 0.3), layout) for i in range(50)]
+    dys = [_laid(1e-5 * t, layout) for t in tokens]
+    y, dx, dg = (_laid(torch.zeros(S, C, device=DEV), layout) for _ in range(3))
+    state, grad, spare, spare_grad = (torch.ones(S, C, device=DEV) for _ in range(4))
+    want, want_grad = (torch.ones(S, C, device=DEV, dtype=torch.float64) for _ in range(2))
+    x64, dy64 = [t.double() for t in tokens], [t.double() for t in dys]
+    for i in range(N):
+        B.def_recurrence_forward(tokens[i % 50], gate, y, h0=state, h_last=spare, sequences=S)
+        B.def_recurrence_backward(dys[i % 50], tokens[0], gate, y, dx, dg, dh_last=grad, dh0=spare_grad, sequences=S)
+        state, spare, grad, spare_grad = spare, state, spare_grad, grad
+        want = (1 - c) * want + c * x64[i % 50]
+        want_grad = (1 - c) * (want_grad + dy64[i % 50])
+    # (backward dy + mu is rounded, too)
+    for got, exact, roundings in ((state, want, 1), (grad, want_grad, 2)):
+        off = (got.double() - exact) / exact
+        most = 8 * 2.0 ** -24 * N / math.sqrt(50) * math.sqrt(roundings / 12)
+        assert float(off.abs().max()) < most and abs(float(off.mean())) < most / math.sqrt(S * C)
