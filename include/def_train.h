@@ -183,9 +183,9 @@ int def_logprob_backward(int32_t dtype, int64_t T, int64_t V, const void *logits
  * written; a sequence without tokens hands on its h0; h_last is other memory than h0).  y may be x itself (same stride) where no
  * backward pass will need x.
  * One token of each sequence: T = sequences, offsets NULL, h_last of one call is the next one's h0.
- * The state is fp32, each step of it one rounding; what runs of 8 or 16 steps keep of it is found without the rounding of 1 - c, so
- * that within a call memories of many tokens (c down to 2^-18 or so) drift by no more than 2^-26 of the state a step.  In calls of
- * one token each that rounding stays, 2^-25 a step.  An infinity or a NaN stays within its sequence and channel.
+ * The state is fp32.  What is handed on, from run to run of 8 or 16 steps and in h_last, is free of the rounding of 1 - c, so that memories
+ * of many tokens (c of 2^-17 and less) do not drift by up to 2^-25 of the state a step.  An infinity or a NaN stays within its sequence
+ * and channel.
  * The workspace holds maps of parts of long narrow calls; def_recurrence_workspace says how much is needed (at most
  * 4096 C bytes; the same forward and backward).
  */

@@ -11,8 +11,8 @@
 // Every sum is taken in one order.
 //
 // It is bound by what a round of a cluster's blocks waits for, not by memory.  Measured, of the copy rate of 6562 GB/s: 16384 x 4096
-// bf16 in 8 sequences forward 117 us (3.4 TB/s), backward 182 (4.4); 8192 x 4096 fp32 84 (4.8) and 172 (4.7); 16384 x 512 fp32 in
-// parts 31 and 51; rows off alignment, 16384 x 4097 bf16, 256 and 523.
+// bf16 in 8 sequences forward 114 us (3.5 TB/s), backward 177 (4.5); 8192 x 4096 fp32 82 (4.9) and 166 (4.8); 16384 x 512 fp32 in
+// parts 30 and 51; rows off alignment, 16384 x 4097 bf16, 234 and 436.
 //
 // Sequences lie one behind another; at a sequence's first step the state is replaced, P becomes -0 ("nothing from before":
 // with a zero of that sign no infinity or NaN of another sequence gets in).
@@ -42,6 +42,7 @@ struct Recurrence {
     float2 *summary;                            // (P, L) of each part and channel: [parts][C], or of pairs of channels (P, P, L, L)
 };
 
+template <bool B> struct Known { static constexpr bool value = B; };
 // 1 / (1 + exp(g)) = 1 - a.
 template <typename T> __device__ __forceinline__ float logistic_back(float g) { return logistic<T>(-g); }
 
@@ -81,8 +82,9 @@ template <typename T, int V> __device__ __forceinline__ void store_few(T *p, con
 // what it lets go, Q = c + (1 - c) Q', in which nothing is lost.  Only so do memories of many tokens last as long as they should: for c =
 // 2^-17 a state that is multiplied with a rounded 1 - c at every step may be off by a 256th.  (A start sets Q to 1.)  Within a run the
 // rounded 1 - c serves, since what its steps are off there is not handed on; but for runs whose state leaves the call (one token of each
-// sequence, say): there what the rounding takes from 1 - c (`lost`, exact) is multiplied, too.  Q takes 3 % (16384 x 4096 bf16 forward 114.4
-// to 118.3 us).
+// sequence, say): there what the rounding takes from 1 - c (`lost`, exact) is multiplied, too.  Kernels of their own for calls that hand
+// states on: 16384 x 4096 bf16 in 8 sequences 114 us forward without Q, 115 with it, 131 and 135 with states in and out; rows of even width
+// off 16 bytes, 16384 x 4098 bf16, 211 and 204, 211 and 250.
 __device__ __forceinline__ float kept_by(float P, float Q) { return Q < 0.5f ? 1.f - Q : P; }
 __device__ __forceinline__ float lost(float keep, float c) { return (1.f - keep) - c; }
 __device__ __forceinline__ float finite(float s) { return fminf(fmaxf(s, -3.402823466e38f), 3.402823466e38f); }   // 0 times infinity is no number
@@ -276,11 +278,20 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
                 }
         }
 
-        const bool handed = HANDED && leaves;
+        // is_handed: the state leaves from one of these steps
+        const auto in_turn = [&](const auto &step) {
+            if (HANDED && leaves) {
+#pragma unroll
+                for (int j = 0; j < kRun; ++j) step(j, Known<true>());
+            } else {
+#pragma unroll
+                for (int j = 0; j < kRun; ++j) step(j, Known<false>());
+            }
+        };
         if constexpr (!BACK) {
             T *py = (T *)a.y + t0 * a.ldy + col;
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) {
+            in_turn([&](int j, auto is_handed) {
+                constexpr bool kHanded = decltype(is_handed)::value;
                 if (enters >> j & 1u) {
                     const int q = __shfl_sync(0xffffffffu, seq, j);
 #pragma unroll
@@ -290,17 +301,17 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
                 for (int v = 0; v < V; ++v) {
                     const float keep = 1.f - c[j][v];
                     float in = c[j][v] * to_float<T>(in_b[j].v[v]);
-                    if (handed) in = fmaf(lost(keep, c[j][v]), finite(s[v]), in);
+                    if (kHanded) in = fmaf(lost(keep, c[j][v]), finite(s[v]), in);
                     s[v] = fmaf(keep, s[v], in);
                 }
                 if (is_there >> j & 1u) store_few<T, V>(py + j * a.ldy, s);
-                if (HANDED && (leaves >> j & 1u)) {
+                if (kHanded && (leaves >> j & 1u)) {
                     const int q = __shfl_sync(0xffffffffu, seq, j);
                     if (mine)
 #pragma unroll
                         for (int v = 0; v < V; ++v) leave_to[(int64_t)q * a.C + col + v] = s[v];
                 }
-            }
+            });
         } else {
             const T *px = (const T *)a.x + t0 * a.ldx + col, *py = (const T *)a.y + (t0 - 1) * a.ldy + col;
             T *pdx = (T *)a.dx + t0 * a.lddx + col, *pdg = (T *)a.dgate + t0 * a.lddg + col;
@@ -310,8 +321,8 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
                 in_x[j] = is_there >> j & 1u ? load_few<T, V>(px - j * a.ldx) : no_few<T, V>();
                 in_y[j] = (is_there & ~leaves) >> j & 1u ? load_few<T, V>(py - j * a.ldy) : no_few<T, V>();
             }
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) {
+            in_turn([&](int j, auto is_handed) {
+                constexpr bool kHanded = decltype(is_handed)::value;
                 if (enters >> j & 1u) {
                     const int q = __shfl_sync(0xffffffffu, seq, j);
 #pragma unroll
@@ -331,19 +342,19 @@ __global__ void __launch_bounds__(32 * kRecWarps, 4) recurrence_kernel(const Rec
                     const float lambda = to_float<T>(in_b[j].v[v]) + s[v], keep = 1.f - c[j][v];
                     dx[v] = c[j][v] * lambda;
                     dg[v] = lambda * (before[v] - to_float<T>(in_x[j].v[v])) * (keep * c[j][v]);
-                    s[v] = handed ? fmaf(keep, lambda, lost(keep, c[j][v]) * finite(lambda)) : keep * lambda;
+                    s[v] = kHanded ? fmaf(keep, lambda, lost(keep, c[j][v]) * finite(lambda)) : keep * lambda;
                 }
                 if (is_there >> j & 1u) {
                     store_few<T, V>(pdx - j * a.lddx, dx);
                     store_few<T, V>(pdg - j * a.lddg, dg);
                 }
-                if (HANDED && (leaves >> j & 1u)) {
+                if (kHanded && (leaves >> j & 1u)) {
                     const int q = __shfl_sync(0xffffffffu, seq, j);
                     if (mine)
 #pragma unroll
                         for (int v = 0; v < V; ++v) leave_to[(int64_t)q * a.C + col + v] = s[v];
                 }
-            }
+            });
         }
     }
     if (PART) {
@@ -445,7 +456,6 @@ __device__ __forceinline__ Pair finite(Pair s) {
     split_pair(s, a, b);
     return make_pair(finite(a), finite(b));
 }
-template <bool B> struct Known { static constexpr bool value = B; };
 struct alignas(16) Map2 { Pair P, L; };          // (P, L) of two channels
 // `calm`: no sequence starts there.
 template <bool CALM> __device__ __forceinline__ Pair advance2(const Map2 &m, Pair s) {
